@@ -1,7 +1,8 @@
 /*
  * moe.h -- C ABI of the MI355X (gfx950) MoE-layer hot path: the forward of the
- * layer's four stages, their backward, the FP8 expert FFN and one GPU's step of
- * expert-parallel dispatch.
+ * layer's four stages, their backward, the FP8 expert FFN, one GPU's step of
+ * expert-parallel dispatch, and what follows the gradients in a training step:
+ * the router's balance loss, the gradients' norm and the AdamW step.
  *
  * The library computes, on one GPU with all experts local, the
  * Mixture-of-Experts layer of arXiv 2504.14960:
@@ -314,6 +315,72 @@ moe_status_t moe_router_backward(const void* x, const void* w_router, const floa
                                  float* dw_router, float* dbias, void* workspace,
                                  size_t workspace_bytes, moe_stream_t stream);
 
+/* moe_router_backward with a gradient that reaches the logits by another path
+ * (moe_balance_loss_backward): dlogits_addend [T,E] fp32 is added to dlogits before
+ * dx, dw_router and dbias are formed.  It must not overlap dlogits; NULL adds
+ * nothing and gives moe_router_backward's results bit for bit. */
+moe_status_t moe_router_backward_addend(const void* x, const void* w_router, const float* logits,
+                                        const int32_t* topk_idx, const float* dgate,
+                                        const float* dlogits_addend, int T, int H, int E, int K,
+                                        int renormalize, moe_dtype_t dt, float* dlogits, void* dx,
+                                        float* dw_router, float* dbias, void* workspace,
+                                        size_t workspace_bytes, moe_stream_t stream);
+
+/*
+ * Balance loss and z loss of a router, with the per-expert counts they need.  The
+ * paper trains its routers with an auxiliary loss but gives no formula; this is the
+ * usual one (mean share of assignments times mean probability), kept per sequence
+ * where sequences are given.
+ *
+ * Tokens t of sequence s = rows [seq_offsets[s], seq_offsets[s+1]); a token counts
+ * unless token_mask[t] == 0.  With p = softmax(logits[t,:]), lse = log sum_e
+ * exp(logits[t,e]), n_s = tokens of s that count and n = sum_s n_s:
+ *
+ *   counts[s,e]    = assignments (t,k) of s with topk_idx[t,k] == e         (int32)
+ *   prob_sums[s,e] = sum_t p[t,e]                                           (fp32)
+ *   losses[0] = balance_coef * E / (K n) * sum_s 1/n_s sum_e counts[s,e] prob_sums[s,e]
+ *   losses[1] = z_coef / n * sum_t lse_t^2
+ *
+ * losses[0] is balance_coef where every expert has 1/E of the assignments and of the
+ * probability; a sequence weighs by its tokens.  counts are taken before any
+ * capacity drops assignments.  What a token that does not count holds (logits, NaN
+ * included, and indices) is not looked at.  A token whose logits are all -inf has no
+ * probability and adds nothing to either loss.  n == 0: both losses are 0.
+ *
+ * logits [T,E] fp32 and topk_idx [T,K] int32 as moe_router_topk leaves them (entries
+ * outside [0,E) count nowhere); token_mask [T] uint8 or NULL (all count);
+ * seq_offsets [n_seq+1] int32, non-decreasing from 0 to T, or NULL (one sequence,
+ * n_seq = 1).  Outputs: counts, prob_sums [n_seq,E]; seq_tokens [n_seq+1] int32 (n_s,
+ * then n); losses [2] fp32.  Sums over tokens are taken in an order that the sizes and
+ * seq_offsets fix.  E <= 256, K <= min(E,64), 1 <= n_seq <= 65536.
+ */
+size_t moe_balance_loss_workspace_bytes(int T, int E, int n_seq);
+moe_status_t moe_balance_loss(const float* logits, const int32_t* topk_idx,
+                              const uint8_t* token_mask, const int32_t* seq_offsets, int T, int E,
+                              int K, int n_seq, float balance_coef, float z_coef, int32_t* counts,
+                              float* prob_sums, int32_t* seq_tokens, float* losses,
+                              void* workspace, size_t workspace_bytes, moe_stream_t stream);
+
+/*
+ * Its gradient in the logits, for upstream gradients dlosses[0], dlosses[1] (device,
+ * fp32; NULL = 1, 1).  counts are constants (the selection has no gradient).  With
+ * g[s,e] = dlosses[0] balance_coef E / (K n n_s) counts[s,e]:
+ *
+ *   dlogits[t,e] = p[t,e] (g[s,e] - sum_j p[t,j] g[s,j])
+ *                  + dlosses[1] 2 z_coef / n * lse_t p[t,e]      (+ addend[t,e])
+ *
+ * and 0 (+ addend) for a token that does not count.  counts [n_seq,E] and seq_tokens
+ * [n_seq+1] as moe_balance_loss wrote them, or their sums over the ranks of a
+ * data-parallel group.  addend [T,E] fp32 or NULL; it may be dlogits itself.  Rows
+ * outside every sequence are left untouched.  No workspace.
+ */
+moe_status_t moe_balance_loss_backward(const float* logits, const uint8_t* token_mask,
+                                       const int32_t* seq_offsets, const int32_t* counts,
+                                       const int32_t* seq_tokens, const float* dlosses,
+                                       const float* addend, int T, int E, int K, int n_seq,
+                                       float balance_coef, float z_coef, float* dlogits,
+                                       moe_stream_t stream);
+
 /*
  * Backward of a3, the grouped SwiGLU expert FFN (bf16 only; Section 3.3: the
  * backward workflow mirrors the forward; f_e of Eq. 1 by the chain rule).  With
@@ -402,6 +469,107 @@ moe_status_t moe_layer_backward(const void* x, const void* w_router, const void*
                                 float* dw_router, float* dbias, void* dw_gate, void* dw_up,
                                 void* dw_down, void* workspace, size_t workspace_bytes,
                                 moe_stream_t stream);
+
+/* moe_layer_backward with a gradient that reaches the router's logits by another
+ * path: dlogits_addend as in moe_router_backward_addend.  NULL gives
+ * moe_layer_backward's results bit for bit. */
+moe_status_t moe_layer_backward_addend(const void* x, const void* w_router, const void* w_gate,
+                                       const void* w_up, const void* wgu_t, const void* wd_t,
+                                       const void* dy, const float* dlogits_addend, int T, int H,
+                                       int E, int K, int F, int renormalize, int capacity,
+                                       const void* forward_workspace, const void* gu, void* dx,
+                                       float* dw_router, float* dbias, void* dw_gate, void* dw_up,
+                                       void* dw_down, void* workspace, size_t workspace_bytes,
+                                       moe_stream_t stream);
+
+/*
+ * Norm of a list of gradients and the factor that clips it:
+ *
+ *   out[0] = |multiplier| * sqrt(sum_i sum_j grad_i[j]^2)
+ *   out[1] = multiplier * min(1, max_norm / (out[0] + 1e-6))    (max_norm > 0)
+ *          = multiplier                                        (max_norm <= 0: no clipping)
+ *          = NaN where out[0] is not finite: moe_adamw_step then changes nothing
+ *
+ * multiplier undoes a loss scale.  Squares are summed in 64 bits, in an order that the
+ * sizes fix.  `tensors` is HOST memory, read during the call; gradients are device
+ * memory of n elements of dt, 16-byte aligned (n == 0: none, pointer not looked at;
+ * n <= 2^34).
+ * out [2] fp32 in device memory.  workspace: moe_grad_norm_workspace_bytes(count).
+ */
+typedef struct {
+    const void* grad;
+    int64_t n;
+    moe_dtype_t dt;
+} moe_grad_tensor_t;
+
+size_t moe_grad_norm_workspace_bytes(int count);
+moe_status_t moe_grad_norm(const moe_grad_tensor_t* tensors, int count, float max_norm,
+                           float multiplier, float* out, void* workspace, size_t workspace_bytes,
+                           moe_stream_t stream);
+
+/*
+ * One AdamW step (decoupled weight decay) over a list of tensors.  Per element, with
+ * g = *grad_scale * grad (grad_scale: device, fp32, e.g. moe_grad_norm's out + 1; NULL
+ * = 1), lr_i = lr * lr_scale and t = step:
+ *
+ *   m = beta1 m + (1 - beta1) g          v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr_i weight_decay)
+ *       - lr_i / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ *
+ * computed in fp32, m and v with every operation rounded (no fused multiply-add).  A
+ * NaN in *grad_scale: nothing is changed.
+ *
+ * Weights (param_dt, master):
+ *   MOE_F32,  NULL      fp32
+ *   MOE_BF16, master    master [n] fp32 is stepped, param becomes its nearest bf16 value
+ *   MOE_BF16, NULL      bf16 alone, rounded stochastically (a step is far smaller than
+ *                       half the distance of two bf16 values, and would be lost)
+ * Gradients: fp32 or bf16.
+ * States (state):
+ *   MOE_STATE_F32       exp_avg, exp_avg_sq [n] fp32; the scale pointers are not used
+ *   MOE_STATE_MXFP8     exp_avg, exp_avg_sq [n] E4M3 codes, one E8M0 scale (a byte b
+ *                       stands for 2^(b-127), 255 for NaN) to every 32 elements in
+ *                       exp_avg_scale, exp_avg_sq_scale [ceil(n/32)]: the smallest power
+ *                       of two, from 2^-126, that leaves at most 448.  m and v are used
+ *                       for p before they are rounded.  Rounding is stochastic (beta2 near
+ *                       1 changes v by less than half a step of any 8-bit format: to the
+ *                       nearest, v would never move); a v above 0 stays above 0.  A block
+ *                       with a value that is not finite gets scale 255 and codes 0x7f.
+ *                       Zero codes with any scale but 255 are fresh states.
+ *
+ * Random bits: with mix(x): x ^= x>>16; x *= 0x7feb352d; x ^= x>>15; x *= 0x846ca68b;
+ * x ^= x>>16 on 32 bits, element j of tensor i (its place in the list) has
+ *   r = mix(low32(j) ^ mix(seed + 0x9e3779b9 (i + 1) + 0x85ebca6b high32(j)))
+ * m is rounded with r & 0xffff, v with r >> 16 and a bf16 weight with the upper 16 of
+ * the low 32 bits of 0x9e3779b1 r.  The same seed gives the same results; a caller
+ * passes another one in every step.  A 16-bit number u rounds up where the part cut
+ * off is at least 1 - (u + 1/2) / 65536 of a step (E4M3), 1 - u / 65536 (bf16).
+ *
+ * `tensors` is HOST memory, read during the call.  All pointers but the scales are
+ * 16-byte aligned; 0 <= n <= 2^34; tensors must not overlap.  step >= 1, lr >= 0, 0 <= beta1,
+ * beta2 < 1, eps > 0.  No workspace.
+ */
+typedef enum { MOE_STATE_F32 = 0, MOE_STATE_MXFP8 = 1 } moe_state_t;
+
+typedef struct {
+    void* param;               /* [n] param_dt */
+    float* master;             /* [n] or NULL */
+    const void* grad;          /* [n] grad_dt */
+    void* exp_avg;             /* [n] fp32 or E4M3 */
+    void* exp_avg_sq;          /* [n] fp32 or E4M3 */
+    uint8_t* exp_avg_scale;    /* [ceil(n/32)] E8M0, MOE_STATE_MXFP8 only */
+    uint8_t* exp_avg_sq_scale; /* [ceil(n/32)] E8M0, MOE_STATE_MXFP8 only */
+    int64_t n;
+    float weight_decay;
+    float lr_scale;
+    moe_dtype_t param_dt;
+    moe_dtype_t grad_dt;
+    moe_state_t state;
+} moe_adamw_tensor_t;
+
+moe_status_t moe_adamw_step(const moe_adamw_tensor_t* tensors, int count, double lr, double beta1,
+                            double beta2, double eps, int64_t step, uint32_t seed,
+                            const float* grad_scale, moe_stream_t stream);
 
 /* Where moe_layer_forward keeps its intermediates inside `workspace`, for
  * tests and profiling.  Writes 11 byte offsets into byte_offsets[0..10], in

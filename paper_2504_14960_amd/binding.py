@@ -15,6 +15,8 @@ import torch
 
 MOE_F32 = 0
 MOE_BF16 = 1
+MOE_STATE_F32 = 0
+MOE_STATE_MXFP8 = 1
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libmoe_hip.so")
@@ -25,6 +27,17 @@ class MoeError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"moe status {status}: {message}")
         self.status = status
+
+
+class _GradTensor(C.Structure):      # moe_grad_tensor_t
+    _fields_ = [("grad", C.c_void_p), ("n", C.c_int64), ("dt", C.c_int)]
+
+
+class _AdamWTensor(C.Structure):     # moe_adamw_tensor_t
+    _fields_ = [("param", C.c_void_p), ("master", C.c_void_p), ("grad", C.c_void_p), ("exp_avg", C.c_void_p),
+                ("exp_avg_sq", C.c_void_p), ("exp_avg_scale", C.c_void_p), ("exp_avg_sq_scale", C.c_void_p),
+                ("n", C.c_int64), ("weight_decay", C.c_float), ("lr_scale", C.c_float), ("param_dt", C.c_int),
+                ("grad_dt", C.c_int), ("state", C.c_int)]
 
 
 def lib_path() -> str:
@@ -110,6 +123,22 @@ def lib() -> C.CDLL:
     L.moe_layer_workspace_layout.argtypes = [i, i, i, i, i, i, i, i, C.POINTER(sz), i]
     L.moe_layer_forward.restype = i
     L.moe_layer_forward.argtypes = [vp] * 9 + [i] * 9 + [vp, vp, sz, vp]
+    L.moe_router_backward_addend.restype = i
+    L.moe_router_backward_addend.argtypes = [vp] * 6 + [i] * 6 + [vp] * 5 + [sz, vp]
+    L.moe_layer_backward_addend.restype = i
+    L.moe_layer_backward_addend.argtypes = [vp] * 8 + [i] * 7 + [vp] * 9 + [sz, vp]
+    L.moe_balance_loss_workspace_bytes.restype = sz
+    L.moe_balance_loss_workspace_bytes.argtypes = [i] * 3
+    L.moe_balance_loss.restype = i
+    L.moe_balance_loss.argtypes = [vp] * 4 + [i] * 4 + [C.c_float] * 2 + [vp] * 5 + [sz, vp]
+    L.moe_balance_loss_backward.restype = i
+    L.moe_balance_loss_backward.argtypes = [vp] * 7 + [i] * 4 + [C.c_float] * 2 + [vp] * 2
+    L.moe_grad_norm_workspace_bytes.restype = sz
+    L.moe_grad_norm_workspace_bytes.argtypes = [i]
+    L.moe_grad_norm.restype = i
+    L.moe_grad_norm.argtypes = [vp, i, C.c_float, C.c_float, vp, vp, sz, vp]
+    L.moe_adamw_step.restype = i
+    L.moe_adamw_step.argtypes = [vp, i] + [f] * 4 + [C.c_int64, C.c_uint32, vp, vp]
     L.moe_set_option.restype = i
     L.moe_set_option.argtypes = [C.c_char_p, i]
     f = C.c_float
@@ -311,14 +340,156 @@ def router_backward_workspace_bytes(T: int, H: int, E: int) -> int:
 def router_backward(x: torch.Tensor, w_router: torch.Tensor, logits: torch.Tensor, topk_idx: torch.Tensor,
                     dgate: torch.Tensor, renormalize: bool, dlogits: torch.Tensor, dx: Optional[torch.Tensor],
                     dw_router: Optional[torch.Tensor], dbias: Optional[torch.Tensor],
-                    workspace: Optional[torch.Tensor]) -> None:
+                    workspace: Optional[torch.Tensor], dlogits_addend: Optional[torch.Tensor] = None) -> None:
     T, E = logits.shape
     K = topk_idx.shape[1]
     H = x.shape[1]
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    if dlogits_addend is not None:
+        _expect("dlogits_addend", dlogits_addend, torch.float32, T * E)
+        _check(lib().moe_router_backward_addend(_ptr(x), _ptr(w_router), _ptr(logits), _ptr(topk_idx), _ptr(dgate),
+                                                _ptr(dlogits_addend), T, H, E, K, int(bool(renormalize)), _dt(x),
+                                                _ptr(dlogits), _ptr(dx), _ptr(dw_router), _ptr(dbias), _ptr(workspace),
+                                                nbytes, _stream()))
+        return
     _check(lib().moe_router_backward(_ptr(x), _ptr(w_router), _ptr(logits), _ptr(topk_idx), _ptr(dgate), T, H, E, K,
                                      int(bool(renormalize)), _dt(x), _ptr(dlogits), _ptr(dx), _ptr(dw_router),
                                      _ptr(dbias), _ptr(workspace), nbytes, _stream()))
+
+
+# ---- what follows the gradients in a training step: balance loss, gradient norm, AdamW ----
+def _expect(name: str, t: torch.Tensor, dtype, numel: int) -> None:
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.numel() != numel:
+        raise ValueError(f"{name} must have {numel} elements, not {t.numel()}")
+
+
+def _sequences(T: int, token_mask: Optional[torch.Tensor], seq_offsets: Optional[torch.Tensor]) -> int:
+    """Checks mask and offsets; the number of sequences."""
+    if token_mask is not None and token_mask.dtype != torch.bool:
+        _expect("token_mask", token_mask, torch.uint8, T)
+    elif token_mask is not None:
+        _expect("token_mask", token_mask, torch.bool, T)
+    if seq_offsets is None:
+        return 1
+    _expect("seq_offsets", seq_offsets, torch.int32, max(2, seq_offsets.numel()))
+    return seq_offsets.numel() - 1
+
+
+def balance_loss_workspace_bytes(T: int, E: int, n_seq: int = 1) -> int:
+    return int(lib().moe_balance_loss_workspace_bytes(T, E, n_seq))
+
+
+def balance_loss(logits: torch.Tensor, topk_idx: torch.Tensor, balance_coef: float, z_coef: float, counts: torch.Tensor,
+                 prob_sums: torch.Tensor, seq_tokens: torch.Tensor, losses: torch.Tensor, workspace: torch.Tensor,
+                 token_mask: Optional[torch.Tensor] = None, seq_offsets: Optional[torch.Tensor] = None) -> None:
+    """losses [2] = balance and z loss of a router's logits [T, E] and selection [T, K]; counts and prob_sums [n_seq, E],
+    seq_tokens [n_seq + 1].  token_mask [T] (uint8 or bool): tokens that count; seq_offsets [n_seq + 1] int32."""
+    T, E = logits.shape
+    n_seq = _sequences(T, token_mask, seq_offsets)
+    _expect("logits", logits, torch.float32, T * E)
+    _expect("topk_idx", topk_idx, torch.int32, T * topk_idx.shape[1])
+    _expect("counts", counts, torch.int32, n_seq * E)
+    _expect("prob_sums", prob_sums, torch.float32, n_seq * E)
+    _expect("seq_tokens", seq_tokens, torch.int32, n_seq + 1)
+    _expect("losses", losses, torch.float32, 2)
+    _check(lib().moe_balance_loss(_ptr(logits), _ptr(topk_idx), _ptr(token_mask), _ptr(seq_offsets), T, E,
+                                  topk_idx.shape[1], n_seq, balance_coef, z_coef, _ptr(counts), _ptr(prob_sums),
+                                  _ptr(seq_tokens), _ptr(losses), _ptr(workspace),
+                                  workspace.numel() * workspace.element_size(), _stream()))
+
+
+def balance_loss_backward(logits: torch.Tensor, counts: torch.Tensor, seq_tokens: torch.Tensor,
+                          dlosses: Optional[torch.Tensor], K: int, balance_coef: float, z_coef: float,
+                          dlogits: torch.Tensor, addend: Optional[torch.Tensor] = None,
+                          token_mask: Optional[torch.Tensor] = None, seq_offsets: Optional[torch.Tensor] = None) -> None:
+    """dlogits [T, E] = gradient of dlosses . losses in the logits, plus addend [T, E] (which may be dlogits)."""
+    T, E = logits.shape
+    n_seq = _sequences(T, token_mask, seq_offsets)
+    _expect("logits", logits, torch.float32, T * E)
+    _expect("counts", counts, torch.int32, n_seq * E)
+    _expect("seq_tokens", seq_tokens, torch.int32, n_seq + 1)
+    _expect("dlogits", dlogits, torch.float32, T * E)
+    if dlosses is not None:
+        _expect("dlosses", dlosses, torch.float32, 2)
+    if addend is not None:
+        _expect("addend", addend, torch.float32, T * E)
+    _check(lib().moe_balance_loss_backward(_ptr(logits), _ptr(token_mask), _ptr(seq_offsets), _ptr(counts),
+                                           _ptr(seq_tokens), _ptr(dlosses), _ptr(addend), T, E, K, n_seq, balance_coef,
+                                           z_coef, _ptr(dlogits), _stream()))
+
+
+class GradTensors:
+    """A list of gradients (fp32 or bf16) that grad_norm goes over: built once, kept as long as the buffers are used."""
+
+    def __init__(self, grads) -> None:
+        self.grads = list(grads)
+        self._list = (_GradTensor * len(self.grads))(*((_ptr(g), g.numel(), _dt(g)) for g in self.grads))
+
+
+def grad_norm_workspace_bytes(count: int) -> int:
+    return int(lib().moe_grad_norm_workspace_bytes(count))
+
+
+def grad_norm(tensors, out: torch.Tensor, workspace: torch.Tensor, max_norm: float = 0.0, multiplier: float = 1.0) -> None:
+    """out [2] = norm of multiplier * the gradients of a GradTensors (or an AdamWTensors), and the factor that
+    adamw_step takes as grad_scale: multiplier, clipped to max_norm (0: not), NaN where the norm is not finite."""
+    grads = tensors.grads if isinstance(tensors, AdamWTensors) else tensors
+    _expect("out", out, torch.float32, 2)
+    _check(lib().moe_grad_norm(grads._list, len(grads._list), max_norm, multiplier, _ptr(out), _ptr(workspace),
+                               workspace.numel() * workspace.element_size(), _stream()))
+
+
+class AdamWTensors:
+    """The tensors of an AdamW step: built once from the buffers a program trains with, and kept.
+
+    params fp32 or bf16; masters: fp32 copies that are stepped in place of bf16 params (None, or None in places: bf16
+    alone, rounded stochastically); grads fp32 or bf16; exp_avgs and exp_avg_sqs fp32, or uint8 E4M3 codes with
+    uint8 E8M0 exp_avg_scales and exp_avg_sq_scales, one to every 32 elements (zeros are fresh states)."""
+
+    def __init__(self, params, grads, exp_avgs, exp_avg_sqs, masters=None, exp_avg_scales=None, exp_avg_sq_scales=None,
+                 weight_decays=None, lr_scales=None) -> None:
+        n = len(params)
+        columns = [params, masters, grads, exp_avgs, exp_avg_sqs, exp_avg_scales, exp_avg_sq_scales]
+        columns = [[None] * n if c is None else list(c) for c in columns]
+        decays = [0.0] * n if weight_decays is None else list(weight_decays)
+        scales = [1.0] * n if lr_scales is None else list(lr_scales)
+        if any(len(c) != n for c in columns + [decays, scales]):
+            raise ValueError("every list must have as many entries as params")
+        self.tensors = list(zip(*columns))       # keeps the buffers alive
+        self._list = (_AdamWTensor * n)(*(self._entry(*row, d, s) for row, d, s in zip(self.tensors, decays, scales)))
+        self.grads = GradTensors(columns[2])
+
+    @staticmethod
+    def _entry(param, master, grad, m, v, m_scale, v_scale, decay, lr_scale):
+        count = param.numel()
+        state = MOE_STATE_MXFP8 if m.dtype == torch.uint8 else MOE_STATE_F32
+        kind = torch.uint8 if state == MOE_STATE_MXFP8 else torch.float32
+        _expect("exp_avg", m, kind, count)
+        _expect("exp_avg_sq", v, kind, count)
+        _expect("grad", grad, grad.dtype, count)
+        if master is not None:
+            _expect("master", master, torch.float32, count)
+        for name, t in (("exp_avg_scale", m_scale), ("exp_avg_sq_scale", v_scale)):
+            if state == MOE_STATE_MXFP8:
+                if t is None:
+                    raise ValueError(f"8-bit states need {name}s")
+                _expect(name, t, torch.uint8, (count + 31) // 32)
+            elif t is not None:
+                raise ValueError(f"{name} goes with 8-bit states only")
+        return (_ptr(param), _ptr(master), _ptr(grad), _ptr(m), _ptr(v), _ptr(m_scale), _ptr(v_scale), count, decay,
+                lr_scale, _dt(param), _dt(grad), state)
+
+
+def adamw_step(tensors: AdamWTensors, lr: float, beta1: float, beta2: float, eps: float, step: int, seed: int = 0,
+               grad_scale: Optional[torch.Tensor] = None) -> None:
+    """One AdamW step (the first has step = 1) over all tensors.  grad_scale [1] fp32 on the device multiplies every
+    gradient; NaN in it leaves everything as it is.  seed: of stochastic rounding, another one in every step."""
+    if grad_scale is not None:
+        _expect("grad_scale", grad_scale, torch.float32, 1)
+    _check(lib().moe_adamw_step(tensors._list, len(tensors._list), lr, beta1, beta2, eps, step, seed & 0xffffffff,
+                                _ptr(grad_scale), _stream()))
 
 
 def expert_backward_workspace_bytes(R_max: int, H: int, F: int, E: int) -> int:
@@ -429,9 +600,19 @@ def layer_backward(x: torch.Tensor, w_router: torch.Tensor, w_gate: torch.Tensor
                    wgu_t: torch.Tensor, wd_t: torch.Tensor, dy: torch.Tensor, K: int, renormalize: bool, capacity: int,
                    forward_workspace: torch.Tensor, gu: Optional[torch.Tensor], dx: torch.Tensor,
                    dw_router: Optional[torch.Tensor], dbias: Optional[torch.Tensor], dw_gate: torch.Tensor,
-                   dw_up: torch.Tensor, dw_down: torch.Tensor, workspace: torch.Tensor) -> None:
+                   dw_up: torch.Tensor, dw_down: torch.Tensor, workspace: torch.Tensor,
+                   dlogits_addend: Optional[torch.Tensor] = None) -> None:
     T, H = x.shape
     E, F, _ = w_gate.shape
+    if dlogits_addend is not None:
+        _expect("dlogits_addend", dlogits_addend, torch.float32, T * E)
+        _check(lib().moe_layer_backward_addend(_ptr(x), _ptr(w_router), _ptr(w_gate), _ptr(w_up), _ptr(wgu_t),
+                                               _ptr(wd_t), _ptr(dy), _ptr(dlogits_addend), T, H, E, K, F,
+                                               int(renormalize), int(capacity), _ptr(forward_workspace), _ptr(gu),
+                                               _ptr(dx), _ptr(dw_router), _ptr(dbias), _ptr(dw_gate), _ptr(dw_up),
+                                               _ptr(dw_down), _ptr(workspace),
+                                               workspace.numel() * workspace.element_size(), _stream()))
+        return
     _check(lib().moe_layer_backward(_ptr(x), _ptr(w_router), _ptr(w_gate), _ptr(w_up), _ptr(wgu_t), _ptr(wd_t),
                                     _ptr(dy), T, H, E, K, F, int(renormalize), int(capacity), _ptr(forward_workspace),
                                     _ptr(gu), _ptr(dx), _ptr(dw_router), _ptr(dbias), _ptr(dw_gate), _ptr(dw_up),

@@ -50,6 +50,20 @@ static moe_status_t check_dims(const char* fn, int T, int H, int E, int K, moe_d
         if (!aligned16(p)) return fail(MOE_ERR_INVALID_ARG, "%s: %s is not 16-byte aligned", fn, #p); \
     } while (0)
 
+// one entry of a list of tensors
+static moe_status_t check_list_entry(const char* fn, int i, int64_t n, moe_dtype_t dt, const char* what) {
+    if (dt != MOE_F32 && dt != MOE_BF16) return fail(MOE_ERR_INVALID_ARG, "%s: tensor %d: unknown %s %d", fn, i, what, (int)dt);
+    if (n < 0) return fail(MOE_ERR_INVALID_ARG, "%s: tensor %d: n=%lld", fn, i, (long long)n);
+    if (n > kMaxListElements) return fail(MOE_ERR_UNSUPPORTED, "%s: tensor %d: n=%lld exceeds the limit 2^34", fn, i, (long long)n);
+    return MOE_OK;
+}
+
+static moe_status_t check_list_ptr(const char* fn, int i, const void* p, const char* what) {
+    if (p == nullptr) return fail(MOE_ERR_INVALID_ARG, "%s: tensor %d: %s is NULL", fn, i, what);
+    if (!aligned16(p)) return fail(MOE_ERR_INVALID_ARG, "%s: tensor %d: %s is not 16-byte aligned", fn, i, what);
+    return MOE_OK;
+}
+
 struct LayerLayout {
     size_t logits, idx, gate, counts, offsets, roa, aor, perm_ws, x_perm, h, y_perm;
     size_t s_offsets, s_h, s_y, total, part_bytes;
@@ -398,12 +412,11 @@ size_t moe_router_backward_workspace_bytes(int T, int H, int E) {
     return router_backward_workspace_bytes(T, H, E);
 }
 
-moe_status_t moe_router_backward(const void* x, const void* w_router, const float* logits,
-                                 const int32_t* topk_idx, const float* dgate, int T, int H, int E,
-                                 int K, int renormalize, moe_dtype_t dt, float* dlogits, void* dx,
-                                 float* dw_router, float* dbias, void* workspace,
-                                 size_t workspace_bytes, moe_stream_t stream) {
-    static const char* fn = "moe_router_backward";
+static moe_status_t router_backward(const char* fn, const void* x, const void* w_router, const float* logits,
+                                    const int32_t* topk_idx, const float* dgate, const float* dlogits_addend, int T, int H,
+                                    int E, int K, int renormalize, moe_dtype_t dt, float* dlogits, void* dx,
+                                    float* dw_router, float* dbias, void* workspace, size_t workspace_bytes,
+                                    moe_stream_t stream) {
     if (moe_status_t st = check_dims(fn, T, H, E, K, dt)) return st;
     if (H % 8) return fail(MOE_ERR_UNSUPPORTED, "%s: H=%d must be a multiple of 8", fn, H);
     if (T == 0) {
@@ -416,6 +429,8 @@ moe_status_t moe_router_backward(const void* x, const void* w_router, const floa
     REQUIRE_PTR(fn, topk_idx);
     REQUIRE_PTR(fn, dgate);
     REQUIRE_PTR(fn, dlogits);
+    if (dlogits_addend) REQUIRE_PTR(fn, dlogits_addend);
+    if (dlogits_addend == dlogits) return fail(MOE_ERR_INVALID_ARG, "%s: dlogits_addend is dlogits", fn);
     if (dx) {
         REQUIRE_PTR(fn, dx);
         REQUIRE_PTR(fn, w_router);
@@ -430,8 +445,95 @@ moe_status_t moe_router_backward(const void* x, const void* w_router, const floa
         REQUIRE_PTR(fn, workspace);
     }
     if (dbias && (reinterpret_cast<uintptr_t>(dbias) & 3u)) return fail(MOE_ERR_INVALID_ARG, "%s: dbias is not 4-byte aligned", fn);
-    launch_router_backward(x, w_router, logits, topk_idx, dgate, T, H, E, K, renormalize != 0, dt, dlogits, dx,
+    launch_router_backward(x, w_router, logits, topk_idx, dgate, dlogits_addend, T, H, E, K, renormalize != 0, dt, dlogits, dx,
                            dw_router, dbias, workspace, static_cast<hipStream_t>(stream));
+    return check_launch(fn);
+}
+
+moe_status_t moe_router_backward(const void* x, const void* w_router, const float* logits,
+                                 const int32_t* topk_idx, const float* dgate, int T, int H, int E,
+                                 int K, int renormalize, moe_dtype_t dt, float* dlogits, void* dx,
+                                 float* dw_router, float* dbias, void* workspace,
+                                 size_t workspace_bytes, moe_stream_t stream) {
+    return router_backward("moe_router_backward", x, w_router, logits, topk_idx, dgate, nullptr, T, H, E, K, renormalize, dt,
+                           dlogits, dx, dw_router, dbias, workspace, workspace_bytes, stream);
+}
+
+moe_status_t moe_router_backward_addend(const void* x, const void* w_router, const float* logits,
+                                        const int32_t* topk_idx, const float* dgate,
+                                        const float* dlogits_addend, int T, int H, int E, int K,
+                                        int renormalize, moe_dtype_t dt, float* dlogits, void* dx,
+                                        float* dw_router, float* dbias, void* workspace,
+                                        size_t workspace_bytes, moe_stream_t stream) {
+    return router_backward("moe_router_backward_addend", x, w_router, logits, topk_idx, dgate, dlogits_addend, T, H, E, K,
+                           renormalize, dt, dlogits, dx, dw_router, dbias, workspace, workspace_bytes, stream);
+}
+
+static moe_status_t check_balance(const char* fn, int T, int E, int K, int n_seq, const int32_t* seq_offsets,
+                                  float balance_coef, float z_coef) {
+    if (moe_status_t st = check_dims(fn, T, 4, E, K, MOE_F32)) return st;
+    if (n_seq < 1) return fail(MOE_ERR_INVALID_ARG, "%s: need n_seq >= 1 (n_seq=%d)", fn, n_seq);
+    if (n_seq > kMaxSequences) return fail(MOE_ERR_UNSUPPORTED, "%s: n_seq=%d exceeds the limit %d", fn, n_seq, kMaxSequences);
+    if (seq_offsets == nullptr && n_seq != 1)
+        return fail(MOE_ERR_INVALID_ARG, "%s: %d sequences and no seq_offsets", fn, n_seq);
+    if (reinterpret_cast<uintptr_t>(seq_offsets) & 3u)
+        return fail(MOE_ERR_INVALID_ARG, "%s: seq_offsets is not 4-byte aligned", fn);
+    if (!std::isfinite(balance_coef) || !std::isfinite(z_coef))
+        return fail(MOE_ERR_INVALID_ARG, "%s: balance_coef and z_coef must be finite", fn);
+    return MOE_OK;
+}
+
+size_t moe_balance_loss_workspace_bytes(int T, int E, int n_seq) {
+    if (T < 0 || E <= 0 || n_seq <= 0) return 0;
+    return balance_loss_workspace_bytes(T, E, n_seq);
+}
+
+moe_status_t moe_balance_loss(const float* logits, const int32_t* topk_idx,
+                              const uint8_t* token_mask, const int32_t* seq_offsets, int T, int E,
+                              int K, int n_seq, float balance_coef, float z_coef, int32_t* counts,
+                              float* prob_sums, int32_t* seq_tokens, float* losses,
+                              void* workspace, size_t workspace_bytes, moe_stream_t stream) {
+    static const char* fn = "moe_balance_loss";
+    if (moe_status_t st = check_balance(fn, T, E, K, n_seq, seq_offsets, balance_coef, z_coef)) return st;
+    REQUIRE_PTR(fn, counts);
+    REQUIRE_PTR(fn, prob_sums);
+    if (seq_tokens == nullptr || losses == nullptr)
+        return fail(MOE_ERR_INVALID_ARG, "%s: %s is NULL", fn, seq_tokens ? "losses" : "seq_tokens");
+    if ((reinterpret_cast<uintptr_t>(seq_tokens) | reinterpret_cast<uintptr_t>(losses)) & 3u)
+        return fail(MOE_ERR_INVALID_ARG, "%s: seq_tokens or losses is not 4-byte aligned", fn);
+    if (T > 0) {
+        REQUIRE_PTR(fn, logits);
+        REQUIRE_PTR(fn, topk_idx);
+    }
+    const size_t need = balance_loss_workspace_bytes(T, E, n_seq);
+    if (workspace == nullptr || workspace_bytes < need)
+        return fail(MOE_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need,
+                    workspace ? workspace_bytes : (size_t)0);
+    REQUIRE_PTR(fn, workspace);
+    // no tokens: the outputs are still written (zeros)
+    launch_balance_loss(logits, topk_idx, token_mask, seq_offsets, T, E, K, n_seq, balance_coef, z_coef, counts, prob_sums,
+                        seq_tokens, losses, workspace, static_cast<hipStream_t>(stream));
+    return check_launch(fn);
+}
+
+moe_status_t moe_balance_loss_backward(const float* logits, const uint8_t* token_mask,
+                                       const int32_t* seq_offsets, const int32_t* counts,
+                                       const int32_t* seq_tokens, const float* dlosses,
+                                       const float* addend, int T, int E, int K, int n_seq,
+                                       float balance_coef, float z_coef, float* dlogits,
+                                       moe_stream_t stream) {
+    static const char* fn = "moe_balance_loss_backward";
+    if (moe_status_t st = check_balance(fn, T, E, K, n_seq, seq_offsets, balance_coef, z_coef)) return st;
+    if (T == 0) return MOE_OK;
+    REQUIRE_PTR(fn, logits);
+    REQUIRE_PTR(fn, counts);
+    REQUIRE_PTR(fn, dlogits);
+    if (addend) REQUIRE_PTR(fn, addend);
+    if (seq_tokens == nullptr) return fail(MOE_ERR_INVALID_ARG, "%s: seq_tokens is NULL", fn);
+    if ((reinterpret_cast<uintptr_t>(seq_tokens) | reinterpret_cast<uintptr_t>(dlosses)) & 3u)
+        return fail(MOE_ERR_INVALID_ARG, "%s: seq_tokens or dlosses is not 4-byte aligned", fn);
+    launch_balance_loss_backward(logits, token_mask, seq_offsets, counts, seq_tokens, dlosses, addend, T, E, K, n_seq,
+                                 balance_coef, z_coef, dlogits, static_cast<hipStream_t>(stream));
     return check_launch(fn);
 }
 
@@ -765,18 +867,17 @@ size_t moe_layer_backward_workspace_bytes(int T, int H, int E, int K, int F, int
     return layer_backward_layout(T, H, E, K, F, capacity).total;
 }
 
-moe_status_t moe_layer_backward(const void* x, const void* w_router, const void* w_gate,
-                                const void* w_up, const void* wgu_t, const void* wd_t, const void* dy,
-                                int T, int H, int E, int K, int F, int renormalize, int capacity,
-                                const void* forward_workspace, const void* gu, void* dx,
-                                float* dw_router, float* dbias, void* dw_gate, void* dw_up,
-                                void* dw_down, void* workspace, size_t workspace_bytes,
-                                moe_stream_t stream) {
-    static const char* fn = "moe_layer_backward";
+static moe_status_t layer_backward(const char* fn, const void* x, const void* w_router, const void* w_gate,
+                                   const void* w_up, const void* wgu_t, const void* wd_t, const void* dy,
+                                   const float* dlogits_addend, int T, int H, int E, int K, int F, int renormalize,
+                                   int capacity, const void* forward_workspace, const void* gu, void* dx, float* dw_router,
+                                   float* dbias, void* dw_gate, void* dw_up, void* dw_down, void* workspace,
+                                   size_t workspace_bytes, moe_stream_t stream) {
     if (moe_status_t st = check_dims(fn, T, H, E, K, MOE_BF16)) return st;
     if (F <= 0) return fail(MOE_ERR_INVALID_ARG, "%s: need F > 0", fn);
     REQUIRE_PTR(fn, forward_workspace);
     REQUIRE_PTR(fn, dx);
+    if (dlogits_addend) REQUIRE_PTR(fn, dlogits_addend);
     const LayerLayout Lf = layer_layout(T, H, E, K, F, 0, capacity, MOE_BF16);
     const LayerBackwardLayout L = layer_backward_layout(T, H, E, K, F, capacity);
     if (workspace == nullptr || workspace_bytes < L.total)
@@ -799,11 +900,105 @@ moe_status_t moe_layer_backward(const void* x, const void* w_router, const void*
                                           w_gate, w_up, wgu_t, wd_t, ws + L.dx_perm, dw_gate, dw_up, dw_down,
                                           ws + L.expert_ws, L.expert_bytes, stream);
     if (st) return st;
-    st = moe_router_backward(x, w_router, logits, idx, dgate, T, H, E, K, renormalize, MOE_BF16,
-                             reinterpret_cast<float*>(ws + L.dlogits), ws + L.dx_router, dw_router, dbias,
-                             ws + L.router_ws, L.router_bytes, stream);
+    st = router_backward("moe_router_backward", x, w_router, logits, idx, dgate, dlogits_addend, T, H, E, K, renormalize,
+                         MOE_BF16, reinterpret_cast<float*>(ws + L.dlogits), ws + L.dx_router, dw_router, dbias,
+                         ws + L.router_ws, L.router_bytes, stream);
     if (st) return st;
     return moe_permute_backward(ws + L.dx_perm, roa, ws + L.dx_router, T, H, K, L.r_max, MOE_BF16, dx, stream);
+}
+
+moe_status_t moe_layer_backward(const void* x, const void* w_router, const void* w_gate,
+                                const void* w_up, const void* wgu_t, const void* wd_t, const void* dy,
+                                int T, int H, int E, int K, int F, int renormalize, int capacity,
+                                const void* forward_workspace, const void* gu, void* dx,
+                                float* dw_router, float* dbias, void* dw_gate, void* dw_up,
+                                void* dw_down, void* workspace, size_t workspace_bytes,
+                                moe_stream_t stream) {
+    return layer_backward("moe_layer_backward", x, w_router, w_gate, w_up, wgu_t, wd_t, dy, nullptr, T, H, E, K, F, renormalize,
+                          capacity, forward_workspace, gu, dx, dw_router, dbias, dw_gate, dw_up, dw_down, workspace,
+                          workspace_bytes, stream);
+}
+
+moe_status_t moe_layer_backward_addend(const void* x, const void* w_router, const void* w_gate,
+                                       const void* w_up, const void* wgu_t, const void* wd_t,
+                                       const void* dy, const float* dlogits_addend, int T, int H,
+                                       int E, int K, int F, int renormalize, int capacity,
+                                       const void* forward_workspace, const void* gu, void* dx,
+                                       float* dw_router, float* dbias, void* dw_gate, void* dw_up,
+                                       void* dw_down, void* workspace, size_t workspace_bytes,
+                                       moe_stream_t stream) {
+    return layer_backward("moe_layer_backward_addend", x, w_router, w_gate, w_up, wgu_t, wd_t, dy, dlogits_addend, T, H, E, K, F,
+                          renormalize, capacity, forward_workspace, gu, dx, dw_router, dbias, dw_gate, dw_up, dw_down,
+                          workspace, workspace_bytes, stream);
+}
+
+size_t moe_grad_norm_workspace_bytes(int count) {
+    return count < 0 ? 0 : grad_norm_workspace_bytes(count);
+}
+
+moe_status_t moe_grad_norm(const moe_grad_tensor_t* tensors, int count, float max_norm,
+                           float multiplier, float* out, void* workspace, size_t workspace_bytes,
+                           moe_stream_t stream) {
+    static const char* fn = "moe_grad_norm";
+    if (count < 0 || (count > 0 && tensors == nullptr))
+        return fail(MOE_ERR_INVALID_ARG, "%s: count=%d, tensors %s", fn, count, tensors ? "given" : "NULL");
+    if (!std::isfinite(multiplier) || std::isnan(max_norm))
+        return fail(MOE_ERR_INVALID_ARG, "%s: multiplier must be finite, max_norm a number", fn);
+    for (int i = 0; i < count; ++i) {
+        const moe_grad_tensor_t& t = tensors[i];
+        if (moe_status_t st = check_list_entry(fn, i, t.n, t.dt, "dt")) return st;
+        if (t.n > 0)
+            if (moe_status_t st = check_list_ptr(fn, i, t.grad, "grad")) return st;
+    }
+    if (out == nullptr || (reinterpret_cast<uintptr_t>(out) & 3u))
+        return fail(MOE_ERR_INVALID_ARG, "%s: out is %s", fn, out ? "not 4-byte aligned" : "NULL");
+    const size_t need = grad_norm_workspace_bytes(count);
+    if (workspace == nullptr || workspace_bytes < need)
+        return fail(MOE_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need,
+                    workspace ? workspace_bytes : (size_t)0);
+    REQUIRE_PTR(fn, workspace);
+    launch_grad_norm(tensors, count, max_norm, multiplier, out, workspace, static_cast<hipStream_t>(stream));
+    return check_launch(fn);
+}
+
+moe_status_t moe_adamw_step(const moe_adamw_tensor_t* tensors, int count, double lr, double beta1,
+                            double beta2, double eps, int64_t step, uint32_t seed,
+                            const float* grad_scale, moe_stream_t stream) {
+    static const char* fn = "moe_adamw_step";
+    if (count < 0 || (count > 0 && tensors == nullptr))
+        return fail(MOE_ERR_INVALID_ARG, "%s: count=%d, tensors %s", fn, count, tensors ? "given" : "NULL");
+    if (step < 1) return fail(MOE_ERR_INVALID_ARG, "%s: step=%lld, the first one is 1", fn, (long long)step);
+    if (!(lr >= 0.0) || !std::isfinite(lr) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) ||
+        !(eps > 0.0) || !std::isfinite(eps))
+        return fail(MOE_ERR_INVALID_ARG, "%s: need lr >= 0, 0 <= beta1, beta2 < 1, eps > 0 (lr=%g beta1=%g beta2=%g eps=%g)",
+                    fn, lr, beta1, beta2, eps);
+    if (reinterpret_cast<uintptr_t>(grad_scale) & 3u)
+        return fail(MOE_ERR_INVALID_ARG, "%s: grad_scale is not 4-byte aligned", fn);
+    bool any = false;
+    for (int i = 0; i < count; ++i) {
+        const moe_adamw_tensor_t& t = tensors[i];
+        if (moe_status_t st = check_list_entry(fn, i, t.n, t.param_dt, "param_dt")) return st;
+        if (moe_status_t st = check_list_entry(fn, i, t.n, t.grad_dt, "grad_dt")) return st;
+        if (t.state != MOE_STATE_F32 && t.state != MOE_STATE_MXFP8)
+            return fail(MOE_ERR_INVALID_ARG, "%s: tensor %d: unknown state %d", fn, i, (int)t.state);
+        if (!std::isfinite(t.weight_decay) || !std::isfinite(t.lr_scale))
+            return fail(MOE_ERR_INVALID_ARG, "%s: tensor %d: weight_decay and lr_scale must be finite", fn, i);
+        if (t.master && t.param_dt != MOE_BF16)
+            return fail(MOE_ERR_INVALID_ARG, "%s: tensor %d: a master goes with bf16 weights only", fn, i);
+        if (t.n == 0) continue;
+        any = true;
+        if (moe_status_t st = check_list_ptr(fn, i, t.param, "param")) return st;
+        if (moe_status_t st = check_list_ptr(fn, i, t.grad, "grad")) return st;
+        if (moe_status_t st = check_list_ptr(fn, i, t.exp_avg, "exp_avg")) return st;
+        if (moe_status_t st = check_list_ptr(fn, i, t.exp_avg_sq, "exp_avg_sq")) return st;
+        if (t.master)
+            if (moe_status_t st = check_list_ptr(fn, i, t.master, "master")) return st;
+        if (t.state == MOE_STATE_MXFP8 && (t.exp_avg_scale == nullptr || t.exp_avg_sq_scale == nullptr))
+            return fail(MOE_ERR_INVALID_ARG, "%s: tensor %d: 8-bit states without their scales", fn, i);
+    }
+    if (!any) return MOE_OK;
+    launch_adamw(tensors, count, lr, beta1, beta2, eps, step, seed, grad_scale, static_cast<hipStream_t>(stream));
+    return check_launch(fn);
 }
 
 float moe_fp8_delayed_scale(const float* amax_history, int len, int margin) {

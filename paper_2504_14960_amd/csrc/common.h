@@ -28,6 +28,8 @@ inline void allow_lds(OncePerDevice& lds, const void* kern, int bytes) {
 constexpr int kWave = 64;
 constexpr int kMaxExperts = 256;
 constexpr int kMaxTopK = 64;
+constexpr int kMaxSequences = 65536;               // of one balance-loss call
+constexpr int64_t kMaxListElements = 1ll << 34;    // of one tensor of a gradient-norm or AdamW call
 
 __device__ __forceinline__ float bf16_to_f32(bf16_t v) {
     return __uint_as_float(static_cast<uint32_t>(v) << 16);
@@ -67,9 +69,26 @@ void launch_router(const void* x, const void* w, const float* bias, float* logit
 
 // backward of the router: dlogits always; dx, dw, dbias where non-NULL; ws of router_backward_workspace_bytes
 size_t router_backward_workspace_bytes(int T, int H, int E);
+// addend [T,E] or null is added to dlogits
 void launch_router_backward(const void* x, const void* w, const float* logits, const int32_t* idx, const float* dgate,
-                            int T, int H, int E, int K, int renorm, moe_dtype_t dt, float* dlogits, void* dx,
-                            float* dw, float* dbias, void* ws, hipStream_t s);
+                            const float* addend, int T, int H, int E, int K, int renorm, moe_dtype_t dt, float* dlogits,
+                            void* dx, float* dw, float* dbias, void* ws, hipStream_t s);
+
+// balance and z loss of the router, per-expert counts, and their gradient; offsets null: one sequence
+size_t balance_loss_workspace_bytes(int T, int E, int n_seq);
+void launch_balance_loss(const float* logits, const int32_t* idx, const uint8_t* mask, const int32_t* offsets, int T, int E,
+                         int K, int n_seq, float balance_coef, float z_coef, int32_t* counts, float* prob_sums,
+                         int32_t* seq_tokens, float* losses, void* ws, hipStream_t s);
+void launch_balance_loss_backward(const float* logits, const uint8_t* mask, const int32_t* offsets, const int32_t* counts,
+                                  const int32_t* seq_tokens, const float* dlosses, const float* addend, int T, int E, int K,
+                                  int n_seq, float balance_coef, float z_coef, float* dlogits, hipStream_t s);
+
+// gradient norm and AdamW over lists of tensors (host memory, checked by the caller)
+size_t grad_norm_workspace_bytes(int count);
+void launch_grad_norm(const moe_grad_tensor_t* tensors, int count, float max_norm, float multiplier, float* out, void* ws,
+                      hipStream_t s);
+void launch_adamw(const moe_adamw_tensor_t* tensors, int count, double lr, double beta1, double beta2, double eps,
+                  int64_t step, uint32_t seed, const float* grad_scale, hipStream_t s);
 
 // router: 16-token blocks per workgroup (1, 2 or 4); 0 = chosen from T and E
 void set_router_tile(int mb);

@@ -27,7 +27,8 @@ namespace {
 
 __global__ __launch_bounds__(64) void router_dlogits_kernel(const float* __restrict__ logits,
                                                              const int32_t* __restrict__ idx,
-                                                             const float* __restrict__ dgate, int T, int E, int K,
+                                                             const float* __restrict__ dgate,
+                                                             const float* __restrict__ addend, int T, int E, int K,
                                                              int renorm, float* __restrict__ dlogits) {
     const int t = blockIdx.x * 64 + threadIdx.x;
     if (t >= T) return;
@@ -64,6 +65,8 @@ __global__ __launch_bounds__(64) void router_dlogits_kernel(const float* __restr
         const float q = renorm ? (dg[k] - a) / S : dg[k];
         dl[e] += q * (expf(l[e] - m) * rz);
     }
+    if (addend)
+        for (int e = 0; e < E; ++e) dl[e] += addend[(size_t)t * E + e];
 }
 
 // One wave per token: lane l holds the logits of experts l, l + 64, .. and slot l.  The lane form above is a chain of 4 E
@@ -72,7 +75,8 @@ __global__ __launch_bounds__(64) void router_dlogits_kernel(const float* __restr
 template <int VPL>
 __global__ __launch_bounds__(256) void router_dlogits_wave_kernel(const float* __restrict__ logits,
                                                                   const int32_t* __restrict__ idx,
-                                                                  const float* __restrict__ dgate, int T, int E, int K,
+                                                                  const float* __restrict__ dgate,
+                                                                  const float* __restrict__ addend, int T, int E, int K,
                                                                   int renorm, float* __restrict__ dlogits) {
     const int lane = threadIdx.x & 63;
     const int t = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
@@ -128,6 +132,11 @@ __global__ __launch_bounds__(256) void router_dlogits_wave_kernel(const float* _
 #pragma unroll
         for (int j = 0; j < VPL; ++j)
             if (ek == lane + 64 * j) p[j] += ck;
+    }
+    if (addend) {
+#pragma unroll
+        for (int j = 0; j < VPL; ++j)
+            if (lane + 64 * j < E) p[j] += addend[(size_t)t * E + lane + 64 * j];
     }
 #pragma unroll
     for (int j = 0; j < VPL; ++j)
@@ -405,22 +414,22 @@ size_t router_backward_workspace_bytes(int T, int H, int E) {
 }
 
 void launch_router_backward(const void* x, const void* w, const float* logits, const int32_t* idx, const float* dgate,
-                            int T, int H, int E, int K, int renorm, moe_dtype_t dt, float* dlogits, void* dx,
-                            float* dw, float* dbias, void* ws, hipStream_t s) {
+                            const float* addend, int T, int H, int E, int K, int renorm, moe_dtype_t dt, float* dlogits,
+                            void* dx, float* dw, float* dbias, void* ws, hipStream_t s) {
     // One lane per token only where few experts leave most of a wave idle (us, lane / wave): 8 experts, 8192 tokens 7.8 /
     // 5.7, 16384 tokens 7.8 / 8.5, 65536 tokens 9.1 / 24.7; 16 experts, 16384 tokens 11.7 / 8.6, 32768 tokens 12.4 / 13.9;
     // 64 experts, 1024 tokens 41.0 / 4.2, 65536 tokens 72.9 / 27.2; 256 experts, 4096 tokens 125 / 5.9.
     if (E < 32 && T > 1024 * E)
-        hipLaunchKernelGGL(router_dlogits_kernel, dim3((T + 63) / 64), dim3(64), 0, s, logits, idx, dgate, T, E, K,
+        hipLaunchKernelGGL(router_dlogits_kernel, dim3((T + 63) / 64), dim3(64), 0, s, logits, idx, dgate, addend, T, E, K,
                            renorm, dlogits);
     else if (E <= 64)
-        hipLaunchKernelGGL(router_dlogits_wave_kernel<1>, dim3((T + 3) / 4), dim3(256), 0, s, logits, idx, dgate, T, E, K,
+        hipLaunchKernelGGL(router_dlogits_wave_kernel<1>, dim3((T + 3) / 4), dim3(256), 0, s, logits, idx, dgate, addend, T, E, K,
                            renorm, dlogits);
     else if (E <= 128)
-        hipLaunchKernelGGL(router_dlogits_wave_kernel<2>, dim3((T + 3) / 4), dim3(256), 0, s, logits, idx, dgate, T, E, K,
+        hipLaunchKernelGGL(router_dlogits_wave_kernel<2>, dim3((T + 3) / 4), dim3(256), 0, s, logits, idx, dgate, addend, T, E, K,
                            renorm, dlogits);
     else
-        hipLaunchKernelGGL(router_dlogits_wave_kernel<4>, dim3((T + 3) / 4), dim3(256), 0, s, logits, idx, dgate, T, E, K,
+        hipLaunchKernelGGL(router_dlogits_wave_kernel<4>, dim3((T + 3) / 4), dim3(256), 0, s, logits, idx, dgate, addend, T, E, K,
                            renorm, dlogits);
     const bool bf16 = dt == MOE_BF16;
     if (dx) {

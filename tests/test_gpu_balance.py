@@ -1,0 +1,313 @@
+"""Balance loss, z loss, per-expert counts and their gradient against the float64 oracle, at the sizes, masks and values
+where they can go wrong.
+
+Tolerances.  eps = 2^-24 is half a unit of fp32.  A probability comes from a difference, an exponential (2 eps and the
+difference's rounding, which the exponential turns into |x - max| eps), a sum of up to 256 terms (at most 8 levels of a
+tree or of 4 terms a lane and 6 levels) and a division: under 16 + |x - max| eps where |x - max| <= 24 carries any weight,
+so 40 eps.  Sums over tokens add at most one eps for each of the at most 256 additions of a chunk before sums go on in 64
+bits; errors of that kind are random and stay far below, 300 eps bounds them in any order.  An element of the gradient is
+bounded by 64 eps times the sum of the magnitudes that it is added up from."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+from oracle import training as o
+
+EPS = 2.0 ** -24
+
+
+def _inputs(T, E, K, S=1, masked=0.0, seed=0, spread=2.0):
+    rng = np.random.default_rng(seed + 1000 * T + E)
+    logits = (rng.standard_normal((T, E)) * spread + rng.standard_normal(E)).astype(np.float32)
+    idx = np.argsort(-logits, axis=1, kind="stable")[:, :K].astype(np.int32)
+    mask = (rng.random(T) >= masked).astype(np.uint8) if masked else None
+    offsets = np.concatenate([[0], np.sort(rng.integers(0, T + 1, S - 1)), [T]]).astype(np.int32) if S > 1 else None
+    return logits, idx, mask, offsets
+
+
+def _dev(a):
+    import torch
+    return None if a is None else torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def _forward(logits, idx, mask, offsets, cb=0.01, cz=0.001):
+    import torch
+    import paper_2504_14960_amd as moe
+    T, E = logits.shape
+    S = 1 if offsets is None else len(offsets) - 1
+    counts = torch.full((S, E), -7, dtype=torch.int32, device="cuda")
+    sums = torch.full((S, E), -7.0, device="cuda")
+    n = torch.full((S + 1,), -7, dtype=torch.int32, device="cuda")
+    losses = torch.full((2,), -7.0, device="cuda")
+    ws = torch.full((moe.balance_loss_workspace_bytes(T, E, S),), 0xff, dtype=torch.uint8, device="cuda")
+    moe.balance_loss(_dev(logits), _dev(idx), cb, cz, counts, sums, n, losses, ws, token_mask=_dev(mask),
+                     seq_offsets=_dev(offsets))
+    return counts, sums, n, losses
+
+
+def _backward(logits, K, counts, n, mask, offsets, dlosses, addend=None, cb=0.01, cz=0.001):
+    import torch
+    import paper_2504_14960_amd as moe
+    out = torch.full(logits.shape, -7.0, device="cuda")
+    moe.balance_loss_backward(_dev(logits), counts, n, _dev(dlosses), K, cb, cz, out, addend=_dev(addend),
+                              token_mask=_dev(mask), seq_offsets=_dev(offsets))
+    return out
+
+
+def _check(logits, idx, mask, offsets, dlosses=np.array([1.25, -0.75], dtype=np.float32), addend=None):
+    K = idx.shape[1]
+    counts, sums, n, losses = _forward(logits, idx, mask, offsets)
+    want = o.balance_loss(logits, idx, np.float32(0.01), np.float32(0.001), mask, offsets)
+    np.testing.assert_array_equal(counts.cpu().numpy(), want[0])
+    np.testing.assert_array_equal(n.cpu().numpy(), want[2])
+    np.testing.assert_allclose(sums.cpu().numpy(), want[1], rtol=340 * EPS, atol=1e-30)
+    np.testing.assert_allclose(losses.cpu().numpy(), want[3], rtol=400 * EPS, atol=1e-30)
+    got = _backward(logits, K, counts, n, mask, offsets, dlosses, addend).cpu().numpy()
+    ups = (1.0, 1.0) if dlosses is None else dlosses.astype(np.float64)
+    d, size = o.balance_loss_backward(logits, want[0], want[2], ups, K, np.float32(0.01), np.float32(0.001), mask, offsets)
+    if addend is not None:
+        d, size = d + addend, size + abs(addend)
+    assert (abs(got - d) <= 64 * EPS * size + 1e-37).all(), abs((got - d) / (size + 1e-37)).max() / EPS
+    return counts, sums, n, losses
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,E,K", [(1, 1, 1), (1, 256, 64), (2, 2, 2), (3, 3, 1), (63, 8, 2), (64, 8, 2), (65, 5, 5),
+                                   (130, 64, 8), (257, 65, 3), (500, 16, 4), (1023, 60, 4), (1500, 127, 2), (777, 128, 8),
+                                   (600, 129, 6), (2049, 255, 7), (300, 256, 1), (5000, 4, 2), (4100, 7, 3)])
+def test_one_sequence(T, E, K):
+    logits, idx, _, _ = _inputs(T, E, K)
+    _check(logits, idx, None, None)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,E,K,S,masked", [(1, 3, 1, 5, 0.0), (100, 8, 2, 2, 0.0), (100, 8, 2, 40, 0.2), (777, 60, 4, 23, 0.1),
+                                            (64, 33, 2, 64, 0.5), (1000, 64, 6, 300, 0.0), (513, 256, 8, 3, 0.9),
+                                            (50, 12, 3, 1000, 0.0), (3000, 100, 4, 7, 0.3)])
+def test_packed_sequences(T, E, K, S, masked):
+    _check(*_inputs(T, E, K, S, masked), addend=np.random.default_rng(1).standard_normal((T, E)).astype(np.float32) * 1e-4)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,S", [(70000, 1), (70001, 5)])
+def test_many_tokens(T, S):
+    logits, idx, mask, offsets = _inputs(T, 6, 2, S, 0.05)
+    _check(logits, idx, mask, offsets, dlosses=None)
+
+
+@pytest.mark.gpu
+def test_no_tokens_gives_zeros():
+    import torch
+    counts, sums, n, losses = _forward(np.zeros((0, 8), np.float32), np.zeros((0, 2), np.int32), None, None)
+    for t in (counts, sums, n, losses):
+        assert int(torch.count_nonzero(t)) == 0
+    counts, sums, n, losses = _forward(np.zeros((0, 8), np.float32), np.zeros((0, 2), np.int32), None, np.zeros(4, np.int32))
+    for t in (counts, sums, n, losses):
+        assert int(torch.count_nonzero(t)) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("S", [1, 3])
+def test_every_token_masked(S):
+    logits, idx, _, offsets = _inputs(200, 9, 2, S)
+    logits[:] = np.nan
+    mask = np.zeros(200, np.uint8)
+    addend = np.arange(1800, dtype=np.float32).reshape(200, 9)
+    counts, sums, n, losses = _forward(logits, idx, mask, offsets)
+    for t in (counts, sums, n, losses):
+        assert (t.cpu().numpy() == 0).all()
+    assert (_backward(logits, 2, counts, n, mask, offsets, None).cpu().numpy() == 0).all()
+    np.testing.assert_array_equal(_backward(logits, 2, counts, n, mask, offsets, None, addend).cpu().numpy(), addend)
+
+
+@pytest.mark.gpu
+def test_what_masked_tokens_hold_is_not_looked_at():
+    logits, idx, mask, offsets = _inputs(700, 40, 4, 6, 0.3)
+    clean = _check(logits, idx, mask, offsets)
+    gone = mask == 0
+    logits[gone] = np.tile(np.array([np.nan, np.inf, -np.inf, 3e38], np.float32), 10)
+    idx[gone] = 1 << 30
+    again = _check(logits, idx, mask, offsets)
+    for a, b in zip(clean, again):
+        np.testing.assert_array_equal(a.cpu().numpy(), b.cpu().numpy())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("E", [4, 60, 200])
+def test_experts_switched_off_and_rows_of_nothing(E):
+    logits, idx, _, _ = _inputs(300, E, 2)
+    logits[:, 1] = -np.inf                                   # an expert that is switched off
+    logits[7] = -np.inf                                      # a token without any expert
+    logits[8, 2:] = -np.inf                                  # a token with one
+    logits[9] = np.finfo(np.float32).min / 2 ** 64           # very low, all alike
+    logits[10, :] = np.float32(-1e4)
+    logits[10, 0] = np.float32(1e4)                          # sure of one
+    counts, sums, n, _ = _check(logits, idx, None, None)
+    assert float(sums[0, 1]) == pytest.approx(1 / E, rel=1e-5)   # token 9 alone
+
+
+@pytest.mark.gpu
+def test_nan_in_a_token_that_counts_is_seen():
+    logits, idx, _, _ = _inputs(100, 8, 2)
+    for bad in (np.nan, np.inf):
+        logits[3] = -np.inf
+        logits[3, 5] = bad
+        counts, sums, n, losses = _forward(logits, idx, None, None)
+        assert not np.isfinite(losses.cpu().numpy()).any()
+        d = _backward(logits, 2, counts, n, None, None, None).cpu().numpy()
+        assert np.isnan(d[3]).any() and np.isfinite(np.delete(d, 3, 0)).all()
+
+
+@pytest.mark.gpu
+def test_indices_outside_the_experts_count_nowhere():
+    logits, idx, _, _ = _inputs(100, 8, 3)
+    idx[::3, 0] = -1
+    idx[1::5, 2] = 8
+    idx[50] = [np.iinfo(np.int32).max, np.iinfo(np.int32).min, 2]
+    idx[51] = 4                                              # the same expert three times
+    _check(logits, idx, None, None)
+
+
+@pytest.mark.gpu
+def test_same_inputs_same_bits_and_other_streams():
+    import torch
+    logits, idx, mask, offsets = _inputs(20000, 64, 6, 4, 0.1)
+    first = _forward(logits, idx, mask, offsets)
+    d = _backward(logits, 6, first[0], first[2], mask, offsets, None)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        again = _forward(logits, idx, mask, offsets)
+        d2 = _backward(logits, 6, again[0], again[2], mask, offsets, None)
+        torch.cuda.current_stream().synchronize()
+    for a, b in zip(first + (d,), again + (d2,)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+def test_addend_in_place_and_masks_at_odd_addresses():
+    import torch
+    import paper_2504_14960_amd as moe
+    logits, idx, mask, offsets = _inputs(300, 20, 2, 3, 0.3)
+    counts, _, n, _ = _forward(logits, idx, mask, offsets)
+    addend = np.random.default_rng(3).standard_normal((300, 20)).astype(np.float32)
+    want = _backward(logits, 2, counts, n, mask, offsets, None, addend)
+    out = _dev(addend)
+    room = torch.zeros(301, dtype=torch.uint8, device="cuda")
+    room[1:] = _dev(mask)
+    moe.balance_loss_backward(_dev(logits), counts, n, None, 2, 0.01, 0.001, out, addend=out, token_mask=room[1:],
+                              seq_offsets=_dev(offsets))
+    assert torch.equal(out, want)
+    moe.balance_loss_backward(_dev(logits), counts, n, None, 2, 0.01, 0.001, out.copy_(_dev(addend)), addend=out,
+                              token_mask=room[1:].bool(), seq_offsets=_dev(offsets))
+    assert torch.equal(out, want)
+
+
+@pytest.mark.gpu
+def test_offsets_that_break_their_rules_stay_in_bounds():
+    """Offsets are device data that nobody checks: whatever they hold, only rows of the call are read and written."""
+    import torch
+    import paper_2504_14960_amd as moe
+    logits, idx, _, _ = _inputs(500, 8, 2)
+    for bad in ([0, 400, 100, 500], [-5, 1 << 30, 250, -(1 << 31)], [500, 0, 0, 0], [3, 3, 3, 3]):
+        offsets = np.array(bad, dtype=np.int32)
+        counts, sums, n, losses = _forward(logits, idx, None, offsets)
+        room = torch.full((700, 8), -7.0, device="cuda")
+        moe.balance_loss_backward(_dev(logits), counts, n, None, 2, 0.01, 0.001, room[100:600], seq_offsets=_dev(offsets))
+        torch.cuda.synchronize()
+        assert (room[:100] == -7).all() and (room[600:] == -7).all()
+
+
+@pytest.mark.gpu
+def test_replayed_in_a_graph():
+    import torch
+    import paper_2504_14960_amd as moe
+    logits, idx, mask, offsets = (_dev(a) for a in _inputs(3000, 64, 6, 5, 0.1))
+    counts, sums = torch.zeros((5, 64), dtype=torch.int32, device="cuda"), torch.zeros((5, 64), device="cuda")
+    n, losses, out = torch.zeros(6, dtype=torch.int32, device="cuda"), torch.zeros(2, device="cuda"), torch.zeros((3000, 64), device="cuda")
+    ws = torch.empty(moe.balance_loss_workspace_bytes(3000, 64, 5), dtype=torch.uint8, device="cuda")
+
+    def step():
+        moe.balance_loss(logits, idx, 0.01, 0.001, counts, sums, n, losses, ws, token_mask=mask, seq_offsets=offsets)
+        moe.balance_loss_backward(logits, counts, n, None, 6, 0.01, 0.001, out, token_mask=mask, seq_offsets=offsets)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(4):
+        logits.mul_(1.1)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (counts, sums, n, losses, out)]
+        step()
+        torch.cuda.synchronize()
+        for a, b in zip(got, (counts, sums, n, losses, out)):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,E,K", [(100, 8, 2), (40000, 8, 2), (300, 64, 6), (200, 100, 4), (200, 200, 8)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_router_backward_adds_the_gradient(T, E, K, dtype):
+    """dlogits = the gates' gradient + the addend, one rounding; dx, dW and dbias from the sum, in fp32 (as many products
+    as there are tokens or experts: 300 eps) and, for bf16 dx, one rounding more (2^-8)."""
+    import torch
+    import paper_2504_14960_amd as moe
+    H = 64
+    kind = torch.float32 if dtype == "f32" else torch.bfloat16
+    logits, idx, _, _ = _inputs(T, E, K)
+    rng = np.random.default_rng(5)
+    x, w = (_dev(rng.standard_normal(s).astype(np.float32)).to(kind) for s in ((T, H), (E, H)))
+    dgate = _dev(rng.standard_normal((T, K)).astype(np.float32))
+    addend = _dev(rng.standard_normal((T, E)).astype(np.float32) * 0.1)
+    ws = torch.empty(moe.router_backward_workspace_bytes(T, H, E), dtype=torch.uint8, device="cuda")
+
+    def call(addend):
+        dl, dx = torch.empty((T, E), device="cuda"), torch.empty((T, H), dtype=kind, device="cuda")
+        dw, db = torch.empty((E, H), device="cuda"), torch.empty(E, device="cuda")
+        moe.router_backward(x, w, _dev(logits), _dev(idx), dgate, True, dl, dx, dw, db, ws, dlogits_addend=addend)
+        return dl, dx, dw, db
+
+    plain, added, zero = call(None), call(addend), call(torch.zeros_like(addend))
+    for a, b in zip(plain, zero):
+        assert torch.equal(a, b)
+    assert torch.equal(added[0], plain[0] + addend)
+    dl, wd, xd = added[0].double().cpu(), w.double().cpu(), x.double().cpu()
+    for got, want, size, tol in ((added[1], dl @ wd, dl.abs() @ wd.abs(), 300 * EPS + (2.0 ** -8 if dtype == "bf16" else 0)),
+                                 (added[2], dl.T @ xd, dl.T.abs() @ xd.abs(), 300 * EPS),
+                                 (added[3], dl.sum(0), dl.abs().sum(0), 300 * EPS)):
+        assert ((got.double().cpu() - want).abs() <= tol * size + 1e-30).all()
+
+
+def test_refusals():
+    import paper_2504_14960_amd as moe
+    L = moe.lib()
+    p, odd = C.c_void_p(0x1000), C.c_void_p(0x1004)
+
+    def forward(logits=p, idx=p, mask=None, offsets=None, T=16, E=8, K=2, S=1, cb=1.0, cz=1.0, counts=p, sums=p, n=p,
+                losses=p, ws=p, size=1 << 20):
+        return L.moe_balance_loss(logits, idx, mask, offsets, T, E, K, S, cb, cz, counts, sums, n, losses, ws, size, None)
+
+    def backward(logits=p, mask=None, offsets=None, counts=p, n=p, d=None, addend=None, T=16, E=8, K=2, S=1, cb=1.0, cz=1.0,
+                 out=p):
+        return L.moe_balance_loss_backward(logits, mask, offsets, counts, n, d, addend, T, E, K, S, cb, cz, out, None)
+
+    nan = float("nan")
+    for kw, status, word in [(dict(T=-1), 1, b"T >= 0"), (dict(K=9), 1, b"exceeds E"), (dict(E=257), 2, b"limit"),
+                             (dict(S=0), 1, b"n_seq"), (dict(S=2), 1, b"seq_offsets"), (dict(S=65537, offsets=p), 2, b"limit"),
+                             (dict(cb=nan), 1, b"finite"), (dict(cz=float("inf")), 1, b"finite"),
+                             (dict(logits=None), 1, b"NULL"), (dict(logits=odd), 1, b"aligned"), (dict(counts=None), 1, b"NULL"),
+                             (dict(offsets=C.c_void_p(0x1002)), 1, b"aligned"), (dict(n=None), 1, b"NULL")]:
+        for call in (forward, backward):
+            assert call(**kw) == status and word in L.moe_last_error(), (call.__name__, kw, L.moe_last_error())
+    for kw, status in [(dict(idx=None), 1), (dict(sums=odd), 1), (dict(losses=None), 1), (dict(losses=C.c_void_p(0x1001)), 1),
+                       (dict(ws=None), 3), (dict(size=16), 3), (dict(ws=odd), 1)]:
+        assert forward(**kw) == status, kw
+    for kw in (dict(out=None), dict(addend=odd), dict(d=C.c_void_p(0x1002)), dict(out=odd)):
+        assert backward(**kw) == 1, kw
+    assert backward(T=0, logits=None) == 0
+    st = L.moe_router_backward_addend(p, p, p, p, p, p, 16, 64, 8, 2, 0, moe.MOE_BF16, p, p, p, None, p, 1 << 30, None)
+    assert st == 1 and b"dlogits_addend is dlogits" in L.moe_last_error()
+    assert moe.balance_loss_workspace_bytes(-1, 8) == 0
