@@ -9,19 +9,22 @@ namespace moe {
 namespace {
 
 constexpr int kListTensors = 48;   // 80 bytes each: a launch's arguments are limited to 4 KiB
-constexpr int kChunk = 2048;       // elements of a workgroup; a multiple of the 8-bit states' blocks
+constexpr int kChunk = 4096;       // elements of a workgroup; a multiple of the 8-bit states' blocks
 constexpr int kBlock = 32;         // elements that share a scale
 constexpr int64_t kLaunchChunks = (1 << 24) - 1;   // 256 threads each: a grid has less than 2^32 threads
 
 // -------------------------------------------------------------------------------------------------------------
 // lists
 
+// A gradient's bytes are cut into runs; the tensors of a launch have at most 192 pointers, lengths and first runs in 4 KiB.
+constexpr int kGradTensors = 192;
+constexpr int kRunBytes = 256 * 16 * 4;   // four 16-byte loads of every thread
+
 struct GradList {
-    const void* grad[kListTensors];
-    int64_t n[kListTensors];
-    int32_t first[kListTensors];   // first chunk
-    uint8_t bf16[kListTensors];
-    int32_t count, chunks;
+    const void* grad[kGradTensors];
+    uint64_t n[kGradTensors];        // elements; bit 63: bf16
+    int32_t first[kGradTensors];     // first run
+    int32_t count, runs;
 };
 
 template <typename List>
@@ -54,16 +57,60 @@ __device__ __forceinline__ double group_sum(double v, double* red) {
     return red[0];
 }
 
+// Sum of the squares of 16 bytes of values.  In 64 bits: a square of an fp32 number neither overflows nor vanishes, and the
+// additions stay far below the rate at which memory delivers.
+template <bool BF16>
+__device__ __forceinline__ double square_sum(const u32x4& r) {
+    double a = 0., b = 0.;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (BF16) {
+            const double lo = __uint_as_float(r[j] << 16), hi = __uint_as_float(r[j] & 0xffff0000u);
+            a = fma(lo, lo, a);
+            b = fma(hi, hi, b);
+        } else {
+            const double x = __uint_as_float(r[j]);
+            if (j & 1) b = fma(x, x, b);
+            else a = fma(x, x, a);
+        }
+    }
+    return a + b;
+}
+
+template <bool BF16>
+__device__ __forceinline__ double run_square_sum(const void* grad, uint64_t n, uint64_t run) {
+    constexpr int kVec = BF16 ? 8 : 4;                     // elements of a load
+    constexpr int kElements = kRunBytes / (BF16 ? 2 : 4);
+    const uint64_t at = run * kElements;
+    if (at + kElements <= n) {
+        const u32x4* p = reinterpret_cast<const u32x4*>(grad) + at / kVec + threadIdx.x;
+        u32x4 r[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) r[u] = __builtin_nontemporal_load(p + u * 256);
+        double acc = 0.;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) acc += square_sum<BF16>(r[u]);
+        return acc;
+    }
+    double acc = 0.;
+    for (uint64_t j = at + threadIdx.x; j < n; j += 256) {
+        const double g = load_value(grad, BF16, (int64_t)j);
+        acc = fma(g, g, acc);
+    }
+    return acc;
+}
+
+// Workgroup g takes the runs [g runs / G, (g + 1) runs / G): the order of the sums depends on the sizes alone.
 __global__ __launch_bounds__(256) void grad_norm_partial_kernel(GradList l, double* __restrict__ partial) {
     __shared__ double red[256];
+    const int from = (int)((int64_t)l.runs * blockIdx.x / gridDim.x), to = (int)((int64_t)l.runs * (blockIdx.x + 1) / gridDim.x);
     double acc = 0.;
-    for (int chunk = blockIdx.x; chunk < l.chunks; chunk += gridDim.x) {
-        const int i = find_tensor(l, chunk);
-        const int64_t at = (int64_t)(chunk - l.first[i]) * kChunk;
-        for (int64_t j = at + threadIdx.x; j < min(at + kChunk, l.n[i]); j += 256) {
-            const double g = load_value(l.grad[i], l.bf16[i], j);
-            acc += g * g;
-        }
+    int i = find_tensor(l, from);
+    for (int run = from; run < to; ++run) {
+        while (i + 1 < l.count && l.first[i + 1] <= run) ++i;
+        const uint64_t n = l.n[i];
+        acc += n >> 63 ? run_square_sum<true>(l.grad[i], n & ~(1ull << 63), run - l.first[i])
+                       : run_square_sum<false>(l.grad[i], n, run - l.first[i]);
     }
     acc = group_sum(acc, red);
     if (threadIdx.x == 0) partial[blockIdx.x] = acc;
@@ -98,7 +145,7 @@ struct AdamTensor {
     int64_t n;
     float decay, step_size;   // 1 - lr wd, lr / (1 - beta1^t)
     int32_t index;            // place in the caller's list
-    uint8_t param_bf16, grad_bf16, mxfp8;
+    int32_t kind;
 };
 
 struct AdamList {
@@ -137,8 +184,6 @@ __device__ __forceinline__ uint32_t scale_of(uint32_t top) {
     return (uint32_t)max((int)((top + 0x1fffffu) >> 23) - 8, 1);
 }
 
-__device__ __forceinline__ float from_e4m3(uint32_t code) { return __builtin_amdgcn_cvt_f32_fp8((int)code, 0); }
-
 // magnitude of an E4M3 code, |x| <= 448, rounded up with the probability of the part cut off: 16 random bits in the middle
 // of their step are added below the last kept bit
 __device__ __forceinline__ uint32_t to_e4m3(float magnitude, uint32_t random16) {
@@ -147,74 +192,205 @@ __device__ __forceinline__ uint32_t to_e4m3(float magnitude, uint32_t random16) 
     return ((uint32_t)(magnitude * 0x1p29f) + r) >> 20;   // steps of 2^-9
 }
 
-__global__ __launch_bounds__(256) void adamw_kernel(AdamList l, AdamStep h) {
+// Four consecutive values; in a tensor's last ones, where fewer are left, one by one.
+__device__ __forceinline__ void load4(const float* p, int64_t j, int left, float (&x)[4]) {
+    if (left >= 4) {
+        const f32x4 r = *reinterpret_cast<const f32x4*>(p + j);
+        x[0] = r[0]; x[1] = r[1]; x[2] = r[2]; x[3] = r[3];
+    } else {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[u] = u < left ? p[j + u] : 0.f;
+    }
+}
+__device__ __forceinline__ void load4(const bf16_t* p, int64_t j, int left, float (&x)[4]) {
+    if (left >= 4) {
+        const u32x2 r = *reinterpret_cast<const u32x2*>(p + j);
+        x[0] = __uint_as_float(r[0] << 16);
+        x[1] = __uint_as_float(r[0] & 0xffff0000u);
+        x[2] = __uint_as_float(r[1] << 16);
+        x[3] = __uint_as_float(r[1] & 0xffff0000u);
+    } else {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[u] = u < left ? bf16_to_f32(p[j + u]) : 0.f;
+    }
+}
+__device__ __forceinline__ uint32_t load4(const uint8_t* p, int64_t j, int left) {
+    if (left >= 4) return *reinterpret_cast<const uint32_t*>(p + j);
+    uint32_t r = 0;
+#pragma unroll
+    for (int u = 0; u < 3; ++u) r |= u < left ? (uint32_t)p[j + u] << (8 * u) : 0u;
+    return r;
+}
+__device__ __forceinline__ void store4(float* p, int64_t j, int left, const float (&x)[4]) {
+    if (left >= 4) {
+        *reinterpret_cast<f32x4*>(p + j) = f32x4{x[0], x[1], x[2], x[3]};
+    } else {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (u < left) p[j + u] = x[u];
+    }
+}
+__device__ __forceinline__ void store4(bf16_t* p, int64_t j, int left, uint32_t lo, uint32_t hi) {
+    if (left >= 4) {
+        *reinterpret_cast<u32x2*>(p + j) = u32x2{lo, hi};
+    } else {
+        if (left > 0) p[j] = (bf16_t)lo;
+        if (left > 1) p[j + 1] = (bf16_t)(lo >> 16);
+        if (left > 2) p[j + 2] = (bf16_t)hi;
+    }
+}
+__device__ __forceinline__ void store4(uint8_t* p, int64_t j, int left, uint32_t r) {
+    if (left >= 4) {
+        *reinterpret_cast<uint32_t*>(p + j) = r;
+    } else {
+#pragma unroll
+        for (int u = 0; u < 3; ++u)
+            if (u < left) p[j + u] = (uint8_t)(r >> (8 * u));
+    }
+}
+
+enum { kParamF32, kParamMaster, kParamBf16 };
+
+// The largest magnitude, as bits, of the 8 lanes that hold a block of 32 elements.
+__device__ __forceinline__ uint32_t block_max(uint32_t v) {
+    v = max(v, (uint32_t)__shfl_xor((int)v, 1, 64));
+    v = max(v, (uint32_t)__shfl_xor((int)v, 2, 64));
+    return max(v, (uint32_t)__shfl_xor((int)v, 4, 64));
+}
+
+// Codes and scale of a lane's four values.
+template <bool POSITIVE>
+__device__ __forceinline__ uint32_t quantize4(const float (&x)[4], const uint32_t (&random16)[4], uint32_t& scale) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) top = max(top, __float_as_uint(x[u]) & 0x7fffffffu);
+    scale = scale_of(block_max(top));
+    if (scale == 255) return 0x7f7f7f7fu;
+    const float inverse = __uint_as_float((254 - scale) << 23);
+    uint32_t codes = 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const float y = x[u] * inverse;
+        uint32_t c = to_e4m3(fabsf(y), random16[u]);
+        if (POSITIVE) c = c == 0 && x[u] > 0.f ? 1u : c;
+        else c |= __float_as_uint(y) >> 24 & 0x80u;
+        codes |= c << (8 * u);
+    }
+    return codes;
+}
+
+template <int PARAM, bool GRAD_BF16, bool MXFP8>
+__device__ __forceinline__ void adamw_chunk(const AdamTensor& t, const AdamStep& h, float scale, int64_t at) {
 #pragma clang fp contract(off)
+    const int64_t end = min(at + kChunk, t.n);
+    for (int64_t base = at; base < end; base += 1024) {
+        const int64_t j = base + 4 * threadIdx.x;
+        const int left = (int)min((int64_t)4, end - j);   // none or negative: this lane has nothing
+        const int64_t block = min(j, end - 1) / kBlock;
+        float p[4], g[4], m[4], v[4];
+        if (GRAD_BF16) load4(static_cast<const bf16_t*>(t.grad), j, left, g);
+        else load4(static_cast<const float*>(t.grad), j, left, g);
+        if (PARAM == kParamF32) load4(static_cast<const float*>(t.param), j, left, p);
+        else if (PARAM == kParamMaster) load4(t.master, j, left, p);
+        else load4(static_cast<const bf16_t*>(t.param), j, left, p);
+        if (MXFP8) {
+            const uint32_t cm = load4(static_cast<const uint8_t*>(t.m), j, left), cv = load4(static_cast<const uint8_t*>(t.v), j, left);
+            const float sm = scale_value(t.m_scale[block]), sv = scale_value(t.v_scale[block]);
+            m[0] = __builtin_amdgcn_cvt_f32_fp8((int)cm, 0) * sm;
+            m[1] = __builtin_amdgcn_cvt_f32_fp8((int)cm, 1) * sm;
+            m[2] = __builtin_amdgcn_cvt_f32_fp8((int)cm, 2) * sm;
+            m[3] = __builtin_amdgcn_cvt_f32_fp8((int)cm, 3) * sm;
+            v[0] = __builtin_amdgcn_cvt_f32_fp8((int)cv, 0) * sv;
+            v[1] = __builtin_amdgcn_cvt_f32_fp8((int)cv, 1) * sv;
+            v[2] = __builtin_amdgcn_cvt_f32_fp8((int)cv, 2) * sv;
+            v[3] = __builtin_amdgcn_cvt_f32_fp8((int)cv, 3) * sv;
+        } else {
+            load4(static_cast<const float*>(t.m), j, left, m);
+            load4(static_cast<const float*>(t.v), j, left, v);
+        }
+        uint32_t bits[4] = {0, 0, 0, 0};
+        if (MXFP8 || PARAM == kParamBf16) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) bits[u] = random_bits(h.seed, t.index, j + u);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            g[u] *= scale;
+            m[u] = m[u] * h.beta1 + g[u] * h.one_minus_beta1;
+            v[u] = v[u] * h.beta2 + (g[u] * g[u]) * h.one_minus_beta2;
+            const float denom = sqrtf(v[u]) * h.rsqrt_bc2 + h.eps;
+            p[u] = p[u] * t.decay - (m[u] / denom) * t.step_size;
+        }
+        if (MXFP8) {
+            if (left <= 0) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) m[u] = v[u] = 0.f;
+            } else {
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (u >= left) m[u] = v[u] = 0.f;
+            }
+            uint32_t rm[4], rv[4], sm, sv;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                rm[u] = bits[u] & 0xffffu;
+                rv[u] = bits[u] >> 16;
+            }
+            const uint32_t cm = quantize4<false>(m, rm, sm), cv = quantize4<true>(v, rv, sv);
+            store4(static_cast<uint8_t*>(t.m), j, left, cm);
+            store4(static_cast<uint8_t*>(t.v), j, left, cv);
+            if (threadIdx.x % 8 == 0 && left > 0) {
+                t.m_scale[block] = (uint8_t)sm;
+                t.v_scale[block] = (uint8_t)sv;
+            }
+        } else {
+            store4(static_cast<float*>(t.m), j, left, m);
+            store4(static_cast<float*>(t.v), j, left, v);
+        }
+        if (PARAM == kParamF32) {
+            store4(static_cast<float*>(t.param), j, left, p);
+        } else if (PARAM == kParamMaster) {
+            store4(t.master, j, left, p);
+            store4(static_cast<bf16_t*>(t.param), j, left, pack2_bf16(p[0], p[1]), pack2_bf16(p[2], p[3]));
+        } else {
+            uint32_t r[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const uint32_t x = __float_as_uint(p[u]);
+                const bool finite = (x & 0x7f800000u) != 0x7f800000u;
+                r[u] = finite ? (x + ((bits[u] * 0x9e3779b1u) >> 16)) >> 16 : (uint32_t)f32_to_bf16(p[u]);
+            }
+            store4(static_cast<bf16_t*>(t.param), j, left, r[0] | r[1] << 16, r[2] | r[3] << 16);
+        }
+    }
+}
+
+__global__ __launch_bounds__(256) void adamw_kernel(AdamList l, AdamStep h) {
     const float scale = h.grad_scale ? *h.grad_scale : 1.f;
     if (scale != scale) return;
     const int i = find_tensor(l, blockIdx.x);
     const AdamTensor& t = l.t[i];
     const int64_t at = (int64_t)((int)blockIdx.x - l.first[i]) * kChunk;
-    for (int64_t j = at + threadIdx.x; j - (int)threadIdx.x < min(at + kChunk, t.n); j += 256) {
-        const bool ok = j < t.n;
-        const int64_t k = ok ? j : t.n - 1;
-        const int64_t block = k / kBlock;
-        const float g = load_value(t.grad, t.grad_bf16, k) * scale;
-        float p = t.master ? t.master[k] : load_value(t.param, t.param_bf16, k);
-        float m, v;
-        if (t.mxfp8) {
-            m = from_e4m3(static_cast<uint8_t*>(t.m)[k]) * scale_value(t.m_scale[block]);
-            v = from_e4m3(static_cast<uint8_t*>(t.v)[k]) * scale_value(t.v_scale[block]);
-        } else {
-            m = static_cast<float*>(t.m)[k];
-            v = static_cast<float*>(t.v)[k];
-        }
-        m = m * h.beta1 + g * h.one_minus_beta1;
-        v = v * h.beta2 + (g * g) * h.one_minus_beta2;
-        const float denom = sqrtf(v) * h.rsqrt_bc2 + h.eps;
-        p = p * t.decay - (m / denom) * t.step_size;
-        const uint32_t bits = random_bits(h.seed, t.index, k);
-        if (t.mxfp8) {
-            // the largest magnitudes of the block: 32 lanes, as bits, which order NaN above all
-            uint32_t top_m = ok ? __float_as_uint(m) & 0x7fffffffu : 0u, top_v = ok ? __float_as_uint(v) & 0x7fffffffu : 0u;
-#pragma unroll
-            for (int off = 16; off > 0; off >>= 1) {
-                top_m = max(top_m, (uint32_t)__shfl_xor((int)top_m, off, 32));
-                top_v = max(top_v, (uint32_t)__shfl_xor((int)top_v, off, 32));
-            }
-            const uint32_t sm = scale_of(top_m), sv = scale_of(top_v);
-            uint32_t cm = 0x7f, cv = 0x7f;
-            if (sm != 255) {
-                const float y = m * __uint_as_float((254 - sm) << 23);
-                cm = to_e4m3(fabsf(y), bits & 0xffffu) | (__float_as_uint(y) >> 24 & 0x80u);
-            }
-            if (sv != 255) {
-                cv = to_e4m3(v * __uint_as_float((254 - sv) << 23), bits >> 16);
-                if (cv == 0 && v > 0.f) cv = 1;
-            }
-            if (ok) {
-                static_cast<uint8_t*>(t.m)[k] = (uint8_t)cm;
-                static_cast<uint8_t*>(t.v)[k] = (uint8_t)cv;
-                if (k % kBlock == 0) {
-                    t.m_scale[block] = (uint8_t)sm;
-                    t.v_scale[block] = (uint8_t)sv;
-                }
-            }
-        } else if (ok) {
-            static_cast<float*>(t.m)[k] = m;
-            static_cast<float*>(t.v)[k] = v;
-        }
-        if (!ok) continue;
-        if (!t.param_bf16) {
-            static_cast<float*>(t.param)[k] = p;
-        } else if (t.master) {
-            t.master[k] = p;
-            static_cast<bf16_t*>(t.param)[k] = f32_to_bf16(p);
-        } else {
-            const uint32_t u = __float_as_uint(p);
-            const bool finite = (u & 0x7f800000u) != 0x7f800000u;
-            static_cast<bf16_t*>(t.param)[k] = finite ? (bf16_t)((u + ((bits * 0x9e3779b1u) >> 16)) >> 16) : f32_to_bf16(p);
-        }
+    switch (t.kind) {
+        case 0: return adamw_chunk<kParamF32, false, false>(t, h, scale, at);
+        case 1: return adamw_chunk<kParamF32, true, false>(t, h, scale, at);
+        case 2: return adamw_chunk<kParamMaster, false, false>(t, h, scale, at);
+        case 3: return adamw_chunk<kParamMaster, true, false>(t, h, scale, at);
+        case 4: return adamw_chunk<kParamBf16, false, false>(t, h, scale, at);
+        case 5: return adamw_chunk<kParamBf16, true, false>(t, h, scale, at);
+        case 6: return adamw_chunk<kParamF32, false, true>(t, h, scale, at);
+        case 7: return adamw_chunk<kParamF32, true, true>(t, h, scale, at);
+        case 8: return adamw_chunk<kParamMaster, false, true>(t, h, scale, at);
+        case 9: return adamw_chunk<kParamMaster, true, true>(t, h, scale, at);
+        case 10: return adamw_chunk<kParamBf16, false, true>(t, h, scale, at);
+        default: return adamw_chunk<kParamBf16, true, true>(t, h, scale, at);
     }
+}
+
+// place of a tensor's types in the switch above
+inline int kind_of(const moe_adamw_tensor_t& t) {
+    const int param = t.param_dt == MOE_F32 ? kParamF32 : t.master ? kParamMaster : kParamBf16;
+    return (t.state == MOE_STATE_MXFP8 ? 6 : 0) + 2 * param + (t.grad_dt == MOE_BF16 ? 1 : 0);
 }
 
 inline int64_t chunks_of(int64_t n) { return (n + kChunk - 1) / kChunk; }
@@ -222,7 +398,7 @@ inline int64_t chunks_of(int64_t n) { return (n + kChunk - 1) / kChunk; }
 }  // namespace
 
 size_t grad_norm_workspace_bytes(int count) {
-    // a launch takes one tensor at least; more than one launch for fewer than kListTensors only where chunks run out
+    // a launch takes one tensor at least; fewer than kGradTensors only where the runs run out
     return (size_t)(count > 0 ? count : 1) * kNormGroups * sizeof(double);
 }
 
@@ -231,26 +407,26 @@ void launch_grad_norm(const moe_grad_tensor_t* tensors, int count, float max_nor
     double* partial = static_cast<double*>(ws);
     int parts = 0;
     GradList l;
-    int64_t chunks = 0;
+    int64_t runs = 0;
     l.count = 0;
     auto flush = [&] {
         if (l.count == 0) return;
-        l.chunks = (int32_t)chunks;
-        const int groups = (int)(chunks < kNormGroups ? chunks : kNormGroups);
+        l.runs = (int32_t)runs;
+        const int groups = (int)(runs < kNormGroups ? runs : kNormGroups);
         hipLaunchKernelGGL(grad_norm_partial_kernel, dim3(groups), dim3(256), 0, s, l, partial + parts);
         parts += groups;
         l.count = 0;
-        chunks = 0;
+        runs = 0;
     };
     for (int i = 0; i < count; ++i) {
-        const int64_t more = chunks_of(tensors[i].n);
+        const bool bf16 = tensors[i].dt == MOE_BF16;
+        const int64_t more = (tensors[i].n * (bf16 ? 2 : 4) + kRunBytes - 1) / kRunBytes;
         if (more == 0) continue;
-        if (l.count == kListTensors || chunks + more > kLaunchChunks) flush();
+        if (l.count == kGradTensors || runs + more > (1 << 30)) flush();
         l.grad[l.count] = tensors[i].grad;
-        l.n[l.count] = tensors[i].n;
-        l.bf16[l.count] = tensors[i].dt == MOE_BF16;
-        l.first[l.count++] = (int32_t)chunks;
-        chunks += more;
+        l.n[l.count] = (uint64_t)tensors[i].n | (bf16 ? 1ull << 63 : 0);
+        l.first[l.count++] = (int32_t)runs;
+        runs += more;
     }
     flush();
     hipLaunchKernelGGL(grad_norm_finish_kernel, dim3(1), dim3(256), 0, s, partial, parts, max_norm, multiplier, out);
@@ -277,8 +453,7 @@ void launch_adamw(const moe_adamw_tensor_t* tensors, int count, double lr, doubl
         const double lr_i = lr * t.lr_scale;
         l.first[l.count] = (int32_t)chunks;
         l.t[l.count++] = {t.param, t.master, t.grad, t.exp_avg, t.exp_avg_sq, t.exp_avg_scale, t.exp_avg_sq_scale, t.n,
-                          (float)(1. - lr_i * t.weight_decay), (float)(lr_i / bc1), i, t.param_dt == MOE_BF16,
-                          t.grad_dt == MOE_BF16, t.state == MOE_STATE_MXFP8};
+                          (float)(1. - lr_i * t.weight_decay), (float)(lr_i / bc1), i, kind_of(t)};
         chunks += more;
     }
     flush();
