@@ -184,183 +184,214 @@ __device__ __forceinline__ uint32_t scale_of(uint32_t top) {
     return (uint32_t)max((int)((top + 0x1fffffu) >> 23) - 8, 1);
 }
 
-// magnitude of an E4M3 code, |x| <= 448, rounded up with the probability of the part cut off: 16 random bits in the middle
-// of their step are added below the last kept bit
-__device__ __forceinline__ uint32_t to_e4m3(float magnitude, uint32_t random16) {
-    const uint32_t r = (random16 << 4) | 8u;
-    if (magnitude >= 0x1p-6f) return ((__float_as_uint(magnitude) + r) >> 20) - (120u << 3);
-    return ((uint32_t)(magnitude * 0x1p29f) + r) >> 20;   // steps of 2^-9
-}
-
-// Four consecutive values; in a tensor's last ones, where fewer are left, one by one.
-__device__ __forceinline__ void load4(const float* p, int64_t j, int left, float (&x)[4]) {
-    if (left >= 4) {
-        const f32x4 r = *reinterpret_cast<const f32x4*>(p + j);
-        x[0] = r[0]; x[1] = r[1]; x[2] = r[2]; x[3] = r[3];
+// A lane's V consecutive values; where fewer are left at a tensor's end, one by one.
+template <int V>
+__device__ __forceinline__ void load(const float* p, int64_t j, int left, float (&x)[V]) {
+    if (left >= V) {
+#pragma unroll
+        for (int q = 0; q < V; q += 4) {
+            const f32x4 r = *reinterpret_cast<const f32x4*>(p + j + q);
+            x[q] = r[0]; x[q + 1] = r[1]; x[q + 2] = r[2]; x[q + 3] = r[3];
+        }
     } else {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) x[u] = u < left ? p[j + u] : 0.f;
+        for (int u = 0; u < V; ++u) x[u] = u < left ? p[j + u] : 0.f;
     }
 }
-__device__ __forceinline__ void load4(const bf16_t* p, int64_t j, int left, float (&x)[4]) {
-    if (left >= 4) {
-        const u32x2 r = *reinterpret_cast<const u32x2*>(p + j);
-        x[0] = __uint_as_float(r[0] << 16);
-        x[1] = __uint_as_float(r[0] & 0xffff0000u);
-        x[2] = __uint_as_float(r[1] << 16);
-        x[3] = __uint_as_float(r[1] & 0xffff0000u);
+template <int V>
+__device__ __forceinline__ void load(const bf16_t* p, int64_t j, int left, float (&x)[V]) {
+    if (left >= V) {
+        typedef __attribute__((ext_vector_type(V / 2))) uint32_t words;
+        const words r = *reinterpret_cast<const words*>(p + j);
+#pragma unroll
+        for (int q = 0; q < V / 2; ++q) {
+            x[2 * q] = __uint_as_float(r[q] << 16);
+            x[2 * q + 1] = __uint_as_float(r[q] & 0xffff0000u);
+        }
     } else {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) x[u] = u < left ? bf16_to_f32(p[j + u]) : 0.f;
+        for (int u = 0; u < V; ++u) x[u] = u < left ? bf16_to_f32(p[j + u]) : 0.f;
     }
 }
-__device__ __forceinline__ uint32_t load4(const uint8_t* p, int64_t j, int left) {
-    if (left >= 4) return *reinterpret_cast<const uint32_t*>(p + j);
-    uint32_t r = 0;
+template <int V>
+__device__ __forceinline__ void load(const uint8_t* p, int64_t j, int left, uint32_t (&x)[V / 4]) {
+    if (left >= V) {
+        typedef __attribute__((ext_vector_type(V / 4))) uint32_t words;
+        const words r = *reinterpret_cast<const words*>(p + j);
 #pragma unroll
-    for (int u = 0; u < 3; ++u) r |= u < left ? (uint32_t)p[j + u] << (8 * u) : 0u;
-    return r;
-}
-__device__ __forceinline__ void store4(float* p, int64_t j, int left, const float (&x)[4]) {
-    if (left >= 4) {
-        *reinterpret_cast<f32x4*>(p + j) = f32x4{x[0], x[1], x[2], x[3]};
+        for (int q = 0; q < V / 4; ++q) x[q] = r[q];
     } else {
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+        for (int q = 0; q < V / 4; ++q) x[q] = 0;
+#pragma unroll
+        for (int u = 0; u < V; ++u) x[u / 4] |= u < left ? (uint32_t)p[j + u] << (8 * (u % 4)) : 0u;
+    }
+}
+template <int V>
+__device__ __forceinline__ void store(float* p, int64_t j, int left, const float (&x)[V]) {
+    if (left >= V) {
+#pragma unroll
+        for (int q = 0; q < V; q += 4) *reinterpret_cast<f32x4*>(p + j + q) = f32x4{x[q], x[q + 1], x[q + 2], x[q + 3]};
+    } else {
+#pragma unroll
+        for (int u = 0; u < V; ++u)
             if (u < left) p[j + u] = x[u];
     }
 }
-__device__ __forceinline__ void store4(bf16_t* p, int64_t j, int left, uint32_t lo, uint32_t hi) {
-    if (left >= 4) {
-        *reinterpret_cast<u32x2*>(p + j) = u32x2{lo, hi};
-    } else {
-        if (left > 0) p[j] = (bf16_t)lo;
-        if (left > 1) p[j + 1] = (bf16_t)(lo >> 16);
-        if (left > 2) p[j + 2] = (bf16_t)hi;
-    }
-}
-__device__ __forceinline__ void store4(uint8_t* p, int64_t j, int left, uint32_t r) {
-    if (left >= 4) {
-        *reinterpret_cast<uint32_t*>(p + j) = r;
-    } else {
+// packed values of 32 / N bits each
+template <int V, typename T, int W>
+__device__ __forceinline__ void store_packed(T* p, int64_t j, int left, const uint32_t (&x)[W]) {
+    if (left >= V) {
+        typedef __attribute__((ext_vector_type(W))) uint32_t words;
+        words r;
 #pragma unroll
-        for (int u = 0; u < 3; ++u)
-            if (u < left) p[j + u] = (uint8_t)(r >> (8 * u));
+        for (int q = 0; q < W; ++q) r[q] = x[q];
+        *reinterpret_cast<words*>(p + j) = r;
+    } else {
+        constexpr int kPer = V / W, kBits = 32 / kPer;
+#pragma unroll
+        for (int u = 0; u < V; ++u)
+            if (u < left) p[j + u] = (T)(x[u / kPer] >> (kBits * (u % kPer)));
     }
 }
 
 enum { kParamF32, kParamMaster, kParamBf16 };
 
-// The largest magnitude, as bits, of the 8 lanes that hold a block of 32 elements.
+// The largest of the four neighbouring lanes that hold a block of 32 elements.
 __device__ __forceinline__ uint32_t block_max(uint32_t v) {
-    v = max(v, (uint32_t)__shfl_xor((int)v, 1, 64));
-    v = max(v, (uint32_t)__shfl_xor((int)v, 2, 64));
-    return max(v, (uint32_t)__shfl_xor((int)v, 4, 64));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, true));          // quad_perm 1, 0, 3, 2
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, true));       // quad_perm 2, 3, 0, 1
 }
 
-// Codes and scale of a lane's four values.
-template <bool POSITIVE>
-__device__ __forceinline__ uint32_t quantize4(const float (&x)[4], const uint32_t (&random16)[4], uint32_t& scale) {
+// E4M3 codes and scale of a lane's eight values.  The conversion instruction adds the upper 20 bits of its random number
+// below the last bit that is kept, in the denormal range too, and truncates: the rounding the interface defines, with 16
+// random bits in the middle of their step.  UPPER: which half of a value's 32 bits is its random number; those of the
+// second moment, which also stays above zero where it is (2^-9 is the smallest code).
+template <bool UPPER>
+__device__ __forceinline__ void quantize(const float (&x)[8], const uint32_t (&bits)[8], uint32_t (&codes)[2], uint32_t& scale) {
     uint32_t top = 0;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) top = max(top, __float_as_uint(x[u]) & 0x7fffffffu);
+    for (int u = 0; u < 8; ++u) top = max(top, __float_as_uint(x[u]) & 0x7fffffffu);
     scale = scale_of(block_max(top));
-    if (scale == 255) return 0x7f7f7f7fu;
-    const float inverse = __uint_as_float((254 - scale) << 23);
-    uint32_t codes = 0;
+    const float inverse = __uint_as_float((254 - (int)scale) << 23);
+    float y[8];
+    uint32_t r[8];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const float y = x[u] * inverse;
-        uint32_t c = to_e4m3(fabsf(y), random16[u]);
-        if (POSITIVE) c = c == 0 && x[u] > 0.f ? 1u : c;
-        else c |= __float_as_uint(y) >> 24 & 0x80u;
-        codes |= c << (8 * u);
+    for (int u = 0; u < 8; ++u) {
+        y[u] = x[u] * inverse;
+        if (UPPER) y[u] = fmaxf(y[u], x[u] > 0.f ? 0x1p-9f : 0.f);
+        r[u] = (UPPER ? bits[u] & 0xffff0000u : bits[u] << 16) | 0x8000u;
     }
-    return codes;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        int c = 0;
+        c = __builtin_amdgcn_cvt_sr_fp8_f32(y[4 * q], r[4 * q], c, 0);
+        c = __builtin_amdgcn_cvt_sr_fp8_f32(y[4 * q + 1], r[4 * q + 1], c, 1);
+        c = __builtin_amdgcn_cvt_sr_fp8_f32(y[4 * q + 2], r[4 * q + 2], c, 2);
+        c = __builtin_amdgcn_cvt_sr_fp8_f32(y[4 * q + 3], r[4 * q + 3], c, 3);
+        codes[q] = scale == 255 ? 0x7f7f7f7fu : (uint32_t)c;
+    }
 }
 
+__device__ __forceinline__ void dequantize(const uint32_t (&codes)[2], float scale, float (&x)[8]) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        x[4 * q] = __builtin_amdgcn_cvt_f32_fp8((int)codes[q], 0) * scale;
+        x[4 * q + 1] = __builtin_amdgcn_cvt_f32_fp8((int)codes[q], 1) * scale;
+        x[4 * q + 2] = __builtin_amdgcn_cvt_f32_fp8((int)codes[q], 2) * scale;
+        x[4 * q + 3] = __builtin_amdgcn_cvt_f32_fp8((int)codes[q], 3) * scale;
+    }
+}
+
+// Four elements to a lane with fp32 states, so that every access of a wave is one run of memory; eight with 8-bit ones,
+// where the work on a block is shared by fewer lanes.
 template <int PARAM, bool GRAD_BF16, bool MXFP8>
 __device__ __forceinline__ void adamw_chunk(const AdamTensor& t, const AdamStep& h, float scale, int64_t at) {
 #pragma clang fp contract(off)
+    constexpr int V = MXFP8 ? 8 : 4;
     const int64_t end = min(at + kChunk, t.n);
-    for (int64_t base = at; base < end; base += 1024) {
-        const int64_t j = base + 4 * threadIdx.x;
-        const int left = (int)min((int64_t)4, end - j);   // none or negative: this lane has nothing
+    for (int64_t base = at; base < end; base += 256 * V) {
+        const int64_t j = base + V * threadIdx.x;
+        const int left = (int)min((int64_t)V, end - j);   // none or negative: this lane has nothing
         const int64_t block = min(j, end - 1) / kBlock;
-        float p[4], g[4], m[4], v[4];
-        if (GRAD_BF16) load4(static_cast<const bf16_t*>(t.grad), j, left, g);
-        else load4(static_cast<const float*>(t.grad), j, left, g);
-        if (PARAM == kParamF32) load4(static_cast<const float*>(t.param), j, left, p);
-        else if (PARAM == kParamMaster) load4(t.master, j, left, p);
-        else load4(static_cast<const bf16_t*>(t.param), j, left, p);
-        if (MXFP8) {
-            const uint32_t cm = load4(static_cast<const uint8_t*>(t.m), j, left), cv = load4(static_cast<const uint8_t*>(t.v), j, left);
-            const float sm = scale_value(t.m_scale[block]), sv = scale_value(t.v_scale[block]);
-            m[0] = __builtin_amdgcn_cvt_f32_fp8((int)cm, 0) * sm;
-            m[1] = __builtin_amdgcn_cvt_f32_fp8((int)cm, 1) * sm;
-            m[2] = __builtin_amdgcn_cvt_f32_fp8((int)cm, 2) * sm;
-            m[3] = __builtin_amdgcn_cvt_f32_fp8((int)cm, 3) * sm;
-            v[0] = __builtin_amdgcn_cvt_f32_fp8((int)cv, 0) * sv;
-            v[1] = __builtin_amdgcn_cvt_f32_fp8((int)cv, 1) * sv;
-            v[2] = __builtin_amdgcn_cvt_f32_fp8((int)cv, 2) * sv;
-            v[3] = __builtin_amdgcn_cvt_f32_fp8((int)cv, 3) * sv;
+        float p[V], g[V], m[V], v[V];
+        if constexpr (GRAD_BF16) load<V>(static_cast<const bf16_t*>(t.grad), j, left, g);
+        else load<V>(static_cast<const float*>(t.grad), j, left, g);
+        if constexpr (PARAM == kParamF32) load<V>(static_cast<const float*>(t.param), j, left, p);
+        else if constexpr (PARAM == kParamMaster) load<V>(t.master, j, left, p);
+        else load<V>(static_cast<const bf16_t*>(t.param), j, left, p);
+        if constexpr (MXFP8) {
+            uint32_t cm[2], cv[2];
+            load<V>(static_cast<const uint8_t*>(t.m), j, left, cm);
+            load<V>(static_cast<const uint8_t*>(t.v), j, left, cv);
+            const uint32_t sm = t.m_scale[block], sv = t.v_scale[block];
+            dequantize(cm, scale_value(sm), m);
+            dequantize(cv, scale_value(sv), v);
         } else {
-            load4(static_cast<const float*>(t.m), j, left, m);
-            load4(static_cast<const float*>(t.v), j, left, v);
+            load<V>(static_cast<const float*>(t.m), j, left, m);
+            load<V>(static_cast<const float*>(t.v), j, left, v);
         }
-        uint32_t bits[4] = {0, 0, 0, 0};
+        uint32_t bits[V];
         if (MXFP8 || PARAM == kParamBf16) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) bits[u] = random_bits(h.seed, t.index, j + u);
+            for (int u = 0; u < V; ++u) bits[u] = random_bits(h.seed, t.index, j + u);
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < V; ++u) {
             g[u] *= scale;
             m[u] = m[u] * h.beta1 + g[u] * h.one_minus_beta1;
             v[u] = v[u] * h.beta2 + (g[u] * g[u]) * h.one_minus_beta2;
-            const float denom = sqrtf(v[u]) * h.rsqrt_bc2 + h.eps;
-            p[u] = p[u] * t.decay - (m[u] / denom) * t.step_size;
-        }
-        if (MXFP8) {
-            if (left <= 0) {
-#pragma unroll
-                for (int u = 0; u < 4; ++u) m[u] = v[u] = 0.f;
+            if constexpr (MXFP8) {
+                // the instructions' own square root and reciprocal, each within a unit of fp32: with 8-bit states the kernel
+                // is bound by what it computes
+                const float denom = __builtin_amdgcn_sqrtf(v[u]) * h.rsqrt_bc2 + h.eps;
+                p[u] = p[u] * t.decay - (m[u] * t.step_size) * __builtin_amdgcn_rcpf(denom);
             } else {
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (u >= left) m[u] = v[u] = 0.f;
+                const float denom = sqrtf(v[u]) * h.rsqrt_bc2 + h.eps;
+                p[u] = p[u] * t.decay - (m[u] / denom) * t.step_size;
             }
-            uint32_t rm[4], rv[4], sm, sv;
+        }
+        if constexpr (MXFP8) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                rm[u] = bits[u] & 0xffffu;
-                rv[u] = bits[u] >> 16;
+            for (int u = 0; u < V; ++u) {
+                m[u] = u < left ? m[u] : 0.f;   // what lies past the end has no part in the scale
+                v[u] = u < left ? v[u] : 0.f;
             }
-            const uint32_t cm = quantize4<false>(m, rm, sm), cv = quantize4<true>(v, rv, sv);
-            store4(static_cast<uint8_t*>(t.m), j, left, cm);
-            store4(static_cast<uint8_t*>(t.v), j, left, cv);
-            if (threadIdx.x % 8 == 0 && left > 0) {
+            uint32_t cm[2], cv[2], sm, sv;
+            quantize<false>(m, bits, cm, sm);
+            quantize<true>(v, bits, cv, sv);
+            store_packed<V>(static_cast<uint8_t*>(t.m), j, left, cm);
+            store_packed<V>(static_cast<uint8_t*>(t.v), j, left, cv);
+            if (threadIdx.x % 4 == 0 && left > 0) {
                 t.m_scale[block] = (uint8_t)sm;
                 t.v_scale[block] = (uint8_t)sv;
             }
         } else {
-            store4(static_cast<float*>(t.m), j, left, m);
-            store4(static_cast<float*>(t.v), j, left, v);
+            store<V>(static_cast<float*>(t.m), j, left, m);
+            store<V>(static_cast<float*>(t.v), j, left, v);
         }
-        if (PARAM == kParamF32) {
-            store4(static_cast<float*>(t.param), j, left, p);
-        } else if (PARAM == kParamMaster) {
-            store4(t.master, j, left, p);
-            store4(static_cast<bf16_t*>(t.param), j, left, pack2_bf16(p[0], p[1]), pack2_bf16(p[2], p[3]));
+        if constexpr (PARAM == kParamF32) {
+            store<V>(static_cast<float*>(t.param), j, left, p);
         } else {
-            uint32_t r[4];
+            uint32_t r[V / 2];
+            if constexpr (PARAM == kParamMaster) {
+                store<V>(t.master, j, left, p);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const uint32_t x = __float_as_uint(p[u]);
-                const bool finite = (x & 0x7f800000u) != 0x7f800000u;
-                r[u] = finite ? (x + ((bits[u] * 0x9e3779b1u) >> 16)) >> 16 : (uint32_t)f32_to_bf16(p[u]);
+                for (int q = 0; q < V / 2; ++q) r[q] = pack2_bf16(p[2 * q], p[2 * q + 1]);
+            } else {
+#pragma unroll
+                for (int q = 0; q < V / 2; ++q) {
+                    uint32_t x[2];
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const uint32_t b = __float_as_uint(p[2 * q + u]);
+                        const bool finite = (b & 0x7f800000u) != 0x7f800000u;
+                        x[u] = finite ? b + ((bits[2 * q + u] * 0x9e3779b1u) >> 16) : (uint32_t)f32_to_bf16(p[2 * q + u]) << 16;
+                    }
+                    r[q] = __builtin_amdgcn_perm(x[1], x[0], 0x07060302);   // the upper halves
+                }
             }
-            store4(static_cast<bf16_t*>(t.param), j, left, r[0] | r[1] << 16, r[2] | r[3] << 16);
+            store_packed<V>(static_cast<bf16_t*>(t.param), j, left, r);
         }
     }
 }
