@@ -2,6 +2,8 @@
 //
 // A launch takes up to kListTensors tensors, described in its arguments; every tensor is cut into chunks of kChunk
 // elements, and a workgroup finds its tensor from the first chunks.  Both are bound by memory.
+#include <type_traits>
+
 #include "common.h"
 
 namespace moe {
@@ -184,76 +186,61 @@ __device__ __forceinline__ uint32_t scale_of(uint32_t top) {
     return (uint32_t)max((int)((top + 0x1fffffu) >> 23) - 8, 1);
 }
 
-// A lane's V consecutive values; where fewer are left at a tensor's end, one by one.
-template <int V>
-__device__ __forceinline__ void load(const float* p, int64_t j, int left, float (&x)[V]) {
-    if (left >= V) {
+// V consecutive values of a lane as they lie in memory: words of 32 bits.  `left` of them exist; in a whole piece of a
+// tensor all do, and the access is as wide as it can be.
+template <int V, typename T>
+struct Packed {
+    static constexpr int kWords = V * sizeof(T) / 4, kPer = 4 / sizeof(T), kBits = 8 * sizeof(T);
+    typedef __attribute__((ext_vector_type(kWords < 4 ? kWords : 4))) uint32_t access_t;
+    static constexpr int kAccess = sizeof(access_t) / 4;
+    uint32_t w[kWords];
+
+    __device__ __forceinline__ void load(const void* base, int64_t j) {
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(static_cast<const T*>(base) + j);
 #pragma unroll
-        for (int q = 0; q < V; q += 4) {
-            const f32x4 r = *reinterpret_cast<const f32x4*>(p + j + q);
-            x[q] = r[0]; x[q + 1] = r[1]; x[q + 2] = r[2]; x[q + 3] = r[3];
+        for (int q = 0; q < kWords; q += kAccess) {
+            const access_t r = *reinterpret_cast<const access_t*>(p + q);
+#pragma unroll
+            for (int u = 0; u < kAccess; ++u) w[q + u] = r[u];
         }
-    } else {
-#pragma unroll
-        for (int u = 0; u < V; ++u) x[u] = u < left ? p[j + u] : 0.f;
     }
-}
-template <int V>
-__device__ __forceinline__ void load(const bf16_t* p, int64_t j, int left, float (&x)[V]) {
-    if (left >= V) {
-        typedef __attribute__((ext_vector_type(V / 2))) uint32_t words;
-        const words r = *reinterpret_cast<const words*>(p + j);
+    __device__ __forceinline__ void load_some(const void* base, int64_t j, int left) {
+        const T* p = static_cast<const T*>(base) + j;
 #pragma unroll
-        for (int q = 0; q < V / 2; ++q) {
-            x[2 * q] = __uint_as_float(r[q] << 16);
-            x[2 * q + 1] = __uint_as_float(r[q] & 0xffff0000u);
-        }
-    } else {
-#pragma unroll
-        for (int u = 0; u < V; ++u) x[u] = u < left ? bf16_to_f32(p[j + u]) : 0.f;
-    }
-}
-template <int V>
-__device__ __forceinline__ void load(const uint8_t* p, int64_t j, int left, uint32_t (&x)[V / 4]) {
-    if (left >= V) {
-        typedef __attribute__((ext_vector_type(V / 4))) uint32_t words;
-        const words r = *reinterpret_cast<const words*>(p + j);
-#pragma unroll
-        for (int q = 0; q < V / 4; ++q) x[q] = r[q];
-    } else {
-#pragma unroll
-        for (int q = 0; q < V / 4; ++q) x[q] = 0;
-#pragma unroll
-        for (int u = 0; u < V; ++u) x[u / 4] |= u < left ? (uint32_t)p[j + u] << (8 * (u % 4)) : 0u;
-    }
-}
-template <int V>
-__device__ __forceinline__ void store(float* p, int64_t j, int left, const float (&x)[V]) {
-    if (left >= V) {
-#pragma unroll
-        for (int q = 0; q < V; q += 4) *reinterpret_cast<f32x4*>(p + j + q) = f32x4{x[q], x[q + 1], x[q + 2], x[q + 3]};
-    } else {
+        for (int q = 0; q < kWords; ++q) w[q] = 0;
 #pragma unroll
         for (int u = 0; u < V; ++u)
-            if (u < left) p[j + u] = x[u];
+            if (u < left) w[u / kPer] |= (uint32_t)p[u] << (kBits * (u % kPer));
     }
-}
-// packed values of 32 / N bits each
-template <int V, typename T, int W>
-__device__ __forceinline__ void store_packed(T* p, int64_t j, int left, const uint32_t (&x)[W]) {
-    if (left >= V) {
-        typedef __attribute__((ext_vector_type(W))) uint32_t words;
-        words r;
+    __device__ __forceinline__ void store(void* base, int64_t j) const {
+        uint32_t* p = reinterpret_cast<uint32_t*>(static_cast<T*>(base) + j);
 #pragma unroll
-        for (int q = 0; q < W; ++q) r[q] = x[q];
-        *reinterpret_cast<words*>(p + j) = r;
-    } else {
-        constexpr int kPer = V / W, kBits = 32 / kPer;
+        for (int q = 0; q < kWords; q += kAccess) {
+            access_t r;
+#pragma unroll
+            for (int u = 0; u < kAccess; ++u) r[u] = w[q + u];
+            *reinterpret_cast<access_t*>(p + q) = r;
+        }
+    }
+    __device__ __forceinline__ void store_some(void* base, int64_t j, int left) const {
+        T* p = static_cast<T*>(base) + j;
 #pragma unroll
         for (int u = 0; u < V; ++u)
-            if (u < left) p[j + u] = (T)(x[u / kPer] >> (kBits * (u % kPer)));
+            if (u < left) p[u] = (T)(w[u / kPer] >> (kBits * (u % kPer)));
     }
-}
+    // values of fp32 or bf16 words
+    __device__ __forceinline__ void values(float (&x)[V]) const {
+#pragma unroll
+        for (int u = 0; u < V; ++u) {
+            if (sizeof(T) == 4) x[u] = __uint_as_float(w[u]);
+            else x[u] = __uint_as_float(u & 1 ? w[u / 2] & 0xffff0000u : w[u / 2] << 16);
+        }
+    }
+    __device__ __forceinline__ void set(const float (&x)[V]) {
+#pragma unroll
+        for (int u = 0; u < V; ++u) w[u] = __float_as_uint(x[u]);
+    }
+};
 
 enum { kParamF32, kParamMaster, kParamBf16 };
 
@@ -303,33 +290,67 @@ __device__ __forceinline__ void dequantize(const uint32_t (&codes)[2], float sca
     }
 }
 
+// What a lane reads of its V elements.
+template <int PARAM, bool GRAD_BF16, bool MXFP8>
+struct AdamInput {
+    static constexpr int V = MXFP8 ? 8 : 4;
+    typedef typename std::conditional<GRAD_BF16, bf16_t, uint32_t>::type grad_t;
+    typedef typename std::conditional<PARAM == kParamBf16, bf16_t, uint32_t>::type param_t;   // what is stepped
+    typedef typename std::conditional<MXFP8, uint8_t, uint32_t>::type state_t;
+    Packed<V, grad_t> g;
+    Packed<V, param_t> p;
+    Packed<V, state_t> m, v;
+    uint32_t m_scale, v_scale;
+
+    // piece: 256 V elements from `base` on, of which those below `end` exist
+    __device__ __forceinline__ void load(const AdamTensor& t, int64_t base, int64_t end) {
+        const int64_t j = base + V * threadIdx.x;
+        const void* param = PARAM == kParamMaster ? static_cast<const void*>(t.master) : t.param;
+        if (base + 256 * V <= end) {
+            g.load(t.grad, j);
+            p.load(param, j);
+            m.load(t.m, j);
+            v.load(t.v, j);
+        } else {
+            const int left = (int)min((int64_t)V, end - j);   // none or negative: this lane has nothing
+            g.load_some(t.grad, j, left);
+            p.load_some(param, j, left);
+            m.load_some(t.m, j, left);
+            v.load_some(t.v, j, left);
+        }
+        if constexpr (MXFP8) {
+            const int64_t block = min(j, end - 1) / kBlock;
+            m_scale = t.m_scale[block];
+            v_scale = t.v_scale[block];
+        }
+    }
+};
+
 // Four elements to a lane with fp32 states, so that every access of a wave is one run of memory; eight with 8-bit ones,
-// where the work on a block is shared by fewer lanes.
+// where the work on a block is shared by fewer lanes.  The next piece is on its way while one is worked on.
 template <int PARAM, bool GRAD_BF16, bool MXFP8>
 __device__ __forceinline__ void adamw_chunk(const AdamTensor& t, const AdamStep& h, float scale, int64_t at) {
 #pragma clang fp contract(off)
-    constexpr int V = MXFP8 ? 8 : 4;
+    typedef AdamInput<PARAM, GRAD_BF16, MXFP8> Input;
+    constexpr int V = Input::V;
     const int64_t end = min(at + kChunk, t.n);
+    Input in;
+    in.load(t, at, end);
     for (int64_t base = at; base < end; base += 256 * V) {
+        const Input cur = in;
+        if (base + 256 * V < end) in.load(t, base + 256 * V, end);
         const int64_t j = base + V * threadIdx.x;
-        const int left = (int)min((int64_t)V, end - j);   // none or negative: this lane has nothing
-        const int64_t block = min(j, end - 1) / kBlock;
+        const bool whole = base + 256 * V <= end;
+        const int left = (int)min((int64_t)V, end - j);
         float p[V], g[V], m[V], v[V];
-        if constexpr (GRAD_BF16) load<V>(static_cast<const bf16_t*>(t.grad), j, left, g);
-        else load<V>(static_cast<const float*>(t.grad), j, left, g);
-        if constexpr (PARAM == kParamF32) load<V>(static_cast<const float*>(t.param), j, left, p);
-        else if constexpr (PARAM == kParamMaster) load<V>(t.master, j, left, p);
-        else load<V>(static_cast<const bf16_t*>(t.param), j, left, p);
+        cur.g.values(g);
+        cur.p.values(p);
         if constexpr (MXFP8) {
-            uint32_t cm[2], cv[2];
-            load<V>(static_cast<const uint8_t*>(t.m), j, left, cm);
-            load<V>(static_cast<const uint8_t*>(t.v), j, left, cv);
-            const uint32_t sm = t.m_scale[block], sv = t.v_scale[block];
-            dequantize(cm, scale_value(sm), m);
-            dequantize(cv, scale_value(sv), v);
+            dequantize(cur.m.w, scale_value(cur.m_scale), m);
+            dequantize(cur.v.w, scale_value(cur.v_scale), v);
         } else {
-            load<V>(static_cast<const float*>(t.m), j, left, m);
-            load<V>(static_cast<const float*>(t.v), j, left, v);
+            cur.m.values(m);
+            cur.v.values(v);
         }
         uint32_t bits[V];
         if (MXFP8 || PARAM == kParamBf16) {
@@ -351,47 +372,59 @@ __device__ __forceinline__ void adamw_chunk(const AdamTensor& t, const AdamStep&
                 p[u] = p[u] * t.decay - (m[u] / denom) * t.step_size;
             }
         }
-        if constexpr (MXFP8) {
+        // new weights and states as they go to memory
+        Packed<V, uint32_t> p32;
+        Packed<V, bf16_t> p16;
+        Packed<V, typename Input::state_t> pm, pv;
+        if (PARAM != kParamBf16) p32.set(p);
+        if constexpr (PARAM == kParamMaster) {
 #pragma unroll
-            for (int u = 0; u < V; ++u) {
-                m[u] = u < left ? m[u] : 0.f;   // what lies past the end has no part in the scale
-                v[u] = u < left ? v[u] : 0.f;
-            }
-            uint32_t cm[2], cv[2], sm, sv;
-            quantize<false>(m, bits, cm, sm);
-            quantize<true>(v, bits, cv, sv);
-            store_packed<V>(static_cast<uint8_t*>(t.m), j, left, cm);
-            store_packed<V>(static_cast<uint8_t*>(t.v), j, left, cv);
-            if (threadIdx.x % 4 == 0 && left > 0) {
-                t.m_scale[block] = (uint8_t)sm;
-                t.v_scale[block] = (uint8_t)sv;
-            }
-        } else {
-            store<V>(static_cast<float*>(t.m), j, left, m);
-            store<V>(static_cast<float*>(t.v), j, left, v);
+            for (int q = 0; q < V / 2; ++q) p16.w[q] = pack2_bf16(p[2 * q], p[2 * q + 1]);
         }
-        if constexpr (PARAM == kParamF32) {
-            store<V>(static_cast<float*>(t.param), j, left, p);
-        } else {
-            uint32_t r[V / 2];
-            if constexpr (PARAM == kParamMaster) {
-                store<V>(t.master, j, left, p);
+        if constexpr (PARAM == kParamBf16) {
 #pragma unroll
-                for (int q = 0; q < V / 2; ++q) r[q] = pack2_bf16(p[2 * q], p[2 * q + 1]);
-            } else {
+            for (int q = 0; q < V / 2; ++q) {
+                uint32_t x[2];
 #pragma unroll
-                for (int q = 0; q < V / 2; ++q) {
-                    uint32_t x[2];
+                for (int u = 0; u < 2; ++u) {
+                    const uint32_t b = __float_as_uint(p[2 * q + u]);
+                    const bool finite = (b & 0x7f800000u) != 0x7f800000u;
+                    x[u] = finite ? b + ((bits[2 * q + u] * 0x9e3779b1u) >> 16) : (uint32_t)f32_to_bf16(p[2 * q + u]) << 16;
+                }
+                p16.w[q] = __builtin_amdgcn_perm(x[1], x[0], 0x07060302);   // the upper halves
+            }
+        }
+        uint32_t sm, sv;
+        if constexpr (MXFP8) {
+            if (!whole) {
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const uint32_t b = __float_as_uint(p[2 * q + u]);
-                        const bool finite = (b & 0x7f800000u) != 0x7f800000u;
-                        x[u] = finite ? b + ((bits[2 * q + u] * 0x9e3779b1u) >> 16) : (uint32_t)f32_to_bf16(p[2 * q + u]) << 16;
-                    }
-                    r[q] = __builtin_amdgcn_perm(x[1], x[0], 0x07060302);   // the upper halves
+                for (int u = 0; u < V; ++u) {
+                    m[u] = u < left ? m[u] : 0.f;   // what lies past the end has no part in the scale
+                    v[u] = u < left ? v[u] : 0.f;
                 }
             }
-            store_packed<V>(static_cast<bf16_t*>(t.param), j, left, r);
+            quantize<false>(m, bits, pm.w, sm);
+            quantize<true>(v, bits, pv.w, sv);
+        } else {
+            pm.set(m);
+            pv.set(v);
+        }
+        if (whole) {
+            if (PARAM != kParamBf16) p32.store(PARAM == kParamMaster ? static_cast<void*>(t.master) : t.param, j);
+            if (PARAM != kParamF32) p16.store(t.param, j);
+            pm.store(t.m, j);
+            pv.store(t.v, j);
+        } else {
+            if (PARAM != kParamBf16) p32.store_some(PARAM == kParamMaster ? static_cast<void*>(t.master) : t.param, j, left);
+            if (PARAM != kParamF32) p16.store_some(t.param, j, left);
+            pm.store_some(t.m, j, left);
+            pv.store_some(t.v, j, left);
+        }
+        if constexpr (MXFP8) {
+            if (threadIdx.x % 4 == 0 && left > 0) {
+                t.m_scale[j / kBlock] = (uint8_t)sm;
+                t.v_scale[j / kBlock] = (uint8_t)sv;
+            }
         }
     }
 }
