@@ -256,9 +256,9 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v) {
 // second moment, which also stays above zero where it is (2^-9 is the smallest code).
 template <bool UPPER>
 __device__ __forceinline__ void quantize(const float (&x)[8], const uint32_t (&bits)[8], uint32_t (&codes)[2], uint32_t& scale) {
-    uint32_t top = 0;
+    uint32_t top = 0;   // as bits, which order NaN above all; the second moment has no sign but a NaN's
 #pragma unroll
-    for (int u = 0; u < 8; ++u) top = max(top, __float_as_uint(x[u]) & 0x7fffffffu);
+    for (int u = 0; u < 8; ++u) top = max(top, UPPER ? __float_as_uint(x[u]) : __float_as_uint(x[u]) & 0x7fffffffu);
     scale = scale_of(block_max(top));
     const float inverse = __uint_as_float((254 - (int)scale) << 23);
     float y[8];
@@ -365,8 +365,8 @@ __device__ __forceinline__ void adamw_chunk(const AdamTensor& t, const AdamStep&
             if constexpr (MXFP8) {
                 // the instructions' own square root and reciprocal, each within a unit of fp32: with 8-bit states the kernel
                 // is bound by what it computes
-                const float denom = __builtin_amdgcn_sqrtf(v[u]) * h.rsqrt_bc2 + h.eps;
-                p[u] = p[u] * t.decay - (m[u] * t.step_size) * __builtin_amdgcn_rcpf(denom);
+                const float denom = fmaf(__builtin_amdgcn_sqrtf(v[u]), h.rsqrt_bc2, h.eps);
+                p[u] = fmaf(-t.step_size * m[u], __builtin_amdgcn_rcpf(denom), p[u] * t.decay);
             } else {
                 const float denom = sqrtf(v[u]) * h.rsqrt_bc2 + h.eps;
                 p[u] = p[u] * t.decay - (m[u] / denom) * t.step_size;
@@ -387,9 +387,9 @@ __device__ __forceinline__ void adamw_chunk(const AdamTensor& t, const AdamStep&
                 uint32_t x[2];
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const uint32_t b = __float_as_uint(p[2 * q + u]);
-                    const bool finite = (b & 0x7f800000u) != 0x7f800000u;
-                    x[u] = finite ? b + ((bits[2 * q + u] * 0x9e3779b1u) >> 16) : (uint32_t)f32_to_bf16(p[2 * q + u]) << 16;
+                    // 16 random bits below the last kept one; infinities stay what they are, a NaN might carry over
+                    const float x32 = p[2 * q + u];
+                    x[u] = x32 != x32 ? 0x7fc00000u : __float_as_uint(x32) + ((bits[2 * q + u] * 0x9e3779b1u) >> 16);
                 }
                 p16.w[q] = __builtin_amdgcn_perm(x[1], x[0], 0x07060302);   // the upper halves
             }
