@@ -11,7 +11,7 @@ namespace moe {
 namespace {
 
 constexpr int kListTensors = 48;   // 80 bytes each: a launch's arguments are limited to 4 KiB
-constexpr int kChunk = 4096;       // elements of a workgroup; a multiple of the 8-bit states' blocks
+constexpr int kChunk = 2048;       // elements of a workgroup; a multiple of the 8-bit states' blocks
 constexpr int kBlock = 32;         // elements that share a scale
 constexpr int64_t kLaunchChunks = (1 << 24) - 1;   // 256 threads each: a grid has less than 2^32 threads
 
@@ -199,7 +199,7 @@ struct Packed {
         const uint32_t* p = reinterpret_cast<const uint32_t*>(static_cast<const T*>(base) + j);
 #pragma unroll
         for (int q = 0; q < kWords; q += kAccess) {
-            const access_t r = *reinterpret_cast<const access_t*>(p + q);
+            const access_t r = __builtin_nontemporal_load(reinterpret_cast<const access_t*>(p + q));
 #pragma unroll
             for (int u = 0; u < kAccess; ++u) w[q + u] = r[u];
         }
@@ -219,7 +219,7 @@ struct Packed {
             access_t r;
 #pragma unroll
             for (int u = 0; u < kAccess; ++u) r[u] = w[q + u];
-            *reinterpret_cast<access_t*>(p + q) = r;
+            __builtin_nontemporal_store(r, reinterpret_cast<access_t*>(p + q));
         }
     }
     __device__ __forceinline__ void store_some(void* base, int64_t j, int left) const {
