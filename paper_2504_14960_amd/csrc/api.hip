@@ -54,7 +54,7 @@ static moe_status_t check_dims(const char* fn, int T, int H, int E, int K, moe_d
 static moe_status_t check_list_entry(const char* fn, int i, int64_t n, moe_dtype_t dt, const char* what) {
     if (dt != MOE_F32 && dt != MOE_BF16) return fail(MOE_ERR_INVALID_ARG, "%s: tensor %d: unknown %s %d", fn, i, what, (int)dt);
     if (n < 0) return fail(MOE_ERR_INVALID_ARG, "%s: tensor %d: n=%lld", fn, i, (long long)n);
-    if (n > kMaxListElements) return fail(MOE_ERR_UNSUPPORTED, "%s: tensor %d: n=%lld exceeds the limit 2^34", fn, i, (long long)n);
+    if (n > kMaxListElements) return fail(MOE_ERR_UNSUPPORTED, "%s: tensor %d: n=%lld exceeds the limit 2^33", fn, i, (long long)n);
     return MOE_OK;
 }
 

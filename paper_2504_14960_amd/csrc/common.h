@@ -29,7 +29,7 @@ constexpr int kWave = 64;
 constexpr int kMaxExperts = 256;
 constexpr int kMaxTopK = 64;
 constexpr int kMaxSequences = 65536;               // of one balance-loss call
-constexpr int64_t kMaxListElements = 1ll << 34;    // of one tensor of a gradient-norm or AdamW call
+constexpr int64_t kMaxListElements = 1ll << 33;    // of one tensor of a gradient-norm or AdamW call
 
 __device__ __forceinline__ float bf16_to_f32(bf16_t v) {
     return __uint_as_float(static_cast<uint32_t>(v) << 16);

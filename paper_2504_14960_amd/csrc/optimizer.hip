@@ -1,7 +1,7 @@
 // What ends a training step: the norm of all gradients, and AdamW over a list of tensors (formulas in include/moe.h).
 //
-// A launch takes up to kListTensors tensors, described in its arguments; every tensor is cut into chunks of kChunk
-// elements, and a workgroup finds its tensor from the first chunks.  Both are bound by memory.
+// A launch takes a list of tensors, described in its arguments; every tensor is cut into pieces, and a workgroup finds its
+// tensor from the first pieces.  Both are bound by memory.
 #include <type_traits>
 
 #include "common.h"
@@ -11,9 +11,9 @@ namespace moe {
 namespace {
 
 constexpr int kListTensors = 48;   // 80 bytes each: a launch's arguments are limited to 4 KiB
-constexpr int kChunk = 2048;       // elements of a workgroup; a multiple of the 8-bit states' blocks
+constexpr int kPieceF32 = 1024, kPieceMxfp8 = 2048;   // elements of an AdamW workgroup, by states
 constexpr int kBlock = 32;         // elements that share a scale
-constexpr int64_t kLaunchChunks = (1 << 24) - 1;   // 256 threads each: a grid has less than 2^32 threads
+constexpr int64_t kLaunchPieces = (1 << 24) - 1;   // 256 threads each: a grid has less than 2^32 threads
 
 // -------------------------------------------------------------------------------------------------------------
 // lists
@@ -30,11 +30,11 @@ struct GradList {
 };
 
 template <typename List>
-__device__ __forceinline__ int find_tensor(const List& l, int chunk) {
+__device__ __forceinline__ int find_tensor(const List& l, int piece) {
     int lo = 0, hi = l.count;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (l.first[mid] <= chunk) lo = mid;
+        if (l.first[mid] <= piece) lo = mid;
         else hi = mid;
     }
     return lo;
@@ -152,7 +152,7 @@ struct AdamTensor {
 
 struct AdamList {
     AdamTensor t[kListTensors];
-    int32_t first[kListTensors];
+    int32_t first[kListTensors];   // first piece
     int32_t count;
 };
 
@@ -290,10 +290,11 @@ __device__ __forceinline__ void dequantize(const uint32_t (&codes)[2], float sca
     }
 }
 
-// What a lane reads of its V elements.
+// What a lane reads of its V elements: four with fp32 states, so that every access of a wave is one run of memory; eight
+// with 8-bit ones, where the work on a block is shared by fewer lanes.
 template <int PARAM, bool GRAD_BF16, bool MXFP8>
 struct AdamInput {
-    static constexpr int V = MXFP8 ? 8 : 4;
+    static constexpr int V = MXFP8 ? kPieceMxfp8 / 256 : kPieceF32 / 256;
     typedef typename std::conditional<GRAD_BF16, bf16_t, uint32_t>::type grad_t;
     typedef typename std::conditional<PARAM == kParamBf16, bf16_t, uint32_t>::type param_t;   // what is stepped
     typedef typename std::conditional<MXFP8, uint8_t, uint32_t>::type state_t;
@@ -302,129 +303,120 @@ struct AdamInput {
     Packed<V, state_t> m, v;
     uint32_t m_scale, v_scale;
 
-    // piece: 256 V elements from `base` on, of which those below `end` exist
-    __device__ __forceinline__ void load(const AdamTensor& t, int64_t base, int64_t end) {
-        const int64_t j = base + V * threadIdx.x;
+    __device__ __forceinline__ void load(const AdamTensor& t, int64_t j, bool whole, int left) {
         const void* param = PARAM == kParamMaster ? static_cast<const void*>(t.master) : t.param;
-        if (base + 256 * V <= end) {
+        if (whole) {
             g.load(t.grad, j);
             p.load(param, j);
             m.load(t.m, j);
             v.load(t.v, j);
         } else {
-            const int left = (int)min((int64_t)V, end - j);   // none or negative: this lane has nothing
             g.load_some(t.grad, j, left);
             p.load_some(param, j, left);
             m.load_some(t.m, j, left);
             v.load_some(t.v, j, left);
         }
         if constexpr (MXFP8) {
-            const int64_t block = min(j, end - 1) / kBlock;
+            const int64_t block = min(j, t.n - 1) / kBlock;
             m_scale = t.m_scale[block];
             v_scale = t.v_scale[block];
         }
     }
 };
 
-// Four elements to a lane with fp32 states, so that every access of a wave is one run of memory; eight with 8-bit ones,
-// where the work on a block is shared by fewer lanes.  The next piece is on its way while one is worked on.
+// One piece of a tensor.
 template <int PARAM, bool GRAD_BF16, bool MXFP8>
-__device__ __forceinline__ void adamw_chunk(const AdamTensor& t, const AdamStep& h, float scale, int64_t at) {
+__device__ __forceinline__ void adamw_piece(const AdamTensor& t, const AdamStep& h, float scale, int64_t piece) {
 #pragma clang fp contract(off)
     typedef AdamInput<PARAM, GRAD_BF16, MXFP8> Input;
     constexpr int V = Input::V;
-    const int64_t end = min(at + kChunk, t.n);
-    Input in;
-    in.load(t, at, end);
-    for (int64_t base = at; base < end; base += 256 * V) {
-        const Input cur = in;
-        if (base + 256 * V < end) in.load(t, base + 256 * V, end);
-        const int64_t j = base + V * threadIdx.x;
-        const bool whole = base + 256 * V <= end;
-        const int left = (int)min((int64_t)V, end - j);
-        float p[V], g[V], m[V], v[V];
-        cur.g.values(g);
-        cur.p.values(p);
+    const int64_t base = piece * (256 * V), j = base + V * threadIdx.x;
+    const bool whole = base + 256 * V <= t.n;
+    const int left = (int)min((int64_t)V, t.n - j);   // none or negative: this lane has nothing
+    Input cur;
+    cur.load(t, j, whole, left);
+    float p[V], g[V], m[V], v[V];
+    cur.g.values(g);
+    cur.p.values(p);
+    if constexpr (MXFP8) {
+        dequantize(cur.m.w, scale_value(cur.m_scale), m);
+        dequantize(cur.v.w, scale_value(cur.v_scale), v);
+    } else {
+        cur.m.values(m);
+        cur.v.values(v);
+    }
+    uint32_t bits[V];
+    if (MXFP8 || PARAM == kParamBf16) {
+#pragma unroll
+        for (int u = 0; u < V; ++u) bits[u] = random_bits(h.seed, t.index, j + u);
+    }
+#pragma unroll
+    for (int u = 0; u < V; ++u) {
+        g[u] *= scale;
+        m[u] = m[u] * h.beta1 + g[u] * h.one_minus_beta1;
+        v[u] = v[u] * h.beta2 + (g[u] * g[u]) * h.one_minus_beta2;
         if constexpr (MXFP8) {
-            dequantize(cur.m.w, scale_value(cur.m_scale), m);
-            dequantize(cur.v.w, scale_value(cur.v_scale), v);
+            // the instructions' own square root and reciprocal, each within a unit of fp32: with 8-bit states the kernel
+            // is bound by what it computes
+            const float denom = fmaf(__builtin_amdgcn_sqrtf(v[u]), h.rsqrt_bc2, h.eps);
+            p[u] = fmaf(-t.step_size * m[u], __builtin_amdgcn_rcpf(denom), p[u] * t.decay);
         } else {
-            cur.m.values(m);
-            cur.v.values(v);
+            const float denom = sqrtf(v[u]) * h.rsqrt_bc2 + h.eps;
+            p[u] = p[u] * t.decay - (m[u] / denom) * t.step_size;
         }
-        uint32_t bits[V];
-        if (MXFP8 || PARAM == kParamBf16) {
+    }
+    // new weights and states as they go to memory
+    Packed<V, uint32_t> p32;
+    Packed<V, bf16_t> p16;
+    Packed<V, typename Input::state_t> pm, pv;
+    if (PARAM != kParamBf16) p32.set(p);
+    if constexpr (PARAM == kParamMaster) {
 #pragma unroll
-            for (int u = 0; u < V; ++u) bits[u] = random_bits(h.seed, t.index, j + u);
+        for (int q = 0; q < V / 2; ++q) p16.w[q] = pack2_bf16(p[2 * q], p[2 * q + 1]);
+    }
+    if constexpr (PARAM == kParamBf16) {
+#pragma unroll
+        for (int q = 0; q < V / 2; ++q) {
+            uint32_t x[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                // 16 random bits below the last kept one; infinities stay what they are, a NaN might carry over
+                const float x32 = p[2 * q + u];
+                x[u] = x32 != x32 ? 0x7fc00000u : __float_as_uint(x32) + ((bits[2 * q + u] * 0x9e3779b1u) >> 16);
+            }
+            p16.w[q] = __builtin_amdgcn_perm(x[1], x[0], 0x07060302);   // the upper halves
         }
+    }
+    uint32_t sm, sv;
+    if constexpr (MXFP8) {
+        if (!whole) {
 #pragma unroll
-        for (int u = 0; u < V; ++u) {
-            g[u] *= scale;
-            m[u] = m[u] * h.beta1 + g[u] * h.one_minus_beta1;
-            v[u] = v[u] * h.beta2 + (g[u] * g[u]) * h.one_minus_beta2;
-            if constexpr (MXFP8) {
-                // the instructions' own square root and reciprocal, each within a unit of fp32: with 8-bit states the kernel
-                // is bound by what it computes
-                const float denom = fmaf(__builtin_amdgcn_sqrtf(v[u]), h.rsqrt_bc2, h.eps);
-                p[u] = fmaf(-t.step_size * m[u], __builtin_amdgcn_rcpf(denom), p[u] * t.decay);
-            } else {
-                const float denom = sqrtf(v[u]) * h.rsqrt_bc2 + h.eps;
-                p[u] = p[u] * t.decay - (m[u] / denom) * t.step_size;
+            for (int u = 0; u < V; ++u) {
+                m[u] = u < left ? m[u] : 0.f;   // what lies past the end has no part in the scale
+                v[u] = u < left ? v[u] : 0.f;
             }
         }
-        // new weights and states as they go to memory
-        Packed<V, uint32_t> p32;
-        Packed<V, bf16_t> p16;
-        Packed<V, typename Input::state_t> pm, pv;
-        if (PARAM != kParamBf16) p32.set(p);
-        if constexpr (PARAM == kParamMaster) {
-#pragma unroll
-            for (int q = 0; q < V / 2; ++q) p16.w[q] = pack2_bf16(p[2 * q], p[2 * q + 1]);
-        }
-        if constexpr (PARAM == kParamBf16) {
-#pragma unroll
-            for (int q = 0; q < V / 2; ++q) {
-                uint32_t x[2];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    // 16 random bits below the last kept one; infinities stay what they are, a NaN might carry over
-                    const float x32 = p[2 * q + u];
-                    x[u] = x32 != x32 ? 0x7fc00000u : __float_as_uint(x32) + ((bits[2 * q + u] * 0x9e3779b1u) >> 16);
-                }
-                p16.w[q] = __builtin_amdgcn_perm(x[1], x[0], 0x07060302);   // the upper halves
-            }
-        }
-        uint32_t sm, sv;
-        if constexpr (MXFP8) {
-            if (!whole) {
-#pragma unroll
-                for (int u = 0; u < V; ++u) {
-                    m[u] = u < left ? m[u] : 0.f;   // what lies past the end has no part in the scale
-                    v[u] = u < left ? v[u] : 0.f;
-                }
-            }
-            quantize<false>(m, bits, pm.w, sm);
-            quantize<true>(v, bits, pv.w, sv);
-        } else {
-            pm.set(m);
-            pv.set(v);
-        }
-        if (whole) {
-            if (PARAM != kParamBf16) p32.store(PARAM == kParamMaster ? static_cast<void*>(t.master) : t.param, j);
-            if (PARAM != kParamF32) p16.store(t.param, j);
-            pm.store(t.m, j);
-            pv.store(t.v, j);
-        } else {
-            if (PARAM != kParamBf16) p32.store_some(PARAM == kParamMaster ? static_cast<void*>(t.master) : t.param, j, left);
-            if (PARAM != kParamF32) p16.store_some(t.param, j, left);
-            pm.store_some(t.m, j, left);
-            pv.store_some(t.v, j, left);
-        }
-        if constexpr (MXFP8) {
-            if (threadIdx.x % 4 == 0 && left > 0) {
-                t.m_scale[j / kBlock] = (uint8_t)sm;
-                t.v_scale[j / kBlock] = (uint8_t)sv;
-            }
+        quantize<false>(m, bits, pm.w, sm);
+        quantize<true>(v, bits, pv.w, sv);
+    } else {
+        pm.set(m);
+        pv.set(v);
+    }
+    if (whole) {
+        if (PARAM != kParamBf16) p32.store(PARAM == kParamMaster ? static_cast<void*>(t.master) : t.param, j);
+        if (PARAM != kParamF32) p16.store(t.param, j);
+        pm.store(t.m, j);
+        pv.store(t.v, j);
+    } else {
+        if (PARAM != kParamBf16) p32.store_some(PARAM == kParamMaster ? static_cast<void*>(t.master) : t.param, j, left);
+        if (PARAM != kParamF32) p16.store_some(t.param, j, left);
+        pm.store_some(t.m, j, left);
+        pv.store_some(t.v, j, left);
+    }
+    if constexpr (MXFP8) {
+        if (threadIdx.x % 4 == 0 && left > 0) {
+            t.m_scale[j / kBlock] = (uint8_t)sm;
+            t.v_scale[j / kBlock] = (uint8_t)sv;
         }
     }
 }
@@ -434,20 +426,20 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamList l, AdamStep h) {
     if (scale != scale) return;
     const int i = find_tensor(l, blockIdx.x);
     const AdamTensor& t = l.t[i];
-    const int64_t at = (int64_t)((int)blockIdx.x - l.first[i]) * kChunk;
+    const int64_t piece = (int)blockIdx.x - l.first[i];
     switch (t.kind) {
-        case 0: return adamw_chunk<kParamF32, false, false>(t, h, scale, at);
-        case 1: return adamw_chunk<kParamF32, true, false>(t, h, scale, at);
-        case 2: return adamw_chunk<kParamMaster, false, false>(t, h, scale, at);
-        case 3: return adamw_chunk<kParamMaster, true, false>(t, h, scale, at);
-        case 4: return adamw_chunk<kParamBf16, false, false>(t, h, scale, at);
-        case 5: return adamw_chunk<kParamBf16, true, false>(t, h, scale, at);
-        case 6: return adamw_chunk<kParamF32, false, true>(t, h, scale, at);
-        case 7: return adamw_chunk<kParamF32, true, true>(t, h, scale, at);
-        case 8: return adamw_chunk<kParamMaster, false, true>(t, h, scale, at);
-        case 9: return adamw_chunk<kParamMaster, true, true>(t, h, scale, at);
-        case 10: return adamw_chunk<kParamBf16, false, true>(t, h, scale, at);
-        default: return adamw_chunk<kParamBf16, true, true>(t, h, scale, at);
+        case 0: return adamw_piece<kParamF32, false, false>(t, h, scale, piece);
+        case 1: return adamw_piece<kParamF32, true, false>(t, h, scale, piece);
+        case 2: return adamw_piece<kParamMaster, false, false>(t, h, scale, piece);
+        case 3: return adamw_piece<kParamMaster, true, false>(t, h, scale, piece);
+        case 4: return adamw_piece<kParamBf16, false, false>(t, h, scale, piece);
+        case 5: return adamw_piece<kParamBf16, true, false>(t, h, scale, piece);
+        case 6: return adamw_piece<kParamF32, false, true>(t, h, scale, piece);
+        case 7: return adamw_piece<kParamF32, true, true>(t, h, scale, piece);
+        case 8: return adamw_piece<kParamMaster, false, true>(t, h, scale, piece);
+        case 9: return adamw_piece<kParamMaster, true, true>(t, h, scale, piece);
+        case 10: return adamw_piece<kParamBf16, false, true>(t, h, scale, piece);
+        default: return adamw_piece<kParamBf16, true, true>(t, h, scale, piece);
     }
 }
 
@@ -457,7 +449,10 @@ inline int kind_of(const moe_adamw_tensor_t& t) {
     return (t.state == MOE_STATE_MXFP8 ? 6 : 0) + 2 * param + (t.grad_dt == MOE_BF16 ? 1 : 0);
 }
 
-inline int64_t chunks_of(int64_t n) { return (n + kChunk - 1) / kChunk; }
+inline int64_t pieces_of(const moe_adamw_tensor_t& t) {
+    const int piece = t.state == MOE_STATE_MXFP8 ? kPieceMxfp8 : kPieceF32;
+    return (t.n + piece - 1) / piece;
+}
 
 }  // namespace
 
@@ -502,23 +497,23 @@ void launch_adamw(const moe_adamw_tensor_t* tensors, int count, double lr, doubl
     const AdamStep h = {(float)beta1, (float)(1. - beta1), (float)beta2, (float)(1. - beta2), (float)eps,
                         (float)(1. / sqrt(bc2)), seed, grad_scale};
     AdamList l;
-    int64_t chunks = 0;
+    int64_t pieces = 0;
     l.count = 0;
     auto flush = [&] {
-        if (l.count) hipLaunchKernelGGL(adamw_kernel, dim3((unsigned)chunks), dim3(256), 0, s, l, h);
+        if (l.count) hipLaunchKernelGGL(adamw_kernel, dim3((unsigned)pieces), dim3(256), 0, s, l, h);
         l.count = 0;
-        chunks = 0;
+        pieces = 0;
     };
     for (int i = 0; i < count; ++i) {
         const moe_adamw_tensor_t& t = tensors[i];
-        const int64_t more = chunks_of(t.n);
+        const int64_t more = pieces_of(t);
         if (more == 0) continue;
-        if (l.count == kListTensors || chunks + more > kLaunchChunks) flush();
+        if (l.count == kListTensors || pieces + more > kLaunchPieces) flush();
         const double lr_i = lr * t.lr_scale;
-        l.first[l.count] = (int32_t)chunks;
+        l.first[l.count] = (int32_t)pieces;
         l.t[l.count++] = {t.param, t.master, t.grad, t.exp_avg, t.exp_avg_sq, t.exp_avg_scale, t.exp_avg_sq_scale, t.n,
                           (float)(1. - lr_i * t.weight_decay), (float)(lr_i / bc1), i, kind_of(t)};
-        chunks += more;
+        pieces += more;
     }
     flush();
 }
