@@ -2,91 +2,109 @@
 //
 //   balance_partial_kernel   a chunk of one sequence's tokens: sums of probabilities, counts, squares of the
 //                            log-sum-exps and valid tokens of the chunk
-//   balance_sequence_kernel  the chunks of one sequence added up in order
+//   balance_sequence_kernel  the chunks of one sequence added up in order (64 experts to a workgroup)
 //   balance_total_kernel     the two losses from all sequences
+//   balance_single_kernel    the last two in one, for one sequence
 //   balance_backward_kernel  the gradient, token by token
 //
-// All are bound by memory: the forward reads the logits once, the backward reads and writes them once.
+// All are bound by memory: the forward reads the logits once, the backward reads and writes them once.  A token's logits lie
+// four to a lane in as many lanes as its experts need (a power of two, LPT), so that 64 / LPT tokens share a wave, a lane
+// always has the same experts and keeps its sums of probabilities in registers; four batches of tokens are in flight.
+#include <type_traits>
+
 #include "common.h"
 
 namespace moe {
 
 namespace {
 
-// Tokens of a chunk: a function of T only, so that the order of the sums is reproducible.
-__host__ __device__ inline int chunk_tokens(int T) { return T > 65536 ? 256 : 64; }
+constexpr int kBatches = 4;        // tokens a lane has in flight
+constexpr int kSlab = 64;          // experts of a workgroup of balance_sequence_kernel
+
+// Tokens of a chunk and threads of its workgroup: functions of T (and of whether there are sequences) only, so that the
+// order of the sums is reproducible.  One sequence: up to 256 chunks, one to a compute unit, that one workgroup can add up.
+__host__ __device__ inline int chunk_tokens(int T, bool packed) {
+    if (packed) return T > 65536 ? 256 : 64;
+    const int c = (T + 255) / 256;
+    return c < 64 ? 64 : (c + 15) & ~15;
+}
 
 inline int chunk_count(int T, int n_seq, bool packed) {
-    const int c = chunk_tokens(T);
+    const int c = chunk_tokens(T, packed);
     return packed ? T / c + n_seq : (T + c - 1) / c + (T == 0);
 }
 
 __device__ __forceinline__ int clamp_token(int t, int T) { return min(max(t, 0), T); }
 
-// Chunks are numbered across the sequences without a table: sequence s starts at chunk offsets[s] / c + s, which leaves it
-// ceil(length / c) of them or one more (floor((a + n) / c) + 1 - floor(a / c) >= ceil(n / c)).
-__device__ __forceinline__ int first_chunk(const int32_t* offsets, int s, int T) {
-    return clamp_token(offsets[s], T) / chunk_tokens(T) + s;
-}
+// Chunks of C tokens are numbered across the sequences without a table: sequence s starts at chunk offsets[s] / C + s, which
+// leaves it ceil(length / C) of them or one more (floor((a + n) / C) + 1 - floor(a / C) >= ceil(n / C)).
+__device__ __forceinline__ int first_chunk(const int32_t* offsets, int s, int T, int C) { return clamp_token(offsets[s], T) / C + s; }
 
 struct Chunk {
     int seq, t0, t1;
 };
 
-__device__ __forceinline__ Chunk find_chunk(int b, const int32_t* offsets, int n_seq, int T) {
-    const int c = chunk_tokens(T);
-    if (offsets == nullptr) return {0, b * c, min(T, (b + 1) * c)};
+__device__ __forceinline__ Chunk find_chunk(int b, const int32_t* offsets, int n_seq, int T, int C) {
+    if (offsets == nullptr) return {0, b * C, b * C + min(T - b * C, C)};
     int lo = 0, hi = n_seq;   // the last sequence that starts at chunk b or before it
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (first_chunk(offsets, mid, T) <= b) lo = mid;
+        if (first_chunk(offsets, mid, T, C) <= b) lo = mid;
         else hi = mid;
     }
     const int begin = clamp_token(offsets[lo], T), end = clamp_token(offsets[lo + 1], T);
-    const long long t0 = begin + (long long)(b - first_chunk(offsets, lo, T)) * c;
-    const int from = (int)(t0 < end ? t0 : end);
-    return {lo, max(from, 0), min(end, max(from, 0) + c)};
+    const long long t0 = begin + (long long)(b - first_chunk(offsets, lo, T, C)) * C;
+    const int from = max((int)(t0 < end ? t0 : end), 0);
+    return {lo, from, from + min(end - from, C)};
 }
 
-__device__ __forceinline__ float wave_max(float v) {
+// Sum and maximum over the LPT lanes of a token.
+template <int LPT>
+__device__ __forceinline__ float group_max(float v) {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
+    for (int off = LPT / 2; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
+    return v;
+}
+template <int LPT>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+    for (int off = LPT / 2; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
     return v;
 }
 
-__device__ __forceinline__ float wave_sum(float v) {
+// A lane's four logits of a token; -inf past the last expert.
+__device__ __forceinline__ f32x4 load_logits(const float* row, int e, int E, bool vec) {
+    f32x4 x = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    if (vec) {
+        if (e < E) x = *reinterpret_cast<const f32x4*>(row + e);
+    } else {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-    return v;
+        for (int u = 0; u < 4; ++u)
+            if (e + u < E) x[u] = row[e + u];
+    }
+    return x;
 }
 
-// p[j] = softmax of the token's logits for expert lane + 64 j; returns the log-sum-exp.  NaN stays NaN; a token of -inf
-// only has p = 0 and a log-sum-exp that counts as 0.
-__device__ __forceinline__ float token_softmax(const float* logits, int E, int lane, float (&p)[4]) {
-    float m = -INFINITY;
-    bool nan = false;
+// x becomes the softmax of a token; top and z are the largest logit and the sum of exp(x - top), so that the log-sum-exp is
+// top + log z.  ok = false: zeros, z = 1, whatever x holds, and so for a token of -inf only.  A NaN spreads to the token.
+template <int LPT>
+__device__ __forceinline__ void softmax(f32x4& x, bool ok, float& top, float& z) {
+    constexpr float kLog2E = 1.44269504f;
+    const float m = group_max<LPT>(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
+    const float from = m == -INFINITY ? 0.f : m;   // exp(-inf - 0) = 0: all -inf gives zeros, NaN stays NaN
+    float s = 0.f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        p[j] = lane + 64 * j < E ? logits[lane + 64 * j] : -INFINITY;
-        nan |= p[j] != p[j];
-        m = fmaxf(m, p[j]);
+    for (int u = 0; u < 4; ++u) {
+        x[u] = __builtin_amdgcn_exp2f((x[u] - from) * kLog2E);
+        s += x[u];
     }
-    m = wave_max(m);
-    if (m == -INFINITY && !__any(nan)) {
+    s = group_sum<LPT>(s);
+    ok = ok && s != 0.f;
+    const float r = __builtin_amdgcn_rcpf(s);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) p[j] = 0.f;
-        return 0.f;
-    }
-    float z = 0.f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        p[j] = lane + 64 * j < E ? expf(p[j] - m) : 0.f;
-        z += p[j];
-    }
-    z = wave_sum(z);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) p[j] /= z;
-    return m + logf(z);
+    for (int u = 0; u < 4; ++u) x[u] = ok ? x[u] * r : 0.f;
+    top = ok ? from : 0.f;
+    z = ok ? s : 1.f;
 }
 
 // Workspace: what every chunk leaves, then what every sequence leaves.
@@ -95,9 +113,11 @@ struct Partials {
     int32_t* count;   // [chunks, E]
     float* z;         // [chunks]
     int32_t* tokens;  // [chunks]
-    double* seq_loss; // [n_seq]
+    double* seq_loss; // [n_seq, slabs]
     double* seq_z;    // [n_seq]
 };
+
+inline int slabs_of(int E) { return (E + kSlab - 1) / kSlab; }
 
 inline size_t carve(void* ws, int chunks, int E, int n_seq, Partials* out) {
     uint8_t* base = static_cast<uint8_t*>(ws);
@@ -108,160 +128,297 @@ inline size_t carve(void* ws, int chunks, int E, int n_seq, Partials* out) {
     p.count = reinterpret_cast<int32_t*>(take((size_t)chunks * E * 4));
     p.z = reinterpret_cast<float*>(take((size_t)chunks * 4));
     p.tokens = reinterpret_cast<int32_t*>(take((size_t)chunks * 4));
-    p.seq_loss = reinterpret_cast<double*>(take((size_t)n_seq * 8));
+    p.seq_loss = reinterpret_cast<double*>(take((size_t)n_seq * slabs_of(E) * 8));
     p.seq_z = reinterpret_cast<double*>(take((size_t)n_seq * 8));
     if (out) *out = p;
     return o;
 }
 
-__global__ __launch_bounds__(256) void balance_partial_kernel(const float* __restrict__ logits, const int32_t* __restrict__ idx,
-                                                              const uint8_t* __restrict__ mask,
-                                                              const int32_t* __restrict__ offsets, int T, int E, int K,
-                                                              int n_seq, Partials out) {
-    __shared__ int32_t hist[kMaxExperts];
-    __shared__ float sums[4][kMaxExperts];
-    __shared__ float zs[4];
-    __shared__ int32_t ns[4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = blockIdx.x;
-    const Chunk c = find_chunk(b, offsets, n_seq, T);
-    hist[threadIdx.x] = 0;
+// One chunk to a workgroup of up to 16 waves.
+template <int LPT>
+__global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __restrict__ logits, const int32_t* __restrict__ idx,
+                                                               const uint8_t* __restrict__ mask,
+                                                               const int32_t* __restrict__ offsets, int T, int E, int K,
+                                                               int n_seq, int C, Partials out) {
+    constexpr int kTokens = 64 / LPT, kExperts = 4 * LPT;
+    __shared__ int32_t hist[kExperts];
+    __shared__ float sums[16][kExperts];
+    __shared__ float zs[16];
+    __shared__ int32_t ns[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, b = blockIdx.x;
+    const int q = lane % LPT, e = 4 * q;
+    const bool vec = E % 4 == 0;
+    const Chunk c = find_chunk(b, offsets, n_seq, T, C);
+    if (threadIdx.x < kExperts) hist[threadIdx.x] = 0;
     __syncthreads();
-    float acc[4] = {0.f, 0.f, 0.f, 0.f}, z = 0.f;
+    // counts: every assignment of the chunk once, whole numbers in any order
+    const int64_t a1 = (int64_t)c.t1 * K;
+    for (int64_t a = (int64_t)c.t0 * K + threadIdx.x; a < a1; a += blockDim.x) {
+        const int i = idx[a];
+        if ((unsigned)i < (unsigned)E && (mask == nullptr || mask[(uint32_t)a / (uint32_t)K] != 0)) atomicAdd(&hist[i], 1);
+    }
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    float zsum = 0.f;
     int n = 0;
-    for (int t = c.t0 + wave; t < c.t1; t += 4) {
-        if (mask && mask[t] == 0) continue;
-        ++n;
-        float p[4];
-        const float lse = token_softmax(logits + (size_t)t * E, E, lane, p);
-        z += lse * lse;
+    const int step = waves * kTokens;
+    for (int t = c.t0 + wave * kTokens + lane / LPT; t - lane / LPT < c.t1; t += kBatches * step) {
+        f32x4 x[kBatches];
+        bool ok[kBatches];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j] += p[j];
-        if (lane < K) {
-            const int e = idx[(size_t)t * K + lane];
-            if ((unsigned)e < (unsigned)E) atomicAdd(&hist[e], 1);
+        for (int u = 0; u < kBatches; ++u) {
+            const int tu = t + u * step;
+            ok[u] = tu < c.t1;
+            const size_t row = ok[u] ? tu : c.t1 - 1;
+            x[u] = load_logits(logits + row * E, e, E, vec);
+            if (mask) ok[u] = ok[u] && mask[row] != 0;
+        }
+        float top[kBatches], z[kBatches];
+#pragma unroll
+        for (int u = 0; u < kBatches; ++u) {
+            softmax<LPT>(x[u], ok[u], top[u], z[u]);
+            acc += x[u];
+            if (q == 0) n += ok[u];
+        }
+        // the logarithms: lane u of a token's lanes takes its batch u
+        constexpr int kShare = LPT < kBatches ? LPT : kBatches;
+#pragma unroll
+        for (int v = 0; v < kBatches; v += kShare) {
+            float tv = top[v], zv = z[v];
+#pragma unroll
+            for (int u = 1; u < kShare; ++u) {
+                tv = q == u ? top[v + u] : tv;
+                zv = q == u ? z[v + u] : zv;
+            }
+            const float lse = tv + logf(zv);
+            if (q < kShare) zsum = fmaf(lse, lse, zsum);
         }
     }
+    // lanes with the same experts, then waves
 #pragma unroll
-    for (int j = 0; j < 4; ++j) sums[wave][lane + 64 * j] = acc[j];
+    for (int off = LPT; off < 64; off <<= 1)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) acc[u] += __shfl_xor(acc[u], off, 64);
+    zsum = group_sum<64>(zsum);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off, 64);
+    if (lane < LPT) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) sums[wave][e + u] = acc[u];
+    }
     if (lane == 0) {
-        zs[wave] = z;
+        zs[wave] = zsum;
         ns[wave] = n;
     }
     __syncthreads();
-    const int e = threadIdx.x;
-    if (e < E) {
-        out.prob[(size_t)b * E + e] = (sums[0][e] + sums[1][e]) + (sums[2][e] + sums[3][e]);
-        out.count[(size_t)b * E + e] = hist[e];
+    if (threadIdx.x < E) {
+        float p = 0.f;
+        for (int w = 0; w < waves; ++w) p += sums[w][threadIdx.x];
+        out.prob[(size_t)b * E + threadIdx.x] = p;
+        out.count[(size_t)b * E + threadIdx.x] = hist[threadIdx.x];
     }
-    if (e == 0) {
-        out.z[b] = (zs[0] + zs[1]) + (zs[2] + zs[3]);
-        out.tokens[b] = ns[0] + ns[1] + ns[2] + ns[3];
+    if (threadIdx.x == 0) {
+        float z = 0.f;
+        int tokens = 0;
+        for (int w = 0; w < waves; ++w) {
+            z += zs[w];
+            tokens += ns[w];
+        }
+        out.z[b] = z;
+        out.tokens[b] = tokens;
+    }
+}
+
+// Sums over the workgroup's 1024 or 256 threads, in all of them; `red` holds one value a wave.
+template <typename T>
+__device__ __forceinline__ T workgroup_sum(T v, T* red) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    T s = 0;
+    for (int w = 0; w < (int)blockDim.x >> 6; ++w) s += red[w];
+    return s;
+}
+
+// What the chunks [b0, b1) leave for the experts [e0, e0 + width), added up by `rows` rows of threads of `width` each (a power
+// of two) and written; returns sum_e count * prob of them in thread 0.
+__device__ __forceinline__ double add_chunks(const Partials& in, int b0, int b1, int E, int e0, int width, int32_t* counts,
+                                             float* prob_sums, double* red_p, int32_t* red_n) {
+    const int col = threadIdx.x & (width - 1), row = threadIdx.x / width, rows = blockDim.x / width, e = e0 + col;
+    double p = 0.;
+    int n = 0;
+    if (e < E) {
+#pragma unroll 8
+        for (int b = b0 + row; b < b1; b += rows) {
+            p += in.prob[(size_t)b * E + e];
+            n += in.count[(size_t)b * E + e];
+        }
+    }
+    red_p[threadIdx.x] = p;
+    red_n[threadIdx.x] = n;
+    __syncthreads();
+    for (int d = rows >> 1; d > 0; d >>= 1) {
+        if (row < d) {
+            red_p[threadIdx.x] += red_p[threadIdx.x + d * width];
+            red_n[threadIdx.x] += red_n[threadIdx.x + d * width];
+        }
+        __syncthreads();
+    }
+    double loss = 0.;
+    if (row == 0 && e < E) {
+        counts[e] = red_n[col];
+        prob_sums[e] = (float)red_p[col];
+        loss = red_p[col] * red_n[col];
+    }
+    return workgroup_sum(loss, red_p);
+}
+
+__device__ __forceinline__ void chunk_totals(const Partials& in, int b0, int b1, double* red, int32_t* red_n, double& z, int& n) {
+    z = 0.;
+    n = 0;
+    for (int b = b0 + threadIdx.x; b < b1; b += blockDim.x) {
+        z += in.z[b];
+        n += in.tokens[b];
+    }
+    z = workgroup_sum(z, red);
+    n = workgroup_sum(n, red_n);
+}
+
+__device__ __forceinline__ void write_losses(double loss, double z, int n, int E, int K, float balance_coef, float z_coef,
+                                             int32_t* all_tokens, float* losses) {
+    *all_tokens = n;
+    losses[0] = n ? (float)(loss * balance_coef * E / ((double)K * n)) : 0.f;
+    losses[1] = n ? (float)(z * z_coef / n) : 0.f;
+}
+
+__global__ __launch_bounds__(1024) void balance_single_kernel(int E, int K, int chunks, int width, float balance_coef,
+                                                              float z_coef, Partials in, int32_t* __restrict__ counts,
+                                                              float* __restrict__ prob_sums, int32_t* __restrict__ seq_tokens,
+                                                              float* __restrict__ losses) {
+    __shared__ double red_p[1024];
+    __shared__ int32_t red_n[1024];
+    const double loss = add_chunks(in, 0, chunks, E, 0, width, counts, prob_sums, red_p, red_n);
+    double z;
+    int n;
+    chunk_totals(in, 0, chunks, red_p, red_n, z, n);
+    if (threadIdx.x == 0) {
+        seq_tokens[0] = n;
+        write_losses(n ? loss / n : 0., z, n, E, K, balance_coef, z_coef, seq_tokens + 1, losses);
     }
 }
 
 __global__ __launch_bounds__(256) void balance_sequence_kernel(const int32_t* __restrict__ offsets, int T, int E, int chunks,
-                                                               int n_seq, Partials in, int32_t* __restrict__ counts,
+                                                               int C, int width, Partials in, int32_t* __restrict__ counts,
                                                                float* __restrict__ prob_sums,
                                                                int32_t* __restrict__ seq_tokens) {
-    __shared__ double red[256];
-    const int s = blockIdx.x, e = threadIdx.x;
-    int b0 = 0, b1 = chunks;
-    if (offsets) {
-        b0 = min(first_chunk(offsets, s, T), chunks);
-        b1 = min(first_chunk(offsets, s + 1, T), chunks);
-    }
-    double p = 0., z = 0.;
-    int n = 0, tokens = 0;
-    for (int b = b0; b < b1; ++b) {
-        if (e < E) {
-            p += in.prob[(size_t)b * E + e];
-            n += in.count[(size_t)b * E + e];
+    __shared__ double red_p[256];
+    __shared__ int32_t red_n[256];
+    const int s = blockIdx.x, slab = blockIdx.y;
+    const int b0 = min(first_chunk(offsets, s, T, C), chunks), b1 = min(first_chunk(offsets, s + 1, T, C), chunks);
+    const double loss = add_chunks(in, b0, b1, E, slab * kSlab, width, counts + (size_t)s * E, prob_sums + (size_t)s * E, red_p, red_n);
+    double z;
+    int n;
+    chunk_totals(in, b0, b1, red_p, red_n, z, n);
+    if (threadIdx.x == 0) {
+        in.seq_loss[(size_t)s * gridDim.y + slab] = n ? loss / n : 0.;
+        if (slab == 0) {
+            seq_tokens[s] = n;
+            in.seq_z[s] = z;
         }
-        z += in.z[b];
-        tokens += in.tokens[b];
-    }
-    if (e < E) {
-        counts[(size_t)s * E + e] = n;
-        prob_sums[(size_t)s * E + e] = (float)p;
-    }
-    red[e] = (double)n * p;
-    __syncthreads();
-    for (int d = 128; d > 0; d >>= 1) {
-        if (e < d) red[e] += red[e + d];
-        __syncthreads();
-    }
-    if (e == 0) {
-        seq_tokens[s] = tokens;
-        in.seq_loss[s] = tokens ? red[0] / tokens : 0.;
-        in.seq_z[s] = z;
     }
 }
 
-__global__ __launch_bounds__(256) void balance_total_kernel(int E, int K, int n_seq, float balance_coef, float z_coef,
-                                                            Partials in, int32_t* __restrict__ seq_tokens,
-                                                            float* __restrict__ losses) {
-    __shared__ double red_l[256], red_z[256];
-    __shared__ int red_n[256];
-    const int i = threadIdx.x;
+__global__ __launch_bounds__(1024) void balance_total_kernel(int E, int K, int n_seq, int slabs, float balance_coef, float z_coef,
+                                                             Partials in, int32_t* __restrict__ seq_tokens,
+                                                             float* __restrict__ losses) {
+    __shared__ double red[16];
+    __shared__ int32_t red_n[16];
     double l = 0., z = 0.;
     int n = 0;
-    for (int s = i; s < n_seq; s += 256) {
-        l += in.seq_loss[s];
+    for (int s = threadIdx.x; s < n_seq; s += 1024) {
         z += in.seq_z[s];
         n += seq_tokens[s];
     }
-    red_l[i] = l;
-    red_z[i] = z;
-    red_n[i] = n;
-    __syncthreads();
-    for (int d = 128; d > 0; d >>= 1) {
-        if (i < d) {
-            red_l[i] += red_l[i + d];
-            red_z[i] += red_z[i + d];
-            red_n[i] += red_n[i + d];
-        }
-        __syncthreads();
-    }
-    if (i == 0) {
-        const int total = red_n[0];
-        seq_tokens[n_seq] = total;
-        losses[0] = total ? (float)(red_l[0] * balance_coef * E / ((double)K * total)) : 0.f;
-        losses[1] = total ? (float)(red_z[0] * z_coef / total) : 0.f;
-    }
+    for (int i = threadIdx.x; i < n_seq * slabs; i += 1024) l += in.seq_loss[i];
+    l = workgroup_sum(l, red);
+    z = workgroup_sum(z, red);
+    n = workgroup_sum(n, red_n);
+    if (threadIdx.x == 0) write_losses(l, z, n, E, K, balance_coef, z_coef, seq_tokens + n_seq, losses);
 }
 
+template <int LPT>
 __global__ __launch_bounds__(256) void balance_backward_kernel(const float* __restrict__ logits,
                                                                const uint8_t* __restrict__ mask,
                                                                const int32_t* __restrict__ offsets,
                                                                const int32_t* __restrict__ counts,
                                                                const int32_t* __restrict__ seq_tokens,
                                                                const float* __restrict__ dlosses, const float* addend, int T,
-                                                               int E, int K, int n_seq, float balance_coef, float z_coef,
-                                                               float* dlogits) {
+                                                               int E, int K, int n_seq, int C, float balance_coef,
+                                                               float z_coef, float* dlogits) {
+    constexpr int kTokens = 64 / LPT;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const Chunk c = find_chunk(blockIdx.x, offsets, n_seq, T);
+    const int q = lane % LPT, e = 4 * q;
+    const bool vec = E % 4 == 0;
+    const Chunk c = find_chunk(blockIdx.x, offsets, n_seq, T, C);
     const float n = (float)max(seq_tokens[n_seq], 1), n_s = (float)max(seq_tokens[c.seq], 1);
     const float db = dlosses ? dlosses[0] : 1.f, dz = dlosses ? dlosses[1] : 1.f;
     const float a = db * balance_coef * E / (K * n) / n_s, az = dz * 2.f * z_coef / n;
-    float g[4];
+    f32x4 g;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) g[j] = lane + 64 * j < E ? a * counts[(size_t)c.seq * E + lane + 64 * j] : 0.f;
-    for (int t = c.t0 + wave; t < c.t1; t += 4) {
-        float p[4] = {0.f, 0.f, 0.f, 0.f}, lse = 0.f;
-        if (!mask || mask[t] != 0) lse = token_softmax(logits + (size_t)t * E, E, lane, p);
-        float dot = 0.f;
+    for (int u = 0; u < 4; ++u) g[u] = e + u < E ? a * counts[(size_t)c.seq * E + e + u] : 0.f;
+    for (int t = c.t0 + wave * kTokens + lane / LPT; t - lane / LPT < c.t1; t += kBatches * 4 * kTokens) {
+        f32x4 x[kBatches], more[kBatches];
+        bool in[kBatches], ok[kBatches];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) dot += p[j] * g[j];
-        dot = wave_sum(dot);
+        for (int u = 0; u < kBatches; ++u) {
+            const int tu = t + u * 4 * kTokens;
+            in[u] = tu < c.t1;
+            const size_t row = in[u] ? tu : c.t1 - 1;
+            x[u] = load_logits(logits + row * E, e, E, vec);
+            more[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (addend) more[u] = load_logits(addend + row * E, e, E, vec);
+            ok[u] = mask == nullptr || mask[row] != 0;
+        }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int e = lane + 64 * j;
-            if (e >= E) continue;
-            const size_t at = (size_t)t * E + e;
-            const float d = p[j] * (g[j] - dot + az * lse);
-            dlogits[at] = addend ? d + addend[at] : d;
+        for (int u = 0; u < kBatches; ++u) {
+            float top, z;
+            softmax<LPT>(x[u], ok[u], top, z);
+            const float dot = group_sum<LPT>((x[u][0] * g[0] + x[u][1] * g[1]) + (x[u][2] * g[2] + x[u][3] * g[3]));
+            const float shift = fmaf(az, top + logf(z), -dot);
+            f32x4 d;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) d[v] = x[u][v] * (g[v] + shift) + more[u][v];
+            if (!in[u]) continue;
+            float* row = dlogits + (size_t)(t + u * 4 * kTokens) * E;
+            if (vec) {
+                if (e < E) *reinterpret_cast<f32x4*>(row + e) = d;
+            } else {
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+                    if (e + v < E) row[e + v] = d[v];
+            }
         }
     }
+}
+
+// Calls f with the lanes a token of E experts takes.
+template <typename F>
+void with_lanes(int E, F&& f) {
+    if (E <= 4) f(std::integral_constant<int, 1>());
+    else if (E <= 8) f(std::integral_constant<int, 2>());
+    else if (E <= 16) f(std::integral_constant<int, 4>());
+    else if (E <= 32) f(std::integral_constant<int, 8>());
+    else if (E <= 64) f(std::integral_constant<int, 16>());
+    else if (E <= 128) f(std::integral_constant<int, 32>());
+    else f(std::integral_constant<int, 64>());
+}
+
+// the smallest power of two that is n or more
+inline int power_of_two(int n) {
+    int w = 1;
+    while (w < n) w *= 2;
+    return w;
 }
 
 }  // namespace
@@ -274,21 +431,35 @@ size_t balance_loss_workspace_bytes(int T, int E, int n_seq) {
 void launch_balance_loss(const float* logits, const int32_t* idx, const uint8_t* mask, const int32_t* offsets, int T, int E,
                          int K, int n_seq, float balance_coef, float z_coef, int32_t* counts, float* prob_sums,
                          int32_t* seq_tokens, float* losses, void* ws, hipStream_t s) {
-    const int chunks = chunk_count(T, n_seq, offsets != nullptr);
+    const bool packed = offsets != nullptr;
+    const int chunks = chunk_count(T, n_seq, packed), C = chunk_tokens(T, packed);
     Partials p;
     carve(ws, chunks, E, n_seq, &p);
-    hipLaunchKernelGGL(balance_partial_kernel, dim3(chunks), dim3(256), 0, s, logits, idx, mask, offsets, T, E, K, n_seq, p);
-    hipLaunchKernelGGL(balance_sequence_kernel, dim3(n_seq), dim3(256), 0, s, offsets, T, E, chunks, n_seq, p, counts,
-                       prob_sums, seq_tokens);
-    hipLaunchKernelGGL(balance_total_kernel, dim3(1), dim3(256), 0, s, E, K, n_seq, balance_coef, z_coef, p, seq_tokens,
+    with_lanes(E, [&](auto lanes) {
+        hipLaunchKernelGGL(balance_partial_kernel<lanes.value>, dim3(chunks), dim3(packed ? 256 : 1024), 0, s, logits, idx, mask,
+                           offsets, T, E, K, n_seq, C, p);
+    });
+    if (!packed) {
+        hipLaunchKernelGGL(balance_single_kernel, dim3(1), dim3(1024), 0, s, E, K, chunks, power_of_two(E), balance_coef, z_coef,
+                           p, counts, prob_sums, seq_tokens, losses);
+        return;
+    }
+    const int slabs = slabs_of(E);
+    hipLaunchKernelGGL(balance_sequence_kernel, dim3(n_seq, slabs), dim3(256), 0, s, offsets, T, E, chunks, C,
+                       power_of_two(E < kSlab ? E : kSlab), p, counts, prob_sums, seq_tokens);
+    hipLaunchKernelGGL(balance_total_kernel, dim3(1), dim3(1024), 0, s, E, K, n_seq, slabs, balance_coef, z_coef, p, seq_tokens,
                        losses);
 }
 
 void launch_balance_loss_backward(const float* logits, const uint8_t* mask, const int32_t* offsets, const int32_t* counts,
                                   const int32_t* seq_tokens, const float* dlosses, const float* addend, int T, int E, int K,
                                   int n_seq, float balance_coef, float z_coef, float* dlogits, hipStream_t s) {
-    hipLaunchKernelGGL(balance_backward_kernel, dim3(chunk_count(T, n_seq, offsets != nullptr)), dim3(256), 0, s, logits, mask,
-                       offsets, counts, seq_tokens, dlosses, addend, T, E, K, n_seq, balance_coef, z_coef, dlogits);
+    const bool packed = offsets != nullptr;
+    const int C = 64, chunks = packed ? T / C + n_seq : (T + C - 1) / C;
+    with_lanes(E, [&](auto lanes) {
+        hipLaunchKernelGGL(balance_backward_kernel<lanes.value>, dim3(chunks), dim3(256), 0, s, logits, mask, offsets, counts,
+                           seq_tokens, dlosses, addend, T, E, K, n_seq, C, balance_coef, z_coef, dlogits);
+    });
 }
 
 }  // namespace moe

@@ -295,7 +295,7 @@ def test_refusals():
         return L.moe_balance_loss_backward(logits, mask, offsets, counts, n, d, addend, T, E, K, S, cb, cz, out, None)
 
     nan = float("nan")
-    for kw, status, word in [(dict(T=-1), 1, b"T >= 0"), (dict(K=9), 1, b"exceeds E"), (dict(E=257), 2, b"limit"),
+    for kw, status, word in [(dict(T=-1), 1, b"T >= 0"), (dict(K=9), 1, b"exceeds E"), (dict(E=257), 2, b"limit"), (dict(T=(1 << 30) + 1, K=1), 2, b"limit"),
                              (dict(S=0), 1, b"n_seq"), (dict(S=2), 1, b"seq_offsets"), (dict(S=65537, offsets=p), 2, b"limit"),
                              (dict(cb=nan), 1, b"finite"), (dict(cz=float("inf")), 1, b"finite"),
                              (dict(logits=None), 1, b"NULL"), (dict(logits=odd), 1, b"aligned"), (dict(counts=None), 1, b"NULL"),
