@@ -182,7 +182,8 @@ def _dt(t: torch.Tensor) -> int:
 
 
 def _stream():
-    return torch.cuda.current_stream().cuda_stream
+    # torch.cuda.current_stream().cuda_stream without the Stream object: 0.3 us instead of 2.8, a quarter of a small call
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def version() -> str:

@@ -58,18 +58,35 @@ __device__ __forceinline__ Chunk find_chunk(int b, const int32_t* offsets, int n
     return {lo, from, from + min(end - from, C)};
 }
 
-// Sum and maximum over the LPT lanes of a token.
-template <int LPT>
-__device__ __forceinline__ float group_max(float v) {
-#pragma unroll
-    for (int off = LPT / 2; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
+// Sum and maximum over the LPT neighbouring lanes of a token, in all of them: within a row of 16 lanes by data-parallel
+// primitives (quads by permutation, then mirrored halves and rows), then rows and halves of the wave swapped.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+template <int LPT, typename F>
+__device__ __forceinline__ float group_reduce(float v, F&& f) {
+    if (LPT >= 2) v = f(v, dpp<0xb1>(v));     // quad_perm 1, 0, 3, 2
+    if (LPT >= 4) v = f(v, dpp<0x4e>(v));     // quad_perm 2, 3, 0, 1
+    if (LPT >= 8) v = f(v, dpp<0x141>(v));    // row_half_mirror
+    if (LPT >= 16) v = f(v, dpp<0x140>(v));   // row_mirror
+    if (LPT >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    if (LPT >= 64) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
     return v;
 }
 template <int LPT>
+__device__ __forceinline__ float group_max(float v) {
+    return group_reduce<LPT>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int LPT>
 __device__ __forceinline__ float group_sum(float v) {
-#pragma unroll
-    for (int off = LPT / 2; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-    return v;
+    return group_reduce<LPT>(v, [](float a, float b) { return a + b; });
 }
 
 // A lane's four logits of a token; -inf past the last expert.
@@ -85,26 +102,15 @@ __device__ __forceinline__ f32x4 load_logits(const float* row, int e, int E, boo
     return x;
 }
 
-// x becomes the softmax of a token; top and z are the largest logit and the sum of exp(x - top), so that the log-sum-exp is
-// top + log z.  ok = false: zeros, z = 1, whatever x holds, and so for a token of -inf only.  A NaN spreads to the token.
+// x becomes exp(x - top) of a token's logits, top being the largest; returns the lane's sum of them.  All of -inf: zeros.
 template <int LPT>
-__device__ __forceinline__ void softmax(f32x4& x, bool ok, float& top, float& z) {
+__device__ __forceinline__ float exponentials(f32x4& x, float& top) {
     constexpr float kLog2E = 1.44269504f;
     const float m = group_max<LPT>(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
-    const float from = m == -INFINITY ? 0.f : m;   // exp(-inf - 0) = 0: all -inf gives zeros, NaN stays NaN
-    float s = 0.f;
+    top = m == -INFINITY ? 0.f : m;   // exp(-inf - 0) = 0: all -inf gives zeros, NaN stays NaN
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        x[u] = __builtin_amdgcn_exp2f((x[u] - from) * kLog2E);
-        s += x[u];
-    }
-    s = group_sum<LPT>(s);
-    ok = ok && s != 0.f;
-    const float r = __builtin_amdgcn_rcpf(s);
-#pragma unroll
-    for (int u = 0; u < 4; ++u) x[u] = ok ? x[u] * r : 0.f;
-    top = ok ? from : 0.f;
-    z = ok ? s : 1.f;
+    for (int u = 0; u < 4; ++u) x[u] = __builtin_amdgcn_exp2f((x[u] - top) * kLog2E);
+    return (x[0] + x[1]) + (x[2] + x[3]);
 }
 
 // Workspace: what every chunk leaves, then what every sequence leaves.
@@ -134,6 +140,23 @@ inline size_t carve(void* ws, int chunks, int E, int n_seq, Partials* out) {
     return o;
 }
 
+// A lane's logits of its next tokens: one in each of kBatches batches of `step` tokens.
+struct Batches {
+    f32x4 x[kBatches];
+    bool ok[kBatches];
+
+    __device__ __forceinline__ void load(const float* logits, const uint8_t* mask, int t, int step, int end, int e, int E, bool vec) {
+#pragma unroll
+        for (int u = 0; u < kBatches; ++u) {
+            const int tu = t + u * step;
+            ok[u] = tu < end;
+            const size_t row = ok[u] ? tu : end - 1;
+            x[u] = load_logits(logits + row * E, e, E, vec);
+            if (mask) ok[u] = ok[u] && mask[row] != 0;
+        }
+    }
+};
+
 // One chunk to a workgroup of up to 16 waves.
 template <int LPT>
 __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __restrict__ logits, const int32_t* __restrict__ idx,
@@ -149,6 +172,10 @@ __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __re
     const int q = lane % LPT, e = 4 * q;
     const bool vec = E % 4 == 0;
     const Chunk c = find_chunk(b, offsets, n_seq, T, C);
+    const int step = waves * kTokens, own = lane / LPT;
+    int t = c.t0 + wave * kTokens;
+    Batches next;
+    if (t < c.t1) next.load(logits, mask, t + own, step, c.t1, e, E, vec);
     if (threadIdx.x < kExperts) hist[threadIdx.x] = 0;
     __syncthreads();
     // counts: every assignment of the chunk once, whole numbers in any order
@@ -160,24 +187,23 @@ __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __re
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     float zsum = 0.f;
     int n = 0;
-    const int step = waves * kTokens;
-    for (int t = c.t0 + wave * kTokens + lane / LPT; t - lane / LPT < c.t1; t += kBatches * step) {
-        f32x4 x[kBatches];
-        bool ok[kBatches];
-#pragma unroll
-        for (int u = 0; u < kBatches; ++u) {
-            const int tu = t + u * step;
-            ok[u] = tu < c.t1;
-            const size_t row = ok[u] ? tu : c.t1 - 1;
-            x[u] = load_logits(logits + row * E, e, E, vec);
-            if (mask) ok[u] = ok[u] && mask[row] != 0;
-        }
+    while (t < c.t1) {
+        Batches cur = next;
+        t += kBatches * step;
+        if (t < c.t1) next.load(logits, mask, t + own, step, c.t1, e, E, vec);
         float top[kBatches], z[kBatches];
 #pragma unroll
         for (int u = 0; u < kBatches; ++u) {
-            softmax<LPT>(x[u], ok[u], top[u], z[u]);
-            acc += x[u];
-            if (q == 0) n += ok[u];
+            f32x4& x = cur.x[u];
+            const float s = group_sum<LPT>(exponentials<LPT>(x, top[u]));
+            // a token that does not count, or has no probability, adds nothing and a log-sum-exp of 0
+            const bool ok = cur.ok[u] && s != 0.f;
+            const float r = __builtin_amdgcn_rcpf(s);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) acc[v] += ok ? x[v] * r : 0.f;
+            top[u] = ok ? top[u] : 0.f;
+            z[u] = ok ? s : 1.f;
+            if (q == 0) n += cur.ok[u];
         }
         // the logarithms: lane u of a token's lanes takes its batch u
         constexpr int kShare = LPT < kBatches ? LPT : kBatches;
@@ -382,21 +408,24 @@ __global__ __launch_bounds__(256) void balance_backward_kernel(const float* __re
         }
 #pragma unroll
         for (int u = 0; u < kBatches; ++u) {
-            float top, z;
-            softmax<LPT>(x[u], ok[u], top, z);
-            const float dot = group_sum<LPT>((x[u][0] * g[0] + x[u][1] * g[1]) + (x[u][2] * g[2] + x[u][3] * g[3]));
-            const float shift = fmaf(az, top + logf(z), -dot);
+            float top;
+            const float s = group_sum<LPT>(exponentials<LPT>(x[u], top));
+            const float w = group_sum<LPT>((x[u][0] * g[0] + x[u][1] * g[1]) + (x[u][2] * g[2] + x[u][3] * g[3]));
+            const float r = __builtin_amdgcn_rcpf(s);
+            const float shift = fmaf(az, top + logf(s), -(w * r));
+            const bool zero = !ok[u] || s == 0.f;   // does not count, or has no probability
             f32x4 d;
 #pragma unroll
-            for (int v = 0; v < 4; ++v) d[v] = x[u][v] * (g[v] + shift) + more[u][v];
-            if (!in[u]) continue;
-            float* row = dlogits + (size_t)(t + u * 4 * kTokens) * E;
-            if (vec) {
-                if (e < E) *reinterpret_cast<f32x4*>(row + e) = d;
-            } else {
+            for (int v = 0; v < 4; ++v) d[v] = (zero ? 0.f : x[u][v] * r * (g[v] + shift)) + more[u][v];
+            if (in[u]) {
+                float* row = dlogits + (size_t)(t + u * 4 * kTokens) * E;
+                if (vec) {
+                    if (e < E) *reinterpret_cast<f32x4*>(row + e) = d;
+                } else {
 #pragma unroll
-                for (int v = 0; v < 4; ++v)
-                    if (e + v < E) row[e + v] = d[v];
+                    for (int v = 0; v < 4; ++v)
+                        if (e + v < E) row[e + v] = d[v];
+                }
             }
         }
     }
