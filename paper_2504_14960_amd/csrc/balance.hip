@@ -58,35 +58,69 @@ __device__ __forceinline__ Chunk find_chunk(int b, const int32_t* offsets, int n
     return {lo, from, from + min(end - from, C)};
 }
 
-// Sum and maximum over the LPT neighbouring lanes of a token, in all of them: within a row of 16 lanes by data-parallel
-// primitives (quads by permutation, then mirrored halves and rows), then rows and halves of the wave swapped.
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) {
     return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
 }
+
+// One number for each of a lane's kBatches tokens, the same in all lanes of a token.  With four lanes to a token or more each
+// lane holds only that of token lane % 4, so that what is worked out from it (a reciprocal, a logarithm) is worked out once.
+template <int LPT>
+struct PerToken {
+    static constexpr int N = LPT >= 4 ? 1 : kBatches;
+    float v[N];
+
+    template <int U>
+    __device__ __forceinline__ float get() const {
+        if constexpr (LPT >= 4) return dpp<0x55 * U>(v[0]);   // quad_perm U, U, U, U
+        else return v[U];
+    }
+};
+
+// Reduces each token's numbers over its LPT neighbouring lanes.  Within a quad the four tokens are dealt to the four lanes (two
+// exchanges of halves instead of two reductions for every token), then quads are joined by rotations of a row of 16, rows and
+// halves of the wave by swaps.
 template <int LPT, typename F>
-__device__ __forceinline__ float group_reduce(float v, F&& f) {
-    if (LPT >= 2) v = f(v, dpp<0xb1>(v));     // quad_perm 1, 0, 3, 2
-    if (LPT >= 4) v = f(v, dpp<0x4e>(v));     // quad_perm 2, 3, 0, 1
-    if (LPT >= 8) v = f(v, dpp<0x141>(v));    // row_half_mirror
-    if (LPT >= 16) v = f(v, dpp<0x140>(v));   // row_mirror
-    if (LPT >= 32) {
-        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+__device__ __forceinline__ PerToken<LPT> reduce(float (&a)[kBatches], F&& f) {
+    static_assert(kBatches == 4, "a quad holds four tokens");
+    PerToken<LPT> out;
+    if constexpr (LPT < 4) {
+#pragma unroll
+        for (int u = 0; u < kBatches; ++u) out.v[u] = LPT == 2 ? f(a[u], dpp<0xb1>(a[u])) : a[u];
+    } else {
+        if constexpr (LPT == 8) {
+#pragma unroll
+            for (int u = 0; u < kBatches; ++u) a[u] = f(a[u], dpp<0x141>(a[u]));   // row_half_mirror: the other quad
+        }
+        const bool odd = threadIdx.x & 1, high = threadIdx.x & 2;
+        const float lo = f(odd ? a[1] : a[0], dpp<0xb1>(odd ? a[0] : a[1]));       // quad_perm 1, 0, 3, 2
+        const float hi = f(odd ? a[3] : a[2], dpp<0xb1>(odd ? a[2] : a[3]));
+        float v = f(high ? hi : lo, dpp<0x4e>(high ? lo : hi));                    // quad_perm 2, 3, 0, 1
+        if constexpr (LPT >= 16) {
+            v = f(v, dpp<0x124>(v));                                               // row_ror 4, then 8
+            v = f(v, dpp<0x128>(v));
+        }
+        if constexpr (LPT >= 32) {
+            const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+            v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+        }
+        if constexpr (LPT >= 64) {
+            const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+            v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+        }
+        out.v[0] = v;
     }
-    if (LPT >= 64) {
-        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
-    }
+    return out;
+}
+template <int LPT>
+__device__ __forceinline__ PerToken<LPT> reduce_sum(float (&a)[kBatches]) {
+    return reduce<LPT>(a, [](float x, float y) { return x + y; });
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
     return v;
-}
-template <int LPT>
-__device__ __forceinline__ float group_max(float v) {
-    return group_reduce<LPT>(v, [](float a, float b) { return fmaxf(a, b); });
-}
-template <int LPT>
-__device__ __forceinline__ float group_sum(float v) {
-    return group_reduce<LPT>(v, [](float a, float b) { return a + b; });
 }
 
 // A lane's four logits of a token; -inf past the last expert.
@@ -102,16 +136,63 @@ __device__ __forceinline__ f32x4 load_logits(const float* row, int e, int E, boo
     return x;
 }
 
-// x becomes exp(x - top) of a token's logits, top being the largest; returns the lane's sum of them.  All of -inf: zeros.
-template <int LPT>
-__device__ __forceinline__ float exponentials(f32x4& x, float& top) {
-    constexpr float kLog2E = 1.44269504f;
-    const float m = group_max<LPT>(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
-    top = m == -INFINITY ? 0.f : m;   // exp(-inf - 0) = 0: all -inf gives zeros, NaN stays NaN
+// A lane's logits of its next tokens, one in each of kBatches batches of `step` tokens.  ok: bit u is set where token u counts;
+// what others hold is replaced, so that it cannot spread.
+struct Batches {
+    f32x4 x[kBatches];
+    uint32_t ok;
+
+    __device__ __forceinline__ void load(const float* logits, const uint8_t* mask, int t, int step, int end, int e, int E, bool vec) {
+        ok = 0;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) x[u] = __builtin_amdgcn_exp2f((x[u] - top) * kLog2E);
-    return (x[0] + x[1]) + (x[2] + x[3]);
+        for (int u = 0; u < kBatches; ++u) {
+            const int tu = t + u * step;
+            const bool in = tu < end;
+            const size_t row = in ? tu : end - 1;
+            x[u] = load_logits(logits + row * E, e, E, vec);
+            ok |= (in && (mask == nullptr || mask[row] != 0) ? 1u : 0u) << u;
+        }
+    }
+    __device__ __forceinline__ void hide_masked() {
+#pragma unroll
+        for (int u = 0; u < kBatches; ++u)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) x[u][v] = ok >> u & 1 ? x[u][v] : 0.f;
+    }
+};
+
+// x becomes exp(x - top), top being a token's largest logit, and `sums` the lane's sums of them.  All of -inf: zeros, top 0.
+template <int LPT>
+__device__ __forceinline__ PerToken<LPT> exponentials(f32x4 (&x)[kBatches], float (&sums)[kBatches]) {
+    constexpr float kLog2E = 1.44269504f;
+    float m[kBatches];
+#pragma unroll
+    for (int u = 0; u < kBatches; ++u) m[u] = fmaxf(fmaxf(x[u][0], x[u][1]), fmaxf(x[u][2], x[u][3]));
+    PerToken<LPT> top = reduce<LPT>(m, [](float a, float b) { return fmaxf(a, b); });
+#pragma unroll
+    for (int i = 0; i < PerToken<LPT>::N; ++i) top.v[i] = top.v[i] == -INFINITY ? 0.f : top.v[i];   // exp(-inf - 0) = 0, NaN stays
+    auto one = [&](auto index) {
+        constexpr int u = index.value;
+        const float from = top.template get<u>();
+#pragma unroll
+        for (int v = 0; v < 4; ++v) x[u][v] = __builtin_amdgcn_exp2f((x[u][v] - from) * kLog2E);
+        sums[u] = (x[u][0] + x[u][1]) + (x[u][2] + x[u][3]);
+    };
+    one(std::integral_constant<int, 0>());
+    one(std::integral_constant<int, 1>());
+    one(std::integral_constant<int, 2>());
+    one(std::integral_constant<int, 3>());
+    return top;
 }
+
+// Whether the token counts that entry i of a PerToken stands for.
+template <int LPT>
+__device__ __forceinline__ bool counts_at(uint32_t ok, int i) {
+    return ok >> (LPT >= 4 ? threadIdx.x & 3 : i) & 1;
+}
+
+// log-sum-exp from the largest logit and the sum of exp(x - top), which is 1 at least; the instruction's own logarithm
+__device__ __forceinline__ float log_sum(float top, float s) { return fmaf(__builtin_amdgcn_logf(s), 0.693147181f, top); }
 
 // Workspace: what every chunk leaves, then what every sequence leaves.
 struct Partials {
@@ -139,23 +220,6 @@ inline size_t carve(void* ws, int chunks, int E, int n_seq, Partials* out) {
     if (out) *out = p;
     return o;
 }
-
-// A lane's logits of its next tokens: one in each of kBatches batches of `step` tokens.
-struct Batches {
-    f32x4 x[kBatches];
-    bool ok[kBatches];
-
-    __device__ __forceinline__ void load(const float* logits, const uint8_t* mask, int t, int step, int end, int e, int E, bool vec) {
-#pragma unroll
-        for (int u = 0; u < kBatches; ++u) {
-            const int tu = t + u * step;
-            ok[u] = tu < end;
-            const size_t row = ok[u] ? tu : end - 1;
-            x[u] = load_logits(logits + row * E, e, E, vec);
-            if (mask) ok[u] = ok[u] && mask[row] != 0;
-        }
-    }
-};
 
 // One chunk to a workgroup of up to 16 waves.
 template <int LPT>
@@ -191,40 +255,36 @@ __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __re
         Batches cur = next;
         t += kBatches * step;
         if (t < c.t1) next.load(logits, mask, t + own, step, c.t1, e, E, vec);
-        float top[kBatches], z[kBatches];
+        if (mask) cur.hide_masked();
+        float sums[kBatches];
+        const PerToken<LPT> top = exponentials<LPT>(cur.x, sums);
+        PerToken<LPT> s = reduce_sum<LPT>(sums);
 #pragma unroll
-        for (int u = 0; u < kBatches; ++u) {
-            f32x4& x = cur.x[u];
-            const float s = group_sum<LPT>(exponentials<LPT>(x, top[u]));
-            // a token that does not count, or has no probability, adds nothing and a log-sum-exp of 0
-            const bool ok = cur.ok[u] && s != 0.f;
-            const float r = __builtin_amdgcn_rcpf(s);
-#pragma unroll
-            for (int v = 0; v < 4; ++v) acc[v] += ok ? x[v] * r : 0.f;
-            top[u] = ok ? top[u] : 0.f;
-            z[u] = ok ? s : 1.f;
-            if (q == 0) n += cur.ok[u];
+        for (int i = 0; i < PerToken<LPT>::N; ++i) {
+            // a token that does not count, or has no probability, adds nothing to either loss
+            const bool ok = counts_at<LPT>(cur.ok, i) && s.v[i] != 0.f;
+            const float lse = ok ? log_sum(top.v[i], s.v[i]) : 0.f;
+            if (q < (LPT >= 4 ? 4 : 1)) zsum = fmaf(lse, lse, zsum);
+            s.v[i] = ok ? __builtin_amdgcn_rcpf(s.v[i]) : 0.f;
         }
-        // the logarithms: lane u of a token's lanes takes its batch u
-        constexpr int kShare = LPT < kBatches ? LPT : kBatches;
+        if (q == 0) n += __popc(cur.ok);
+        auto add = [&](auto index) {
+            constexpr int u = index.value;
+            const float r = s.template get<u>();
 #pragma unroll
-        for (int v = 0; v < kBatches; v += kShare) {
-            float tv = top[v], zv = z[v];
-#pragma unroll
-            for (int u = 1; u < kShare; ++u) {
-                tv = q == u ? top[v + u] : tv;
-                zv = q == u ? z[v + u] : zv;
-            }
-            const float lse = tv + logf(zv);
-            if (q < kShare) zsum = fmaf(lse, lse, zsum);
-        }
+            for (int v = 0; v < 4; ++v) acc[v] = fmaf(cur.x[u][v], r, acc[v]);
+        };
+        add(std::integral_constant<int, 0>());
+        add(std::integral_constant<int, 1>());
+        add(std::integral_constant<int, 2>());
+        add(std::integral_constant<int, 3>());
     }
     // lanes with the same experts, then waves
 #pragma unroll
     for (int off = LPT; off < 64; off <<= 1)
 #pragma unroll
         for (int u = 0; u < 4; ++u) acc[u] += __shfl_xor(acc[u], off, 64);
-    zsum = group_sum<64>(zsum);
+    zsum = wave_sum(zsum);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off, 64);
     if (lane < LPT) {
@@ -393,32 +453,41 @@ __global__ __launch_bounds__(256) void balance_backward_kernel(const float* __re
     f32x4 g;
 #pragma unroll
     for (int u = 0; u < 4; ++u) g[u] = e + u < E ? a * counts[(size_t)c.seq * E + e + u] : 0.f;
-    for (int t = c.t0 + wave * kTokens + lane / LPT; t - lane / LPT < c.t1; t += kBatches * 4 * kTokens) {
-        f32x4 x[kBatches], more[kBatches];
-        bool in[kBatches], ok[kBatches];
+    const int step = 4 * kTokens;
+    for (int t = c.t0 + wave * kTokens + lane / LPT; t - lane / LPT < c.t1; t += kBatches * step) {
+        Batches b;
+        b.load(logits, mask, t, step, c.t1, e, E, vec);
+        f32x4 more[kBatches];
+        if (addend) {
 #pragma unroll
-        for (int u = 0; u < kBatches; ++u) {
-            const int tu = t + u * 4 * kTokens;
-            in[u] = tu < c.t1;
-            const size_t row = in[u] ? tu : c.t1 - 1;
-            x[u] = load_logits(logits + row * E, e, E, vec);
-            more[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (addend) more[u] = load_logits(addend + row * E, e, E, vec);
-            ok[u] = mask == nullptr || mask[row] != 0;
+            for (int u = 0; u < kBatches; ++u) more[u] = load_logits(addend + (size_t)min(t + u * step, c.t1 - 1) * E, e, E, vec);
+        } else {
+#pragma unroll
+            for (int u = 0; u < kBatches; ++u) more[u] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
+        if (mask) b.hide_masked();
+        float sums[kBatches], dots[kBatches];
+        const PerToken<LPT> top = exponentials<LPT>(b.x, sums);
 #pragma unroll
-        for (int u = 0; u < kBatches; ++u) {
-            float top;
-            const float s = group_sum<LPT>(exponentials<LPT>(x[u], top));
-            const float w = group_sum<LPT>((x[u][0] * g[0] + x[u][1] * g[1]) + (x[u][2] * g[2] + x[u][3] * g[3]));
-            const float r = __builtin_amdgcn_rcpf(s);
-            const float shift = fmaf(az, top + logf(s), -(w * r));
-            const bool zero = !ok[u] || s == 0.f;   // does not count, or has no probability
+        for (int u = 0; u < kBatches; ++u)
+            dots[u] = (b.x[u][0] * g[0] + b.x[u][1] * g[1]) + (b.x[u][2] * g[2] + b.x[u][3] * g[3]);
+        PerToken<LPT> r = reduce_sum<LPT>(sums), shift = reduce_sum<LPT>(dots);
+#pragma unroll
+        for (int i = 0; i < PerToken<LPT>::N; ++i) {
+            // r = 0 where a token does not count or has no probability
+            const bool ok = counts_at<LPT>(b.ok, i) && r.v[i] != 0.f;
+            const float lse = log_sum(top.v[i], r.v[i]);
+            r.v[i] = ok ? __builtin_amdgcn_rcpf(r.v[i]) : 0.f;
+            shift.v[i] = ok ? fmaf(az, lse, -(shift.v[i] * r.v[i])) : 0.f;
+        }
+        auto write = [&](auto index) {
+            constexpr int u = index.value;
+            const float ru = r.template get<u>(), su = shift.template get<u>();
             f32x4 d;
 #pragma unroll
-            for (int v = 0; v < 4; ++v) d[v] = (zero ? 0.f : x[u][v] * r * (g[v] + shift)) + more[u][v];
-            if (in[u]) {
-                float* row = dlogits + (size_t)(t + u * 4 * kTokens) * E;
+            for (int v = 0; v < 4; ++v) d[v] = fmaf(b.x[u][v] * ru, g[v] + su, more[u][v]);
+            if (t + u * step < c.t1) {
+                float* row = dlogits + (size_t)(t + u * step) * E;
                 if (vec) {
                     if (e < E) *reinterpret_cast<f32x4*>(row + e) = d;
                 } else {
@@ -427,7 +496,11 @@ __global__ __launch_bounds__(256) void balance_backward_kernel(const float* __re
                         if (e + v < E) row[e + v] = d[v];
                 }
             }
-        }
+        };
+        write(std::integral_constant<int, 0>());
+        write(std::integral_constant<int, 1>());
+        write(std::integral_constant<int, 2>());
+        write(std::integral_constant<int, 3>());
     }
 }
 
