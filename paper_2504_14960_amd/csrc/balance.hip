@@ -1,10 +1,10 @@
 // Balance loss and z loss of a router, per-expert counts, and their gradient in the logits (formulas in include/moe.h).
 //
 //   balance_partial_kernel   a chunk of one sequence's tokens: sums of probabilities, counts, squares of the
-//                            log-sum-exps and valid tokens of the chunk
-//   balance_sequence_kernel  the chunks of one sequence added up in order (64 experts to a workgroup)
-//   balance_total_kernel     the two losses from all sequences
-//   balance_single_kernel    the last two in one, for one sequence
+//                            log-sum-exps and valid tokens of the chunk; a small call's only chunk writes the results
+//   balance_finish_kernel    the chunks of one sequence added up in order (some experts to a workgroup); the last
+//                            workgroup adds up the sequences
+//   balance_total_kernel     the same, where there are many sequences
 //   balance_backward_kernel  the gradient, token by token
 //
 // All are bound by memory: the forward reads the logits once, the backward reads and writes them once.  A token's logits lie
@@ -19,20 +19,33 @@ namespace moe {
 namespace {
 
 constexpr int kBatches = 4;        // tokens a lane has in flight
-constexpr int kSlab = 64;          // experts of a workgroup of balance_sequence_kernel
+constexpr int kTicketGroups = 64;  // workgroups of balance_finish_kernel of which the last one adds up the sequences
 
-// Tokens of a chunk and threads of its workgroup: functions of T (and of whether there are sequences) only, so that the
-// order of the sums is reproducible.  One sequence: up to 256 chunks, one to a compute unit, that one workgroup can add up.
-__host__ __device__ inline int chunk_tokens(int T, bool packed) {
-    if (packed) return T > 65536 ? 256 : 64;
-    const int c = (T + 255) / 256;
-    return c < 64 ? 64 : (c + 15) & ~15;
-}
+// How a call is cut, by its sizes alone, so that the order of the sums is reproducible.
+struct Cut {
+    int chunk_tokens, chunks, threads;   // balance_partial_kernel
+    int slab, slabs, finish_threads;     // balance_finish_kernel: experts of a workgroup, workgroups of a sequence
+    bool direct, ticket;
 
-inline int chunk_count(int T, int n_seq, bool packed) {
-    const int c = chunk_tokens(T, packed);
-    return packed ? T / c + n_seq : (T + c - 1) / c + (T == 0);
-}
+    Cut(int T, int E, int n_seq, bool packed) {
+        if (packed) {
+            chunk_tokens = T > 65536 ? 256 : 64;
+            chunks = T / chunk_tokens + n_seq;
+            threads = 256;
+        } else {
+            // up to 256 chunks, one to a compute unit; a small call is one
+            const int c = (T + 255) / 256;
+            chunk_tokens = (long long)T * E <= 16384 ? (T > 0 ? T : 1) : c < 64 ? 64 : (c + 15) & ~15;
+            chunks = T > 0 ? (T + chunk_tokens - 1) / chunk_tokens : 1;
+            threads = 1024;
+        }
+        direct = !packed && chunks == 1;
+        slab = packed || E <= 64 ? 64 : 16;
+        slabs = (E + slab - 1) / slab;
+        finish_threads = chunks / n_seq > 32 ? 1024 : 256;
+        ticket = n_seq * slabs <= kTicketGroups;
+    }
+};
 
 __device__ __forceinline__ int clamp_token(int t, int T) { return min(max(t, 0), T); }
 
@@ -195,39 +208,92 @@ __device__ __forceinline__ bool counts_at(uint32_t ok, int i) {
 __device__ __forceinline__ float log_sum(float top, float s) { return fmaf(__builtin_amdgcn_logf(s), 0.693147181f, top); }
 
 // Workspace: what every chunk leaves, then what every sequence leaves.
+struct Cell {
+    float prob;
+    int32_t count;
+};
+struct Tail {
+    float z;
+    int32_t tokens;
+};
 struct Partials {
-    float* prob;      // [chunks, E]
-    int32_t* count;   // [chunks, E]
-    float* z;         // [chunks]
-    int32_t* tokens;  // [chunks]
-    double* seq_loss; // [n_seq, slabs]
-    double* seq_z;    // [n_seq]
+    Cell* cell;       // [chunks, E]
+    Tail* tail;       // [chunks]
+    double* loss;     // [n_seq, slabs]
+    double* z;        // [n_seq]
+    uint32_t* ticket; // workgroups of balance_finish_kernel that are done; cleared by balance_partial_kernel
 };
 
-inline int slabs_of(int E) { return (E + kSlab - 1) / kSlab; }
-
-inline size_t carve(void* ws, int chunks, int E, int n_seq, Partials* out) {
+inline size_t carve(void* ws, const Cut& cut, int E, int n_seq, Partials* out) {
     uint8_t* base = static_cast<uint8_t*>(ws);
     size_t o = 0;
     auto take = [&](size_t bytes) { uint8_t* p = base + o; o = up256(o + bytes); return p; };
     Partials p;
-    p.prob = reinterpret_cast<float*>(take((size_t)chunks * E * 4));
-    p.count = reinterpret_cast<int32_t*>(take((size_t)chunks * E * 4));
-    p.z = reinterpret_cast<float*>(take((size_t)chunks * 4));
-    p.tokens = reinterpret_cast<int32_t*>(take((size_t)chunks * 4));
-    p.seq_loss = reinterpret_cast<double*>(take((size_t)n_seq * slabs_of(E) * 8));
-    p.seq_z = reinterpret_cast<double*>(take((size_t)n_seq * 8));
+    p.cell = reinterpret_cast<Cell*>(take((size_t)cut.chunks * E * sizeof(Cell)));
+    p.tail = reinterpret_cast<Tail*>(take((size_t)cut.chunks * sizeof(Tail)));
+    p.loss = reinterpret_cast<double*>(take((size_t)n_seq * cut.slabs * 8));
+    p.z = reinterpret_cast<double*>(take((size_t)n_seq * 8));
+    p.ticket = reinterpret_cast<uint32_t*>(take(4));
     if (out) *out = p;
     return o;
 }
+
+struct Results {
+    int32_t* counts;
+    float* prob_sums;
+    int32_t* seq_tokens;
+    float* losses;
+    float balance_coef, z_coef;
+    int E, K, n_seq;
+
+    // loss: sum over sequences of sum_e counts prob_sums / n_s
+    __device__ __forceinline__ void write_losses(double loss, double z, int n) const {
+        seq_tokens[n_seq] = n;
+        losses[0] = n ? (float)(loss * balance_coef * E / ((double)K * n)) : 0.f;
+        losses[1] = n ? (float)(z * z_coef / n) : 0.f;
+    }
+};
+
+// Three sums over the workgroup in one exchange, valid in the first wave.
+struct Three {
+    double a[16], b[16];
+    int32_t n[16];
+
+    __device__ __forceinline__ void sum(double& x, double& y, int& m) {
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) {
+            x += __shfl_xor(x, off, 64);
+            y += __shfl_xor(y, off, 64);
+            m += __shfl_xor(m, off, 64);
+        }
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+        if (lane == 0) {
+            a[wave] = x;
+            b[wave] = y;
+            n[wave] = m;
+        }
+        __syncthreads();
+        if (wave > 0) return;
+        x = lane < waves ? a[lane] : 0.;
+        y = lane < waves ? b[lane] : 0.;
+        m = lane < waves ? n[lane] : 0;
+#pragma unroll
+        for (int off = 8; off > 0; off >>= 1) {
+            x += __shfl_xor(x, off, 64);
+            y += __shfl_xor(y, off, 64);
+            m += __shfl_xor(m, off, 64);
+        }
+    }
+};
 
 // One chunk to a workgroup of up to 16 waves.
 template <int LPT>
 __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __restrict__ logits, const int32_t* __restrict__ idx,
                                                                const uint8_t* __restrict__ mask,
                                                                const int32_t* __restrict__ offsets, int T, int E, int K,
-                                                               int n_seq, int C, Partials out) {
+                                                               int n_seq, int C, bool direct, Partials out, Results res) {
     constexpr int kTokens = 64 / LPT, kExperts = 4 * LPT;
+    __shared__ Three three;
     __shared__ int32_t hist[kExperts];
     __shared__ float sums[16][kExperts];
     __shared__ float zs[16];
@@ -296,49 +362,81 @@ __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __re
         ns[wave] = n;
     }
     __syncthreads();
+    float p = 0.f;
+    int count = 0;
     if (threadIdx.x < E) {
-        float p = 0.f;
         for (int w = 0; w < waves; ++w) p += sums[w][threadIdx.x];
-        out.prob[(size_t)b * E + threadIdx.x] = p;
-        out.count[(size_t)b * E + threadIdx.x] = hist[threadIdx.x];
+        count = hist[threadIdx.x];
     }
-    if (threadIdx.x == 0) {
-        float z = 0.f;
-        int tokens = 0;
+    float z = 0.f;
+    int tokens = 0;
+    if (threadIdx.x == 0)
         for (int w = 0; w < waves; ++w) {
             z += zs[w];
             tokens += ns[w];
         }
-        out.z[b] = z;
-        out.tokens[b] = tokens;
+    if (direct) {
+        if (threadIdx.x < E) {
+            res.counts[threadIdx.x] = count;
+            res.prob_sums[threadIdx.x] = p;
+        }
+        double loss = (double)count * p, zd = z;
+        three.sum(loss, zd, tokens);
+        if (threadIdx.x == 0) {
+            res.seq_tokens[0] = tokens;
+            res.write_losses(tokens ? loss / tokens : 0., zd, tokens);
+        }
+        return;
+    }
+    if (threadIdx.x < E) out.cell[(size_t)b * E + threadIdx.x] = {p, count};
+    if (threadIdx.x == 0) {
+        out.tail[b] = {z, tokens};
+        if (b == 0) *out.ticket = 0;
     }
 }
 
-// Sums over the workgroup's 1024 or 256 threads, in all of them; `red` holds one value a wave.
-template <typename T>
-__device__ __forceinline__ T workgroup_sum(T v, T* red) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    T s = 0;
-    for (int w = 0; w < (int)blockDim.x >> 6; ++w) s += red[w];
-    return s;
+// The sums over sequences from what the workgroups of balance_finish_kernel left, in a fixed order.
+__device__ __forceinline__ void add_sequences(const Partials& in, const Results& res, int slabs, Three& three) {
+    double loss = 0., z = 0.;
+    int n = 0;
+    for (int s = threadIdx.x; s < res.n_seq; s += blockDim.x) {
+        z += in.z[s];
+        n += res.seq_tokens[s];
+    }
+    for (int i = threadIdx.x; i < res.n_seq * slabs; i += blockDim.x) loss += in.loss[i];
+    three.sum(loss, z, n);
+    if (threadIdx.x == 0) res.write_losses(loss, z, n);
 }
 
-// What the chunks [b0, b1) leave for the experts [e0, e0 + width), added up by `rows` rows of threads of `width` each (a power
-// of two) and written; returns sum_e count * prob of them in thread 0.
-__device__ __forceinline__ double add_chunks(const Partials& in, int b0, int b1, int E, int e0, int width, int32_t* counts,
-                                             float* prob_sums, double* red_p, int32_t* red_n) {
-    const int col = threadIdx.x & (width - 1), row = threadIdx.x / width, rows = blockDim.x / width, e = e0 + col;
-    double p = 0.;
-    int n = 0;
-    if (e < E) {
+// Workgroup (s, i): the chunks of sequence s for the experts [i slab, (i + 1) slab), one to a thread of a row, the chunks dealt
+// over the rows; slab is a power of two or all experts are in it.
+__global__ __launch_bounds__(1024) void balance_finish_kernel(const int32_t* __restrict__ offsets, int T, int C, int chunks,
+                                                              int slab, int width, bool ticket, Partials in, Results res) {
+    __shared__ double red_p[1024];
+    __shared__ int32_t red_n[1024];
+    __shared__ Three three;
+    __shared__ bool last;
+    const int s = blockIdx.x, E = res.E;
+    int b0 = 0, b1 = chunks;
+    if (offsets) {
+        b0 = min(first_chunk(offsets, s, T, C), chunks);
+        b1 = min(first_chunk(offsets, s + 1, T, C), chunks);
+    }
+    const int col = threadIdx.x & (width - 1), row = threadIdx.x / width, rows = blockDim.x / width;
+    const int e = blockIdx.y * slab + col;
+    double p = 0., z = 0.;
+    int n = 0, tokens = 0;
+    for (int b = b0 + threadIdx.x; b < b1; b += blockDim.x) {
+        const Tail t = in.tail[b];
+        z += t.z;
+        tokens += t.tokens;
+    }
+    if (col < slab && e < E) {
 #pragma unroll 8
         for (int b = b0 + row; b < b1; b += rows) {
-            p += in.prob[(size_t)b * E + e];
-            n += in.count[(size_t)b * E + e];
+            const Cell c = in.cell[(size_t)b * E + e];
+            p += c.prob;
+            n += c.count;
         }
     }
     red_p[threadIdx.x] = p;
@@ -352,85 +450,40 @@ __device__ __forceinline__ double add_chunks(const Partials& in, int b0, int b1,
         __syncthreads();
     }
     double loss = 0.;
-    if (row == 0 && e < E) {
-        counts[e] = red_n[col];
-        prob_sums[e] = (float)red_p[col];
+    if (row == 0 && col < slab && e < E) {
+        res.counts[(size_t)s * E + e] = red_n[col];
+        res.prob_sums[(size_t)s * E + e] = (float)red_p[col];
         loss = red_p[col] * red_n[col];
     }
-    return workgroup_sum(loss, red_p);
-}
-
-__device__ __forceinline__ void chunk_totals(const Partials& in, int b0, int b1, double* red, int32_t* red_n, double& z, int& n) {
-    z = 0.;
-    n = 0;
-    for (int b = b0 + threadIdx.x; b < b1; b += blockDim.x) {
-        z += in.z[b];
-        n += in.tokens[b];
+    three.sum(loss, z, tokens);
+    if (gridDim.x * gridDim.y == 1) {
+        if (threadIdx.x == 0) {
+            res.seq_tokens[0] = tokens;
+            res.write_losses(tokens ? loss / tokens : 0., z, tokens);
+        }
+        return;
     }
-    z = workgroup_sum(z, red);
-    n = workgroup_sum(n, red_n);
-}
-
-__device__ __forceinline__ void write_losses(double loss, double z, int n, int E, int K, float balance_coef, float z_coef,
-                                             int32_t* all_tokens, float* losses) {
-    *all_tokens = n;
-    losses[0] = n ? (float)(loss * balance_coef * E / ((double)K * n)) : 0.f;
-    losses[1] = n ? (float)(z * z_coef / n) : 0.f;
-}
-
-__global__ __launch_bounds__(1024) void balance_single_kernel(int E, int K, int chunks, int width, float balance_coef,
-                                                              float z_coef, Partials in, int32_t* __restrict__ counts,
-                                                              float* __restrict__ prob_sums, int32_t* __restrict__ seq_tokens,
-                                                              float* __restrict__ losses) {
-    __shared__ double red_p[1024];
-    __shared__ int32_t red_n[1024];
-    const double loss = add_chunks(in, 0, chunks, E, 0, width, counts, prob_sums, red_p, red_n);
-    double z;
-    int n;
-    chunk_totals(in, 0, chunks, red_p, red_n, z, n);
     if (threadIdx.x == 0) {
-        seq_tokens[0] = n;
-        write_losses(n ? loss / n : 0., z, n, E, K, balance_coef, z_coef, seq_tokens + 1, losses);
-    }
-}
-
-__global__ __launch_bounds__(256) void balance_sequence_kernel(const int32_t* __restrict__ offsets, int T, int E, int chunks,
-                                                               int C, int width, Partials in, int32_t* __restrict__ counts,
-                                                               float* __restrict__ prob_sums,
-                                                               int32_t* __restrict__ seq_tokens) {
-    __shared__ double red_p[256];
-    __shared__ int32_t red_n[256];
-    const int s = blockIdx.x, slab = blockIdx.y;
-    const int b0 = min(first_chunk(offsets, s, T, C), chunks), b1 = min(first_chunk(offsets, s + 1, T, C), chunks);
-    const double loss = add_chunks(in, b0, b1, E, slab * kSlab, width, counts + (size_t)s * E, prob_sums + (size_t)s * E, red_p, red_n);
-    double z;
-    int n;
-    chunk_totals(in, b0, b1, red_p, red_n, z, n);
-    if (threadIdx.x == 0) {
-        in.seq_loss[(size_t)s * gridDim.y + slab] = n ? loss / n : 0.;
-        if (slab == 0) {
-            seq_tokens[s] = n;
-            in.seq_z[s] = z;
+        in.loss[(size_t)s * gridDim.y + blockIdx.y] = tokens ? loss / tokens : 0.;
+        if (blockIdx.y == 0) {
+            res.seq_tokens[s] = tokens;
+            in.z[s] = z;
         }
     }
+    if (!ticket) return;
+    // the workgroup that ends last sees what all others wrote, and adds it up in the order of the sequences
+    if (threadIdx.x == 0) {
+        __threadfence();
+        last = atomicAdd(in.ticket, 1u) == gridDim.x * gridDim.y - 1;
+        __threadfence();
+    }
+    __syncthreads();
+    if (last) add_sequences(in, res, gridDim.y, three);
 }
 
-__global__ __launch_bounds__(1024) void balance_total_kernel(int E, int K, int n_seq, int slabs, float balance_coef, float z_coef,
-                                                             Partials in, int32_t* __restrict__ seq_tokens,
-                                                             float* __restrict__ losses) {
-    __shared__ double red[16];
-    __shared__ int32_t red_n[16];
-    double l = 0., z = 0.;
-    int n = 0;
-    for (int s = threadIdx.x; s < n_seq; s += 1024) {
-        z += in.seq_z[s];
-        n += seq_tokens[s];
-    }
-    for (int i = threadIdx.x; i < n_seq * slabs; i += 1024) l += in.seq_loss[i];
-    l = workgroup_sum(l, red);
-    z = workgroup_sum(z, red);
-    n = workgroup_sum(n, red_n);
-    if (threadIdx.x == 0) write_losses(l, z, n, E, K, balance_coef, z_coef, seq_tokens + n_seq, losses);
+__global__ __launch_bounds__(1024) void balance_total_kernel(int slabs, Partials in, Results res) {
+    __shared__ Three three;
+    add_sequences(in, res, slabs, three);
 }
 
 template <int LPT>
@@ -526,31 +579,25 @@ inline int power_of_two(int n) {
 }  // namespace
 
 size_t balance_loss_workspace_bytes(int T, int E, int n_seq) {
-    // with offsets or without: the larger of the two numbers of chunks
-    return carve(nullptr, max(chunk_count(T, n_seq, true), chunk_count(T, n_seq, false)), E, n_seq, nullptr);
+    // with offsets or without: the larger of the two
+    return max(carve(nullptr, Cut(T, E, n_seq, true), E, n_seq, nullptr), carve(nullptr, Cut(T, E, n_seq, false), E, n_seq, nullptr));
 }
 
 void launch_balance_loss(const float* logits, const int32_t* idx, const uint8_t* mask, const int32_t* offsets, int T, int E,
                          int K, int n_seq, float balance_coef, float z_coef, int32_t* counts, float* prob_sums,
                          int32_t* seq_tokens, float* losses, void* ws, hipStream_t s) {
-    const bool packed = offsets != nullptr;
-    const int chunks = chunk_count(T, n_seq, packed), C = chunk_tokens(T, packed);
+    const Cut cut(T, E, n_seq, offsets != nullptr);
     Partials p;
-    carve(ws, chunks, E, n_seq, &p);
+    carve(ws, cut, E, n_seq, &p);
+    const Results res = {counts, prob_sums, seq_tokens, losses, balance_coef, z_coef, E, K, n_seq};
     with_lanes(E, [&](auto lanes) {
-        hipLaunchKernelGGL(balance_partial_kernel<lanes.value>, dim3(chunks), dim3(packed ? 256 : 1024), 0, s, logits, idx, mask,
-                           offsets, T, E, K, n_seq, C, p);
+        hipLaunchKernelGGL(balance_partial_kernel<lanes.value>, dim3(cut.chunks), dim3(cut.threads), 0, s, logits, idx, mask,
+                           offsets, T, E, K, n_seq, cut.chunk_tokens, cut.direct, p, res);
     });
-    if (!packed) {
-        hipLaunchKernelGGL(balance_single_kernel, dim3(1), dim3(1024), 0, s, E, K, chunks, power_of_two(E), balance_coef, z_coef,
-                           p, counts, prob_sums, seq_tokens, losses);
-        return;
-    }
-    const int slabs = slabs_of(E);
-    hipLaunchKernelGGL(balance_sequence_kernel, dim3(n_seq, slabs), dim3(256), 0, s, offsets, T, E, chunks, C,
-                       power_of_two(E < kSlab ? E : kSlab), p, counts, prob_sums, seq_tokens);
-    hipLaunchKernelGGL(balance_total_kernel, dim3(1), dim3(1024), 0, s, E, K, n_seq, slabs, balance_coef, z_coef, p, seq_tokens,
-                       losses);
+    if (cut.direct) return;
+    hipLaunchKernelGGL(balance_finish_kernel, dim3(n_seq, cut.slabs), dim3(cut.finish_threads), 0, s, offsets, T,
+                       cut.chunk_tokens, cut.chunks, cut.slab, power_of_two(E < cut.slab ? E : cut.slab), cut.ticket, p, res);
+    if (!cut.ticket) hipLaunchKernelGGL(balance_total_kernel, dim3(1), dim3(1024), 0, s, cut.slabs, p, res);
 }
 
 void launch_balance_loss_backward(const float* logits, const uint8_t* mask, const int32_t* offsets, const int32_t* counts,
