@@ -347,9 +347,8 @@ def router_backward(x: torch.Tensor, w_router: torch.Tensor, logits: torch.Tenso
     H = x.shape[1]
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     if dlogits_addend is not None:
-        _expect("dlogits_addend", dlogits_addend, torch.float32, T * E)
-        _check(lib().moe_router_backward_addend(_ptr(x), _ptr(w_router), _ptr(logits), _ptr(topk_idx), _ptr(dgate),
-                                                _ptr(dlogits_addend), T, H, E, K, int(bool(renormalize)), _dt(x),
+        addend = _expect("dlogits_addend", dlogits_addend, torch.float32, T * E)
+        _check(lib().moe_router_backward_addend(_ptr(x), _ptr(w_router), _ptr(logits), _ptr(topk_idx), _ptr(dgate), addend, T, H, E, K, int(bool(renormalize)), _dt(x),
                                                 _ptr(dlogits), _ptr(dx), _ptr(dw_router), _ptr(dbias), _ptr(workspace),
                                                 nbytes, _stream()))
         return
@@ -359,23 +358,31 @@ def router_backward(x: torch.Tensor, w_router: torch.Tensor, logits: torch.Tenso
 
 
 # ---- what follows the gradients in a training step: balance loss, gradient norm, AdamW ----
-def _expect(name: str, t: torch.Tensor, dtype, numel: int) -> None:
+def _is(name: str, t: torch.Tensor, dtype, numel: int) -> None:
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
     if t.numel() != numel:
         raise ValueError(f"{name} must have {numel} elements, not {t.numel()}")
 
 
-def _sequences(T: int, token_mask: Optional[torch.Tensor], seq_offsets: Optional[torch.Tensor]) -> int:
-    """Checks mask and offsets; the number of sequences."""
-    if token_mask is not None and token_mask.dtype != torch.bool:
-        _expect("token_mask", token_mask, torch.uint8, T)
-    elif token_mask is not None:
-        _expect("token_mask", token_mask, torch.bool, T)
+def _expect(name: str, t: torch.Tensor, dtype, numel: int):
+    """The device pointer of a tensor of this type and size."""
+    _is(name, t, dtype, numel)
+    return _ptr(t)
+
+
+def _mask(token_mask: Optional[torch.Tensor], T: int):
+    if token_mask is None:
+        return None
+    return _expect("token_mask", token_mask, torch.bool if token_mask.dtype == torch.bool else torch.uint8, T)
+
+
+def _offsets(seq_offsets: Optional[torch.Tensor]):
+    """Pointer and number of sequences."""
     if seq_offsets is None:
-        return 1
-    _expect("seq_offsets", seq_offsets, torch.int32, max(2, seq_offsets.numel()))
-    return seq_offsets.numel() - 1
+        return None, 1
+    n = seq_offsets.numel()
+    return _expect("seq_offsets", seq_offsets, torch.int32, max(2, n)), n - 1
 
 
 def balance_loss_workspace_bytes(T: int, E: int, n_seq: int = 1) -> int:
@@ -388,17 +395,14 @@ def balance_loss(logits: torch.Tensor, topk_idx: torch.Tensor, balance_coef: flo
     """losses [2] = balance and z loss of a router's logits [T, E] and selection [T, K]; counts and prob_sums [n_seq, E],
     seq_tokens [n_seq + 1].  token_mask [T] (uint8 or bool): tokens that count; seq_offsets [n_seq + 1] int32."""
     T, E = logits.shape
-    n_seq = _sequences(T, token_mask, seq_offsets)
-    _expect("logits", logits, torch.float32, T * E)
-    _expect("topk_idx", topk_idx, torch.int32, T * topk_idx.shape[1])
-    _expect("counts", counts, torch.int32, n_seq * E)
-    _expect("prob_sums", prob_sums, torch.float32, n_seq * E)
-    _expect("seq_tokens", seq_tokens, torch.int32, n_seq + 1)
-    _expect("losses", losses, torch.float32, 2)
-    _check(lib().moe_balance_loss(_ptr(logits), _ptr(topk_idx), _ptr(token_mask), _ptr(seq_offsets), T, E,
-                                  topk_idx.shape[1], n_seq, balance_coef, z_coef, _ptr(counts), _ptr(prob_sums),
-                                  _ptr(seq_tokens), _ptr(losses), _ptr(workspace),
-                                  workspace.numel() * workspace.element_size(), _stream()))
+    K = topk_idx.shape[1]
+    offsets, n_seq = _offsets(seq_offsets)
+    f32, i32 = torch.float32, torch.int32
+    _check(lib().moe_balance_loss(
+        _expect("logits", logits, f32, T * E), _expect("topk_idx", topk_idx, i32, T * K), _mask(token_mask, T), offsets, T, E, K,
+        n_seq, balance_coef, z_coef, _expect("counts", counts, i32, n_seq * E),
+        _expect("prob_sums", prob_sums, f32, n_seq * E), _expect("seq_tokens", seq_tokens, i32, n_seq + 1),
+        _expect("losses", losses, f32, 2), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()))
 
 
 def balance_loss_backward(logits: torch.Tensor, counts: torch.Tensor, seq_tokens: torch.Tensor,
@@ -407,18 +411,13 @@ def balance_loss_backward(logits: torch.Tensor, counts: torch.Tensor, seq_tokens
                           token_mask: Optional[torch.Tensor] = None, seq_offsets: Optional[torch.Tensor] = None) -> None:
     """dlogits [T, E] = gradient of dlosses . losses in the logits, plus addend [T, E] (which may be dlogits)."""
     T, E = logits.shape
-    n_seq = _sequences(T, token_mask, seq_offsets)
-    _expect("logits", logits, torch.float32, T * E)
-    _expect("counts", counts, torch.int32, n_seq * E)
-    _expect("seq_tokens", seq_tokens, torch.int32, n_seq + 1)
-    _expect("dlogits", dlogits, torch.float32, T * E)
-    if dlosses is not None:
-        _expect("dlosses", dlosses, torch.float32, 2)
-    if addend is not None:
-        _expect("addend", addend, torch.float32, T * E)
-    _check(lib().moe_balance_loss_backward(_ptr(logits), _ptr(token_mask), _ptr(seq_offsets), _ptr(counts),
-                                           _ptr(seq_tokens), _ptr(dlosses), _ptr(addend), T, E, K, n_seq, balance_coef,
-                                           z_coef, _ptr(dlogits), _stream()))
+    offsets, n_seq = _offsets(seq_offsets)
+    f32, i32 = torch.float32, torch.int32
+    _check(lib().moe_balance_loss_backward(
+        _expect("logits", logits, f32, T * E), _mask(token_mask, T), offsets, _expect("counts", counts, i32, n_seq * E),
+        _expect("seq_tokens", seq_tokens, i32, n_seq + 1), None if dlosses is None else _expect("dlosses", dlosses, f32, 2),
+        None if addend is None else _expect("addend", addend, f32, T * E), T, E, K, n_seq, balance_coef, z_coef,
+        _expect("dlogits", dlogits, f32, T * E), _stream()))
 
 
 class GradTensors:
@@ -437,9 +436,8 @@ def grad_norm(tensors, out: torch.Tensor, workspace: torch.Tensor, max_norm: flo
     """out [2] = norm of multiplier * the gradients of a GradTensors (or an AdamWTensors), and the factor that
     adamw_step takes as grad_scale: multiplier, clipped to max_norm (0: not), NaN where the norm is not finite."""
     grads = tensors.grads if isinstance(tensors, AdamWTensors) else tensors
-    _expect("out", out, torch.float32, 2)
-    _check(lib().moe_grad_norm(grads._list, len(grads._list), max_norm, multiplier, _ptr(out), _ptr(workspace),
-                               workspace.numel() * workspace.element_size(), _stream()))
+    _check(lib().moe_grad_norm(grads._list, len(grads._list), max_norm, multiplier, _expect("out", out, torch.float32, 2),
+                               _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()))
 
 
 class AdamWTensors:
@@ -467,18 +465,16 @@ class AdamWTensors:
         count = param.numel()
         state = MOE_STATE_MXFP8 if m.dtype == torch.uint8 else MOE_STATE_F32
         kind = torch.uint8 if state == MOE_STATE_MXFP8 else torch.float32
-        _expect("exp_avg", m, kind, count)
-        _expect("exp_avg_sq", v, kind, count)
-        _expect("grad", grad, grad.dtype, count)
+        _is("exp_avg", m, kind, count)
+        _is("exp_avg_sq", v, kind, count)
+        _is("grad", grad, grad.dtype, count)
         if master is not None:
-            _expect("master", master, torch.float32, count)
+            _is("master", master, torch.float32, count)
         for name, t in (("exp_avg_scale", m_scale), ("exp_avg_sq_scale", v_scale)):
-            if state == MOE_STATE_MXFP8:
-                if t is None:
-                    raise ValueError(f"8-bit states need {name}s")
-                _expect(name, t, torch.uint8, (count + 31) // 32)
-            elif t is not None:
-                raise ValueError(f"{name} goes with 8-bit states only")
+            if (t is None) != (state == MOE_STATE_F32):
+                raise ValueError(f"8-bit states need {name}s" if t is None else f"{name} goes with 8-bit states only")
+            if t is not None:
+                _is(name, t, torch.uint8, (count + 31) // 32)
         return (_ptr(param), _ptr(master), _ptr(grad), _ptr(m), _ptr(v), _ptr(m_scale), _ptr(v_scale), count, decay,
                 lr_scale, _dt(param), _dt(grad), state)
 
@@ -487,10 +483,9 @@ def adamw_step(tensors: AdamWTensors, lr: float, beta1: float, beta2: float, eps
                grad_scale: Optional[torch.Tensor] = None) -> None:
     """One AdamW step (the first has step = 1) over all tensors.  grad_scale [1] fp32 on the device multiplies every
     gradient; NaN in it leaves everything as it is.  seed: of stochastic rounding, another one in every step."""
-    if grad_scale is not None:
-        _expect("grad_scale", grad_scale, torch.float32, 1)
-    _check(lib().moe_adamw_step(tensors._list, len(tensors._list), lr, beta1, beta2, eps, step, seed & 0xffffffff,
-                                _ptr(grad_scale), _stream()))
+    scale = None if grad_scale is None else _expect("grad_scale", grad_scale, torch.float32, 1)
+    _check(lib().moe_adamw_step(tensors._list, len(tensors._list), lr, beta1, beta2, eps, step, seed & 0xffffffff, scale,
+                                _stream()))
 
 
 def expert_backward_workspace_bytes(R_max: int, H: int, F: int, E: int) -> int:
@@ -606,9 +601,9 @@ def layer_backward(x: torch.Tensor, w_router: torch.Tensor, w_gate: torch.Tensor
     T, H = x.shape
     E, F, _ = w_gate.shape
     if dlogits_addend is not None:
-        _expect("dlogits_addend", dlogits_addend, torch.float32, T * E)
+        addend = _expect("dlogits_addend", dlogits_addend, torch.float32, T * E)
         _check(lib().moe_layer_backward_addend(_ptr(x), _ptr(w_router), _ptr(w_gate), _ptr(w_up), _ptr(wgu_t),
-                                               _ptr(wd_t), _ptr(dy), _ptr(dlogits_addend), T, H, E, K, F,
+                                               _ptr(wd_t), _ptr(dy), addend, T, H, E, K, F,
                                                int(renormalize), int(capacity), _ptr(forward_workspace), _ptr(gu),
                                                _ptr(dx), _ptr(dw_router), _ptr(dbias), _ptr(dw_gate), _ptr(dw_up),
                                                _ptr(dw_down), _ptr(workspace),

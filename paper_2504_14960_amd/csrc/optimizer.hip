@@ -2,6 +2,8 @@
 //
 // A launch takes a list of tensors, described in its arguments; every tensor is cut into pieces, and a workgroup finds its
 // tensor from the first pieces.  Both are bound by memory.
+#include <string.h>
+
 #include <type_traits>
 
 #include "common.h"
@@ -10,7 +12,6 @@ namespace moe {
 
 namespace {
 
-constexpr int kListTensors = 48;   // 80 bytes each: a launch's arguments are limited to 4 KiB
 constexpr int kPieceF32 = 1024, kPieceMxfp8 = 2048;   // elements of an AdamW workgroup, by states
 constexpr int kBlock = 32;         // elements that share a scale
 constexpr int64_t kLaunchPieces = (1 << 24) - 1;   // 256 threads each: a grid has less than 2^32 threads
@@ -136,24 +137,30 @@ __global__ __launch_bounds__(256) void grad_norm_finish_kernel(const double* __r
 // -------------------------------------------------------------------------------------------------------------
 // AdamW
 
+// A tensor in a launch's arguments, which are limited to 4 KiB: six words of 64 bits and one or two more where its types need
+// them, so that a launch takes 72 tensors in fp32, 61 in bf16 with masters, 48 of those with 8-bit states.
+//   n | kind << 48;  1 - lr wd, lr / (1 - beta1^t);  grad;  what is stepped (param or master);  m;  v;
+//   [param, where there is a master];  [scales of m; of v]
+constexpr int kAdamTensors = 72, kAdamWords = 432;
+
+struct AdamList {
+    uint64_t word[kAdamWords];
+    int32_t first[kAdamTensors];   // first piece
+    uint16_t at[kAdamTensors];     // first word
+    int32_t count, index;          // index: place of the first in the caller's list
+};
+
 struct AdamTensor {
-    void* param;
-    float* master;
     const void* grad;
+    void* stepped;
     void* m;
     void* v;
+    void* copy;                // the bf16 weights beside a master
     uint8_t* m_scale;
     uint8_t* v_scale;
     int64_t n;
-    float decay, step_size;   // 1 - lr wd, lr / (1 - beta1^t)
-    int32_t index;            // place in the caller's list
-    int32_t kind;
-};
-
-struct AdamList {
-    AdamTensor t[kListTensors];
-    int32_t first[kListTensors];   // first piece
-    int32_t count;
+    float decay, step_size;
+    int index;
 };
 
 struct AdamStep {
@@ -304,15 +311,14 @@ struct AdamInput {
     uint32_t m_scale, v_scale;
 
     __device__ __forceinline__ void load(const AdamTensor& t, int64_t j, bool whole, int left) {
-        const void* param = PARAM == kParamMaster ? static_cast<const void*>(t.master) : t.param;
         if (whole) {
             g.load(t.grad, j);
-            p.load(param, j);
+            p.load(t.stepped, j);
             m.load(t.m, j);
             v.load(t.v, j);
         } else {
             g.load_some(t.grad, j, left);
-            p.load_some(param, j, left);
+            p.load_some(t.stepped, j, left);
             m.load_some(t.m, j, left);
             v.load_some(t.v, j, left);
         }
@@ -403,13 +409,13 @@ __device__ __forceinline__ void adamw_piece(const AdamTensor& t, const AdamStep&
         pv.set(v);
     }
     if (whole) {
-        if (PARAM != kParamBf16) p32.store(PARAM == kParamMaster ? static_cast<void*>(t.master) : t.param, j);
-        if (PARAM != kParamF32) p16.store(t.param, j);
+        if (PARAM != kParamBf16) p32.store(t.stepped, j);
+        if (PARAM != kParamF32) p16.store(PARAM == kParamMaster ? t.copy : t.stepped, j);
         pm.store(t.m, j);
         pv.store(t.v, j);
     } else {
-        if (PARAM != kParamBf16) p32.store_some(PARAM == kParamMaster ? static_cast<void*>(t.master) : t.param, j, left);
-        if (PARAM != kParamF32) p16.store_some(t.param, j, left);
+        if (PARAM != kParamBf16) p32.store_some(t.stepped, j, left);
+        if (PARAM != kParamF32) p16.store_some(PARAM == kParamMaster ? t.copy : t.stepped, j, left);
         pm.store_some(t.m, j, left);
         pv.store_some(t.v, j, left);
     }
@@ -425,9 +431,17 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamList l, AdamStep h) {
     const float scale = h.grad_scale ? *h.grad_scale : 1.f;
     if (scale != scale) return;
     const int i = find_tensor(l, blockIdx.x);
-    const AdamTensor& t = l.t[i];
     const int64_t piece = (int)blockIdx.x - l.first[i];
-    switch (t.kind) {
+    const uint64_t* w = l.word + l.at[i];
+    const int kind = (int)(w[0] >> 48);
+    const bool master = kind % 6 / 2 == kParamMaster, mxfp8 = kind >= 6;
+    const uint64_t* scales = w + (mxfp8 ? 6 + master : 0);   // in range and not used where there are none
+    const AdamTensor t = {reinterpret_cast<const void*>(w[2]), reinterpret_cast<void*>(w[3]), reinterpret_cast<void*>(w[4]),
+                          reinterpret_cast<void*>(w[5]), reinterpret_cast<void*>(w[master ? 6 : 0]),
+                          reinterpret_cast<uint8_t*>(scales[0]), reinterpret_cast<uint8_t*>(scales[1]),
+                          (int64_t)(w[0] & ((1ull << 48) - 1)), __uint_as_float((uint32_t)w[1]),
+                          __uint_as_float((uint32_t)(w[1] >> 32)), l.index + i};
+    switch (kind) {
         case 0: return adamw_piece<kParamF32, false, false>(t, h, scale, piece);
         case 1: return adamw_piece<kParamF32, true, false>(t, h, scale, piece);
         case 2: return adamw_piece<kParamMaster, false, false>(t, h, scale, piece);
@@ -457,7 +471,7 @@ inline int64_t pieces_of(const moe_adamw_tensor_t& t) {
 }  // namespace
 
 size_t grad_norm_workspace_bytes(int count) {
-    // a launch takes one tensor at least; fewer than kGradTensors only where the runs run out
+    // a launch takes one tensor at least; fewer than kGradTensors only where there are too many runs
     return (size_t)(count > 0 ? count : 1) * kNormGroups * sizeof(double);
 }
 
@@ -498,21 +512,41 @@ void launch_adamw(const moe_adamw_tensor_t* tensors, int count, double lr, doubl
                         (float)(1. / sqrt(bc2)), seed, grad_scale};
     AdamList l;
     int64_t pieces = 0;
+    int words = 0;
     l.count = 0;
     auto flush = [&] {
-        if (l.count) hipLaunchKernelGGL(adamw_kernel, dim3((unsigned)pieces), dim3(256), 0, s, l, h);
-        l.count = 0;
+        if (pieces) hipLaunchKernelGGL(adamw_kernel, dim3((unsigned)pieces), dim3(256), 0, s, l, h);
+        l.count = words = 0;
         pieces = 0;
+    };
+    auto put = [&](const void* p) { l.word[words++] = reinterpret_cast<uint64_t>(p); };
+    auto bits = [](double x) {
+        const float f = (float)x;
+        uint32_t u;
+        memcpy(&u, &f, sizeof u);
+        return (uint64_t)u;
     };
     for (int i = 0; i < count; ++i) {
         const moe_adamw_tensor_t& t = tensors[i];
         const int64_t more = pieces_of(t);
-        if (more == 0) continue;
-        if (l.count == kListTensors || pieces + more > kLaunchPieces) flush();
+        const bool mxfp8 = t.state == MOE_STATE_MXFP8;
+        if (l.count == kAdamTensors || words + 6 + (t.master ? 1 : 0) + (mxfp8 ? 2 : 0) > kAdamWords || pieces + more > kLaunchPieces)
+            flush();
+        if (l.count == 0) l.index = i;
         const double lr_i = lr * t.lr_scale;
         l.first[l.count] = (int32_t)pieces;
-        l.t[l.count++] = {t.param, t.master, t.grad, t.exp_avg, t.exp_avg_sq, t.exp_avg_scale, t.exp_avg_sq_scale, t.n,
-                          (float)(1. - lr_i * t.weight_decay), (float)(lr_i / bc1), i, kind_of(t)};
+        l.at[l.count++] = (uint16_t)words;
+        l.word[words++] = (uint64_t)t.n | (uint64_t)kind_of(t) << 48;
+        l.word[words++] = bits(1. - lr_i * t.weight_decay) | bits(lr_i / bc1) << 32;
+        put(t.grad);
+        put(t.master ? t.master : t.param);
+        put(t.exp_avg);
+        put(t.exp_avg_sq);
+        if (t.master) put(t.param);
+        if (mxfp8) {
+            put(t.exp_avg_scale);
+            put(t.exp_avg_sq_scale);
+        }
         pieces += more;
     }
     flush();
