@@ -30,12 +30,11 @@ struct GradList {
     int32_t count, runs;
 };
 
-template <typename List>
-__device__ __forceinline__ int find_tensor(const List& l, int piece) {
+__device__ __forceinline__ int find_tensor(const GradList& l, int run) {
     int lo = 0, hi = l.count;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (l.first[mid] <= piece) lo = mid;
+        if (l.first[mid] <= run) lo = mid;
         else hi = mid;
     }
     return lo;
@@ -137,17 +136,19 @@ __global__ __launch_bounds__(256) void grad_norm_finish_kernel(const double* __r
 // -------------------------------------------------------------------------------------------------------------
 // AdamW
 
-// A tensor in a launch's arguments, which are limited to 4 KiB: six words of 64 bits and one or two more where its types need
-// them, so that a launch takes 72 tensors in fp32, 61 in bf16 with masters, 48 of those with 8-bit states.
+// A tensor in a launch's arguments, which are limited to 4 KiB: six words of 64 bits and up to three more where its types need
+// them, so that a launch takes 70 tensors in fp32, 60 in bf16 with masters, 46 of those with 8-bit states.
 //   n | kind << 48;  1 - lr wd, lr / (1 - beta1^t);  grad;  what is stepped (param or master);  m;  v;
-//   [param, where there is a master];  [scales of m; of v]
-constexpr int kAdamTensors = 72, kAdamWords = 432;
+//   [scales of m; of v];  [param, where there is a master]
+constexpr int kAdamTensors = 70, kAdamWords = 420, kWordsMost = 9;
 
 struct AdamList {
-    uint64_t word[kAdamWords];
-    int32_t first[kAdamTensors];   // first piece
-    uint16_t at[kAdamTensors];     // first word
-    int32_t count, index;          // index: place of the first in the caller's list
+    // pointers, so that they are known to point to device memory; as many as the longest tensor has are read of each
+    void* word[kAdamWords + kWordsMost - 6];
+    struct {
+        int32_t first, at;                        // first piece, first word
+    } tensor[kAdamTensors];
+    int32_t count, index;                         // index: place of the first in the caller's list
 };
 
 struct AdamTensor {
@@ -341,6 +342,7 @@ __device__ __forceinline__ void adamw_piece(const AdamTensor& t, const AdamStep&
     const int left = (int)min((int64_t)V, t.n - j);   // none or negative: this lane has nothing
     Input cur;
     cur.load(t, j, whole, left);
+    if (scale != scale) return;   // here, where what is read is on its way
     float p[V], g[V], m[V], v[V];
     cur.g.values(g);
     cur.p.values(p);
@@ -429,18 +431,27 @@ __device__ __forceinline__ void adamw_piece(const AdamTensor& t, const AdamStep&
 
 __global__ __launch_bounds__(256) void adamw_kernel(AdamList l, AdamStep h) {
     const float scale = h.grad_scale ? *h.grad_scale : 1.f;
-    if (scale != scale) return;
-    const int i = find_tensor(l, blockIdx.x);
-    const int64_t piece = (int)blockIdx.x - l.first[i];
-    const uint64_t* w = l.word + l.at[i];
-    const int kind = (int)(w[0] >> 48);
-    const bool master = kind % 6 / 2 == kParamMaster, mxfp8 = kind >= 6;
-    const uint64_t* scales = w + (mxfp8 ? 6 + master : 0);   // in range and not used where there are none
-    const AdamTensor t = {reinterpret_cast<const void*>(w[2]), reinterpret_cast<void*>(w[3]), reinterpret_cast<void*>(w[4]),
-                          reinterpret_cast<void*>(w[5]), reinterpret_cast<void*>(w[master ? 6 : 0]),
-                          reinterpret_cast<uint8_t*>(scales[0]), reinterpret_cast<uint8_t*>(scales[1]),
-                          (int64_t)(w[0] & ((1ull << 48) - 1)), __uint_as_float((uint32_t)w[1]),
-                          __uint_as_float((uint32_t)(w[1] >> 32)), l.index + i};
+    int lo = 0, hi = l.count, first = 0, at = 0;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        const auto m = l.tensor[mid];
+        if (m.first <= (int)blockIdx.x) {
+            lo = mid;
+            first = m.first;
+            at = m.at;
+        } else {
+            hi = mid;
+        }
+    }
+    const int64_t piece = (int)blockIdx.x - first;
+    void* w[kWordsMost];
+#pragma unroll
+    for (int k = 0; k < kWordsMost; ++k) w[k] = l.word[at + k];
+    const uint64_t size = reinterpret_cast<uint64_t>(w[0]), rates = reinterpret_cast<uint64_t>(w[1]);
+    const int kind = (int)(size >> 48);
+    const AdamTensor t = {w[2], w[3], w[4], w[5], kind >= 6 ? w[8] : w[6], static_cast<uint8_t*>(w[6]), static_cast<uint8_t*>(w[7]),
+                          (int64_t)(size & ((1ull << 48) - 1)), __uint_as_float((uint32_t)rates),
+                          __uint_as_float((uint32_t)(rates >> 32)), l.index + lo};
     switch (kind) {
         case 0: return adamw_piece<kParamF32, false, false>(t, h, scale, piece);
         case 1: return adamw_piece<kParamF32, true, false>(t, h, scale, piece);
@@ -519,7 +530,8 @@ void launch_adamw(const moe_adamw_tensor_t* tensors, int count, double lr, doubl
         l.count = words = 0;
         pieces = 0;
     };
-    auto put = [&](const void* p) { l.word[words++] = reinterpret_cast<uint64_t>(p); };
+    auto put = [&](const void* p) { l.word[words++] = const_cast<void*>(p); };
+    auto put_bits = [&](uint64_t b) { l.word[words++] = reinterpret_cast<void*>(b); };
     auto bits = [](double x) {
         const float f = (float)x;
         uint32_t u;
@@ -534,19 +546,19 @@ void launch_adamw(const moe_adamw_tensor_t* tensors, int count, double lr, doubl
             flush();
         if (l.count == 0) l.index = i;
         const double lr_i = lr * t.lr_scale;
-        l.first[l.count] = (int32_t)pieces;
-        l.at[l.count++] = (uint16_t)words;
-        l.word[words++] = (uint64_t)t.n | (uint64_t)kind_of(t) << 48;
-        l.word[words++] = bits(1. - lr_i * t.weight_decay) | bits(lr_i / bc1) << 32;
+        l.tensor[l.count].first = (int32_t)pieces;
+        l.tensor[l.count++].at = words;
+        put_bits((uint64_t)t.n | (uint64_t)kind_of(t) << 48);
+        put_bits(bits(1. - lr_i * t.weight_decay) | bits(lr_i / bc1) << 32);
         put(t.grad);
         put(t.master ? t.master : t.param);
         put(t.exp_avg);
         put(t.exp_avg_sq);
-        if (t.master) put(t.param);
         if (mxfp8) {
             put(t.exp_avg_scale);
             put(t.exp_avg_sq_scale);
         }
+        if (t.master) put(t.param);
         pieces += more;
     }
     flush();
