@@ -302,7 +302,7 @@ __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __re
                                                                const int32_t* __restrict__ offsets, int T, int E, int K,
                                                                int n_seq, int C, bool direct, Partials out, Results res) {
     constexpr int kTokens = 64 / LPT, kExperts = 4 * LPT;
-    __shared__ Three three;
+    __shared__ double parts[4];
     __shared__ int32_t hist[kExperts];
     __shared__ float sums[16][kExperts];
     __shared__ float zs[16];
@@ -381,33 +381,40 @@ __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __re
     float p = 0.f;
     int count = 0;
     if (threadIdx.x < E) {
-        for (int w = 0; w < waves; ++w) p += sums[w][threadIdx.x];
+#pragma unroll
+        for (int w = 0; w < 16; ++w) p += w < waves ? sums[w][threadIdx.x] : 0.f;
         count = hist[threadIdx.x];
     }
-    float z = 0.f;
+    double z = 0., loss = 0.;
     int tokens = 0;
-    if (threadIdx.x == 0)
-        for (int w = 0; w < waves; ++w) {
-            z += zs[w];
-            tokens += ns[w];
-        }
-    if (direct) {
-        if (threadIdx.x < E) {
-            res.counts[threadIdx.x] = count;
-            res.prob_sums[threadIdx.x] = p;
-        }
-        double loss = (double)count * p, zd = z;
-        three.sum(loss, zd, tokens);
+    if (wave == 0) {
+        z = lane < waves ? (double)zs[lane] : 0.;
+        tokens = lane < waves ? ns[lane] : 0;
+        add_over_wave(z, tokens);
+    }
+    if (!direct) {
+        if (threadIdx.x < E) out.cell[(size_t)b * E + threadIdx.x] = {p, count};
         if (threadIdx.x == 0) {
-            res.seq_tokens[0] = tokens;
-            res.write_losses(tokens ? loss / tokens : 0., zd, tokens);
+            out.tail[b] = {(float)z, tokens};
+            if (b == 0) *out.ticket = 0;
         }
         return;
     }
-    if (threadIdx.x < E) out.cell[(size_t)b * E + threadIdx.x] = {p, count};
+    if (threadIdx.x < E) {
+        res.counts[threadIdx.x] = count;
+        res.prob_sums[threadIdx.x] = p;
+        loss = (double)p * count;
+    }
+    int none = 0;
+    add_over_wave(loss, none);
+    if (kExperts > 64) {
+        if (lane == 0 && wave < 4) parts[wave] = loss;
+        __syncthreads();
+        loss = (parts[0] + parts[1]) + (parts[2] + parts[3]);
+    }
     if (threadIdx.x == 0) {
-        out.tail[b] = {z, tokens};
-        if (b == 0) *out.ticket = 0;
+        res.seq_tokens[0] = tokens;
+        res.write_losses(tokens ? loss / tokens : 0., z, tokens);
     }
 }
 
@@ -479,9 +486,10 @@ __global__ __launch_bounds__(1024) void balance_finish_kernel(const int32_t* __r
         if (lane < width && e < E) {
             p = 0.;
             n = 0;
-            for (int w = 0; w < waves; ++w) {
-                p += red_p[w][lane];
-                n += red_n[w][lane];
+#pragma unroll
+            for (int w = 0; w < 16; ++w) {
+                p += w < waves ? red_p[w][lane] : 0.;
+                n += w < waves ? red_n[w][lane] : 0;
             }
             res.counts[(size_t)s * E + e] = n;
             res.prob_sums[(size_t)s * E + e] = (float)p;

@@ -49,14 +49,13 @@ __device__ __forceinline__ float load_value(const void* p, bool bf16, int64_t i)
 
 constexpr int kNormGroups = 1024;   // workgroups, and partial sums, of a launch at most
 
+// Sum over the workgroup's four waves, in its first wave.
 __device__ __forceinline__ double group_sum(double v, double* red) {
-    red[threadIdx.x] = v;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
-    for (int d = 128; d > 0; d >>= 1) {
-        if (threadIdx.x < d) red[threadIdx.x] += red[threadIdx.x + d];
-        __syncthreads();
-    }
-    return red[0];
+    return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
 // Sum of the squares of 16 bytes of values.  In 64 bits: a square of an fp32 number neither overflows nor vanishes, and the
@@ -104,7 +103,7 @@ __device__ __forceinline__ double run_square_sum(const void* grad, uint64_t n, u
 
 // Workgroup g takes the runs [g runs / G, (g + 1) runs / G): the order of the sums depends on the sizes alone.
 __global__ __launch_bounds__(256) void grad_norm_partial_kernel(GradList l, double* __restrict__ partial) {
-    __shared__ double red[256];
+    __shared__ double red[4];
     const int from = (int)((int64_t)l.runs * blockIdx.x / gridDim.x), to = (int)((int64_t)l.runs * (blockIdx.x + 1) / gridDim.x);
     double acc = 0.;
     int i = find_tensor(l, from);
@@ -120,7 +119,7 @@ __global__ __launch_bounds__(256) void grad_norm_partial_kernel(GradList l, doub
 
 __global__ __launch_bounds__(256) void grad_norm_finish_kernel(const double* __restrict__ partial, int parts, float max_norm,
                                                                float multiplier, float* __restrict__ out) {
-    __shared__ double red[256];
+    __shared__ double red[4];
     double acc = 0.;
     for (int i = threadIdx.x; i < parts; i += 256) acc += partial[i];
     acc = group_sum(acc, red);
