@@ -12,7 +12,7 @@
 // always has the same experts and keeps its sums of probabilities in registers; four batches of tokens are in flight.
 #include <type_traits>
 
-#include "common.h"
+#include "wave_sum.h"
 
 namespace moe {
 
@@ -72,11 +72,6 @@ __device__ __forceinline__ Chunk find_chunk(int b, const int32_t* offsets, int n
     return {lo, from, from + min(end - from, C)};
 }
 
-template <int CTRL>
-__device__ __forceinline__ float dpp(float v) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
-}
-
 // One number for each of a lane's kBatches tokens, the same in all lanes of a token.  With four lanes to a token or more each
 // lane holds only that of token lane % 4, so that what is worked out from it (a reciprocal, a logarithm) is worked out once.
 template <int LPT>
@@ -114,14 +109,8 @@ __device__ __forceinline__ PerToken<LPT> reduce(float (&a)[kBatches], F&& f) {
             v = f(v, dpp<0x124>(v));                                               // row_ror 4, then 8
             v = f(v, dpp<0x128>(v));
         }
-        if constexpr (LPT >= 32) {
-            const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-            v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
-        }
-        if constexpr (LPT >= 64) {
-            const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-            v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
-        }
+        if constexpr (LPT >= 32) v = with_swapped<false>(v, f);
+        if constexpr (LPT >= 64) v = with_swapped<true>(v, f);
         out.v[0] = v;
     }
     return out;
@@ -129,12 +118,6 @@ __device__ __forceinline__ PerToken<LPT> reduce(float (&a)[kBatches], F&& f) {
 template <int LPT>
 __device__ __forceinline__ PerToken<LPT> reduce_sum(float (&a)[kBatches]) {
     return reduce<LPT>(a, [](float x, float y) { return x + y; });
-}
-
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-    return v;
 }
 
 // A lane's four logits of a token; -inf past the last expert.
@@ -255,26 +238,15 @@ struct Results {
     }
 };
 
-__device__ __forceinline__ void add_over_wave(double& x, int32_t& n) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) {
-        x += __shfl_xor(x, off, 64);
-        n += __shfl_xor(n, off, 64);
-    }
-}
-
 // Three sums over the workgroup in one exchange, valid in the first wave.
 struct Three {
     double a[16], b[16];
     int32_t n[16];
 
     __device__ __forceinline__ void sum(double& x, double& y, int& m) {
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) {
-            x += __shfl_xor(x, off, 64);
-            y += __shfl_xor(y, off, 64);
-            m += __shfl_xor(m, off, 64);
-        }
+        x = wave_sum(x);
+        y = wave_sum(y);
+        m = wave_sum(m);
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
         if (lane == 0) {
             a[wave] = x;
@@ -286,12 +258,9 @@ struct Three {
         x = lane < waves ? a[lane] : 0.;
         y = lane < waves ? b[lane] : 0.;
         m = lane < waves ? n[lane] : 0;
-#pragma unroll
-        for (int off = 8; off > 0; off >>= 1) {
-            x += __shfl_xor(x, off, 64);
-            y += __shfl_xor(y, off, 64);
-            m += __shfl_xor(m, off, 64);
-        }
+        x = wave_sum(x);
+        y = wave_sum(y);
+        m = wave_sum(m);
     }
 };
 
@@ -363,12 +332,9 @@ __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __re
     }
     // lanes with the same experts, then waves
 #pragma unroll
-    for (int off = LPT; off < 64; off <<= 1)
-#pragma unroll
-        for (int u = 0; u < 4; ++u) acc[u] += __shfl_xor(acc[u], off, 64);
+    for (int u = 0; u < 4; ++u) acc[u] = sum_congruent<LPT>((float)acc[u]);
     zsum = wave_sum(zsum);
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off, 64);
+    n = wave_sum(n);
     if (lane < LPT) {
 #pragma unroll
         for (int u = 0; u < 4; ++u) sums[wave][e + u] = acc[u];
@@ -388,9 +354,8 @@ __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __re
     double z = 0., loss = 0.;
     int tokens = 0;
     if (wave == 0) {
-        z = lane < waves ? (double)zs[lane] : 0.;
-        tokens = lane < waves ? ns[lane] : 0;
-        add_over_wave(z, tokens);
+        z = wave_sum(lane < waves ? (double)zs[lane] : 0.);
+        tokens = wave_sum(lane < waves ? ns[lane] : 0);
     }
     if (!direct) {
         if (threadIdx.x < E) out.cell[(size_t)b * E + threadIdx.x] = {p, count};
@@ -405,8 +370,7 @@ __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __re
         res.prob_sums[threadIdx.x] = p;
         loss = (double)p * count;
     }
-    int none = 0;
-    add_over_wave(loss, none);
+    loss = wave_sum(loss);
     if (kExperts > 64) {
         if (lane == 0 && wave < 4) parts[wave] = loss;
         __syncthreads();
@@ -468,7 +432,8 @@ __global__ __launch_bounds__(1024) void balance_finish_kernel(const int32_t* __r
         p += __shfl_xor(p, off, 64);
         n += __shfl_xor(n, off, 64);
     }
-    add_over_wave(z, tokens);
+    z = wave_sum(z);
+    tokens = wave_sum(tokens);
     if (lane < width) {
         red_p[wave][lane] = p;
         red_n[wave][lane] = n;
@@ -480,9 +445,8 @@ __global__ __launch_bounds__(1024) void balance_finish_kernel(const int32_t* __r
     __syncthreads();
     double loss = 0.;
     if (wave == 0) {
-        z = lane < waves ? red_z[lane] : 0.;
-        tokens = lane < waves ? red_tokens[lane] : 0;
-        add_over_wave(z, tokens);
+        z = wave_sum(lane < waves ? red_z[lane] : 0.);
+        tokens = wave_sum(lane < waves ? red_tokens[lane] : 0);
         if (lane < width && e < E) {
             p = 0.;
             n = 0;
@@ -495,8 +459,7 @@ __global__ __launch_bounds__(1024) void balance_finish_kernel(const int32_t* __r
             res.prob_sums[(size_t)s * E + e] = (float)p;
             loss = p * n;
         }
-        int none = 0;
-        add_over_wave(loss, none);
+        loss = wave_sum(loss);
     }
     if (gridDim.x * gridDim.y == 1) {
         if (threadIdx.x == 0) {

@@ -6,7 +6,7 @@
 
 #include <type_traits>
 
-#include "common.h"
+#include "wave_sum.h"
 
 namespace moe {
 
@@ -51,8 +51,7 @@ constexpr int kNormGroups = 1024;   // workgroups, and partial sums, of a launch
 
 // Sum over the workgroup's four waves, in its first wave.
 __device__ __forceinline__ double group_sum(double v, double* red) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    v = wave_sum(v);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
     return (red[0] + red[1]) + (red[2] + red[3]);
