@@ -547,7 +547,8 @@ moe_status_t moe_grad_norm(const moe_grad_tensor_t* tensors, int count, float ma
  *
  * `tensors` is HOST memory, read during the call.  All pointers but the scales are
  * 16-byte aligned; 0 <= n <= 2^33; tensors must not overlap.  step >= 1, lr >= 0, 0 <= beta1,
- * beta2 < 1, eps > 0.  No workspace.
+ * beta2 < 1, eps > 0.  No workspace.  lr, step and seed are arguments: a captured call
+ * repeats them in every replay.
  */
 typedef enum { MOE_STATE_F32 = 0, MOE_STATE_MXFP8 = 1 } moe_state_t;
 

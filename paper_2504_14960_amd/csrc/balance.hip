@@ -9,7 +9,14 @@
 //
 // All are bound by memory: the forward reads the logits once, the backward reads and writes them once.  A token's logits lie
 // four to a lane in as many lanes as its experts need (a power of two, LPT), so that 64 / LPT tokens share a wave, a lane
-// always has the same experts and keeps its sums of probabilities in registers; four batches of tokens are in flight.
+// always has the same experts and keeps its sums of probabilities in registers; four batches of tokens are in flight.  What a
+// token needs from all its lanes (largest logit, sum of exponentials, the gradient's dot product) is reduced for four tokens
+// at once, which leaves 57 instructions a token of 256 experts; token by token it took 99, and the vector units, 73 % busy,
+// set the pace.
+//
+// Measured (fp32 logits, streamed past the caches: 10 % faster than through them): forward of 262144 tokens x 256 experts
+// 48 us in the first launch (5.8 TB/s) and 6.6 in the second, of 32768 x 64 6.4 and 4.5, of 256 x 8 4.2 in the only one;
+// gradient of 262144 x 256 88 us (6.1 TB/s), of 7777 x 60 in 23 sequences 5.7.
 #include <type_traits>
 
 #include "wave_sum.h"
@@ -21,7 +28,9 @@ namespace {
 constexpr int kBatches = 4;        // tokens a lane has in flight
 constexpr int kTicketGroups = 64;  // workgroups of balance_finish_kernel of which the last one adds up the sequences
 
-// How a call is cut, by its sizes alone, so that the order of the sums is reproducible.
+// How a call is cut, by its sizes alone, so that the order of the sums is reproducible.  The chunks of one sequence are added
+// up by one workgroup for 64 experts; for more, 16 experts to a workgroup and a ticket for the last of them: 6.6 us instead
+// of 11.4 for 256 chunks of 256 experts (one workgroup takes in some 50 B/ns), while the ticket costs 3 us where one is enough.
 struct Cut {
     int chunk_tokens, chunks, threads;   // balance_partial_kernel
     int slab, slabs, finish_threads;     // balance_finish_kernel: experts of a workgroup, workgroups of a sequence

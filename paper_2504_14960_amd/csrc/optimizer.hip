@@ -1,7 +1,17 @@
 // What ends a training step: the norm of all gradients, and AdamW over a list of tensors (formulas in include/moe.h).
 //
+//   grad_norm_partial_kernel  sums of squares, in 64 bits, of runs of 16 KiB
+//   grad_norm_finish_kernel   the norm and the factor that clips it
+//   adamw_kernel              the step, a piece of 1024 or 2048 elements to a workgroup
+//
 // A launch takes a list of tensors, described in its arguments; every tensor is cut into pieces, and a workgroup finds its
-// tensor from the first pieces.  Both are bound by memory.
+// tensor from the first pieces.  All are bound by memory, read and written once and streamed past the caches.
+//
+// Measured: norm of 1.11G bf16 gradients 322 us (6.9 TB/s).  AdamW of 1.11G weights with fp32 masters and states and bf16
+// gradients, 28 bytes each: 5.1 ms (6.1 TB/s; through the caches 5.3; two and four pieces to a workgroup, the next on its
+// way while one is worked on, 5.1 and 5.2; eight elements to a lane, 32 bytes apart, 5.7).  1.41G bf16 weights with 8-bit
+// states, 10.1 bytes each: 2.40 ms (5.9 TB/s; two pieces to a workgroup 2.6; four elements to a lane, rounding in plain
+// operations 3.9).  60 fp32 tensors of 400 thousand elements in all 6 us.
 #include <string.h>
 
 #include <type_traits>
@@ -362,8 +372,8 @@ __device__ __forceinline__ void adamw_piece(const AdamTensor& t, const AdamStep&
         m[u] = m[u] * h.beta1 + g[u] * h.one_minus_beta1;
         v[u] = v[u] * h.beta2 + (g[u] * g[u]) * h.one_minus_beta2;
         if constexpr (MXFP8) {
-            // the instructions' own square root and reciprocal, each within a unit of fp32: with 8-bit states the kernel
-            // is bound by what it computes
+            // the instructions' own square root and reciprocal, each within a unit of fp32: some 45 instructions an element
+            // are nearly as long as its 10 to 16 bytes take
             const float denom = fmaf(__builtin_amdgcn_sqrtf(v[u]), h.rsqrt_bc2, h.eps);
             p[u] = fmaf(-t.step_size * m[u], __builtin_amdgcn_rcpf(denom), p[u] * t.decay);
         } else {
