@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -38,6 +39,10 @@ class _AdamWTensor(C.Structure):     # moe_adamw_tensor_t
                 ("exp_avg_sq", C.c_void_p), ("exp_avg_scale", C.c_void_p), ("exp_avg_sq_scale", C.c_void_p),
                 ("n", C.c_int64), ("weight_decay", C.c_float), ("lr_scale", C.c_float), ("param_dt", C.c_int),
                 ("grad_dt", C.c_int), ("state", C.c_int)]
+
+
+# the same in the host's own layout, padded to the alignment of a pointer
+_GRAD_ROW, _ADAMW_ROW = struct.Struct("Pqi0P"), struct.Struct("7Pq2f3i0P")
 
 
 def lib_path() -> str:
@@ -427,7 +432,12 @@ class GradTensors:
 
     def __init__(self, grads) -> None:
         self.grads = list(grads)
-        self._list = (_GradTensor * len(self.grads))(*((_ptr(g), g.numel(), _dt(g)) for g in self.grads))
+        self._list = _packed(_GradTensor, _GRAD_ROW, [(_ptr(g), g.numel(), _dt(g)) for g in self.grads])
+
+
+def _packed(kind, row, rows):
+    """A ctypes array of `kind` from tuples of its fields (a structure made one by one costs twice the time)."""
+    return (kind * len(rows)).from_buffer_copy(b"".join(row.pack(*r) for r in rows))
 
 
 def grad_norm_workspace_bytes(count: int) -> int:
@@ -459,26 +469,28 @@ class AdamWTensors:
         if any(len(c) != n for c in columns + [decays, scales]):
             raise ValueError("every list must have as many entries as params")
         self.tensors = list(zip(*columns))       # keeps the buffers alive
-        self._list = (_AdamWTensor * n)(*(self._entry(*row, d, s) for row, d, s in zip(self.tensors, decays, scales)))
+        self._list = _packed(_AdamWTensor, _ADAMW_ROW, [self._row(*r, d, s) for r, d, s in zip(self.tensors, decays, scales)])
         self.grads = GradTensors(columns[2])
 
     @staticmethod
-    def _entry(param, master, grad, m, v, m_scale, v_scale, decay, lr_scale):
+    def _row(param, master, grad, m, v, m_scale, v_scale, decay, lr_scale):
         count = param.numel()
-        state = MOE_STATE_MXFP8 if m.dtype == torch.uint8 else MOE_STATE_F32
-        kind = torch.uint8 if state == MOE_STATE_MXFP8 else torch.float32
+        small = m.dtype is torch.uint8
+        kind = torch.uint8 if small else torch.float32
         _is("exp_avg", m, kind, count)
         _is("exp_avg_sq", v, kind, count)
         _is("grad", grad, grad.dtype, count)
         if master is not None:
             _is("master", master, torch.float32, count)
-        for name, t in (("exp_avg_scale", m_scale), ("exp_avg_sq_scale", v_scale)):
-            if (t is None) != (state == MOE_STATE_F32):
-                raise ValueError(f"8-bit states need {name}s" if t is None else f"{name} goes with 8-bit states only")
-            if t is not None:
+        if small:
+            for name, t in (("exp_avg_scale", m_scale), ("exp_avg_sq_scale", v_scale)):
+                if t is None:
+                    raise ValueError(f"8-bit states need {name}s")
                 _is(name, t, torch.uint8, (count + 31) // 32)
-        return (_ptr(param), _ptr(master), _ptr(grad), _ptr(m), _ptr(v), _ptr(m_scale), _ptr(v_scale), count, decay,
-                lr_scale, _dt(param), _dt(grad), state)
+        elif m_scale is not None or v_scale is not None:
+            raise ValueError("exp_avg_scales and exp_avg_sq_scales go with 8-bit states only")
+        return (_ptr(param), _ptr(master) or 0, _ptr(grad), _ptr(m), _ptr(v), _ptr(m_scale) or 0, _ptr(v_scale) or 0, count,
+                decay, lr_scale, _dt(param), _dt(grad), MOE_STATE_MXFP8 if small else MOE_STATE_F32)
 
 
 def adamw_step(tensors: AdamWTensors, lr: float, beta1: float, beta2: float, eps: float, step: int, seed: int = 0,
