@@ -336,6 +336,37 @@ def test_same_inputs_same_bits_on_any_stream():
             assert x[k] is None or torch.equal(x[k], y[k])
 
 
+@pytest.mark.gpu
+def test_norm_and_step_replayed_in_a_graph():
+    """Each replay steps from what the last one left, with the step and seed it was captured with, as eager calls do."""
+    import torch
+    import paper_2504_14960_amd as moe
+    kinds = [ALL[i % len(ALL)] for i in range(80)]
+    eager, captured = (Tensors([700 + 31 * i for i in range(80)], kinds, seed=5) for _ in range(2))
+    ws = torch.empty(moe.grad_norm_workspace_bytes(80), dtype=torch.uint8, device="cuda")
+    out = torch.zeros((2, 2), device="cuda")
+
+    def step(t, o):
+        moe.grad_norm(t.list, o, ws, max_norm=0.1)
+        t.step(4, 11, o[1:])
+
+    step(eager, out[0])
+    step(captured, out[1])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(captured, out[1])
+    for _ in range(4):
+        graph.replay()
+        torch.cuda.synchronize()
+        step(eager, out[0])
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], out[1])
+        for x, y in zip(eager.dev, captured.dev):
+            for k in x:
+                assert x[k] is None or torch.equal(x[k], y[k])
+
+
 def _refuse(fn, word, status=1):
     import paper_2504_14960_amd as moe
     L = moe.lib()
