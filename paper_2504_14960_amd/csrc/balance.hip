@@ -50,7 +50,7 @@ struct Cut {
             threads = 1024;
         }
         direct = !packed && chunks == 1;
-        slab = packed || E <= 64 ? 64 : 16;
+        slab = (packed ? chunks / n_seq <= 64 : E <= 64) ? 64 : 16;
         slabs = (E + slab - 1) / slab;
         finish_threads = chunks / n_seq > 32 ? 1024 : 256;
         ticket = n_seq * slabs <= kTicketGroups;
@@ -129,33 +129,53 @@ __device__ __forceinline__ PerToken<LPT> reduce_sum(float (&a)[kBatches]) {
     return reduce<LPT>(a, [](float x, float y) { return x + y; });
 }
 
-// A lane's four logits of a token; -inf past the last expert.
-__device__ __forceinline__ f32x4 load_logits(const float* row, int e, int E, bool vec) {
+// The experts of a lane: four neighbours, read as one piece, where rows are whole 16-byte pieces (WHOLE); else every LPT-th, so
+// that neighbouring lanes read neighbouring values (262144 x 255 logits: gradient 184 us with four neighbours read one by one,
+// 113 as pieces at odd addresses).
+template <int LPT, bool WHOLE>
+__device__ __forceinline__ int expert_of(int q, int u) {
+    return WHOLE ? 4 * q + u : q + u * LPT;
+}
+
+// A lane's four values of a token's row, -inf past its end.
+template <int LPT, bool WHOLE>
+__device__ __forceinline__ f32x4 load_row(const float* row, int q, int E) {
     f32x4 x = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    if (vec) {
-        if (e < E) x = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(row + e));
+    if constexpr (WHOLE) {
+        if (4 * q < E) x = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(row + 4 * q));
     } else {
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-            if (e + u < E) x[u] = row[e + u];
+            if (q + u * LPT < E) x[u] = row[q + u * LPT];
     }
     return x;
+}
+template <int LPT, bool WHOLE>
+__device__ __forceinline__ void store_row(float* row, int q, int E, const f32x4& d) {
+    if constexpr (WHOLE) {
+        if (4 * q < E) __builtin_nontemporal_store(d, reinterpret_cast<f32x4*>(row + 4 * q));
+    } else {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (q + u * LPT < E) row[q + u * LPT] = d[u];
+    }
 }
 
 // A lane's logits of its next tokens, one in each of kBatches batches of `step` tokens.  ok: bit u is set where token u counts;
 // what others hold is replaced, so that it cannot spread.
+template <int LPT, bool WHOLE>
 struct Batches {
     f32x4 x[kBatches];
     uint32_t ok;
 
-    __device__ __forceinline__ void load(const float* logits, const uint8_t* mask, int t, int step, int end, int e, int E, bool vec) {
+    __device__ __forceinline__ void load(const float* logits, const uint8_t* mask, int t, int step, int end, int q, int E) {
         ok = 0;
 #pragma unroll
         for (int u = 0; u < kBatches; ++u) {
             const int tu = t + u * step;
             const bool in = tu < end;
             const size_t row = in ? tu : end - 1;
-            x[u] = load_logits(logits + row * E, e, E, vec);
+            x[u] = load_row<LPT, WHOLE>(logits + row * E, q, E);
             ok |= (in && (mask == nullptr || mask[row] != 0) ? 1u : 0u) << u;
         }
     }
@@ -274,7 +294,7 @@ struct Three {
 };
 
 // One chunk to a workgroup of up to 16 waves.
-template <int LPT>
+template <int LPT, bool WHOLE>
 __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __restrict__ logits, const int32_t* __restrict__ idx,
                                                                const uint8_t* __restrict__ mask,
                                                                const int32_t* __restrict__ offsets, int T, int E, int K,
@@ -286,23 +306,29 @@ __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __re
     __shared__ float zs[16];
     __shared__ int32_t ns[16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, b = blockIdx.x;
-    const int q = lane % LPT, e = 4 * q;
-    const bool vec = E % 4 == 0;
+    const int q = lane % LPT;
     const Chunk c = find_chunk(b, offsets, n_seq, T, C);
     const int step = waves * kTokens, own = lane / LPT;
     int t = c.t0 + wave * kTokens;
-    Batches next;
-    if (t < c.t1) next.load(logits, mask, t + own, step, c.t1, e, E, vec);
+    Batches<LPT, WHOLE> next;
+    if (t < c.t1) next.load(logits, mask, t + own, step, c.t1, q, E);
     if (threadIdx.x < kExperts) hist[threadIdx.x] = 0;
     __syncthreads();
-    // counts: every assignment of the chunk once, whole numbers in any order
-    const int64_t a1 = (int64_t)c.t1 * K;
-    for (int64_t a = (int64_t)c.t0 * K + threadIdx.x; a < a1; a += 4 * blockDim.x) {
+    // counts: every assignment of the chunk once, whole numbers in any order.  The token of a masked one: (a + 1/2) / K is at
+    // least 1 / 2K away from a whole number, more than the roundings of a product below 2^22.
+    const int assigned = max(c.t1 - c.t0, 0) * K;
+    const int32_t* picked = idx + (size_t)c.t0 * K;
+    const float per_token = 1.f / K;
+    for (int a = threadIdx.x; a < assigned; a += 4 * blockDim.x) {
         int i[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const int64_t at = a + u * blockDim.x;
-            i[u] = at < a1 && (mask == nullptr || mask[(uint32_t)at / (uint32_t)K] != 0) ? idx[at] : -1;
+            const int at = a + u * blockDim.x;
+            bool in = at < assigned;
+            const int safe = in ? at : assigned - 1;
+            if (mask) in = in && mask[c.t0 + (assigned < 1 << 22 ? (int)((safe + 0.5f) * per_token) : safe / K)] != 0;
+            i[u] = picked[safe];
+            if (!in) i[u] = -1;
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u)
@@ -312,9 +338,9 @@ __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __re
     float zsum = 0.f;
     int n = 0;
     while (t < c.t1) {
-        Batches cur = next;
+        Batches<LPT, WHOLE> cur = next;
         t += kBatches * step;
-        if (t < c.t1) next.load(logits, mask, t + own, step, c.t1, e, E, vec);
+        if (t < c.t1) next.load(logits, mask, t + own, step, c.t1, q, E);
         if (mask) cur.hide_masked();
         float sums[kBatches];
         const PerToken<LPT> top = exponentials<LPT>(cur.x, sums);
@@ -346,7 +372,7 @@ __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __re
     n = wave_sum(n);
     if (lane < LPT) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) sums[wave][e + u] = acc[u];
+        for (int u = 0; u < 4; ++u) sums[wave][expert_of<LPT, WHOLE>(q, u)] = acc[u];
     }
     if (lane == 0) {
         zs[wave] = zsum;
@@ -500,7 +526,7 @@ __global__ __launch_bounds__(1024) void balance_total_kernel(int slabs, Partials
     add_sequences(in, res, slabs, three);
 }
 
-template <int LPT>
+template <int LPT, bool WHOLE>
 __global__ __launch_bounds__(256) void balance_backward_kernel(const float* __restrict__ logits,
                                                                const uint8_t* __restrict__ mask,
                                                                const int32_t* __restrict__ offsets,
@@ -511,24 +537,26 @@ __global__ __launch_bounds__(256) void balance_backward_kernel(const float* __re
                                                                float z_coef, float* dlogits) {
     constexpr int kTokens = 64 / LPT;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int q = lane % LPT, e = 4 * q;
-    const bool vec = E % 4 == 0;
+    const int q = lane % LPT;
     const Chunk c = find_chunk(blockIdx.x, offsets, n_seq, T, C);
     const float n = (float)max(seq_tokens[n_seq], 1), n_s = (float)max(seq_tokens[c.seq], 1);
     const float db = dlosses ? dlosses[0] : 1.f, dz = dlosses ? dlosses[1] : 1.f;
     const float a = db * balance_coef * E / (K * n) / n_s, az = dz * 2.f * z_coef / n;
     f32x4 g;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) g[u] = e + u < E ? a * counts[(size_t)c.seq * E + e + u] : 0.f;
+    for (int u = 0; u < 4; ++u) {
+        const int e = expert_of<LPT, WHOLE>(q, u);
+        g[u] = e < E ? a * counts[(size_t)c.seq * E + e] : 0.f;
+    }
     const int step = 4 * kTokens;
     const int t = c.t0 + wave * kTokens + lane / LPT;
     if (c.t0 + wave * kTokens >= c.t1) return;
-    Batches b;
-    b.load(logits, mask, t, step, c.t1, e, E, vec);
+    Batches<LPT, WHOLE> b;
+    b.load(logits, mask, t, step, c.t1, q, E);
     f32x4 more[kBatches];
     if (addend) {
 #pragma unroll
-        for (int u = 0; u < kBatches; ++u) more[u] = load_logits(addend + (size_t)min(t + u * step, c.t1 - 1) * E, e, E, vec);
+        for (int u = 0; u < kBatches; ++u) more[u] = load_row<LPT, WHOLE>(addend + (size_t)min(t + u * step, c.t1 - 1) * E, q, E);
     } else {
 #pragma unroll
         for (int u = 0; u < kBatches; ++u) more[u] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -554,16 +582,7 @@ __global__ __launch_bounds__(256) void balance_backward_kernel(const float* __re
         f32x4 d;
 #pragma unroll
         for (int v = 0; v < 4; ++v) d[v] = fmaf(b.x[u][v] * ru, g[v] + su, more[u][v]);
-        if (t + u * step < c.t1) {
-            float* row = dlogits + (size_t)(t + u * step) * E;
-            if (vec) {
-                if (e < E) __builtin_nontemporal_store(d, reinterpret_cast<f32x4*>(row + e));
-            } else {
-#pragma unroll
-                for (int v = 0; v < 4; ++v)
-                    if (e + v < E) row[e + v] = d[v];
-            }
-        }
+        if (t + u * step < c.t1) store_row<LPT, WHOLE>(dlogits + (size_t)(t + u * step) * E, q, E, d);
     };
     write(std::integral_constant<int, 0>());
     write(std::integral_constant<int, 1>());
@@ -571,16 +590,20 @@ __global__ __launch_bounds__(256) void balance_backward_kernel(const float* __re
     write(std::integral_constant<int, 3>());
 }
 
-// Calls f with the lanes a token of E experts takes.
+// Calls f with the lanes a token of E experts takes, and whether its rows are whole pieces.
 template <typename F>
 void with_lanes(int E, F&& f) {
-    if (E <= 4) f(std::integral_constant<int, 1>());
-    else if (E <= 8) f(std::integral_constant<int, 2>());
-    else if (E <= 16) f(std::integral_constant<int, 4>());
-    else if (E <= 32) f(std::integral_constant<int, 8>());
-    else if (E <= 64) f(std::integral_constant<int, 16>());
-    else if (E <= 128) f(std::integral_constant<int, 32>());
-    else f(std::integral_constant<int, 64>());
+    auto call = [&](auto lanes) {
+        if (E % 4 == 0) f(lanes, std::true_type());
+        else f(lanes, std::false_type());
+    };
+    if (E <= 4) call(std::integral_constant<int, 1>());
+    else if (E <= 8) call(std::integral_constant<int, 2>());
+    else if (E <= 16) call(std::integral_constant<int, 4>());
+    else if (E <= 32) call(std::integral_constant<int, 8>());
+    else if (E <= 64) call(std::integral_constant<int, 16>());
+    else if (E <= 128) call(std::integral_constant<int, 32>());
+    else call(std::integral_constant<int, 64>());
 }
 
 // the smallest power of two that is n or more
@@ -604,8 +627,8 @@ void launch_balance_loss(const float* logits, const int32_t* idx, const uint8_t*
     Partials p;
     carve(ws, cut, E, n_seq, &p);
     const Results res = {counts, prob_sums, seq_tokens, losses, balance_coef, z_coef, E, K, n_seq};
-    with_lanes(E, [&](auto lanes) {
-        hipLaunchKernelGGL(balance_partial_kernel<lanes.value>, dim3(cut.chunks), dim3(cut.threads), 0, s, logits, idx, mask,
+    with_lanes(E, [&](auto lanes, auto whole) {
+        hipLaunchKernelGGL((balance_partial_kernel<lanes.value, whole.value>), dim3(cut.chunks), dim3(cut.threads), 0, s, logits, idx, mask,
                            offsets, T, E, K, n_seq, cut.chunk_tokens, cut.direct, p, res);
     });
     if (cut.direct) return;
@@ -618,12 +641,12 @@ void launch_balance_loss_backward(const float* logits, const uint8_t* mask, cons
                                   const int32_t* seq_tokens, const float* dlosses, const float* addend, int T, int E, int K,
                                   int n_seq, float balance_coef, float z_coef, float* dlogits, hipStream_t s) {
     const bool packed = offsets != nullptr;
-    with_lanes(E, [&](auto lanes) {
+    with_lanes(E, [&](auto lanes, auto whole) {
         // one round of four waves: 2 rounds to a workgroup take 7.9 instead of 5.8 us for 65536 tokens x 16 experts and 10.5
         // instead of 7.7 for 65536 x 64, and save 2 of 90 us only for the largest call
         constexpr int C = kBatches * 4 * (64 / lanes.value);
         const int chunks = packed ? T / C + n_seq : (T + C - 1) / C;
-        hipLaunchKernelGGL(balance_backward_kernel<lanes.value>, dim3(chunks), dim3(256), 0, s, logits, mask, offsets, counts,
+        hipLaunchKernelGGL((balance_backward_kernel<lanes.value, whole.value>), dim3(chunks), dim3(256), 0, s, logits, mask, offsets, counts,
                            seq_tokens, dlosses, addend, T, E, K, n_seq, C, balance_coef, z_coef, dlogits);
     });
 }
