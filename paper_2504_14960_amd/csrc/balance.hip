@@ -137,8 +137,10 @@ __device__ __forceinline__ int expert_of(int q, int u) {
     return WHOLE ? 4 * q + u : q + u * LPT;
 }
 
-// A lane's four values of a token's row, -inf past its end.
-template <int LPT, bool WHOLE>
+// A lane's four values of a token's row, -inf past its end.  Streamed past the caches, but for rows that are not whole pieces where
+// nothing is written beside them, whose ends share lines with the next row (us through / past the caches: forward of 262144 x 255
+// 53 / 55 and x 129 45 / 47, gradient 112 / 99 and 72 / 68).
+template <int LPT, bool WHOLE, bool STREAM>
 __device__ __forceinline__ f32x4 load_row(const float* row, int q, int E) {
     f32x4 x = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
     if constexpr (WHOLE) {
@@ -146,7 +148,7 @@ __device__ __forceinline__ f32x4 load_row(const float* row, int q, int E) {
     } else {
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-            if (q + u * LPT < E) x[u] = row[q + u * LPT];
+            if (q + u * LPT < E) x[u] = STREAM ? __builtin_nontemporal_load(row + q + u * LPT) : row[q + u * LPT];
     }
     return x;
 }
@@ -163,7 +165,7 @@ __device__ __forceinline__ void store_row(float* row, int q, int E, const f32x4&
 
 // A lane's logits of its next tokens, one in each of kBatches batches of `step` tokens.  ok: bit u is set where token u counts;
 // what others hold is replaced, so that it cannot spread.
-template <int LPT, bool WHOLE>
+template <int LPT, bool WHOLE, bool STREAM>
 struct Batches {
     f32x4 x[kBatches];
     uint32_t ok;
@@ -175,7 +177,7 @@ struct Batches {
             const int tu = t + u * step;
             const bool in = tu < end;
             const size_t row = in ? tu : end - 1;
-            x[u] = load_row<LPT, WHOLE>(logits + row * E, q, E);
+            x[u] = load_row<LPT, WHOLE, STREAM>(logits + row * E, q, E);
             ok |= (in && (mask == nullptr || mask[row] != 0) ? 1u : 0u) << u;
         }
     }
@@ -310,7 +312,7 @@ __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __re
     const Chunk c = find_chunk(b, offsets, n_seq, T, C);
     const int step = waves * kTokens, own = lane / LPT;
     int t = c.t0 + wave * kTokens;
-    Batches<LPT, WHOLE> next;
+    Batches<LPT, WHOLE, WHOLE> next;
     if (t < c.t1) next.load(logits, mask, t + own, step, c.t1, q, E);
     if (threadIdx.x < kExperts) hist[threadIdx.x] = 0;
     __syncthreads();
@@ -338,7 +340,7 @@ __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __re
     float zsum = 0.f;
     int n = 0;
     while (t < c.t1) {
-        Batches<LPT, WHOLE> cur = next;
+        Batches<LPT, WHOLE, WHOLE> cur = next;
         t += kBatches * step;
         if (t < c.t1) next.load(logits, mask, t + own, step, c.t1, q, E);
         if (mask) cur.hide_masked();
@@ -551,12 +553,12 @@ __global__ __launch_bounds__(256) void balance_backward_kernel(const float* __re
     const int step = 4 * kTokens;
     const int t = c.t0 + wave * kTokens + lane / LPT;
     if (c.t0 + wave * kTokens >= c.t1) return;
-    Batches<LPT, WHOLE> b;
+    Batches<LPT, WHOLE, true> b;
     b.load(logits, mask, t, step, c.t1, q, E);
     f32x4 more[kBatches];
     if (addend) {
 #pragma unroll
-        for (int u = 0; u < kBatches; ++u) more[u] = load_row<LPT, WHOLE>(addend + (size_t)min(t + u * step, c.t1 - 1) * E, q, E);
+        for (int u = 0; u < kBatches; ++u) more[u] = load_row<LPT, WHOLE, true>(addend + (size_t)min(t + u * step, c.t1 - 1) * E, q, E);
     } else {
 #pragma unroll
         for (int u = 0; u < kBatches; ++u) more[u] = f32x4{0.f, 0.f, 0.f, 0.f};
