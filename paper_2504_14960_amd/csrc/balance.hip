@@ -163,29 +163,33 @@ __device__ __forceinline__ void store_row(float* row, int q, int E, const f32x4&
     }
 }
 
-// A lane's logits of its next tokens, one in each of kBatches batches of `step` tokens.  ok: bit u is set where token u counts;
-// what others hold is replaced, so that it cannot spread.
+// A lane's logits of its next tokens, one in each of kBatches batches of `step` tokens, of which those below `end` exist.  load
+// only asks for them: whether a token counts is looked at where they are used, or every load would be waited for at once.
 template <int LPT, bool WHOLE, bool STREAM>
 struct Batches {
     f32x4 x[kBatches];
-    uint32_t ok;
+    uint32_t keep[kBatches];   // bytes of the mask
 
     __device__ __forceinline__ void load(const float* logits, const uint8_t* mask, int t, int step, int end, int q, int E) {
-        ok = 0;
 #pragma unroll
         for (int u = 0; u < kBatches; ++u) {
-            const int tu = t + u * step;
-            const bool in = tu < end;
-            const size_t row = in ? tu : end - 1;
+            const size_t row = min(t + u * step, end - 1);
             x[u] = load_row<LPT, WHOLE, STREAM>(logits + row * E, q, E);
-            ok |= (in && (mask == nullptr || mask[row] != 0) ? 1u : 0u) << u;
+            keep[u] = mask ? mask[row] : 1;
         }
     }
-    __device__ __forceinline__ void hide_masked() {
+    // Bit u is set where token u counts; what a masked one holds is replaced, so that it cannot spread.
+    __device__ __forceinline__ uint32_t settle(bool masked, int t, int step, int end) {
+        uint32_t ok = 0;
 #pragma unroll
-        for (int u = 0; u < kBatches; ++u)
+        for (int u = 0; u < kBatches; ++u) {
+            ok |= (t + u * step < end && keep[u] != 0 ? 1u : 0u) << u;
+            if (masked) {
 #pragma unroll
-            for (int v = 0; v < 4; ++v) x[u][v] = ok >> u & 1 ? x[u][v] : 0.f;
+                for (int v = 0; v < 4; ++v) x[u][v] = keep[u] ? x[u][v] : 0.f;
+            }
+        }
+        return ok;
     }
 };
 
@@ -296,9 +300,9 @@ struct Three {
 };
 
 // One chunk to a workgroup of up to 16 waves.
-template <int LPT, bool WHOLE>
+template <int LPT, bool WHOLE, bool MASKED>
 __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __restrict__ logits, const int32_t* __restrict__ idx,
-                                                               const uint8_t* __restrict__ mask,
+                                                               const uint8_t* __restrict__ token_mask,
                                                                const int32_t* __restrict__ offsets, int T, int E, int K,
                                                                int n_seq, int C, bool direct, Partials out, Results res) {
     constexpr int kTokens = 64 / LPT, kExperts = 4 * LPT;
@@ -307,6 +311,7 @@ __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __re
     __shared__ float sums[16][kExperts];
     __shared__ float zs[16];
     __shared__ int32_t ns[16];
+    const uint8_t* mask = MASKED ? token_mask : nullptr;   // known at compile time: 52 instead of 54 us for 262144 x 256
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, b = blockIdx.x;
     const int q = lane % LPT;
     const Chunk c = find_chunk(b, offsets, n_seq, T, C);
@@ -341,21 +346,22 @@ __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __re
     int n = 0;
     while (t < c.t1) {
         Batches<LPT, WHOLE, WHOLE> cur = next;
+        const int now = t + own;
         t += kBatches * step;
         if (t < c.t1) next.load(logits, mask, t + own, step, c.t1, q, E);
-        if (mask) cur.hide_masked();
+        const uint32_t counted = cur.settle(MASKED, now, step, c.t1);
         float sums[kBatches];
         const PerToken<LPT> top = exponentials<LPT>(cur.x, sums);
         PerToken<LPT> s = reduce_sum<LPT>(sums);
 #pragma unroll
         for (int i = 0; i < PerToken<LPT>::N; ++i) {
             // a token that does not count, or has no probability, adds nothing to either loss
-            const bool ok = counts_at<LPT>(cur.ok, i) && s.v[i] != 0.f;
+            const bool ok = counts_at<LPT>(counted, i) && s.v[i] != 0.f;
             const float lse = ok ? log_sum(top.v[i], s.v[i]) : 0.f;
             if (q < (LPT >= 4 ? 4 : 1)) zsum = fmaf(lse, lse, zsum);
             s.v[i] = ok ? __builtin_amdgcn_rcpf(s.v[i]) : 0.f;
         }
-        if (q == 0) n += __popc(cur.ok);
+        if (q == 0) n += __popc(counted);
         auto add = [&](auto index) {
             constexpr int u = index.value;
             const float r = s.template get<u>();
@@ -563,7 +569,7 @@ __global__ __launch_bounds__(256) void balance_backward_kernel(const float* __re
 #pragma unroll
         for (int u = 0; u < kBatches; ++u) more[u] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    if (mask) b.hide_masked();
+    const uint32_t counted = b.settle(mask != nullptr, t, step, c.t1);
     float sums[kBatches], dots[kBatches];
     const PerToken<LPT> top = exponentials<LPT>(b.x, sums);
 #pragma unroll
@@ -573,7 +579,7 @@ __global__ __launch_bounds__(256) void balance_backward_kernel(const float* __re
 #pragma unroll
     for (int i = 0; i < PerToken<LPT>::N; ++i) {
         // r = 0 where a token does not count or has no probability
-        const bool ok = counts_at<LPT>(b.ok, i) && r.v[i] != 0.f;
+        const bool ok = counts_at<LPT>(counted, i) && r.v[i] != 0.f;
         const float lse = log_sum(top.v[i], r.v[i]);
         r.v[i] = ok ? __builtin_amdgcn_rcpf(r.v[i]) : 0.f;
         shift.v[i] = ok ? fmaf(az, lse, -(shift.v[i] * r.v[i])) : 0.f;
@@ -630,8 +636,9 @@ void launch_balance_loss(const float* logits, const int32_t* idx, const uint8_t*
     carve(ws, cut, E, n_seq, &p);
     const Results res = {counts, prob_sums, seq_tokens, losses, balance_coef, z_coef, E, K, n_seq};
     with_lanes(E, [&](auto lanes, auto whole) {
-        hipLaunchKernelGGL((balance_partial_kernel<lanes.value, whole.value>), dim3(cut.chunks), dim3(cut.threads), 0, s, logits, idx, mask,
-                           offsets, T, E, K, n_seq, cut.chunk_tokens, cut.direct, p, res);
+        auto kernel = mask ? balance_partial_kernel<lanes.value, whole.value, true> : balance_partial_kernel<lanes.value, whole.value, false>;
+        hipLaunchKernelGGL(kernel, dim3(cut.chunks), dim3(cut.threads), 0, s, logits, idx, mask, offsets, T, E, K, n_seq,
+                           cut.chunk_tokens, cut.direct, p, res);
     });
     if (cut.direct) return;
     hipLaunchKernelGGL(balance_finish_kernel, dim3(n_seq, cut.slabs), dim3(cut.finish_threads), 0, s, offsets, T,
