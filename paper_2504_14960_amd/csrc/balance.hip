@@ -15,8 +15,8 @@
 // set the pace.
 //
 // Measured (fp32 logits, streamed past the caches: 10 % faster than through them): forward of 262144 tokens x 256 experts
-// 48 us in the first launch (5.8 TB/s) and 6.6 in the second, of 32768 x 64 6.4 and 4.5, of 256 x 8 4.2 in the only one;
-// gradient of 262144 x 256 88 us (6.1 TB/s), of 7777 x 60 in 23 sequences 5.7.
+// 46 us in the first launch (6.1 TB/s) and 6.6 in the second, of 32768 x 64 6.3 and 4.6, of 256 x 8 3.8 in the only one;
+// gradient of 262144 x 256 86 us (6.2 TB/s), of 7777 x 60 in 23 sequences 4.9.
 #include <type_traits>
 
 #include "wave_sum.h"
