@@ -493,7 +493,7 @@ moe_status_t moe_layer_backward_addend(const void* x, const void* w_router, cons
  * multiplier undoes a loss scale.  Squares are summed in 64 bits, in an order that the
  * sizes fix.  `tensors` is HOST memory, read during the call; gradients are device
  * memory of n elements of dt, 16-byte aligned (n == 0: none, pointer not looked at;
- * n <= 2^33).
+ * n <= 2^33, count <= 2^26).
  * out [2] fp32 in device memory.  workspace: moe_grad_norm_workspace_bytes(count).
  */
 typedef struct {
@@ -546,7 +546,7 @@ moe_status_t moe_grad_norm(const moe_grad_tensor_t* tensors, int count, float ma
  * off is at least 1 - (u + 1/2) / 65536 of a step (E4M3), 1 - u / 65536 (bf16).
  *
  * `tensors` is HOST memory, read during the call.  All pointers but the scales are
- * 16-byte aligned; 0 <= n <= 2^33; tensors must not overlap.  step >= 1, lr >= 0, 0 <= beta1,
+ * 16-byte aligned; 0 <= n <= 2^33, count <= 2^26; tensors must not overlap.  step >= 1, lr >= 0, 0 <= beta1,
  * beta2 < 1, eps > 0.  No workspace.  lr, step and seed are arguments: a captured call
  * repeats them in every replay.
  */

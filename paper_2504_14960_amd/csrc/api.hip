@@ -943,6 +943,7 @@ moe_status_t moe_grad_norm(const moe_grad_tensor_t* tensors, int count, float ma
     static const char* fn = "moe_grad_norm";
     if (count < 0 || (count > 0 && tensors == nullptr))
         return fail(MOE_ERR_INVALID_ARG, "%s: count=%d, tensors %s", fn, count, tensors ? "given" : "NULL");
+    if (count > kMaxListTensors) return fail(MOE_ERR_UNSUPPORTED, "%s: count=%d exceeds the limit 2^26", fn, count);
     if (!std::isfinite(multiplier) || std::isnan(max_norm))
         return fail(MOE_ERR_INVALID_ARG, "%s: multiplier must be finite, max_norm a number", fn);
     for (int i = 0; i < count; ++i) {
@@ -968,6 +969,7 @@ moe_status_t moe_adamw_step(const moe_adamw_tensor_t* tensors, int count, double
     static const char* fn = "moe_adamw_step";
     if (count < 0 || (count > 0 && tensors == nullptr))
         return fail(MOE_ERR_INVALID_ARG, "%s: count=%d, tensors %s", fn, count, tensors ? "given" : "NULL");
+    if (count > kMaxListTensors) return fail(MOE_ERR_UNSUPPORTED, "%s: count=%d exceeds the limit 2^26", fn, count);
     if (step < 1) return fail(MOE_ERR_INVALID_ARG, "%s: step=%lld, the first one is 1", fn, (long long)step);
     if (!(lr >= 0.0) || !std::isfinite(lr) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) ||
         !(eps > 0.0) || !std::isfinite(eps))

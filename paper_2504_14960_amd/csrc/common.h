@@ -29,6 +29,7 @@ constexpr int kWave = 64;
 constexpr int kMaxExperts = 256;
 constexpr int kMaxTopK = 64;
 constexpr int kMaxSequences = 65536;               // of one balance-loss call
+constexpr int kMaxListTensors = 1 << 26;           // of one gradient-norm or AdamW call
 constexpr int64_t kMaxListElements = 1ll << 33;    // of one tensor of a gradient-norm or AdamW call
 
 __device__ __forceinline__ float bf16_to_f32(bf16_t v) {

@@ -8,10 +8,9 @@
 // tensor from the first pieces.  All are bound by memory, read and written once and streamed past the caches.
 //
 // Measured: norm of 1.11G bf16 gradients 322 us (6.9 TB/s).  AdamW of 1.11G weights with fp32 masters and states and bf16
-// gradients, 28 bytes each: 5.1 ms (6.1 TB/s; through the caches 5.3; two and four pieces to a workgroup, the next on its
-// way while one is worked on, 5.1 and 5.2; eight elements to a lane, 32 bytes apart, 5.7).  1.41G bf16 weights with 8-bit
-// states, 10.1 bytes each: 2.40 ms (5.9 TB/s; two pieces to a workgroup 2.6; four elements to a lane, rounding in plain
-// operations 3.9).  60 fp32 tensors of 400 thousand elements in all 6 us.
+// gradients, 28 bytes each: 4.91 ms (6.3 TB/s; with as many waves as there is room for, in workgroups of four, 5.67, and through
+// the caches 5.9).  1.41G bf16 weights with 8-bit states, 10.1 bytes each: 2.40 ms (5.9 TB/s; two pieces to a workgroup 2.6; four
+// elements to a lane, rounding in plain operations 3.9).  60 fp32 tensors of 400 thousand elements in all 6 us.
 #include <string.h>
 
 #include <type_traits>
@@ -22,9 +21,8 @@ namespace moe {
 
 namespace {
 
-constexpr int kPieceF32 = 1024, kPieceMxfp8 = 2048;   // elements of an AdamW workgroup, by states
 constexpr int kBlock = 32;         // elements that share a scale
-constexpr int64_t kLaunchPieces = (1 << 24) - 1;   // 256 threads each: a grid has less than 2^32 threads
+constexpr int64_t kLaunchPieces = (1 << 24) - 1;   // of up to 256 threads: a grid has less than 2^32 of them
 
 // -------------------------------------------------------------------------------------------------------------
 // lists
@@ -146,7 +144,7 @@ __global__ __launch_bounds__(256) void grad_norm_finish_kernel(const double* __r
 
 // A tensor in a launch's arguments, which are limited to 4 KiB: six words of 64 bits and up to three more where its types need
 // them, so that a launch takes 70 tensors in fp32, 60 in bf16 with masters, 46 of those with 8-bit states.
-//   n | kind << 48;  1 - lr wd, lr / (1 - beta1^t);  grad;  what is stepped (param or master);  m;  v;
+//   n | kind << 34 | place in the caller's list << 37;  1 - lr wd, lr / (1 - beta1^t);  grad;  what is stepped (param or master);  m;  v;
 //   [scales of m; of v];  [param, where there is a master]
 constexpr int kAdamTensors = 70, kAdamWords = 420, kWordsMost = 9;
 
@@ -156,7 +154,22 @@ struct AdamList {
     struct {
         int32_t first, at;                        // first piece, first word
     } tensor[kAdamTensors];
-    int32_t count, index;                         // index: place of the first in the caller's list
+    int32_t count;
+};
+
+// How a launch is shaped, by its tensors' states.  With fp32 states fewer waves are better, once enough is in flight: the launch
+// asks for a share of the LDS, which it does not use, so that a compute unit holds six or eight workgroups of two waves.  TB/s
+// with 5, 6, 7, 8 and 10 of them, and with as many as there is room for (400M weights; of type / gradient's): fp32 / fp32 6.08,
+// 6.09, 6.10, 6.12, 6.07, 5.88; fp32 / bf16 6.19, 6.20, 6.36, 6.37, 6.41, 6.15; masters / fp32 6.25, 6.25, 6.18, 6.17, 6.13, 6.02;
+// masters / bf16 6.26, 6.24, 6.23, 6.21, 6.13, 5.76; bf16 / fp32 5.93, 5.96, 6.33, 6.36, 6.31, 6.00; bf16 / bf16 5.66, 5.67, 6.26,
+// 6.22, 6.21, 5.94.  Four waves to a workgroup lose 6 %.  The arithmetic of 8-bit states needs all waves.
+template <bool MXFP8>
+struct Shape {
+    static constexpr int V = MXFP8 ? 8 : 4;               // elements of a lane
+    static constexpr int kThreads = MXFP8 ? 256 : 128;
+    static constexpr int kPiece = V * kThreads;           // elements of a workgroup; a multiple of the 8-bit states' blocks
+    // bytes of LDS to a workgroup, where most elements have masters and where not
+    static int lds(bool masters) { return MXFP8 ? 0 : masters ? 27000 : 20000; }
 };
 
 struct AdamTensor {
@@ -310,7 +323,7 @@ __device__ __forceinline__ void dequantize(const uint32_t (&codes)[2], float sca
 // with 8-bit ones, where the work on a block is shared by fewer lanes.
 template <int PARAM, bool GRAD_BF16, bool MXFP8>
 struct AdamInput {
-    static constexpr int V = MXFP8 ? kPieceMxfp8 / 256 : kPieceF32 / 256;
+    static constexpr int V = Shape<MXFP8>::V;
     typedef typename std::conditional<GRAD_BF16, bf16_t, uint32_t>::type grad_t;
     typedef typename std::conditional<PARAM == kParamBf16, bf16_t, uint32_t>::type param_t;   // what is stepped
     typedef typename std::conditional<MXFP8, uint8_t, uint32_t>::type state_t;
@@ -345,8 +358,8 @@ __device__ __forceinline__ void adamw_piece(const AdamTensor& t, const AdamStep&
 #pragma clang fp contract(off)
     typedef AdamInput<PARAM, GRAD_BF16, MXFP8> Input;
     constexpr int V = Input::V;
-    const int64_t base = piece * (256 * V), j = base + V * threadIdx.x;
-    const bool whole = base + 256 * V <= t.n;
+    const int64_t base = piece * Shape<MXFP8>::kPiece, j = base + V * threadIdx.x;
+    const bool whole = base + Shape<MXFP8>::kPiece <= t.n;
     const int left = (int)min((int64_t)V, t.n - j);   // none or negative: this lane has nothing
     Input cur;
     cur.load(t, j, whole, left);
@@ -437,7 +450,8 @@ __device__ __forceinline__ void adamw_piece(const AdamTensor& t, const AdamStep&
     }
 }
 
-__global__ __launch_bounds__(256) void adamw_kernel(AdamList l, AdamStep h) {
+template <bool MXFP8>
+__global__ __launch_bounds__(Shape<MXFP8>::kThreads) void adamw_kernel(AdamList l, AdamStep h) {
     const float scale = h.grad_scale ? *h.grad_scale : 1.f;
     int lo = 0, hi = l.count, first = 0, at = 0;
     while (hi - lo > 1) {
@@ -456,35 +470,71 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamList l, AdamStep h) {
 #pragma unroll
     for (int k = 0; k < kWordsMost; ++k) w[k] = l.word[at + k];
     const uint64_t size = reinterpret_cast<uint64_t>(w[0]), rates = reinterpret_cast<uint64_t>(w[1]);
-    const int kind = (int)(size >> 48);
-    const AdamTensor t = {w[2], w[3], w[4], w[5], kind >= 6 ? w[8] : w[6], static_cast<uint8_t*>(w[6]), static_cast<uint8_t*>(w[7]),
-                          (int64_t)(size & ((1ull << 48) - 1)), __uint_as_float((uint32_t)rates),
-                          __uint_as_float((uint32_t)(rates >> 32)), l.index + lo};
-    switch (kind) {
-        case 0: return adamw_piece<kParamF32, false, false>(t, h, scale, piece);
-        case 1: return adamw_piece<kParamF32, true, false>(t, h, scale, piece);
-        case 2: return adamw_piece<kParamMaster, false, false>(t, h, scale, piece);
-        case 3: return adamw_piece<kParamMaster, true, false>(t, h, scale, piece);
-        case 4: return adamw_piece<kParamBf16, false, false>(t, h, scale, piece);
-        case 5: return adamw_piece<kParamBf16, true, false>(t, h, scale, piece);
-        case 6: return adamw_piece<kParamF32, false, true>(t, h, scale, piece);
-        case 7: return adamw_piece<kParamF32, true, true>(t, h, scale, piece);
-        case 8: return adamw_piece<kParamMaster, false, true>(t, h, scale, piece);
-        case 9: return adamw_piece<kParamMaster, true, true>(t, h, scale, piece);
-        case 10: return adamw_piece<kParamBf16, false, true>(t, h, scale, piece);
-        default: return adamw_piece<kParamBf16, true, true>(t, h, scale, piece);
+    const AdamTensor t = {w[2], w[3], w[4], w[5], MXFP8 ? w[8] : w[6], static_cast<uint8_t*>(w[6]), static_cast<uint8_t*>(w[7]),
+                          (int64_t)(size & ((1ull << 34) - 1)), __uint_as_float((uint32_t)rates),
+                          __uint_as_float((uint32_t)(rates >> 32)), (int)(size >> 37)};
+    switch ((int)(size >> 34) & 7) {
+        case 0: return adamw_piece<kParamF32, false, MXFP8>(t, h, scale, piece);
+        case 1: return adamw_piece<kParamF32, true, MXFP8>(t, h, scale, piece);
+        case 2: return adamw_piece<kParamMaster, false, MXFP8>(t, h, scale, piece);
+        case 3: return adamw_piece<kParamMaster, true, MXFP8>(t, h, scale, piece);
+        case 4: return adamw_piece<kParamBf16, false, MXFP8>(t, h, scale, piece);
+        default: return adamw_piece<kParamBf16, true, MXFP8>(t, h, scale, piece);
     }
 }
 
 // place of a tensor's types in the switch above
 inline int kind_of(const moe_adamw_tensor_t& t) {
     const int param = t.param_dt == MOE_F32 ? kParamF32 : t.master ? kParamMaster : kParamBf16;
-    return (t.state == MOE_STATE_MXFP8 ? 6 : 0) + 2 * param + (t.grad_dt == MOE_BF16 ? 1 : 0);
+    return 2 * param + (t.grad_dt == MOE_BF16 ? 1 : 0);
 }
 
-inline int64_t pieces_of(const moe_adamw_tensor_t& t) {
-    const int piece = t.state == MOE_STATE_MXFP8 ? kPieceMxfp8 : kPieceF32;
-    return (t.n + piece - 1) / piece;
+// The tensors of one kind of states, in as few launches as hold them.
+template <bool MXFP8>
+void launch_adamw_states(const moe_adamw_tensor_t* tensors, int count, double lr, double bc1, const AdamStep& h, hipStream_t s) {
+    AdamList l;
+    int64_t pieces = 0, all = 0, mastered = 0;
+    int words = 0;
+    l.count = 0;
+    auto flush = [&] {
+        if (pieces)
+            hipLaunchKernelGGL(adamw_kernel<MXFP8>, dim3((unsigned)pieces), dim3(Shape<MXFP8>::kThreads), Shape<MXFP8>::lds(2 * mastered > all), s, l, h);
+        l.count = words = 0;
+        pieces = all = mastered = 0;
+    };
+    auto put = [&](const void* p) { l.word[words++] = const_cast<void*>(p); };
+    auto put_bits = [&](uint64_t b) { l.word[words++] = reinterpret_cast<void*>(b); };
+    auto bits = [](double x) {
+        const float f = (float)x;
+        uint32_t u;
+        memcpy(&u, &f, sizeof u);
+        return (uint64_t)u;
+    };
+    for (int i = 0; i < count; ++i) {
+        const moe_adamw_tensor_t& t = tensors[i];
+        if (t.n == 0 || (t.state == MOE_STATE_MXFP8) != MXFP8) continue;
+        const int64_t more = (t.n + Shape<MXFP8>::kPiece - 1) / Shape<MXFP8>::kPiece;
+        if (l.count == kAdamTensors || words + 6 + (t.master ? 1 : 0) + (MXFP8 ? 2 : 0) > kAdamWords || pieces + more > kLaunchPieces)
+            flush();
+        const double lr_i = lr * t.lr_scale;
+        l.tensor[l.count].first = (int32_t)pieces;
+        l.tensor[l.count++].at = words;
+        put_bits((uint64_t)t.n | (uint64_t)kind_of(t) << 34 | (uint64_t)i << 37);
+        put_bits(bits(1. - lr_i * t.weight_decay) | bits(lr_i / bc1) << 32);
+        put(t.grad);
+        put(t.master ? t.master : t.param);
+        put(t.exp_avg);
+        put(t.exp_avg_sq);
+        if (MXFP8) {
+            put(t.exp_avg_scale);
+            put(t.exp_avg_sq_scale);
+        }
+        if (t.master) put(t.param);
+        pieces += more;
+        all += t.n;
+        if (t.master) mastered += t.n;
+    }
+    flush();
 }
 
 }  // namespace
@@ -529,47 +579,8 @@ void launch_adamw(const moe_adamw_tensor_t* tensors, int count, double lr, doubl
     const double bc1 = 1. - pow(beta1, (double)step), bc2 = 1. - pow(beta2, (double)step);
     const AdamStep h = {(float)beta1, (float)(1. - beta1), (float)beta2, (float)(1. - beta2), (float)eps,
                         (float)(1. / sqrt(bc2)), seed, grad_scale};
-    AdamList l;
-    int64_t pieces = 0;
-    int words = 0;
-    l.count = 0;
-    auto flush = [&] {
-        if (pieces) hipLaunchKernelGGL(adamw_kernel, dim3((unsigned)pieces), dim3(256), 0, s, l, h);
-        l.count = words = 0;
-        pieces = 0;
-    };
-    auto put = [&](const void* p) { l.word[words++] = const_cast<void*>(p); };
-    auto put_bits = [&](uint64_t b) { l.word[words++] = reinterpret_cast<void*>(b); };
-    auto bits = [](double x) {
-        const float f = (float)x;
-        uint32_t u;
-        memcpy(&u, &f, sizeof u);
-        return (uint64_t)u;
-    };
-    for (int i = 0; i < count; ++i) {
-        const moe_adamw_tensor_t& t = tensors[i];
-        const int64_t more = pieces_of(t);
-        const bool mxfp8 = t.state == MOE_STATE_MXFP8;
-        if (l.count == kAdamTensors || words + 6 + (t.master ? 1 : 0) + (mxfp8 ? 2 : 0) > kAdamWords || pieces + more > kLaunchPieces)
-            flush();
-        if (l.count == 0) l.index = i;
-        const double lr_i = lr * t.lr_scale;
-        l.tensor[l.count].first = (int32_t)pieces;
-        l.tensor[l.count++].at = words;
-        put_bits((uint64_t)t.n | (uint64_t)kind_of(t) << 48);
-        put_bits(bits(1. - lr_i * t.weight_decay) | bits(lr_i / bc1) << 32);
-        put(t.grad);
-        put(t.master ? t.master : t.param);
-        put(t.exp_avg);
-        put(t.exp_avg_sq);
-        if (mxfp8) {
-            put(t.exp_avg_scale);
-            put(t.exp_avg_sq_scale);
-        }
-        if (t.master) put(t.param);
-        pieces += more;
-    }
-    flush();
+    launch_adamw_states<false>(tensors, count, lr, bc1, h, s);
+    launch_adamw_states<true>(tensors, count, lr, bc1, h, s);
 }
 
 }  // namespace moe
