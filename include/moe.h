@@ -516,8 +516,10 @@ moe_status_t moe_grad_norm(const moe_grad_tensor_t* tensors, int count, float ma
  *   p = p (1 - lr_i weight_decay)
  *       - lr_i / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  *
- * computed in fp32, m and v with every operation rounded (no fused multiply-add).  A
- * NaN in *grad_scale: nothing is changed.
+ * computed in fp32, m and v with every operation rounded (no fused multiply-add); with
+ * 8-bit states the weight's square root and quotient are within a unit in the last
+ * place, and a v below 2^-126 may count as 0 there.  A NaN in *grad_scale: nothing is
+ * changed.
  *
  * Weights (param_dt, master):
  *   MOE_F32,  NULL      fp32

@@ -393,6 +393,7 @@ def test_refusals():
                      (dict(state=1), b"scales"), (dict(weight_decay=float("inf")), b"finite"), (dict(lr_scale=float("nan")), b"finite")]:
         _refuse(lambda: step(**kw), word)
     _refuse(lambda: step(n=1 << 40), b"limit", 2)
+    _refuse(lambda: step(count=(1 << 26) + 1), b"limit", 2)
     assert step(count=0, tensors=False) == 0 and step(n=0, param=0, grad=0) == 0
 
     def norm(count=1, max_norm=1.0, mult=1.0, out=0x1000, ws=0x2000, size=1 << 20, grad=0x3000, n=10, dt=0):
@@ -403,6 +404,7 @@ def test_refusals():
                      (dict(out=0), b"out"), (dict(out=0x1001), b"out"), (dict(grad=0), b"grad"), (dict(grad=0x3008), b"aligned"),
                      (dict(n=-3), b"n=-3"), (dict(dt=7), b"dt"), (dict(ws=0x2004), b"aligned")]:
         _refuse(lambda: norm(**kw), word)
+    _refuse(lambda: norm(count=(1 << 26) + 1), b"limit", 2)
     _refuse(lambda: norm(size=8), b"workspace", 3)
     _refuse(lambda: norm(ws=0), b"workspace", 3)
     assert moe.grad_norm_workspace_bytes(0) > 0 and moe.grad_norm_workspace_bytes(-1) == 0
