@@ -540,8 +540,8 @@ void launch_adamw_states(const moe_adamw_tensor_t* tensors, int count, double lr
 }  // namespace
 
 size_t grad_norm_workspace_bytes(int count) {
-    // a launch takes one tensor at least; fewer than kGradTensors only where there are too many runs
-    return (size_t)(count > 0 ? count : 1) * kNormGroups * sizeof(double);
+    const size_t launches = ((size_t)count + kGradTensors - 1) / kGradTensors;
+    return (launches > 0 ? launches : 1) * kNormGroups * sizeof(double);
 }
 
 void launch_grad_norm(const moe_grad_tensor_t* tensors, int count, float max_norm, float multiplier, float* out, void* ws,
@@ -564,7 +564,7 @@ void launch_grad_norm(const moe_grad_tensor_t* tensors, int count, float max_nor
         const bool bf16 = tensors[i].dt == MOE_BF16;
         const int64_t more = (tensors[i].n * (bf16 ? 2 : 4) + kRunBytes - 1) / kRunBytes;
         if (more == 0) continue;
-        if (l.count == kGradTensors || runs + more > (1 << 30)) flush();
+        if (l.count == kGradTensors) flush();   // 192 tensors of 2^33 elements at most: under 2^29 runs
         l.grad[l.count] = tensors[i].grad;
         l.n[l.count] = (uint64_t)tensors[i].n | (bf16 ? 1ull << 63 : 0);
         l.first[l.count++] = (int32_t)runs;
