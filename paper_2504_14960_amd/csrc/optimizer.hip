@@ -2,7 +2,7 @@
 //
 //   grad_norm_partial_kernel  sums of squares, in 64 bits, of runs of 16 KiB
 //   grad_norm_finish_kernel   the norm and the factor that clips it
-//   adamw_kernel              the step, a piece of 1024 or 2048 elements to a workgroup
+//   adamw_kernel              the step, a piece of 512 (fp32 states) or 2048 elements (8-bit) to a workgroup
 //
 // A launch takes a list of tensors, described in its arguments; every tensor is cut into pieces, and a workgroup finds its
 // tensor from the first pieces.  All are bound by memory, read and written once and streamed past the caches.
@@ -144,8 +144,8 @@ __global__ __launch_bounds__(256) void grad_norm_finish_kernel(const double* __r
 
 // A tensor in a launch's arguments, which are limited to 4 KiB: six words of 64 bits and up to three more where its types need
 // them, so that a launch takes 70 tensors in fp32, 60 in bf16 with masters, 46 of those with 8-bit states.
-//   n | kind << 34 | place in the caller's list << 37;  1 - lr wd, lr / (1 - beta1^t);  grad;  what is stepped (param or master);  m;  v;
-//   [scales of m; of v];  [param, where there is a master]
+//   n | kind << 34 | place in the caller's list << 37;  1 - lr wd, lr / (1 - beta1^t);  grad;  what is stepped (param or
+//   master);  m;  v;  [scales of m; of v];  [param, where there is a master]
 constexpr int kAdamTensors = 70, kAdamWords = 420, kWordsMost = 9;
 
 struct AdamList {
@@ -498,7 +498,8 @@ void launch_adamw_states(const moe_adamw_tensor_t* tensors, int count, double lr
     l.count = 0;
     auto flush = [&] {
         if (pieces)
-            hipLaunchKernelGGL(adamw_kernel<MXFP8>, dim3((unsigned)pieces), dim3(Shape<MXFP8>::kThreads), Shape<MXFP8>::lds(2 * mastered > all), s, l, h);
+            hipLaunchKernelGGL(adamw_kernel<MXFP8>, dim3((unsigned)pieces), dim3(Shape<MXFP8>::kThreads),
+                               Shape<MXFP8>::lds(2 * mastered > all), s, l, h);
         l.count = words = 0;
         pieces = all = mastered = 0;
     };
