@@ -76,8 +76,10 @@ __device__ __forceinline__ Chunk find_chunk(int b, const int32_t* offsets, int n
         else hi = mid;
     }
     const int begin = clamp_token(offsets[lo], T), end = clamp_token(offsets[lo + 1], T);
-    const long long t0 = begin + (long long)(b - first_chunk(offsets, lo, T, C)) * C;
-    const int from = max((int)(t0 < end ? t0 : end), 0);
+    const int nth = b - first_chunk(offsets, lo, T, C);
+    if (nth < 0) return {lo, begin, begin};   // tokens before the first sequence: nobody's
+    const long long t0 = begin + (long long)nth * C;
+    const int from = (int)(t0 < end ? t0 : end);
     return {lo, from, from + min(end - from, C)};
 }
 

@@ -1,0 +1,42 @@
+"""Balance loss and its gradient at the edges of what the interface promises: rows, values and sizes that ordinary calls do not
+have.  Tolerances are those of test_gpu_balance, which derives them."""
+import numpy as np
+import pytest
+
+from oracle import training as o
+from test_gpu_balance import EPS, _backward, _dev, _forward, _inputs
+
+
+def _gradient_holds(got, logits, counts, n, offsets, addend=None):
+    d, size = o.balance_loss_backward(logits, counts, n, (1.0, 1.0), 2, np.float32(0.01), np.float32(0.001), None, offsets)
+    if addend is not None:
+        d, size = d + addend, size + abs(addend)
+    assert (abs(got - d) <= 64 * EPS * size + 1e-37).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("E", [3, 4, 8, 16, 32, 60, 64, 128, 200, 256])
+@pytest.mark.parametrize("T,offsets", [(400, [100, 300]), (5000, [2100, 2100, 3300, 4800]), (70000, [66000, 68000, 69990])])
+def test_rows_outside_every_sequence_are_left_untouched(E, T, offsets):
+    """Before the first sequence and behind the last one, whatever multiple of a chunk they start at, in place too."""
+    import torch
+    import paper_2504_14960_amd as moe
+    offsets = np.array(offsets, np.int32)
+    logits, idx, _, _ = _inputs(T, E, 2)
+    counts, sums, n, losses = _forward(logits, idx, None, offsets)
+    inside = slice(offsets[0], offsets[-1])
+    want = o.balance_loss(logits[inside], idx[inside], np.float32(0.01), np.float32(0.001), None, offsets - offsets[0])
+    np.testing.assert_array_equal(counts.cpu().numpy(), want[0])
+    np.testing.assert_array_equal(n.cpu().numpy(), want[2])
+    np.testing.assert_allclose(sums.cpu().numpy(), want[1], rtol=340 * EPS, atol=1e-30)
+    np.testing.assert_allclose(losses.cpu().numpy(), want[3], rtol=400 * EPS, atol=1e-30)
+
+    addend = np.random.default_rng(1).standard_normal((T, E)).astype(np.float32) * np.float32(1e-4)
+    out = _dev(addend)
+    moe.balance_loss_backward(_dev(logits), counts, n, None, 2, 0.01, 0.001, out, addend=out, seq_offsets=_dev(offsets))
+    plain = _backward(logits, 2, counts, n, None, offsets, None)
+    torch.cuda.synchronize()
+    for got, add, outside in ((out.cpu().numpy(), addend[inside], addend), (plain.cpu().numpy(), None, np.full((T, E), -7.0, np.float32))):
+        np.testing.assert_array_equal(got[:offsets[0]], outside[:offsets[0]])
+        np.testing.assert_array_equal(got[offsets[-1]:], outside[offsets[-1]:])
+        _gradient_holds(got[inside], logits[inside], want[0], want[2], offsets - offsets[0], add)
