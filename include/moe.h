@@ -352,7 +352,9 @@ moe_status_t moe_router_backward_addend(const void* x, const void* w_router, con
  * seq_offsets [n_seq+1] int32, non-decreasing from 0 to T, or NULL (one sequence,
  * n_seq = 1).  Outputs: counts, prob_sums [n_seq,E]; seq_tokens [n_seq+1] int32 (n_s,
  * then n); losses [2] fp32.  Sums over tokens are taken in an order that the sizes and
- * seq_offsets fix.  E <= 256, K <= min(E,64), T <= 2^30, 1 <= n_seq <= 65536.
+ * seq_offsets fix.  E <= 256, K <= min(E,64), T <= 2^30, 1 <= n_seq <= 65536.  The
+ * workspace's size never falls as T, E or n_seq grow: one for the largest call serves
+ * all of them.
  */
 size_t moe_balance_loss_workspace_bytes(int T, int E, int n_seq);
 moe_status_t moe_balance_loss(const float* logits, const int32_t* topk_idx,

@@ -245,14 +245,14 @@ struct Partials {
     uint32_t* ticket; // workgroups of balance_finish_kernel that are done; cleared by balance_partial_kernel
 };
 
-inline size_t carve(void* ws, const Cut& cut, int E, int n_seq, Partials* out) {
+inline size_t carve(void* ws, int chunks, int slabs, int E, int n_seq, Partials* out) {
     uint8_t* base = static_cast<uint8_t*>(ws);
     size_t o = 0;
     auto take = [&](size_t bytes) { uint8_t* p = base + o; o = up256(o + bytes); return p; };
     Partials p;
-    p.cell = reinterpret_cast<Cell*>(take((size_t)cut.chunks * E * sizeof(Cell)));
-    p.tail = reinterpret_cast<Tail*>(take((size_t)cut.chunks * sizeof(Tail)));
-    p.loss = reinterpret_cast<double*>(take((size_t)n_seq * cut.slabs * 8));
+    p.cell = reinterpret_cast<Cell*>(take((size_t)chunks * E * sizeof(Cell)));
+    p.tail = reinterpret_cast<Tail*>(take((size_t)chunks * sizeof(Tail)));
+    p.loss = reinterpret_cast<double*>(take((size_t)n_seq * slabs * 8));
     p.z = reinterpret_cast<double*>(take((size_t)n_seq * 8));
     p.ticket = reinterpret_cast<uint32_t*>(take(4));
     if (out) *out = p;
@@ -625,9 +625,11 @@ inline int power_of_two(int n) {
 
 }  // namespace
 
+// Room for the chunks and slabs of any Cut of up to T tokens, E experts and n_seq sequences, with offsets or without, so that a
+// workspace for the largest call serves every smaller one (chunks get longer above 65536 tokens, and fewer).
 size_t balance_loss_workspace_bytes(int T, int E, int n_seq) {
-    // with offsets or without: the larger of the two
-    return max(carve(nullptr, Cut(T, E, n_seq, true), E, n_seq, nullptr), carve(nullptr, Cut(T, E, n_seq, false), E, n_seq, nullptr));
+    const int chunks = max(min(T, 65536) / 64, T / 256) + n_seq;
+    return carve(nullptr, chunks, (E + 15) / 16, E, n_seq, nullptr);
 }
 
 void launch_balance_loss(const float* logits, const int32_t* idx, const uint8_t* mask, const int32_t* offsets, int T, int E,
@@ -635,7 +637,7 @@ void launch_balance_loss(const float* logits, const int32_t* idx, const uint8_t*
                          int32_t* seq_tokens, float* losses, void* ws, hipStream_t s) {
     const Cut cut(T, E, n_seq, offsets != nullptr);
     Partials p;
-    carve(ws, cut, E, n_seq, &p);
+    carve(ws, cut.chunks, cut.slabs, E, n_seq, &p);
     const Results res = {counts, prob_sums, seq_tokens, losses, balance_coef, z_coef, E, K, n_seq};
     with_lanes(E, [&](auto lanes, auto whole) {
         auto kernel = mask ? balance_partial_kernel<lanes.value, whole.value, true> : balance_partial_kernel<lanes.value, whole.value, false>;

@@ -40,3 +40,23 @@ def test_rows_outside_every_sequence_are_left_untouched(E, T, offsets):
         np.testing.assert_array_equal(got[:offsets[0]], outside[:offsets[0]])
         np.testing.assert_array_equal(got[offsets[-1]:], outside[offsets[-1]:])
         _gradient_holds(got[inside], logits[inside], want[0], want[2], offsets - offsets[0], add)
+
+
+def test_a_workspace_for_the_largest_call_serves_every_smaller_one():
+    """The bytes asked for never fall as tokens, experts or sequences grow."""
+    import paper_2504_14960_amd as moe
+    need = moe.balance_loss_workspace_bytes
+    tokens = sorted({max(0, t + d) for t in (0, 64, 128, 512, 4096, 16384, 32768, 65536, 131072, 262144, 1 << 20, 1 << 24, 1 << 30)
+                     for d in (-64, -1, 0, 1, 63, 64, 65, 2000) if t + d <= 1 << 30})
+    experts, sequences = (1, 2, 4, 16, 17, 60, 64, 65, 128, 129, 255, 256), (1, 2, 3, 4, 5, 15, 16, 17, 33, 256, 1000, 4096, 65536)
+    for E in experts:
+        for S in sequences:
+            sizes = [need(T, E, S) for T in tokens]
+            assert sizes == sorted(sizes), (E, S)
+    for T in tokens:
+        for S in sequences:
+            sizes = [need(T, E, S) for E in experts]
+            assert sizes == sorted(sizes), (T, S)
+        for E in experts:
+            sizes = [need(T, E, S) for S in sequences]
+            assert sizes == sorted(sizes), (T, E)
