@@ -60,3 +60,10 @@ def test_a_workspace_for_the_largest_call_serves_every_smaller_one():
         for E in experts:
             sizes = [need(T, E, S) for S in sequences]
             assert sizes == sorted(sizes), (T, E)
+
+
+def test_a_workspace_of_several_gigabytes_is_asked_for_whole():
+    """Packed sequences leave a sum and a count of every expert for 256 tokens or fewer: more bytes than 32 bits count."""
+    import paper_2504_14960_amd as moe
+    for T, E, S in ((1 << 28, 256, 1), (1 << 28, 256, 65536), (1 << 29, 129, 3), (1 << 30, 64, 1), (1 << 30, 256, 1)):
+        assert moe.balance_loss_workspace_bytes(T, E, S) >= (T // 256 + S) * E * 8, (T, E, S)
