@@ -354,7 +354,7 @@ moe_status_t moe_router_backward_addend(const void* x, const void* w_router, con
  * then n); losses [2] fp32.  Sums over tokens are taken in an order that the sizes and
  * seq_offsets fix.  E <= 256, K <= min(E,64), T <= 2^30, 1 <= n_seq <= 65536.  The
  * workspace's size never falls as T, E or n_seq grow: one for the largest call serves
- * all of them.
+ * all of them; 0 where a call would be refused.
  */
 size_t moe_balance_loss_workspace_bytes(int T, int E, int n_seq);
 moe_status_t moe_balance_loss(const float* logits, const int32_t* topk_idx,

@@ -472,7 +472,7 @@ moe_status_t moe_router_backward_addend(const void* x, const void* w_router, con
 static moe_status_t check_balance(const char* fn, int T, int E, int K, int n_seq, const int32_t* seq_offsets,
                                   float balance_coef, float z_coef) {
     if (moe_status_t st = check_dims(fn, T, 4, E, K, MOE_F32)) return st;
-    if (T > 1 << 30) return fail(MOE_ERR_UNSUPPORTED, "%s: T=%d exceeds the limit 2^30", fn, T);
+    if (T > kMaxBalanceTokens) return fail(MOE_ERR_UNSUPPORTED, "%s: T=%d exceeds the limit 2^30", fn, T);
     if (n_seq < 1) return fail(MOE_ERR_INVALID_ARG, "%s: need n_seq >= 1 (n_seq=%d)", fn, n_seq);
     if (n_seq > kMaxSequences) return fail(MOE_ERR_UNSUPPORTED, "%s: n_seq=%d exceeds the limit %d", fn, n_seq, kMaxSequences);
     if (seq_offsets == nullptr && n_seq != 1)
@@ -485,7 +485,7 @@ static moe_status_t check_balance(const char* fn, int T, int E, int K, int n_seq
 }
 
 size_t moe_balance_loss_workspace_bytes(int T, int E, int n_seq) {
-    if (T < 0 || E <= 0 || n_seq <= 0) return 0;
+    if (T < 0 || T > kMaxBalanceTokens || E <= 0 || E > kMaxExperts || n_seq <= 0 || n_seq > kMaxSequences) return 0;
     return balance_loss_workspace_bytes(T, E, n_seq);
 }
 

@@ -28,6 +28,7 @@ inline void allow_lds(OncePerDevice& lds, const void* kern, int bytes) {
 constexpr int kWave = 64;
 constexpr int kMaxExperts = 256;
 constexpr int kMaxTopK = 64;
+constexpr int kMaxBalanceTokens = 1 << 30;         // of one balance-loss call
 constexpr int kMaxSequences = 65536;               // of one balance-loss call
 constexpr int kMaxListTensors = 1 << 26;           // of one gradient-norm or AdamW call
 constexpr int64_t kMaxListElements = 1ll << 33;    // of one tensor of a gradient-norm or AdamW call

@@ -67,3 +67,11 @@ def test_a_workspace_of_several_gigabytes_is_asked_for_whole():
     import paper_2504_14960_amd as moe
     for T, E, S in ((1 << 28, 256, 1), (1 << 28, 256, 65536), (1 << 29, 129, 3), (1 << 30, 64, 1), (1 << 30, 256, 1)):
         assert moe.balance_loss_workspace_bytes(T, E, S) >= (T // 256 + S) * E * 8, (T, E, S)
+
+
+def test_sizes_that_a_call_refuses_need_no_workspace():
+    import paper_2504_14960_amd as moe
+    need = moe.balance_loss_workspace_bytes
+    assert need(1 << 30, 256, 65536) > 0
+    for T, E, S in (((1 << 30) + 1, 8, 1), (100, 257, 1), (100, 8, 65537), ((1 << 31) - 1, 8, (1 << 31) - 1)):
+        assert need(T, E, S) == 0, (T, E, S)
