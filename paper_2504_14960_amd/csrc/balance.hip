@@ -590,8 +590,9 @@ __global__ __launch_bounds__(256) void balance_backward_kernel(const float* __re
         constexpr int u = index.value;
         const float ru = r.template get<u>(), su = shift.template get<u>();
         f32x4 d;
+        // not 0 * g where a token does not count: g is infinite or NaN where the losses' own gradient is
 #pragma unroll
-        for (int v = 0; v < 4; ++v) d[v] = fmaf(b.x[u][v] * ru, g[v] + su, more[u][v]);
+        for (int v = 0; v < 4; ++v) d[v] = ru != 0.f ? fmaf(b.x[u][v] * ru, g[v] + su, more[u][v]) : more[u][v];
         if (t + u * step < c.t1) store_row<LPT, WHOLE>(dlogits + (size_t)(t + u * step) * E, q, E, d);
     };
     write(std::integral_constant<int, 0>());

@@ -75,3 +75,22 @@ def test_sizes_that_a_call_refuses_need_no_workspace():
     assert need(1 << 30, 256, 65536) > 0
     for T, E, S in (((1 << 30) + 1, 8, 1), (100, 257, 1), (100, 8, 65537), ((1 << 31) - 1, 8, (1 << 31) - 1)):
         assert need(T, E, S) == 0, (T, E, S)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("up", [np.inf, -np.inf, np.nan, 3e38])
+@pytest.mark.parametrize("E", [3, 8, 16, 60, 64, 200, 256])
+def test_rows_that_do_not_count_whatever_the_upstream_gradient(E, up):
+    """Masked rows and rows of -inf are 0 (+ addend) where the gradient of the others is not finite."""
+    logits, idx, _, offsets = _inputs(500, E, 2, 3)
+    mask = (np.arange(500) % 3 != 0).astype(np.uint8)
+    logits[mask == 0] = np.nan
+    logits[1::9] = -np.inf
+    nothing = (mask == 0) | (logits[:, 0] == -np.inf)
+    counts, _, n, _ = _forward(logits, idx, mask, offsets)
+    addend = np.random.default_rng(2).standard_normal((500, E)).astype(np.float32)
+    ups = np.array([up, up], np.float32)
+    for add in (None, addend):
+        got = _backward(logits, 2, counts, n, mask, offsets, ups, add, cb=3e38, cz=1.0).cpu().numpy()
+        np.testing.assert_array_equal(got[nothing], 0.0 if add is None else add[nothing])
+        assert not np.isfinite(got[~nothing]).all()
