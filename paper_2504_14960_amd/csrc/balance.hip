@@ -234,7 +234,7 @@ struct Cell {
     int32_t count;
 };
 struct Tail {
-    float z;
+    double z;   // in 64 bits from the first square on: that of a row of the lowest fp32 value is 10^77
     int32_t tokens;
 };
 struct Partials {
@@ -311,7 +311,7 @@ __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __re
     __shared__ double parts[4];
     __shared__ int32_t hist[kExperts];
     __shared__ float sums[16][kExperts];
-    __shared__ float zs[16];
+    __shared__ double zs[16];
     __shared__ int32_t ns[16];
     const uint8_t* mask = MASKED ? token_mask : nullptr;   // known at compile time: 52 instead of 54 us for 262144 x 256
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, b = blockIdx.x;
@@ -344,7 +344,7 @@ __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __re
             if ((unsigned)i[u] < (unsigned)E) atomicAdd(&hist[i[u]], 1);
     }
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    float zsum = 0.f;
+    double zsum = 0.;
     int n = 0;
     while (t < c.t1) {
         Batches<LPT, WHOLE, WHOLE> cur = next;
@@ -360,7 +360,7 @@ __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __re
             // a token that does not count, or has no probability, adds nothing to either loss
             const bool ok = counts_at<LPT>(counted, i) && s.v[i] != 0.f;
             const float lse = ok ? log_sum(top.v[i], s.v[i]) : 0.f;
-            if (q < (LPT >= 4 ? 4 : 1)) zsum = fmaf(lse, lse, zsum);
+            if (q < (LPT >= 4 ? 4 : 1)) zsum = fma((double)lse, (double)lse, zsum);
             s.v[i] = ok ? __builtin_amdgcn_rcpf(s.v[i]) : 0.f;
         }
         if (q == 0) n += __popc(counted);
@@ -399,13 +399,13 @@ __global__ __launch_bounds__(1024) void balance_partial_kernel(const float* __re
     double z = 0., loss = 0.;
     int tokens = 0;
     if (wave == 0) {
-        z = wave_sum(lane < waves ? (double)zs[lane] : 0.);
+        z = wave_sum(lane < waves ? zs[lane] : 0.);
         tokens = wave_sum(lane < waves ? ns[lane] : 0);
     }
     if (!direct) {
         if (threadIdx.x < E) out.cell[(size_t)b * E + threadIdx.x] = {p, count};
         if (threadIdx.x == 0) {
-            out.tail[b] = {(float)z, tokens};
+            out.tail[b] = {z, tokens};
             if (b == 0) *out.ticket = 0;
         }
         return;

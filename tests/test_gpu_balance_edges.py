@@ -94,3 +94,30 @@ def test_rows_that_do_not_count_whatever_the_upstream_gradient(E, up):
         got = _backward(logits, 2, counts, n, mask, offsets, ups, add, cb=3e38, cz=1.0).cpu().numpy()
         np.testing.assert_array_equal(got[nothing], 0.0 if add is None else add[nothing])
         assert not np.isfinite(got[~nothing]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,S", [(40, 1), (3000, 1), (3000, 4)])
+def test_logits_of_the_lowest_value(T, S):
+    """Rows whose mask leaves nothing, as the type's lowest value: uniform, with a log-sum-exp whose square passes fp32.  A z
+    loss that is switched off is 0 then, and one that is tiny is what the formula gives."""
+    import torch
+    import paper_2504_14960_amd as moe
+    E = 16
+    logits, idx, _, offsets = _inputs(T, E, 2, S)
+    logits[5] = np.finfo(np.float32).min
+    logits[6] = np.float32(1e20)
+    for cz in (0.0, 2e-38):
+        counts, sums, n, losses = _forward(logits, idx, None, offsets, cz=cz)
+        want = o.balance_loss(logits, idx, np.float32(0.01), np.float32(cz), None, offsets)
+        np.testing.assert_allclose(sums.cpu().numpy(), want[1], rtol=340 * EPS, atol=1e-30)
+        with np.errstate(over="ignore"):
+            np.testing.assert_allclose(losses.cpu().numpy(), want[3].astype(np.float32), rtol=400 * EPS, atol=1e-30)
+    logits[5] = logits[6]
+    losses = _forward(logits, idx, None, offsets, cz=1e-30)[3]
+    want = o.balance_loss(logits, idx, np.float32(0.01), np.float32(1e-30), None, offsets)[3]
+    assert 1e5 < want[1] < 1e10
+    np.testing.assert_allclose(losses.cpu().numpy(), want, rtol=400 * EPS)
+    out = torch.empty((T, E), device="cuda")
+    moe.balance_loss_backward(_dev(logits), counts, n, None, 2, 0.01, 0.0, out, seq_offsets=_dev(offsets))
+    assert torch.isfinite(out).all()
