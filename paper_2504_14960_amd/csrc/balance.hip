@@ -25,8 +25,9 @@ namespace moe {
 
 namespace {
 
-constexpr int kBatches = 4;        // tokens a lane has in flight
-constexpr int kTicketGroups = 64;  // workgroups of balance_finish_kernel of which the last one adds up the sequences
+constexpr int kBatches = 4;            // tokens a lane has in flight
+constexpr int kGridGroups = 1 << 23;  // workgroups of 256 threads in a launch at most: a grid has less than 2^32 threads
+constexpr int kTicketGroups = 64;      // workgroups of balance_finish_kernel of which the last one adds up the sequences
 
 // How a call is cut, by its sizes alone, so that the order of the sums is reproducible.  The chunks of one sequence are added
 // up by one workgroup for 64 experts; for more, 16 experts to a workgroup and a ticket for the last of them: 6.6 us instead
@@ -543,12 +544,12 @@ __global__ __launch_bounds__(256) void balance_backward_kernel(const float* __re
                                                                const int32_t* __restrict__ counts,
                                                                const int32_t* __restrict__ seq_tokens,
                                                                const float* __restrict__ dlosses, const float* addend, int T,
-                                                               int E, int K, int n_seq, int C, float balance_coef,
-                                                               float z_coef, float* dlogits) {
+                                                               int E, int K, int n_seq, int C, int from_chunk,
+                                                               float balance_coef, float z_coef, float* dlogits) {
     constexpr int kTokens = 64 / LPT;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int q = lane % LPT;
-    const Chunk c = find_chunk(blockIdx.x, offsets, n_seq, T, C);
+    const Chunk c = find_chunk(from_chunk + blockIdx.x, offsets, n_seq, T, C);
     const float n = (float)max(seq_tokens[n_seq], 1), n_s = (float)max(seq_tokens[c.seq], 1);
     const float db = dlosses ? dlosses[0] : 1.f, dz = dlosses ? dlosses[1] : 1.f;
     const float a = db * balance_coef * E / (K * n) / n_s, az = dz * 2.f * z_coef / n;
@@ -660,8 +661,10 @@ void launch_balance_loss_backward(const float* logits, const uint8_t* mask, cons
         // instead of 7.7 for 65536 x 64, and save 2 of 90 us only for the largest call
         constexpr int C = kBatches * 4 * (64 / lanes.value);
         const int chunks = packed ? T / C + n_seq : (T + C - 1) / C;
-        hipLaunchKernelGGL((balance_backward_kernel<lanes.value, whole.value>), dim3(chunks), dim3(256), 0, s, logits, mask, offsets, counts,
-                           seq_tokens, dlosses, addend, T, E, K, n_seq, C, balance_coef, z_coef, dlogits);
+        for (int first = 0; first < chunks; first += kGridGroups)
+            hipLaunchKernelGGL((balance_backward_kernel<lanes.value, whole.value>), dim3(min(chunks - first, kGridGroups)), dim3(256), 0, s,
+                               logits, mask, offsets, counts, seq_tokens, dlosses, addend, T, E, K, n_seq, C, first, balance_coef, z_coef,
+                               dlogits);
     });
 }
 

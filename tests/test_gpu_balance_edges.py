@@ -121,3 +121,30 @@ def test_logits_of_the_lowest_value(T, S):
     out = torch.empty((T, E), device="cuda")
     moe.balance_loss_backward(_dev(logits), counts, n, None, 2, 0.01, 0.0, out, seq_offsets=_dev(offsets))
     assert torch.isfinite(out).all()
+
+
+@pytest.mark.gpu
+def test_gradient_of_more_tokens_than_one_row_of_a_grid():
+    """2^28 and some tokens of 129 experts: 2^24 workgroups of 256 threads, 2^32 threads.  All rows but the last thousand are alike."""
+    import torch
+    import paper_2504_14960_amd as moe
+    T, E, tail = (1 << 28) + 777, 129, 1000
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 8 * T * E + (6 << 30):
+        pytest.skip("needs 260 GiB of free device memory")
+    logits, out = torch.zeros((T, E), device="cuda"), torch.full((T, E), -7.0, device="cuda")
+    last = _inputs(tail, E, 2)[0]
+    logits[T - tail:] = _dev(last)
+    rng = np.random.default_rng(4)
+    counts, n = rng.integers(0, 2 * T // E, (1, E)).astype(np.int32), np.array([T, T], np.int32)
+    moe.balance_loss_backward(logits, _dev(counts), _dev(n), _dev(np.array([1e9, 1e9], np.float32)), 2, 0.01, 0.001, out)
+    torch.cuda.synchronize()
+    few = np.concatenate([np.zeros((1, E), np.float32), last])
+    d, size = o.balance_loss_backward(few, counts.astype(np.int64), n.astype(np.int64), (1e9, 1e9), 2, np.float32(0.01), np.float32(0.001))
+    got = torch.cat([out[:1], out[T - tail:]]).cpu().numpy()
+    assert (abs(got - d) <= 64 * EPS * size + 1e-37).all()
+    row = out[0].clone()
+    for a in range(0, T - tail, 1 << 22):
+        assert bool((out[a:min(a + (1 << 22), T - tail)] == row).all()), a
+    del logits, out
+    torch.cuda.empty_cache()
