@@ -124,6 +124,22 @@ def test_logits_of_the_lowest_value(T, S):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T,E,S,masked", [(9000, 64, 2, 0.0), (9000, 64, 2, 0.2), (6000, 65, 1, 0.1), (70000, 64, 2, 0.1), (5000, 256, 1, 0.0)])
+def test_many_chunks_a_sequence(T, E, S, masked):
+    """More than 64 chunks of every sequence, which are added up by several workgroups."""
+    rng = np.random.default_rng(T + E)
+    logits, idx, mask, _ = _inputs(T, E, 2, 1, masked)
+    middle = [T // 2 + int(rng.integers(-9, 9))] if S == 2 else []
+    offsets = np.array([0] + middle + [T], np.int32)
+    counts, sums, n, losses = _forward(logits, idx, mask, offsets)
+    want = o.balance_loss(logits, idx, np.float32(0.01), np.float32(0.001), mask, offsets)
+    np.testing.assert_array_equal(counts.cpu().numpy(), want[0])
+    np.testing.assert_array_equal(n.cpu().numpy(), want[2])
+    np.testing.assert_allclose(sums.cpu().numpy(), want[1], rtol=340 * EPS, atol=1e-30)
+    np.testing.assert_allclose(losses.cpu().numpy(), want[3], rtol=400 * EPS, atol=1e-30)
+
+
+@pytest.mark.gpu
 def test_gradient_of_more_tokens_than_one_row_of_a_grid():
     """2^28 and some tokens of 129 experts: 2^24 workgroups of 256 threads, 2^32 threads.  All rows but the last thousand are alike."""
     import torch
