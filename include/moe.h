@@ -550,9 +550,11 @@ moe_status_t moe_grad_norm(const moe_grad_tensor_t* tensors, int count, float ma
  * off is at least 1 - (u + 1/2) / 65536 of a step (E4M3), 1 - u / 65536 (bf16).
  *
  * `tensors` is HOST memory, read during the call.  All pointers but the scales are
- * 16-byte aligned; 0 <= n <= 2^33, count <= 2^26; tensors must not overlap.  step >= 1, lr >= 0, 0 <= beta1,
- * beta2 < 1, eps > 0.  No workspace.  lr, step and seed are arguments: a captured call
- * repeats them in every replay.
+ * 16-byte aligned; 0 <= n <= 2^33, count <= 2^26; tensors must not overlap.
+ * step >= 1, lr >= 0, 0 <= beta1, beta2 < 1, eps >= 2^-126 (a normal fp32 number, so
+ * that a weight whose gradient has always been 0 is divided by more than 0).  No
+ * workspace.  lr, step and seed are arguments: a captured call repeats them in every
+ * replay.
  */
 typedef enum { MOE_STATE_F32 = 0, MOE_STATE_MXFP8 = 1 } moe_state_t;
 

@@ -972,9 +972,10 @@ moe_status_t moe_adamw_step(const moe_adamw_tensor_t* tensors, int count, double
     if (count > kMaxListTensors) return fail(MOE_ERR_UNSUPPORTED, "%s: count=%d exceeds the limit 2^26", fn, count);
     if (step < 1) return fail(MOE_ERR_INVALID_ARG, "%s: step=%lld, the first one is 1", fn, (long long)step);
     if (!(lr >= 0.0) || !std::isfinite(lr) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) ||
-        !(eps > 0.0) || !std::isfinite(eps))
-        return fail(MOE_ERR_INVALID_ARG, "%s: need lr >= 0, 0 <= beta1, beta2 < 1, eps > 0 (lr=%g beta1=%g beta2=%g eps=%g)",
-                    fn, lr, beta1, beta2, eps);
+        !(eps > 0.0) || !std::isnormal((float)eps))   // the kernels' eps is fp32, and some of their reciprocals take a subnormal one as 0
+        return fail(MOE_ERR_INVALID_ARG,
+                    "%s: need lr >= 0, 0 <= beta1, beta2 < 1, eps a normal fp32 number > 0 (lr=%g beta1=%g beta2=%g eps=%g)", fn, lr,
+                    beta1, beta2, eps);
     if (reinterpret_cast<uintptr_t>(grad_scale) & 3u)
         return fail(MOE_ERR_INVALID_ARG, "%s: grad_scale is not 4-byte aligned", fn);
     bool any = false;

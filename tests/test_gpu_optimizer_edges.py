@@ -1,0 +1,46 @@
+"""Gradient norm and AdamW at the edges: numbers that fp32 cannot hold, arguments of other types, lists that one launch does not
+hold.  Tolerances are those of test_gpu_optimizer, which derives them."""
+import numpy as np
+import pytest
+
+from oracle import training as o
+from test_gpu_optimizer import ADAM_EPS, B1, B2, EPS, LR, Tensors, _bf16, _dev
+
+
+def _row(**kw):
+    from paper_2504_14960_amd.binding import _AdamWTensor
+    return (_AdamWTensor * 1)(_AdamWTensor(**{**dict(
+        param=0x1000, master=0, grad=0x2000, exp_avg=0x3000, exp_avg_sq=0x4000, exp_avg_scale=0, exp_avg_sq_scale=0, n=100,
+        weight_decay=0.0, lr_scale=1.0, param_dt=0, grad_dt=0, state=0), **kw}))
+
+
+def test_an_eps_that_fp32_does_not_hold_is_refused():
+    """Rounded to 0, or taken as 0 by a reciprocal, it would leave 0 / 0 where a gradient has always been 0."""
+    import paper_2504_14960_amd as moe
+    L = moe.lib()
+    for eps in (5e-324, 1e-300, 1e-46, 1e-45, 1e-39, 1.17e-38, 1e39, 1e300):
+        assert L.moe_adamw_step(_row(), 1, 1e-3, 0.9, 0.99, eps, 1, 0, None, None) == 1 and b"eps" in L.moe_last_error(), eps
+    for eps in (2.0 ** -126, 1e-8, 1.0, 3e38):
+        assert L.moe_adamw_step(_row(), 0, 1e-3, 0.9, 0.99, eps, 1, 0, None, None) == 0, eps
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("param", ["f32", "master", "bf16"])
+@pytest.mark.parametrize("state", ["f32", "8bit"])
+def test_weights_without_gradients_at_the_smallest_eps(param, state):
+    import torch
+    import paper_2504_14960_amd as moe
+    t = Tensors([1000, 33], [(param, "f32", state)] * 2, fresh=True)
+    for d in t.dev:
+        d["g"].zero_()
+    before = [{k: x.clone() for k, x in d.items() if x is not None} for d in t.dev]
+    for step in (1, 2):
+        moe.adamw_step(t.list, 0.0, B1, B2, 2.0 ** -126, step, seed=step)
+        moe.adamw_step(moe.AdamWTensors([d["p"] for d in t.dev], [d["g"] for d in t.dev], [d["m"] for d in t.dev],
+                                        [d["v"] for d in t.dev], masters=[d["master"] for d in t.dev],
+                                        exp_avg_scales=[d["ms"] for d in t.dev], exp_avg_sq_scales=[d["vs"] for d in t.dev]),
+                       LR, B1, B2, 2.0 ** -126, step, seed=step)
+    torch.cuda.synchronize()
+    for a, d in zip(before, t.dev):
+        for k in ("p", "master"):
+            assert k not in a or torch.equal(a[k], d[k]), k
