@@ -551,10 +551,10 @@ moe_status_t moe_grad_norm(const moe_grad_tensor_t* tensors, int count, float ma
  *
  * `tensors` is HOST memory, read during the call.  All pointers but the scales are
  * 16-byte aligned; 0 <= n <= 2^33, count <= 2^26; tensors must not overlap.
- * step >= 1, lr >= 0, 0 <= beta1, beta2 < 1, eps >= 2^-126 (a normal fp32 number, so
- * that a weight whose gradient has always been 0 is divided by more than 0).  No
- * workspace.  lr, step and seed are arguments: a captured call repeats them in every
- * replay.
+ * step >= 1, lr >= 0, lr_i / (1 - beta1^t) and 1 - lr_i weight_decay within fp32,
+ * 0 <= beta1, beta2 < 1, eps >= 2^-126 (a normal fp32 number, so that a weight whose
+ * gradient has always been 0 is divided by more than 0).  No workspace.  lr, step and
+ * seed are arguments: a captured call repeats them in every replay.
  */
 typedef enum { MOE_STATE_F32 = 0, MOE_STATE_MXFP8 = 1 } moe_state_t;
 

@@ -978,6 +978,7 @@ moe_status_t moe_adamw_step(const moe_adamw_tensor_t* tensors, int count, double
                     beta1, beta2, eps);
     if (reinterpret_cast<uintptr_t>(grad_scale) & 3u)
         return fail(MOE_ERR_INVALID_ARG, "%s: grad_scale is not 4-byte aligned", fn);
+    const double bc1 = 1. - pow(beta1, (double)step);
     bool any = false;
     for (int i = 0; i < count; ++i) {
         const moe_adamw_tensor_t& t = tensors[i];
@@ -987,6 +988,10 @@ moe_status_t moe_adamw_step(const moe_adamw_tensor_t* tensors, int count, double
             return fail(MOE_ERR_INVALID_ARG, "%s: tensor %d: unknown state %d", fn, i, (int)t.state);
         if (!std::isfinite(t.weight_decay) || !std::isfinite(t.lr_scale))
             return fail(MOE_ERR_INVALID_ARG, "%s: tensor %d: weight_decay and lr_scale must be finite", fn, i);
+        const AdamRates r = adam_rates(t, lr, bc1);
+        if (!std::isfinite(r.decay) || !std::isfinite(r.step_size))
+            return fail(MOE_ERR_INVALID_ARG, "%s: tensor %d: lr * lr_scale (%g * %g) is too large for fp32, or its weight_decay (%g) is",
+                        fn, i, lr, (double)t.lr_scale, (double)t.weight_decay);
         if (t.master && t.param_dt != MOE_BF16)
             return fail(MOE_ERR_INVALID_ARG, "%s: tensor %d: a master goes with bf16 weights only", fn, i);
         if (t.n == 0) continue;

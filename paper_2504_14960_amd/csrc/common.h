@@ -89,6 +89,14 @@ void launch_balance_loss_backward(const float* logits, const uint8_t* mask, cons
 size_t grad_norm_workspace_bytes(int count);
 void launch_grad_norm(const moe_grad_tensor_t* tensors, int count, float max_norm, float multiplier, float* out, void* ws,
                       hipStream_t s);
+// what a tensor's weight is multiplied with, 1 - lr wd, and its update, lr / bc1
+struct AdamRates {
+    float decay, step_size;
+};
+inline AdamRates adam_rates(const moe_adamw_tensor_t& t, double lr, double bc1) {
+    const double lr_i = lr * t.lr_scale;
+    return {(float)(1. - lr_i * t.weight_decay), (float)(lr_i / bc1)};
+}
 void launch_adamw(const moe_adamw_tensor_t* tensors, int count, double lr, double beta1, double beta2, double eps,
                   int64_t step, uint32_t seed, const float* grad_scale, hipStream_t s);
 

@@ -505,8 +505,7 @@ void launch_adamw_states(const moe_adamw_tensor_t* tensors, int count, double lr
     };
     auto put = [&](const void* p) { l.word[words++] = const_cast<void*>(p); };
     auto put_bits = [&](uint64_t b) { l.word[words++] = reinterpret_cast<void*>(b); };
-    auto bits = [](double x) {
-        const float f = (float)x;
+    auto bits = [](float f) {
         uint32_t u;
         memcpy(&u, &f, sizeof u);
         return (uint64_t)u;
@@ -517,11 +516,11 @@ void launch_adamw_states(const moe_adamw_tensor_t* tensors, int count, double lr
         const int64_t more = (t.n + Shape<MXFP8>::kPiece - 1) / Shape<MXFP8>::kPiece;
         if (l.count == kAdamTensors || words + 6 + (t.master ? 1 : 0) + (MXFP8 ? 2 : 0) > kAdamWords || pieces + more > kLaunchPieces)
             flush();
-        const double lr_i = lr * t.lr_scale;
+        const AdamRates rates = adam_rates(t, lr, bc1);
         l.tensor[l.count].first = (int32_t)pieces;
         l.tensor[l.count++].at = words;
         put_bits((uint64_t)t.n | (uint64_t)kind_of(t) << 34 | (uint64_t)i << 37);
-        put_bits(bits(1. - lr_i * t.weight_decay) | bits(lr_i / bc1) << 32);
+        put_bits(bits(rates.decay) | bits(rates.step_size) << 32);
         put(t.grad);
         put(t.master ? t.master : t.param);
         put(t.exp_avg);

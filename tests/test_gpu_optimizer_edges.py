@@ -44,3 +44,13 @@ def test_weights_without_gradients_at_the_smallest_eps(param, state):
     for a, d in zip(before, t.dev):
         for k in ("p", "master"):
             assert k not in a or torch.equal(a[k], d[k]), k
+
+
+def test_rates_that_fp32_does_not_hold_are_refused():
+    """An infinite rate times a moment of 0 would be NaN."""
+    import paper_2504_14960_amd as moe
+    L = moe.lib()
+    for lr, kw in ((1e39, {}), (1e300, dict(lr_scale=1e30)), (1e10, dict(lr_scale=1e30)), (1e30, dict(weight_decay=1e30)),
+                   (1e38, {})):
+        assert L.moe_adamw_step(_row(**kw), 1, lr, 0.9, 0.99, 1e-8, 1, 0, None, None) == 1, (lr, kw)
+        assert b"lr" in L.moe_last_error()
