@@ -448,6 +448,8 @@ def grad_norm(tensors, out: torch.Tensor, workspace: torch.Tensor, max_norm: flo
     """out [2] = norm of multiplier * the gradients of a GradTensors (or an AdamWTensors), and the factor that
     adamw_step takes as grad_scale: multiplier, clipped to max_norm (0: not), NaN where the norm is not finite."""
     grads = tensors.grads if isinstance(tensors, AdamWTensors) else tensors
+    if not isinstance(grads, GradTensors):
+        raise TypeError(f"tensors must be GradTensors or AdamWTensors, not {type(tensors).__name__}")
     _check(lib().moe_grad_norm(grads._list, len(grads._list), max_norm, multiplier, _expect("out", out, torch.float32, 2),
                                _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()))
 
@@ -497,6 +499,8 @@ def adamw_step(tensors: AdamWTensors, lr: float, beta1: float, beta2: float, eps
                grad_scale: Optional[torch.Tensor] = None) -> None:
     """One AdamW step (the first has step = 1) over all tensors.  grad_scale [1] fp32 on the device multiplies every
     gradient; NaN in it leaves everything as it is.  seed: of stochastic rounding, another one in every step."""
+    if not isinstance(tensors, AdamWTensors):        # the rows of a GradTensors are shorter than those the call reads
+        raise TypeError(f"tensors must be AdamWTensors, not {type(tensors).__name__}")
     scale = None if grad_scale is None else _expect("grad_scale", grad_scale, torch.float32, 1)
     _check(lib().moe_adamw_step(tensors._list, len(tensors._list), lr, beta1, beta2, eps, step, seed & 0xffffffff, scale,
                                 _stream()))

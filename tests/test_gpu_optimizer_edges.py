@@ -54,3 +54,14 @@ def test_rates_that_fp32_does_not_hold_are_refused():
                    (1e38, {})):
         assert L.moe_adamw_step(_row(**kw), 1, lr, 0.9, 0.99, 1e-8, 1, 0, None, None) == 1, (lr, kw)
         assert b"lr" in L.moe_last_error()
+
+
+def test_a_step_takes_adamw_tensors_only():
+    """The rows of a list of gradients are shorter than those of a step."""
+    import paper_2504_14960_amd as moe
+    for wrong in (moe.GradTensors([]), [], None):
+        with pytest.raises(TypeError, match="AdamWTensors"):
+            moe.adamw_step(wrong, LR, B1, B2, ADAM_EPS, 1)
+    import torch
+    with pytest.raises(TypeError, match="GradTensors"):
+        moe.grad_norm([], torch.zeros(2), torch.zeros(8, dtype=torch.uint8))
