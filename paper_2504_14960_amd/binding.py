@@ -363,9 +363,9 @@ def router_backward(x: torch.Tensor, w_router: torch.Tensor, logits: torch.Tenso
 
 
 # ---- what follows the gradients in a training step: balance loss, gradient norm, AdamW ----
-def _is(name: str, t: torch.Tensor, dtype, numel: int) -> None:
-    if t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+def _is(name: str, t: torch.Tensor, dtypes, numel: int) -> None:
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be {' or '.join(map(str, dtypes))}, not {t.dtype}")
     if t.numel() != numel:
         raise ValueError(f"{name} must have {numel} elements, not {t.numel()}")
 
@@ -374,7 +374,7 @@ def _expect(name: str, t: torch.Tensor, dtype, numel: int):
     """The device pointer of a tensor of this type and size."""
     if t.dtype is dtype and t.numel() == numel and t.is_cuda and t.is_contiguous():
         return t.data_ptr()
-    _is(name, t, dtype, numel)
+    _is(name, t, (dtype,), numel)
     return _ptr(t)
 
 
@@ -459,7 +459,10 @@ class AdamWTensors:
 
     params fp32 or bf16; masters: fp32 copies that are stepped in place of bf16 params (None, or None in places: bf16
     alone, rounded stochastically); grads fp32 or bf16; exp_avgs and exp_avg_sqs fp32, or uint8 E4M3 codes with
-    uint8 E8M0 exp_avg_scales and exp_avg_sq_scales, one to every 32 elements (zeros are fresh states)."""
+    uint8 E8M0 exp_avg_scales and exp_avg_sq_scales, one to every 32 elements (zeros are fresh states); or the same bytes as
+    float8_e4m3fn and float8_e8m0fnu."""
+
+    _CODES, _SCALES = (torch.uint8, torch.float8_e4m3fn), (torch.uint8, torch.float8_e8m0fnu)
 
     def __init__(self, params, grads, exp_avgs, exp_avg_sqs, masters=None, exp_avg_scales=None, exp_avg_sq_scales=None,
                  weight_decays=None, lr_scales=None) -> None:
@@ -474,21 +477,20 @@ class AdamWTensors:
         self._list = _packed(_AdamWTensor, _ADAMW_ROW, [self._row(*r, d, s) for r, d, s in zip(self.tensors, decays, scales)])
         self.grads = GradTensors(columns[2])
 
-    @staticmethod
-    def _row(param, master, grad, m, v, m_scale, v_scale, decay, lr_scale):
+    @classmethod
+    def _row(cls, param, master, grad, m, v, m_scale, v_scale, decay, lr_scale):
         count = param.numel()
-        small = m.dtype is torch.uint8
-        kind = torch.uint8 if small else torch.float32
-        _is("exp_avg", m, kind, count)
-        _is("exp_avg_sq", v, kind, count)
-        _is("grad", grad, grad.dtype, count)
+        small = m.dtype in cls._CODES
+        _is("exp_avg", m, (torch.float32,) + cls._CODES, count)
+        _is("exp_avg_sq", v, cls._CODES if small else (torch.float32,), count)
+        _is("grad", grad, (grad.dtype,), count)
         if master is not None:
-            _is("master", master, torch.float32, count)
+            _is("master", master, (torch.float32,), count)
         if small:
             for name, t in (("exp_avg_scale", m_scale), ("exp_avg_sq_scale", v_scale)):
                 if t is None:
                     raise ValueError(f"8-bit states need {name}s")
-                _is(name, t, torch.uint8, (count + 31) // 32)
+                _is(name, t, cls._SCALES, (count + 31) // 32)
         elif m_scale is not None or v_scale is not None:
             raise ValueError("exp_avg_scales and exp_avg_sq_scales go with 8-bit states only")
         return (_ptr(param), _ptr(master) or 0, _ptr(grad), _ptr(m), _ptr(v), _ptr(m_scale) or 0, _ptr(v_scale) or 0, count,

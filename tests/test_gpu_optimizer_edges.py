@@ -56,6 +56,41 @@ def test_rates_that_fp32_does_not_hold_are_refused():
         assert b"lr" in L.moe_last_error()
 
 
+@pytest.mark.gpu
+def test_states_in_the_types_they_are_read_as():
+    """float8_e4m3fn states and float8_e8m0fnu scales are the same bytes as uint8 ones."""
+    import torch
+    import paper_2504_14960_amd as moe
+    a, b = (Tensors([1000, 33], [("bf16", "bf16", "8bit")] * 2, seed=3) for _ in range(2))
+    as_type = lambda k, t: [d[k].view(t) for d in b.dev]  # noqa: E731
+    e4m3, e8m0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+    typed = moe.AdamWTensors([d["p"] for d in b.dev], [d["g"] for d in b.dev], as_type("m", e4m3), as_type("v", e4m3),
+                             exp_avg_scales=as_type("ms", e8m0), exp_avg_sq_scales=as_type("vs", e8m0), weight_decays=b.decays,
+                             lr_scales=b.lr_scales)
+    a.step(5, 17)
+    moe.adamw_step(typed, LR, B1, B2, ADAM_EPS, 5, seed=17)
+    for x, y in zip(a.dev, b.dev):
+        for k in ("p", "m", "v", "ms", "vs"):
+            assert torch.equal(x[k], y[k]), k
+
+
+def test_types_of_states_are_checked():
+    import torch
+    import paper_2504_14960_amd as moe
+    x, s = torch.zeros(64), torch.zeros(2, dtype=torch.uint8)
+    small, scale = x.to(torch.float8_e4m3fn), s.view(torch.float8_e8m0fnu)
+    with pytest.raises(ValueError, match="device tensors"):          # the types are right, the place is not
+        moe.AdamWTensors([x], [x], [small], [small], exp_avg_scales=[scale], exp_avg_sq_scales=[s])
+    with pytest.raises(ValueError, match="need exp_avg_scales"):
+        moe.AdamWTensors([x], [x], [small], [small])
+    with pytest.raises(TypeError, match="exp_avg must be .*float8_e4m3fn"):
+        moe.AdamWTensors([x], [x], [x.to(torch.float8_e5m2)], [small], exp_avg_scales=[scale], exp_avg_sq_scales=[scale])
+    with pytest.raises(TypeError, match="exp_avg_sq must be"):
+        moe.AdamWTensors([x], [x], [small], [x], exp_avg_scales=[scale], exp_avg_sq_scales=[scale])
+    with pytest.raises(TypeError, match="exp_avg_sq_scale must be"):
+        moe.AdamWTensors([x], [x], [small], [small], exp_avg_scales=[scale], exp_avg_sq_scales=[torch.ones(2)])
+
+
 def test_a_step_takes_adamw_tensors_only():
     """The rows of a list of gradients are shorter than those of a step."""
     import paper_2504_14960_amd as moe
