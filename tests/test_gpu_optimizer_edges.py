@@ -100,3 +100,17 @@ def test_a_step_takes_adamw_tensors_only():
     import torch
     with pytest.raises(TypeError, match="GradTensors"):
         moe.grad_norm([], torch.zeros(2), torch.zeros(8, dtype=torch.uint8))
+
+
+def test_streams_without_the_short_way(monkeypatch):
+    """torch's own short way to the stream's handle is not public: where it is missing, the public one is taken."""
+    import torch
+    from paper_2504_14960_amd import binding
+
+    class Stream:
+        cuda_stream = 1234
+
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: Stream())
+    assert binding._stream() == 1234
