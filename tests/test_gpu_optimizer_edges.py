@@ -57,6 +57,41 @@ def test_rates_that_fp32_does_not_hold_are_refused():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("kind,count", [(("f32", "f32", "f32"), 145), (("f32", "bf16", "f32"), 71), (("master", "bf16", "f32"), 125),
+                                        (("master", "f32", "f32"), 61), (("bf16", "bf16", "f32"), 150), (("bf16", "f32", "f32"), 141),
+                                        (("f32", "f32", "8bit"), 110), (("master", "bf16", "8bit"), 95), (("bf16", "bf16", "8bit"), 107)],
+                         ids=lambda x: "-".join(x) if isinstance(x, tuple) else str(x))
+def test_one_kind_of_tensors_in_several_launches(kind, count):
+    """Lists of one kind past what a launch holds (70 tensors of fp32 states without masters, 60 with, 52 and 46 of 8-bit ones):
+    the limits on tensors and on words, a place in the list that goes on behind a launch."""
+    rng = np.random.default_rng(count)
+    sizes = [int(n) for n in rng.integers(0, 2500, count)]
+    t = Tensors(sizes, [kind] * count, seed=count)
+    t.step(3, 99)
+    t.check(3, 99)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtypes", [["f32"], ["bf16"], ["bf16", "f32", "f32"]], ids="-".join)
+def test_norm_of_lists_of_more_runs_than_workgroups(dtypes):
+    """A workgroup goes from one tensor to the next, over several of one run, over some of none, and over types."""
+    import torch
+    import paper_2504_14960_amd as moe
+    rng = np.random.default_rng(len(dtypes))
+    sizes = [300_001, 0, 1, 5000, 0, 0, 900_000, 31, 4096, 8192, 1_200_003] * 7 + [2_000_000]
+    kinds = [dtypes[i % len(dtypes)] for i in range(len(sizes))]
+    runs = sum(-(-n * (2 if k == "bf16" else 4) // 16384) for n, k in zip(sizes, kinds))
+    assert runs > 1024
+    # every tensor adds about as much as the others: one left out, taken twice or read as the other type would show
+    g = [(rng.standard_normal(n) * (2000.0 / max(n, 1)) ** 0.5).astype(np.float32) for n in sizes]
+    g = [_bf16(x) if k == "bf16" else x for x, k in zip(g, kinds)]
+    out = torch.zeros(2, device="cuda")
+    ws = torch.full((moe.grad_norm_workspace_bytes(len(sizes)),), 0xff, dtype=torch.uint8, device="cuda")
+    moe.grad_norm(moe.GradTensors([_dev(x, k == "bf16") for x, k in zip(g, kinds)]), out, ws, max_norm=1.0)
+    np.testing.assert_allclose(out.cpu().numpy(), o.grad_norm(g, 1.0), rtol=4 * EPS)
+
+
+@pytest.mark.gpu
 def test_states_in_the_types_they_are_read_as():
     """float8_e4m3fn states and float8_e8m0fnu scales are the same bytes as uint8 ones."""
     import torch
