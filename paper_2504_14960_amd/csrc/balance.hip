@@ -43,10 +43,12 @@ struct Cut {
             chunks = T / chunk_tokens + n_seq;
             threads = 256;
         } else {
-            // up to 256 chunks, one to a compute unit; a small call is one (us, one chunk / many: 512 x 64 and 4096 x 8 logits
-            // 8.1 / 10.4 and 9.0 / 9.7, twice as many tokens 12.2 / 10.3 and 14.8 / 10.3)
+            // up to 256 chunks, one to a compute unit; a small call, of few logits and of few tokens, is one (us, one chunk / many:
+            // 512 x 64 and 4096 x 8 logits 7.4 / 11.0 and 7.5 / 11.0, twice as many tokens 12.2 / 10.3 and 14.8 / 10.3; 8192 x 1, x 2
+            // and x 4 11.0 / 10.9, 11.3 / 10.8 and 8.7 / 10.9, 16384 x 1 and x 2 19.0 / 10.9 and 19.6 / 10.9)
             const int c = (T + 255) / 256;
-            chunk_tokens = (long long)T * E <= 32768 ? (T > 0 ? T : 1) : c < 64 ? 64 : (c + 15) & ~15;
+            const bool small = T <= 8192 && T * E <= 32768;
+            chunk_tokens = small ? (T > 0 ? T : 1) : c < 64 ? 64 : (c + 15) & ~15;
             chunks = T > 0 ? (T + chunk_tokens - 1) / chunk_tokens : 1;
             threads = 1024;
         }

@@ -164,3 +164,15 @@ def test_gradient_of_more_tokens_than_one_row_of_a_grid():
         assert bool((out[a:min(a + (1 << 22), T - tail)] == row).all()), a
     del logits, out
     torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,E,K", [(8192, 1, 1), (8193, 1, 1), (8192, 2, 2), (8193, 2, 2), (16384, 2, 2), (10922, 3, 2), (8192, 4, 4), (8193, 4, 1)])
+def test_few_experts_around_the_line_between_one_chunk_and_many(T, E, K):
+    logits, idx, _, _ = _inputs(T, E, K)
+    counts, sums, n, losses = _forward(logits, idx, None, None)
+    want = o.balance_loss(logits, idx, np.float32(0.01), np.float32(0.001))
+    np.testing.assert_array_equal(counts.cpu().numpy(), want[0])
+    np.testing.assert_array_equal(n.cpu().numpy(), want[2])
+    np.testing.assert_allclose(sums.cpu().numpy(), want[1], rtol=340 * EPS, atol=1e-30)
+    np.testing.assert_allclose(losses.cpu().numpy(), want[3], rtol=400 * EPS, atol=1e-30)
