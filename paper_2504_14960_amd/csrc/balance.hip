@@ -11,12 +11,12 @@
 // four to a lane in as many lanes as its experts need (a power of two, LPT), so that 64 / LPT tokens share a wave, a lane
 // always has the same experts and keeps its sums of probabilities in registers; four batches of tokens are in flight.  What a
 // token needs from all its lanes (largest logit, sum of exponentials, the gradient's dot product) is reduced for four tokens
-// at once, which leaves 57 instructions a token of 256 experts; token by token it took 99, and the vector units, 73 % busy,
-// set the pace.
+// at once, which leaves 57 instructions a token of 256 experts (101 in the backward); token by token it took 99 (131), and the
+// vector units set the pace.
 //
 // Measured (fp32 logits, streamed past the caches: 10 % faster than through them): forward of 262144 tokens x 256 experts
-// 46 us in the first launch (6.1 TB/s) and 6.6 in the second, of 32768 x 64 6.3 and 4.6, of 256 x 8 3.8 in the only one;
-// gradient of 262144 x 256 86 us (6.2 TB/s), of 7777 x 60 in 23 sequences 4.9.
+// 46 us in the first launch (6.0 TB/s) and 6.7 in the second, of 32768 x 64 6.3 and 4.6, of 256 x 8 4.0 in the only one;
+// gradient of 262144 x 256 87 us (6.2 TB/s), of 7777 x 60 in 23 sequences 5.1.
 #include <type_traits>
 
 #include "wave_sum.h"
@@ -135,16 +135,17 @@ __device__ __forceinline__ PerToken<LPT> reduce_sum(float (&a)[kBatches]) {
 }
 
 // The experts of a lane: four neighbours, read as one piece, where rows are whole 16-byte pieces (WHOLE); else every LPT-th, so
-// that neighbouring lanes read neighbouring values (262144 x 255 logits: gradient 184 us with four neighbours read one by one,
-// 113 as pieces at odd addresses).
+// that neighbouring lanes read neighbouring values (262144 x 255 logits, the same ones again: gradient 184 us with four neighbours
+// read one by one, 113 as pieces at odd addresses, 99 so).
 template <int LPT, bool WHOLE>
 __device__ __forceinline__ int expert_of(int q, int u) {
     return WHOLE ? 4 * q + u : q + u * LPT;
 }
 
 // A lane's four values of a token's row, -inf past its end.  Streamed past the caches, but for rows that are not whole pieces where
-// nothing is written beside them, whose ends share lines with the next row (us through / past the caches: forward of 262144 x 255
-// 53 / 55 and x 129 45 / 47, gradient 112 / 99 and 72 / 68).
+// nothing is written beside them, whose ends share lines with the next row (us through / past the caches, inputs in turn: forward of
+// 262144 x 33 17.1 / 18.5, x 65 25.8 / 26.4, x 129 47.5 / 46.2, x 255 58.8 / 56.8, 32768 x 63 11.0 / 11.9 and x 129 14.8 / 15.5;
+// gradient of 262144 x 129 74.1 / 73.1, x 255 114 / 114).
 template <int LPT, bool WHOLE, bool STREAM>
 __device__ __forceinline__ f32x4 load_row(const float* row, int q, int E) {
     f32x4 x = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};

@@ -191,6 +191,7 @@ struct AdamStep {
     const float* grad_scale;
 };
 
+// a mixing function published by C. Wellons, "Prospecting for Hash Functions" (2018)
 __device__ __forceinline__ uint32_t mix(uint32_t x) {
     x ^= x >> 16;
     x *= 0x7feb352du;
