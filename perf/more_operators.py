@@ -141,7 +141,12 @@ def prepare(case, seed):
         # loads of experts that are not balanced yet
         mean = torch.exp(torch.randn(case["E"], generator=gen, device="cuda")) * 64
         counts = torch.poisson(mean.expand(case["rows"], -1).contiguous(), generator=gen).to(torch.int32)
-        return dict(case=case, counts=counts, bias=torch.randn(case["E"], generator=gen, device="cuda") * 0.01)
+        st = dict(case=case, counts=counts, bias=torch.randn(case["E"], generator=gen, device="cuda") * 0.01)
+        if own:
+            import paper_2504_14960_amd as moe
+            st["ws"] = torch.empty(moe.router_bias_update_workspace_bytes(case["rows"], case["E"]), dtype=torch.uint8,
+                                   device="cuda")
+        return st
     if case["kind"] == "weights":
         return _prepare_weights(case, gen)
     return _prepare_ffn(case, gen)
@@ -281,7 +286,7 @@ def _run_route_backward(st):
 def _run_bias_update(st):
     if own:
         import paper_2504_14960_amd as moe
-        moe.router_bias_update(st["counts"], RATE, st["bias"])
+        moe.router_bias_update(st["counts"], RATE, st["bias"], st["ws"])
     else:
         n = st["counts"].sum(0)
         st["bias"] += RATE * torch.sign(n.sum() - n * len(n)).float()
