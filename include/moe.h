@@ -384,6 +384,76 @@ moe_status_t moe_balance_loss_backward(const float* logits, const uint8_t* token
                                        moe_stream_t stream);
 
 /*
+ * Routing by scores: a1 for layers whose experts are chosen by a score plus a balancing
+ * bias, within the best groups of experts (the paper leaves its routers at softmax and
+ * top-K; this is the form of layers that balance without an auxiliary loss and keep a
+ * token's experts on few nodes).
+ *
+ *   s[t,e]   = softmax(logits[t,:])[e] or 1 / (1 + exp(-logits[t,e])), rounded to fp32
+ *              once (from 64 bits: what is selected does not depend on an implementation)
+ *   key[t,e] = s[t,e] + select_bias[e]                                        (fp32)
+ *   groups of E / n_groups neighbouring experts; a group's value is the sum (fp32) of its
+ *   group_best (1 or 2) largest keys; the topk_groups groups of the largest values stay
+ *   topk_idx[t,:] = the K largest keys of their experts, in descending order
+ *   topk_gate[t,k] = gate_scale * the score of topk_idx[t,k] before that rounding, divided
+ *              by the sum of the token's selected ones when renormalize != 0 (0 where that
+ *              sum is 0)
+ *
+ * Of equal keys and of equal groups the lower index comes first.  The bias chooses and has
+ * no part in the gates.  An expert whose logit is -inf or NaN, or whose key is, is not
+ * selected (nor counted in the softmax, where its logit is); slots for which no expert is
+ * left get topk_idx = -1 (a dropped assignment everywhere in this library) and gate 0.
+ *
+ * x, w_router, logit_bias, logits, T, H, E, K, dt, limits and errors as moe_router_topk
+ * (x == NULL: logits is the input).  select_bias [E] fp32 or NULL; 1 <= n_groups divides E,
+ * 1 <= topk_groups <= n_groups, K <= topk_groups * (E / n_groups), gate_scale finite.
+ */
+typedef enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 } moe_score_t;
+
+moe_status_t moe_router_select(const void* x, const void* w_router, const float* logit_bias,
+                               float* logits, const float* select_bias, int T, int H, int E, int K,
+                               moe_score_t score, int n_groups, int topk_groups, int group_best,
+                               int renormalize, float gate_scale, moe_dtype_t dt, int32_t* topk_idx,
+                               float* topk_gate, moe_stream_t stream);
+
+/*
+ * Its backward.  The selection has no gradient.  With r_k = s[idx_k] (renormalize == 0) or
+ * s[idx_k] / sum_j s[idx_j], d_k = gate_scale dgate[t,k] and c_k = r_k d_k or
+ * r_k (d_k - sum_j d_j r_j):
+ *
+ *   dlogits[t,e] = [e == idx_k] c_k - s_e sum_j c_j          softmax
+ *                = [e == idx_k] c_k (1 - s[idx_k])           sigmoid     (+ dlogits_addend[t,e])
+ *
+ * then dx, dw_router and dbias as in moe_router_backward_addend, with its arguments, limits,
+ * workspace and errors.  x and w_router may be NULL where dw_router and dx are not asked
+ * for.  Slots outside [0,E) and experts whose logit is -inf or NaN get no gradient, and
+ * what dgate holds there is not looked at; nor do tokens whose selected scores are all 0 in
+ * fp32.
+ */
+moe_status_t moe_router_select_backward(const void* x, const void* w_router, const float* logits,
+                                        const int32_t* topk_idx, const float* dgate,
+                                        const float* dlogits_addend, int T, int H, int E, int K,
+                                        moe_score_t score, int renormalize, float gate_scale,
+                                        moe_dtype_t dt, float* dlogits, void* dx, float* dw_router,
+                                        float* dbias, void* workspace, size_t workspace_bytes,
+                                        moe_stream_t stream);
+
+/*
+ * One step of the balancing bias: experts with less than the mean load are pulled up by
+ * `rate`, those with more are pushed down.  With n_e = sum_r counts[r,e]:
+ *
+ *   select_bias[e] += rate * sign(sum_j n_j / E - n_e)        (compared in whole numbers)
+ *
+ * counts [n_rows,E] int32, e.g. moe_balance_loss's (a row a sequence, before any capacity),
+ * or their sums over a data-parallel group; n_rows <= 2^20 (0: nothing happens), rate finite.
+ * workspace: moe_router_bias_update_workspace_bytes(n_rows, E), 0 for few rows.
+ */
+size_t moe_router_bias_update_workspace_bytes(int n_rows, int E);
+moe_status_t moe_router_bias_update(const int32_t* counts, int n_rows, int E, float rate,
+                                    float* select_bias, void* workspace, size_t workspace_bytes,
+                                    moe_stream_t stream);
+
+/*
  * Backward of a3, the grouped SwiGLU expert FFN (bf16 only; Section 3.3: the
  * backward workflow mirrors the forward; f_e of Eq. 1 by the chain rule).  With
  * g = x_perm W_gate^T, u = x_perm W_up^T, s = 1/(1+e^-g), h = g s u, for every

@@ -16,6 +16,8 @@ import torch
 
 MOE_F32 = 0
 MOE_BF16 = 1
+MOE_SCORE_SOFTMAX = 0
+MOE_SCORE_SIGMOID = 1
 MOE_STATE_F32 = 0
 MOE_STATE_MXFP8 = 1
 
@@ -132,6 +134,14 @@ def lib() -> C.CDLL:
     L.moe_router_backward_addend.argtypes = [vp] * 6 + [i] * 6 + [vp] * 5 + [sz, vp]
     L.moe_layer_backward_addend.restype = i
     L.moe_layer_backward_addend.argtypes = [vp] * 8 + [i] * 7 + [vp] * 9 + [sz, vp]
+    L.moe_router_select.restype = i
+    L.moe_router_select.argtypes = [vp] * 5 + [i] * 9 + [C.c_float, i] + [vp] * 3
+    L.moe_router_select_backward.restype = i
+    L.moe_router_select_backward.argtypes = [vp] * 6 + [i] * 6 + [C.c_float, i] + [vp] * 5 + [sz, vp]
+    L.moe_router_bias_update_workspace_bytes.restype = sz
+    L.moe_router_bias_update_workspace_bytes.argtypes = [i] * 2
+    L.moe_router_bias_update.restype = i
+    L.moe_router_bias_update.argtypes = [vp, i, i, C.c_float, vp, vp, sz, vp]
     L.moe_balance_loss_workspace_bytes.restype = sz
     L.moe_balance_loss_workspace_bytes.argtypes = [i] * 3
     L.moe_balance_loss.restype = i
@@ -380,6 +390,70 @@ def _expect(name: str, t: torch.Tensor, dtype, numel: int):
         return t.data_ptr()
     _is(name, t, (dtype,), numel)
     return _ptr(t)
+
+
+def _optional(name: str, t: Optional[torch.Tensor], dtype, numel: int):
+    return None if t is None else _expect(name, t, dtype, numel)
+
+
+# ---- routing by scores ----
+def router_select(x: Optional[torch.Tensor], w_router: Optional[torch.Tensor], logit_bias: Optional[torch.Tensor],
+                  logits: torch.Tensor, K: int, topk_idx: torch.Tensor, topk_gate: torch.Tensor, score: int = MOE_SCORE_SIGMOID,
+                  select_bias: Optional[torch.Tensor] = None, n_groups: int = 1, topk_groups: int = 1, group_best: int = 2,
+                  renormalize: bool = True, gate_scale: float = 1.0, dtype: Optional[int] = None) -> None:
+    """topk_idx, topk_gate [T, K] from the scores of logits [T, E] (x given: computed first).  select_bias [E] chooses along
+    and has no part in the gates; the experts come from the topk_groups best of n_groups groups.  -1: no expert was left."""
+    T, E = logits.shape
+    H = 0
+    dt = MOE_BF16 if dtype is None else dtype
+    if x is not None:
+        H, dt = x.shape[1], _dt(x)
+        _is("x", x, (x.dtype,), T * H)
+        _is("w_router", w_router, (x.dtype,), E * H)
+    f32 = torch.float32
+    _check(lib().moe_router_select(
+        _ptr(x), _ptr(w_router), _optional("logit_bias", logit_bias, f32, E), _expect("logits", logits, f32, T * E),
+        _optional("select_bias", select_bias, f32, E), T, H, E, K, score, n_groups, topk_groups, group_best, int(bool(renormalize)),
+        gate_scale, dt, _expect("topk_idx", topk_idx, torch.int32, T * K), _expect("topk_gate", topk_gate, f32, T * K), _stream()))
+
+
+def router_select_backward(x: Optional[torch.Tensor], w_router: Optional[torch.Tensor], logits: torch.Tensor,
+                           topk_idx: torch.Tensor, dgate: torch.Tensor, dlogits: torch.Tensor, dx: Optional[torch.Tensor],
+                           dw_router: Optional[torch.Tensor], dbias: Optional[torch.Tensor], workspace: Optional[torch.Tensor],
+                           score: int = MOE_SCORE_SIGMOID, renormalize: bool = True, gate_scale: float = 1.0,
+                           dlogits_addend: Optional[torch.Tensor] = None) -> None:
+    """dlogits [T, E] = gradient of dgate . topk_gate in the logits (+ dlogits_addend), and what follows from it: dx [T, H],
+    dw_router [E, H] and dbias [E] where they are given (dx takes w_router, dw_router takes x and a workspace of
+    router_backward_workspace_bytes)."""
+    T, E = logits.shape
+    K = topk_idx.shape[1]
+    f32 = torch.float32
+    ref = dx if dx is not None else x
+    H, dt = (0, MOE_BF16) if ref is None else (ref.shape[1], _dt(ref))
+    for name, t, numel in (("x", x, T * H), ("w_router", w_router, E * H), ("dx", dx, T * H)):
+        if t is not None and ref is not None:
+            _is(name, t, (ref.dtype,), numel)
+    _check(lib().moe_router_select_backward(
+        _ptr(x), _ptr(w_router), _expect("logits", logits, f32, T * E), _expect("topk_idx", topk_idx, torch.int32, T * K),
+        _expect("dgate", dgate, f32, T * K), _optional("dlogits_addend", dlogits_addend, f32, T * E), T, H, E, K, score,
+        int(bool(renormalize)), gate_scale, dt, _expect("dlogits", dlogits, f32, T * E), _ptr(dx),
+        _optional("dw_router", dw_router, f32, E * H), _optional("dbias", dbias, f32, E), _ptr(workspace),
+        0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
+
+
+def router_bias_update_workspace_bytes(n_rows: int, E: int) -> int:
+    return int(lib().moe_router_bias_update_workspace_bytes(n_rows, E))
+
+
+def router_bias_update(counts: torch.Tensor, rate: float, select_bias: torch.Tensor,
+                       workspace: Optional[torch.Tensor] = None) -> None:
+    """One step of router_select's bias [E]: rate up for experts below the mean load, down above.  counts [n_rows, E] int32 (or
+    [E]), e.g. balance_loss's."""
+    E = select_bias.numel()
+    rows = counts.numel() // E if E else 0
+    _check(lib().moe_router_bias_update(
+        _expect("counts", counts, torch.int32, rows * E), rows, E, rate, _expect("select_bias", select_bias, torch.float32, E),
+        _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
 
 
 def _mask(token_mask: Optional[torch.Tensor], T: int):

@@ -412,19 +412,14 @@ size_t moe_router_backward_workspace_bytes(int T, int H, int E) {
     return router_backward_workspace_bytes(T, H, E);
 }
 
-static moe_status_t router_backward(const char* fn, const void* x, const void* w_router, const float* logits,
-                                    const int32_t* topk_idx, const float* dgate, const float* dlogits_addend, int T, int H,
-                                    int E, int K, int renormalize, moe_dtype_t dt, float* dlogits, void* dx,
-                                    float* dw_router, float* dbias, void* workspace, size_t workspace_bytes,
-                                    moe_stream_t stream) {
+static moe_status_t check_router_backward(const char* fn, const void* x, const void* w_router, const float* logits,
+                                          const int32_t* topk_idx, const float* dgate, const float* dlogits_addend, int T, int H,
+                                          int E, int K, moe_dtype_t dt, const float* dlogits, const void* dx,
+                                          const float* dw_router, const float* dbias, const void* workspace,
+                                          size_t workspace_bytes) {
     if (moe_status_t st = check_dims(fn, T, H, E, K, dt)) return st;
     if (H % 8) return fail(MOE_ERR_UNSUPPORTED, "%s: H=%d must be a multiple of 8", fn, H);
-    if (T == 0) {
-        // no tokens: the sums over tokens are zero
-        if (dw_router) launch_fill_i32(reinterpret_cast<int32_t*>(dw_router), E * H, 0, 0, static_cast<hipStream_t>(stream));
-        if (dbias) launch_fill_i32(reinterpret_cast<int32_t*>(dbias), E, 0, 0, static_cast<hipStream_t>(stream));
-        return check_launch(fn);
-    }
+    if (T == 0) return MOE_OK;
     REQUIRE_PTR(fn, logits);
     REQUIRE_PTR(fn, topk_idx);
     REQUIRE_PTR(fn, dgate);
@@ -445,6 +440,25 @@ static moe_status_t router_backward(const char* fn, const void* x, const void* w
         REQUIRE_PTR(fn, workspace);
     }
     if (dbias && (reinterpret_cast<uintptr_t>(dbias) & 3u)) return fail(MOE_ERR_INVALID_ARG, "%s: dbias is not 4-byte aligned", fn);
+    return MOE_OK;
+}
+
+// no tokens: the sums over tokens are zero
+static moe_status_t router_backward_no_tokens(const char* fn, int H, int E, float* dw_router, float* dbias, hipStream_t s) {
+    if (dw_router) launch_fill_i32(reinterpret_cast<int32_t*>(dw_router), E * H, 0, 0, s);
+    if (dbias) launch_fill_i32(reinterpret_cast<int32_t*>(dbias), E, 0, 0, s);
+    return check_launch(fn);
+}
+
+static moe_status_t router_backward(const char* fn, const void* x, const void* w_router, const float* logits,
+                                    const int32_t* topk_idx, const float* dgate, const float* dlogits_addend, int T, int H,
+                                    int E, int K, int renormalize, moe_dtype_t dt, float* dlogits, void* dx,
+                                    float* dw_router, float* dbias, void* workspace, size_t workspace_bytes,
+                                    moe_stream_t stream) {
+    if (moe_status_t st = check_router_backward(fn, x, w_router, logits, topk_idx, dgate, dlogits_addend, T, H, E, K, dt, dlogits, dx,
+                                                dw_router, dbias, workspace, workspace_bytes))
+        return st;
+    if (T == 0) return router_backward_no_tokens(fn, H, E, dw_router, dbias, static_cast<hipStream_t>(stream));
     launch_router_backward(x, w_router, logits, topk_idx, dgate, dlogits_addend, T, H, E, K, renormalize != 0, dt, dlogits, dx,
                            dw_router, dbias, workspace, static_cast<hipStream_t>(stream));
     return check_launch(fn);
@@ -467,6 +481,87 @@ moe_status_t moe_router_backward_addend(const void* x, const void* w_router, con
                                         size_t workspace_bytes, moe_stream_t stream) {
     return router_backward("moe_router_backward_addend", x, w_router, logits, topk_idx, dgate, dlogits_addend, T, H, E, K,
                            renormalize, dt, dlogits, dx, dw_router, dbias, workspace, workspace_bytes, stream);
+}
+
+static moe_status_t check_score(const char* fn, moe_score_t score, float gate_scale) {
+    if (score != MOE_SCORE_SOFTMAX && score != MOE_SCORE_SIGMOID)
+        return fail(MOE_ERR_INVALID_ARG, "%s: unknown score %d", fn, (int)score);
+    if (!std::isfinite(gate_scale)) return fail(MOE_ERR_INVALID_ARG, "%s: gate_scale must be finite", fn);
+    return MOE_OK;
+}
+
+moe_status_t moe_router_select(const void* x, const void* w_router, const float* logit_bias,
+                               float* logits, const float* select_bias, int T, int H, int E, int K,
+                               moe_score_t score, int n_groups, int topk_groups, int group_best,
+                               int renormalize, float gate_scale, moe_dtype_t dt, int32_t* topk_idx,
+                               float* topk_gate, moe_stream_t stream) {
+    static const char* fn = "moe_router_select";
+    if (x == nullptr) H = (dt == MOE_BF16) ? 8 : 4;  // ignored, keep the shape check quiet
+    if (moe_status_t st = check_dims(fn, T, H, E, K, dt)) return st;
+    if (moe_status_t st = check_score(fn, score, gate_scale)) return st;
+    if (n_groups < 1 || n_groups > E || E % n_groups != 0)
+        return fail(MOE_ERR_INVALID_ARG, "%s: n_groups=%d must divide E=%d", fn, n_groups, E);
+    if (topk_groups < 1 || topk_groups > n_groups)
+        return fail(MOE_ERR_INVALID_ARG, "%s: need 1 <= topk_groups <= n_groups (topk_groups=%d n_groups=%d)", fn, topk_groups, n_groups);
+    if (group_best != 1 && group_best != 2) return fail(MOE_ERR_INVALID_ARG, "%s: group_best=%d must be 1 or 2", fn, group_best);
+    if (K > topk_groups * (E / n_groups))
+        return fail(MOE_ERR_INVALID_ARG, "%s: K=%d exceeds the %d experts of %d groups", fn, K, topk_groups * (E / n_groups), topk_groups);
+    if (T == 0) return MOE_OK;
+    if (moe_status_t st = check_router_pointers(fn, x, w_router, logit_bias, logits, topk_idx, topk_gate)) return st;
+    if (select_bias && (reinterpret_cast<uintptr_t>(select_bias) & 3u))
+        return fail(MOE_ERR_INVALID_ARG, "%s: select_bias is not 4-byte aligned", fn);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (x) launch_router(x, w_router, logit_bias, logits, T, H, E, 0, 0, dt, topk_idx, topk_gate, s);
+    launch_select(logits, select_bias, T, E, K, score, n_groups, topk_groups, group_best, renormalize != 0, gate_scale, topk_idx,
+                  topk_gate, s);
+    return check_launch(fn);
+}
+
+moe_status_t moe_router_select_backward(const void* x, const void* w_router, const float* logits,
+                                        const int32_t* topk_idx, const float* dgate,
+                                        const float* dlogits_addend, int T, int H, int E, int K,
+                                        moe_score_t score, int renormalize, float gate_scale,
+                                        moe_dtype_t dt, float* dlogits, void* dx, float* dw_router,
+                                        float* dbias, void* workspace, size_t workspace_bytes,
+                                        moe_stream_t stream) {
+    static const char* fn = "moe_router_select_backward";
+    if (!dx && !dw_router) H = 8;  // ignored, keep the shape check quiet
+    if (moe_status_t st = check_score(fn, score, gate_scale)) return st;
+    if (moe_status_t st = check_router_backward(fn, x, w_router, logits, topk_idx, dgate, dlogits_addend, T, H, E, K, dt, dlogits, dx,
+                                                dw_router, dbias, workspace, workspace_bytes))
+        return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (T == 0) return router_backward_no_tokens(fn, H, E, dw_router, dbias, s);
+    launch_select_dlogits(logits, topk_idx, dgate, dlogits_addend, T, E, K, score, renormalize != 0, gate_scale, dlogits, s);
+    launch_router_products(x, w_router, T, H, E, dt, dlogits, dx, dw_router, dbias, workspace, s);
+    return check_launch(fn);
+}
+
+size_t moe_router_bias_update_workspace_bytes(int n_rows, int E) {
+    if (n_rows < 0 || n_rows > kMaxCountRows || E <= 0 || E > kMaxExperts) return 0;
+    return bias_update_workspace_bytes(n_rows, E);
+}
+
+moe_status_t moe_router_bias_update(const int32_t* counts, int n_rows, int E, float rate,
+                                    float* select_bias, void* workspace, size_t workspace_bytes,
+                                    moe_stream_t stream) {
+    static const char* fn = "moe_router_bias_update";
+    if (n_rows < 0 || E <= 0) return fail(MOE_ERR_INVALID_ARG, "%s: need n_rows >= 0 and E > 0 (n_rows=%d E=%d)", fn, n_rows, E);
+    if (E > kMaxExperts) return fail(MOE_ERR_UNSUPPORTED, "%s: E=%d exceeds the limit %d", fn, E, kMaxExperts);
+    if (n_rows > kMaxCountRows) return fail(MOE_ERR_UNSUPPORTED, "%s: n_rows=%d exceeds the limit 2^20", fn, n_rows);
+    if (!std::isfinite(rate)) return fail(MOE_ERR_INVALID_ARG, "%s: rate must be finite", fn);
+    if (n_rows == 0) return MOE_OK;
+    REQUIRE_PTR(fn, counts);
+    if (select_bias == nullptr) return fail(MOE_ERR_INVALID_ARG, "%s: select_bias is NULL", fn);
+    if (reinterpret_cast<uintptr_t>(select_bias) & 3u) return fail(MOE_ERR_INVALID_ARG, "%s: select_bias is not 4-byte aligned", fn);
+    if (const size_t need = bias_update_workspace_bytes(n_rows, E)) {
+        if (workspace == nullptr || workspace_bytes < need)
+            return fail(MOE_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need,
+                        workspace ? workspace_bytes : (size_t)0);
+        REQUIRE_PTR(fn, workspace);
+    }
+    launch_bias_update(counts, n_rows, E, rate, select_bias, workspace, static_cast<hipStream_t>(stream));
+    return check_launch(fn);
 }
 
 static moe_status_t check_balance(const char* fn, int T, int E, int K, int n_seq, const int32_t* seq_offsets,

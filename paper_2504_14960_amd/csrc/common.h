@@ -30,6 +30,7 @@ constexpr int kMaxExperts = 256;
 constexpr int kMaxTopK = 64;
 constexpr int kMaxBalanceTokens = 1 << 30;         // of one balance-loss call
 constexpr int kMaxSequences = 65536;               // of one balance-loss call
+constexpr int kMaxCountRows = 1 << 20;             // of one bias update
 constexpr int kMaxListTensors = 1 << 26;           // of one gradient-norm or AdamW call
 constexpr int64_t kMaxListElements = 1ll << 33;    // of one tensor of a gradient-norm or AdamW call
 
@@ -65,6 +66,7 @@ moe_status_t fail(moe_status_t st, const char* fmt, ...);
 moe_status_t check_launch(const char* what);
 
 // ---- kernel launchers (one per source file); all enqueue on `s` and return ----
+// K = 0: the logits alone (idx and gate are not written)
 void launch_router(const void* x, const void* w, const float* bias, float* logits, int T, int H,
                    int E, int K, int renorm, moe_dtype_t dt, int32_t* idx, float* gate,
                    hipStream_t s);
@@ -99,6 +101,18 @@ inline AdamRates adam_rates(const moe_adamw_tensor_t& t, double lr, double bc1) 
 }
 void launch_adamw(const moe_adamw_tensor_t* tensors, int count, double lr, double beta1, double beta2, double eps,
                   int64_t step, uint32_t seed, const float* grad_scale, hipStream_t s);
+
+// what follows dlogits [T,E]: dx, dw, dbias where non-NULL
+void launch_router_products(const void* x, const void* w, int T, int H, int E, moe_dtype_t dt, const float* dlogits, void* dx,
+                            float* dw, float* dbias, void* ws, hipStream_t s);
+
+// routing by scores: selection from logits, the gradient of its gates in them, the step of the balancing bias
+void launch_select(const float* logits, const float* bias, int T, int E, int K, moe_score_t score, int groups, int topk_groups,
+                   int group_best, int renorm, float scale, int32_t* idx, float* gate, hipStream_t s);
+void launch_select_dlogits(const float* logits, const int32_t* idx, const float* dgate, const float* addend, int T, int E, int K,
+                           moe_score_t score, int renorm, float scale, float* dlogits, hipStream_t s);
+size_t bias_update_workspace_bytes(int n_rows, int E);
+void launch_bias_update(const int32_t* counts, int n_rows, int E, float rate, float* bias, void* ws, hipStream_t s);
 
 // router: 16-token blocks per workgroup (1, 2 or 4); 0 = chosen from T and E
 void set_router_tile(int mb);

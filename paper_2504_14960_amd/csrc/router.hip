@@ -239,9 +239,10 @@ __device__ __forceinline__ void select_lanes_for(const float* rows, int ld, int 
     }
 }
 
-// K <= 8: register lists; larger K: one lane group per token.
+// K <= 8: register lists; larger K: one lane group per token; K = 0: logits alone are asked for.
 __device__ __forceinline__ void select_tokens(const float* rows, int ld, int ntok, int t0, int T, int E,
                                               int K, int renorm, int32_t* topk_idx, float* topk_gate) {
+    if (K == 0) return;
     if (K <= 2)
         select_lanes_for<2>(rows, ld, ntok, t0, T, E, K, renorm, topk_idx, topk_gate);
     else if (K <= 4)
@@ -924,6 +925,7 @@ constexpr int kRankMaxTokens = 4096;
 
 // selection from logits alone
 static void launch_topk(const float* logits, int T, int E, int K, int renorm, int32_t* idx, float* gate, hipStream_t s) {
+    if (K == 0) return;
     if (E <= 128 && T <= kRankMaxTokens) {
         const dim3 grid((T + 3) / 4);
         if (E <= 64) hipLaunchKernelGGL((topk_rank_kernel<1>), grid, dim3(256), 0, s, logits, T, E, K, renorm, idx, gate);

@@ -431,6 +431,11 @@ void launch_router_backward(const void* x, const void* w, const float* logits, c
     else
         hipLaunchKernelGGL(router_dlogits_wave_kernel<4>, dim3((T + 3) / 4), dim3(256), 0, s, logits, idx, dgate, addend, T, E, K,
                            renorm, dlogits);
+    launch_router_products(x, w, T, H, E, dt, dlogits, dx, dw, dbias, ws, s);
+}
+
+void launch_router_products(const void* x, const void* w, int T, int H, int E, moe_dtype_t dt, const float* dlogits, void* dx,
+                            float* dw, float* dbias, void* ws, hipStream_t s) {
     const bool bf16 = dt == MOE_BF16;
     if (dx) {
         const dim3 grid((H + 4 * RB_WCOLS - 1) / (4 * RB_WCOLS), (T + DX_TOK - 1) / DX_TOK);
