@@ -745,6 +745,115 @@ moe_status_t moe_expert_down_fp8(const void* h_fp8, const int32_t* expert_offset
                                  void* y_perm_bf16, moe_stream_t stream);
 
 /*
+ * E4M3 with a scale for every block of 128: the second FP8 recipe of the expert FFN,
+ * which needs no history of maxima and gives a block its own range.
+ *
+ * A scale is a power of two held as E8M0 (a byte b stands for 2^(b-127), 255 for NaN):
+ * the smallest, from 2^-126, that leaves a block's magnitudes at most 448.  Codes are the
+ * nearest E4M3 values of x / scale, ties to even.  A block with a value that is not finite
+ * gets scale 255 and codes 0x7f.  Activations have a scale for every 128 values of a row,
+ * weights one for every 128 x 128.  The powers of two are what the matrix instruction of
+ * this GPU multiplies in by itself, and they make the value of a code and its scale a
+ * bf16 value (four significant bits): weight gradients are formed from just those.
+ *
+ * Scales of rows of C values lie in rows of moe_fp8_block_scale_stride(C) bytes: C / 128,
+ * rounded up to a multiple of 4.  The bytes behind a row's last scale are neither written
+ * nor made use of.
+ */
+int moe_fp8_block_scale_stride(int C);
+
+/* src [rows,C] (dt fp32 or bf16) -> codes [rows,C] and scales [rows, stride(C)], a scale
+ * for every 128 values of a row.  C a multiple of 128.  src and codes 16-byte, scales
+ * 4-byte aligned. */
+moe_status_t moe_fp8_block_quantize(const void* src, moe_dtype_t dt, int rows, int C, void* codes,
+                                    uint8_t* scales, moe_stream_t stream);
+
+/*
+ * A layer's weights (dt fp32, e.g. masters, or bf16), a scale for every 128 x 128 of them,
+ * in the layouts of the forward and of the backward (in which codes and scales are the same
+ * ones, transposed):
+ *
+ *   gate_codes, up_codes [E,F,H]   gate_scales, up_scales [E, F/128, stride(H)]
+ *   down_codes [E,H,F]             down_scales            [E, H/128, stride(F)]
+ *   wgu_t_codes [E,H,2F] = (gate^T | up^T)   wgu_t_scales [E, H/128, stride(2F)]
+ *   wd_t_codes [E,F,H] = down^T              wd_t_scales  [E, F/128, stride(H)]
+ *
+ * The three of the forward, or the two of the backward, may be NULL with their scales.  H
+ * and F multiples of 128, E <= 256.  Valid until the weights change.
+ */
+moe_status_t moe_expert_weights_fp8_block(const void* w_gate, const void* w_up, const void* w_down,
+                                          moe_dtype_t dt, int H, int F, int E, void* gate_codes,
+                                          uint8_t* gate_scales, void* up_codes, uint8_t* up_scales,
+                                          void* down_codes, uint8_t* down_scales, void* wgu_t_codes,
+                                          uint8_t* wgu_t_scales, void* wd_t_codes,
+                                          uint8_t* wd_t_scales, moe_stream_t stream);
+
+/*
+ * a2 fused with the quantisation of its output: as moe_permute on a bf16 x, but x_perm is
+ * written as codes x_codes [R_max,H] and x_scales [R_max, stride(H)].  All other arguments,
+ * outputs, limits and errors as moe_permute; H a multiple of 128.
+ */
+moe_status_t moe_permute_fp8_block(const void* x_bf16, const int32_t* topk_idx, int T, int H, int E,
+                                   int K, int capacity, void* x_codes, uint8_t* x_scales,
+                                   int32_t* expert_counts, int32_t* expert_offsets,
+                                   int32_t* row_of_assign, int32_t* assign_of_row, void* workspace,
+                                   size_t workspace_bytes, moe_stream_t stream);
+
+/*
+ * Grouped SwiGLU expert FFN on them.  With x, w as their codes and scales have them, for
+ * every expert over its rows:
+ *
+ *   g = x . w_gate^T    u = x . w_up^T    h = silu(g) * u     (fp32; rounded to codes once)
+ *   y_perm = h . w_down^T                                     (bf16)
+ *
+ * with fp32 accumulation.  (The matrix instruction adds the products of eight codes that
+ * are neighbours along the contraction with what lies 2^13 below the largest of them cut
+ * off, here as in the products above: sums of 128 random codes are some 2e-5 off.)
+ * h_codes [R_max,F], h_scales [R_max, stride(F)]: workspace and
+ * output.  gu [R_max,2F] = (g | u) in bf16 for the backward, or NULL.  H and F multiples of
+ * 128, E <= 256; otherwise MOE_ERR_UNSUPPORTED.  Rows in [R, R_max) are not touched.
+ * moe_expert_gate_up_fp8_block and moe_expert_down_fp8_block are the two halves.
+ */
+moe_status_t moe_grouped_gemm_swiglu_fp8_block(
+    const void* x_codes, const uint8_t* x_scales, const int32_t* expert_offsets, int R_max, int H,
+    int F, int E, const void* gate_codes, const uint8_t* gate_scales, const void* up_codes,
+    const uint8_t* up_scales, const void* down_codes, const uint8_t* down_scales, void* h_codes,
+    uint8_t* h_scales, void* gu, void* y_perm_bf16, moe_stream_t stream);
+moe_status_t moe_expert_gate_up_fp8_block(const void* x_codes, const uint8_t* x_scales,
+                                          const int32_t* expert_offsets, int R_max, int H, int F,
+                                          int E, const void* gate_codes, const uint8_t* gate_scales,
+                                          const void* up_codes, const uint8_t* up_scales,
+                                          void* h_codes, uint8_t* h_scales, void* gu,
+                                          moe_stream_t stream);
+moe_status_t moe_expert_down_fp8_block(const void* h_codes, const uint8_t* h_scales,
+                                       const int32_t* expert_offsets, int R_max, int H, int F, int E,
+                                       const void* down_codes, const uint8_t* down_scales,
+                                       void* y_perm_bf16, moe_stream_t stream);
+
+/*
+ * Its backward, with the forward's codes, scales and gu.  q(.) is the quantisation of rows
+ * above, wd_t and wgu_t are moe_expert_weights_fp8_block's; s = 1 / (1 + e^-g):
+ *
+ *   dh = q(dy_perm) . w_down     du = dh g s     dg = dh u s (1 + g (1 - s))
+ *   dx_perm = q(dg | du) . (w_gate | w_up)
+ *   dw_down = dy_perm^T h     dw_gate = dg^T x     dw_up = du^T x
+ *
+ * The products for dh and dx_perm are 8-bit products with fp32 accumulation.  The
+ * quantisations count as identities.  The weight gradients contract over rows, along which
+ * no operand has its blocks: they are bf16 products of dy_perm, of dg and du rounded to bf16
+ * once, and of the values that the codes of h and x stand for.  Shapes, outputs, limits and
+ * errors as moe_grouped_gemm_swiglu_backward; experts without rows get zeros.  workspace:
+ * moe_expert_backward_fp8_block_workspace_bytes.
+ */
+size_t moe_expert_backward_fp8_block_workspace_bytes(int R_max, int H, int F, int E);
+moe_status_t moe_grouped_gemm_swiglu_fp8_block_backward(
+    const void* x_codes, const uint8_t* x_scales, const void* h_codes, const uint8_t* h_scales,
+    const void* gu, const void* dy_perm, const int32_t* expert_offsets, int R_max, int H, int F,
+    int E, const void* wgu_t_codes, const uint8_t* wgu_t_scales, const void* wd_t_codes,
+    const uint8_t* wd_t_scales, void* dx_perm, void* dw_gate, void* dw_up, void* dw_down,
+    void* workspace, size_t workspace_bytes, moe_stream_t stream);
+
+/*
  * Measurement probe (not a stage of the layer; for callers that cannot measure
  * the chip's sustained matrix rate otherwise, e.g. bench.py's roofline note).
  * Runs the bare inner loop of the bf16 grouped GEMM: `workgroups` workgroups of

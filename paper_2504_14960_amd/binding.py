@@ -169,6 +169,24 @@ def lib() -> C.CDLL:
     L.moe_expert_gate_up_fp8.argtypes = [vp, vp, i, i, i, i, vp, vp, f, f, f, vp, vp, vp]
     L.moe_expert_down_fp8.restype = i
     L.moe_expert_down_fp8.argtypes = [vp, vp, i, i, i, i, vp, f, vp, vp]
+    L.moe_fp8_block_scale_stride.restype = i
+    L.moe_fp8_block_scale_stride.argtypes = [i]
+    L.moe_fp8_block_quantize.restype = i
+    L.moe_fp8_block_quantize.argtypes = [vp, i, i, i, vp, vp, vp]
+    L.moe_expert_weights_fp8_block.restype = i
+    L.moe_expert_weights_fp8_block.argtypes = [vp] * 3 + [i] * 4 + [vp] * 11
+    L.moe_permute_fp8_block.restype = i
+    L.moe_permute_fp8_block.argtypes = [vp, vp] + [i] * 5 + [vp] * 7 + [sz, vp]
+    L.moe_grouped_gemm_swiglu_fp8_block.restype = i
+    L.moe_grouped_gemm_swiglu_fp8_block.argtypes = [vp] * 3 + [i] * 4 + [vp] * 11
+    L.moe_expert_gate_up_fp8_block.restype = i
+    L.moe_expert_gate_up_fp8_block.argtypes = [vp] * 3 + [i] * 4 + [vp] * 8
+    L.moe_expert_down_fp8_block.restype = i
+    L.moe_expert_down_fp8_block.argtypes = [vp] * 3 + [i] * 4 + [vp] * 4
+    L.moe_expert_backward_fp8_block_workspace_bytes.restype = sz
+    L.moe_expert_backward_fp8_block_workspace_bytes.argtypes = [i] * 4
+    L.moe_grouped_gemm_swiglu_fp8_block_backward.restype = i
+    L.moe_grouped_gemm_swiglu_fp8_block_backward.argtypes = [vp] * 7 + [i] * 4 + [vp] * 9 + [sz, vp]
     _lib = L
     return L
 
@@ -351,6 +369,123 @@ def expert_down_fp8(h: torch.Tensor, expert_offsets: torch.Tensor, w_down: torch
     E, H, _ = w_down.shape
     _check(lib().moe_expert_down_fp8(_ptr(h), _ptr(expert_offsets), R_max, H, F, E, _ptr(w_down), float(dq_down),
                                      _ptr(y_perm), _stream()))
+
+
+# ---- E4M3 with a scale for every block of 128: codes as torch.uint8 or float8_e4m3fn, E8M0 scales as torch.uint8 or
+# float8_e8m0fnu, in rows of fp8_block_scale_stride bytes ----
+_CODES, _SCALES = (torch.uint8, torch.float8_e4m3fn), (torch.uint8, torch.float8_e8m0fnu)
+
+
+def _blocks(name: str, codes: torch.Tensor, scales: torch.Tensor, shape, scale_rows: int):
+    """The device pointers of codes of this shape and of their scales."""
+    if tuple(codes.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(codes.shape)}")
+    _is(name, codes, _CODES, codes.numel())
+    _is(name + "_scales", scales, _SCALES, scale_rows * fp8_block_scale_stride(shape[-1]))
+    return _ptr(codes), _ptr(scales)
+
+
+def _bf16(name: str, t: torch.Tensor, numel: int):
+    return _expect(name, t, torch.bfloat16, numel)
+
+
+def fp8_block_scale_stride(C: int) -> int:
+    return int(lib().moe_fp8_block_scale_stride(C))
+
+
+def fp8_block_quantize(src: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor) -> None:
+    """src [rows, C] (fp32 or bf16) to codes [rows, C] and scales [rows, fp8_block_scale_stride(C)]."""
+    rows, C = src.shape
+    c, s = _blocks("codes", codes, scales, (rows, C), rows)
+    _check(lib().moe_fp8_block_quantize(_ptr(src), _dt(src), rows, C, c, s, _stream()))
+
+
+def expert_weights_fp8_block(w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, gate: Optional[torch.Tensor],
+                             gate_scales: Optional[torch.Tensor], up: Optional[torch.Tensor], up_scales: Optional[torch.Tensor],
+                             down: Optional[torch.Tensor], down_scales: Optional[torch.Tensor],
+                             wgu_t: Optional[torch.Tensor] = None, wgu_t_scales: Optional[torch.Tensor] = None,
+                             wd_t: Optional[torch.Tensor] = None, wd_t_scales: Optional[torch.Tensor] = None) -> None:
+    """A layer's weights (fp32 or bf16) as codes and scales of the forward (gate, up [E, F, H], down [E, H, F]) and of the
+    backward (wgu_t [E, H, 2F], wd_t [E, F, H]); either set may be left out."""
+    E, F, H = w_gate.shape
+    for name, t in (("w_up", w_up), ("w_down", w_down)):
+        _is(name, t, (w_gate.dtype,), E * F * H)
+    out = []
+    for name, codes, scales, shape in (("gate", gate, gate_scales, (E, F, H)), ("up", up, up_scales, (E, F, H)),
+                                       ("down", down, down_scales, (E, H, F)), ("wgu_t", wgu_t, wgu_t_scales, (E, H, 2 * F)),
+                                       ("wd_t", wd_t, wd_t_scales, (E, F, H))):
+        out += (None, None) if codes is None or scales is None else _blocks(name, codes, scales, shape, E * (shape[1] // 128))
+    _check(lib().moe_expert_weights_fp8_block(_ptr(w_gate), _ptr(w_up), _ptr(w_down), _dt(w_gate), H, F, E, *out, _stream()))
+
+
+def permute_fp8_block(x: torch.Tensor, topk_idx: torch.Tensor, E: int, capacity: int, x_perm: torch.Tensor,
+                      x_scales: torch.Tensor, expert_counts: torch.Tensor, expert_offsets: torch.Tensor,
+                      row_of_assign: torch.Tensor, assign_of_row: torch.Tensor, workspace: torch.Tensor) -> None:
+    T, K = topk_idx.shape
+    H, i32 = x.shape[1], torch.int32
+    R = max_rows(T, K, E, int(capacity))
+    c, s = _blocks("x_perm", x_perm, x_scales, (R, H), R)
+    _check(lib().moe_permute_fp8_block(
+        _bf16("x", x, T * H), _expect("topk_idx", topk_idx, i32, T * K), T, H, E, K, int(capacity), c, s,
+        _expect("expert_counts", expert_counts, i32, E), _expect("expert_offsets", expert_offsets, i32, E + 1),
+        _expect("row_of_assign", row_of_assign, i32, T * K), _expect("assign_of_row", assign_of_row, i32, R), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _stream()))
+
+
+def grouped_gemm_swiglu_fp8_block(x_perm: torch.Tensor, x_scales: torch.Tensor, expert_offsets: torch.Tensor, w_gate: torch.Tensor,
+                                  gate_scales: torch.Tensor, w_up: torch.Tensor, up_scales: torch.Tensor, w_down: torch.Tensor,
+                                  down_scales: torch.Tensor, h: torch.Tensor, h_scales: torch.Tensor, gu: Optional[torch.Tensor],
+                                  y_perm: torch.Tensor) -> None:
+    """h (codes and scales) and y_perm (bf16) of x_perm's rows; gu [R, 2F] bf16: also g | u, for the backward."""
+    R, H = x_perm.shape
+    E, F, _ = w_gate.shape
+    n = E * (F // 128)
+    _check(lib().moe_grouped_gemm_swiglu_fp8_block(
+        *_blocks("x_perm", x_perm, x_scales, (R, H), R), _expect("expert_offsets", expert_offsets, torch.int32, E + 1), R, H, F, E,
+        *_blocks("w_gate", w_gate, gate_scales, (E, F, H), n), *_blocks("w_up", w_up, up_scales, (E, F, H), n),
+        *_blocks("w_down", w_down, down_scales, (E, H, F), E * (H // 128)), *_blocks("h", h, h_scales, (R, F), R),
+        None if gu is None else _bf16("gu", gu, R * 2 * F), _bf16("y_perm", y_perm, R * H), _stream()))
+
+
+def expert_gate_up_fp8_block(x_perm: torch.Tensor, x_scales: torch.Tensor, expert_offsets: torch.Tensor, w_gate: torch.Tensor,
+                             gate_scales: torch.Tensor, w_up: torch.Tensor, up_scales: torch.Tensor, h: torch.Tensor,
+                             h_scales: torch.Tensor, gu: Optional[torch.Tensor] = None) -> None:
+    R, H = x_perm.shape
+    E, F, _ = w_gate.shape
+    n = E * (F // 128)
+    _check(lib().moe_expert_gate_up_fp8_block(
+        *_blocks("x_perm", x_perm, x_scales, (R, H), R), _expect("expert_offsets", expert_offsets, torch.int32, E + 1), R, H, F, E,
+        *_blocks("w_gate", w_gate, gate_scales, (E, F, H), n), *_blocks("w_up", w_up, up_scales, (E, F, H), n),
+        *_blocks("h", h, h_scales, (R, F), R), None if gu is None else _bf16("gu", gu, R * 2 * F), _stream()))
+
+
+def expert_down_fp8_block(h: torch.Tensor, h_scales: torch.Tensor, expert_offsets: torch.Tensor, w_down: torch.Tensor,
+                          down_scales: torch.Tensor, y_perm: torch.Tensor) -> None:
+    R, F = h.shape
+    E, H, _ = w_down.shape
+    _check(lib().moe_expert_down_fp8_block(
+        *_blocks("h", h, h_scales, (R, F), R), _expect("expert_offsets", expert_offsets, torch.int32, E + 1), R, H, F, E,
+        *_blocks("w_down", w_down, down_scales, (E, H, F), E * (H // 128)), _bf16("y_perm", y_perm, R * H), _stream()))
+
+
+def expert_backward_fp8_block_workspace_bytes(R_max: int, H: int, F: int, E: int) -> int:
+    return int(lib().moe_expert_backward_fp8_block_workspace_bytes(R_max, H, F, E))
+
+
+def grouped_gemm_swiglu_fp8_block_backward(x_perm: torch.Tensor, x_scales: torch.Tensor, h: torch.Tensor, h_scales: torch.Tensor,
+                                           gu: torch.Tensor, dy_perm: torch.Tensor, expert_offsets: torch.Tensor,
+                                           wgu_t: torch.Tensor, wgu_t_scales: torch.Tensor, wd_t: torch.Tensor,
+                                           wd_t_scales: torch.Tensor, dx_perm: torch.Tensor, dw_gate: torch.Tensor,
+                                           dw_up: torch.Tensor, dw_down: torch.Tensor, workspace: torch.Tensor) -> None:
+    R, H = x_perm.shape
+    E, F, _ = wd_t.shape
+    _check(lib().moe_grouped_gemm_swiglu_fp8_block_backward(
+        *_blocks("x_perm", x_perm, x_scales, (R, H), R), *_blocks("h", h, h_scales, (R, F), R), _bf16("gu", gu, R * 2 * F),
+        _bf16("dy_perm", dy_perm, R * H), _expect("expert_offsets", expert_offsets, torch.int32, E + 1), R, H, F, E,
+        *_blocks("wgu_t", wgu_t, wgu_t_scales, (E, H, 2 * F), E * (H // 128)),
+        *_blocks("wd_t", wd_t, wd_t_scales, (E, F, H), E * (F // 128)), _bf16("dx_perm", dx_perm, R * H),
+        _bf16("dw_gate", dw_gate, E * F * H), _bf16("dw_up", dw_up, E * F * H), _bf16("dw_down", dw_down, E * F * H),
+        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()))
 
 
 def router_backward_workspace_bytes(T: int, H: int, E: int) -> int:

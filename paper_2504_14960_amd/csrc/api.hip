@@ -7,6 +7,7 @@
 #include <cmath>
 
 #include "common.h"
+#include "fp8_block.h"
 #include "gemm_stream.h"
 
 namespace moe {
@@ -1212,6 +1213,258 @@ moe_status_t moe_expert_down_fp8(const void* h_fp8, const int32_t* expert_offset
                                  void* y_perm_bf16, moe_stream_t stream) {
     return expert_ffn_fp8("moe_expert_down_fp8", 2, nullptr, expert_offsets, R_max, H, F, E, nullptr, nullptr,
                           w_down_fp8, 0.f, 0.f, 1.f, dq_down, const_cast<void*>(h_fp8), nullptr, y_perm_bf16, stream);
+}
+
+// ---- E4M3 with a scale for every block of 128 ----
+int moe_fp8_block_scale_stride(int C) { return C <= 0 ? 0 : block_scale_stride(C); }
+
+static bool blocks_fit(int H, int F) { return H % kBlock == 0 && F % kBlock == 0; }
+
+static moe_status_t check_block_ffn(const char* fn, int R_max, int H, int F, int E) {
+    if (R_max < 0 || H <= 0 || F <= 0 || E <= 0)
+        return fail(MOE_ERR_INVALID_ARG, "%s: need R_max >= 0 and H, F, E > 0 (R_max=%d H=%d F=%d E=%d)", fn, R_max, H, F, E);
+    if (E > kMaxExperts) return fail(MOE_ERR_UNSUPPORTED, "%s: E=%d exceeds the limit %d", fn, E, kMaxExperts);
+    if (!blocks_fit(H, F)) return fail(MOE_ERR_UNSUPPORTED, "%s: H=%d and F=%d must be multiples of 128", fn, H, F);
+    if (H > kMaxBlockRow || F > kMaxBlockRow / 2)
+        return fail(MOE_ERR_UNSUPPORTED, "%s: H=%d and 2F=%d exceed the limit %d", fn, H, 2 * F, kMaxBlockRow);
+    return MOE_OK;
+}
+
+#define REQUIRE_SCALES(fn, p)                                                                 \
+    do {                                                                                      \
+        if ((p) == nullptr) return fail(MOE_ERR_INVALID_ARG, "%s: %s is NULL", fn, #p);       \
+        if (reinterpret_cast<uintptr_t>(p) & 3u)                                              \
+            return fail(MOE_ERR_INVALID_ARG, "%s: %s is not 4-byte aligned", fn, #p);         \
+    } while (0)
+
+moe_status_t moe_fp8_block_quantize(const void* src, moe_dtype_t dt, int rows, int C, void* codes,
+                                    uint8_t* scales, moe_stream_t stream) {
+    static const char* fn = "moe_fp8_block_quantize";
+    if (dt != MOE_F32 && dt != MOE_BF16) return fail(MOE_ERR_INVALID_ARG, "%s: unknown dtype %d", fn, (int)dt);
+    if (rows < 0 || C <= 0) return fail(MOE_ERR_INVALID_ARG, "%s: need rows >= 0 and C > 0 (rows=%d C=%d)", fn, rows, C);
+    if (C % kBlock) return fail(MOE_ERR_UNSUPPORTED, "%s: C=%d must be a multiple of 128", fn, C);
+    if (rows == 0) return MOE_OK;
+    REQUIRE_PTR(fn, src);
+    REQUIRE_PTR(fn, codes);
+    REQUIRE_SCALES(fn, scales);
+    launch_block_quantize(src, dt, rows, nullptr, C, codes, scales, static_cast<hipStream_t>(stream));
+    return check_launch(fn);
+}
+
+moe_status_t moe_expert_weights_fp8_block(const void* w_gate, const void* w_up, const void* w_down,
+                                          moe_dtype_t dt, int H, int F, int E, void* gate_codes,
+                                          uint8_t* gate_scales, void* up_codes, uint8_t* up_scales,
+                                          void* down_codes, uint8_t* down_scales, void* wgu_t_codes,
+                                          uint8_t* wgu_t_scales, void* wd_t_codes,
+                                          uint8_t* wd_t_scales, moe_stream_t stream) {
+    static const char* fn = "moe_expert_weights_fp8_block";
+    if (dt != MOE_F32 && dt != MOE_BF16) return fail(MOE_ERR_INVALID_ARG, "%s: unknown dtype %d", fn, (int)dt);
+    if (moe_status_t st = check_block_ffn(fn, 0, H, F, E)) return st;
+    const bool forward = gate_codes || up_codes || down_codes || gate_scales || up_scales || down_scales;
+    const bool backward = wgu_t_codes || wd_t_codes || wgu_t_scales || wd_t_scales;
+    if (!forward && !backward) return fail(MOE_ERR_INVALID_ARG, "%s: no output is given", fn);
+    REQUIRE_PTR(fn, w_gate);
+    REQUIRE_PTR(fn, w_up);
+    REQUIRE_PTR(fn, w_down);
+    if (forward) {
+        REQUIRE_PTR(fn, gate_codes);
+        REQUIRE_PTR(fn, up_codes);
+        REQUIRE_PTR(fn, down_codes);
+        REQUIRE_SCALES(fn, gate_scales);
+        REQUIRE_SCALES(fn, up_scales);
+        REQUIRE_SCALES(fn, down_scales);
+    }
+    if (backward) {
+        REQUIRE_PTR(fn, wgu_t_codes);
+        REQUIRE_PTR(fn, wd_t_codes);
+        REQUIRE_SCALES(fn, wgu_t_scales);
+        REQUIRE_SCALES(fn, wd_t_scales);
+    }
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    launch_block_weights(w_gate, dt, E, F, H, gate_codes, gate_scales, wgu_t_codes, wgu_t_scales, 2 * F, 0, s);
+    launch_block_weights(w_up, dt, E, F, H, up_codes, up_scales, wgu_t_codes, wgu_t_scales, 2 * F, F, s);
+    launch_block_weights(w_down, dt, E, H, F, down_codes, down_scales, wd_t_codes, wd_t_scales, H, 0, s);
+    return check_launch(fn);
+}
+
+moe_status_t moe_permute_fp8_block(const void* x_bf16, const int32_t* topk_idx, int T, int H, int E,
+                                   int K, int capacity, void* x_codes, uint8_t* x_scales,
+                                   int32_t* expert_counts, int32_t* expert_offsets,
+                                   int32_t* row_of_assign, int32_t* assign_of_row, void* workspace,
+                                   size_t workspace_bytes, moe_stream_t stream) {
+    static const char* fn = "moe_permute_fp8_block";
+    if (moe_status_t st = check_dims(fn, T, H, E, K, MOE_BF16)) return st;
+    if (H % kBlock) return fail(MOE_ERR_UNSUPPORTED, "%s: H=%d must be a multiple of 128", fn, H);
+    REQUIRE_PTR(fn, expert_counts);
+    REQUIRE_PTR(fn, expert_offsets);
+    if (T == 0) {
+        launch_fill_i32(expert_counts, E, 0, 0, static_cast<hipStream_t>(stream));
+        launch_fill_i32(expert_offsets, E + 1, 0, 0, static_cast<hipStream_t>(stream));
+        return check_launch(fn);
+    }
+    REQUIRE_PTR(fn, x_bf16);
+    REQUIRE_PTR(fn, x_codes);
+    REQUIRE_SCALES(fn, x_scales);
+    REQUIRE_PTR(fn, topk_idx);
+    REQUIRE_PTR(fn, row_of_assign);
+    REQUIRE_PTR(fn, assign_of_row);
+    const size_t need = permute_workspace_bytes(T, K, E);
+    if (workspace == nullptr || workspace_bytes < need)
+        return fail(MOE_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need,
+                    workspace ? workspace_bytes : (size_t)0);
+    REQUIRE_PTR(fn, workspace);
+    launch_permute_block(x_bf16, topk_idx, T, H, E, K, capacity, moe_max_rows(T, K, E, capacity), x_codes, x_scales, expert_counts,
+                         expert_offsets, row_of_assign, assign_of_row, workspace, static_cast<hipStream_t>(stream));
+    return check_launch(fn);
+}
+
+static moe_status_t expert_ffn_block(const char* fn, int phase, const void* x_codes, const uint8_t* x_scales,
+                                     const int32_t* expert_offsets, int R_max, int H, int F, int E, const void* gate_codes,
+                                     const uint8_t* gate_scales, const void* up_codes, const uint8_t* up_scales,
+                                     const void* down_codes, const uint8_t* down_scales, void* h_codes, uint8_t* h_scales, void* gu,
+                                     void* y_perm_bf16, moe_stream_t stream) {
+    if (moe_status_t st = check_block_ffn(fn, R_max, H, F, E)) return st;
+    if (R_max == 0) return MOE_OK;
+    REQUIRE_PTR(fn, expert_offsets);
+    REQUIRE_PTR(fn, h_codes);
+    REQUIRE_SCALES(fn, h_scales);
+    if (phase & 1) {
+        REQUIRE_PTR(fn, x_codes);
+        REQUIRE_SCALES(fn, x_scales);
+        REQUIRE_PTR(fn, gate_codes);
+        REQUIRE_SCALES(fn, gate_scales);
+        REQUIRE_PTR(fn, up_codes);
+        REQUIRE_SCALES(fn, up_scales);
+        if (gu) REQUIRE_PTR(fn, gu);
+    }
+    if (phase & 2) {
+        REQUIRE_PTR(fn, down_codes);
+        REQUIRE_SCALES(fn, down_scales);
+        REQUIRE_PTR(fn, y_perm_bf16);
+    }
+    auto bytes = [](const void* p) { return static_cast<const uint8_t*>(p); };
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (phase & 1)
+        launch_block_gemm(kBlockSwiglu, {bytes(x_codes), x_scales, expert_offsets, bytes(gate_codes), bytes(up_codes), gate_scales,
+                                         up_scales, h_codes, h_scales, static_cast<bf16_t*>(gu), nullptr, E, F, H, R_max}, s);
+    if (phase & 2)
+        launch_block_gemm(kBlockPlain, {bytes(h_codes), h_scales, expert_offsets, bytes(down_codes), nullptr, down_scales, nullptr,
+                                        y_perm_bf16, nullptr, nullptr, nullptr, E, H, F, R_max}, s);
+    return check_launch(fn);
+}
+
+moe_status_t moe_grouped_gemm_swiglu_fp8_block(
+    const void* x_codes, const uint8_t* x_scales, const int32_t* expert_offsets, int R_max, int H,
+    int F, int E, const void* gate_codes, const uint8_t* gate_scales, const void* up_codes,
+    const uint8_t* up_scales, const void* down_codes, const uint8_t* down_scales, void* h_codes,
+    uint8_t* h_scales, void* gu, void* y_perm_bf16, moe_stream_t stream) {
+    return expert_ffn_block("moe_grouped_gemm_swiglu_fp8_block", 3, x_codes, x_scales, expert_offsets, R_max, H, F, E, gate_codes,
+                            gate_scales, up_codes, up_scales, down_codes, down_scales, h_codes, h_scales, gu, y_perm_bf16, stream);
+}
+
+moe_status_t moe_expert_gate_up_fp8_block(const void* x_codes, const uint8_t* x_scales,
+                                          const int32_t* expert_offsets, int R_max, int H, int F,
+                                          int E, const void* gate_codes, const uint8_t* gate_scales,
+                                          const void* up_codes, const uint8_t* up_scales,
+                                          void* h_codes, uint8_t* h_scales, void* gu,
+                                          moe_stream_t stream) {
+    return expert_ffn_block("moe_expert_gate_up_fp8_block", 1, x_codes, x_scales, expert_offsets, R_max, H, F, E, gate_codes,
+                            gate_scales, up_codes, up_scales, nullptr, nullptr, h_codes, h_scales, gu, nullptr, stream);
+}
+
+moe_status_t moe_expert_down_fp8_block(const void* h_codes, const uint8_t* h_scales,
+                                       const int32_t* expert_offsets, int R_max, int H, int F, int E,
+                                       const void* down_codes, const uint8_t* down_scales,
+                                       void* y_perm_bf16, moe_stream_t stream) {
+    return expert_ffn_block("moe_expert_down_fp8_block", 2, nullptr, nullptr, expert_offsets, R_max, H, F, E, nullptr, nullptr,
+                            nullptr, nullptr, down_codes, down_scales, const_cast<void*>(h_codes), const_cast<uint8_t*>(h_scales),
+                            nullptr, y_perm_bf16, stream);
+}
+
+struct BlockBackwardLayout {
+    size_t dy, dy_scales, dgu, dgu_codes, dgu_scales, dy_t, h_t, dgu_t, x_t, poff, total;
+    int rp_max;
+};
+
+static BlockBackwardLayout block_backward_layout(int R_max, int H, int F, int E) {
+    BlockBackwardLayout L;
+    L.rp_max = backward_layout(R_max, H, F, E).rp_max;
+    size_t o = 0;
+    auto take = [&](size_t bytes) { const size_t at = o; o += up256(bytes); return at; };
+    const size_t R = (size_t)R_max;
+    L.dy = take(R * H);
+    L.dy_scales = take(R * block_scale_stride(H));
+    L.dgu = take(R * F * 4);
+    L.dgu_codes = take(R * F * 2);
+    L.dgu_scales = take(R * block_scale_stride(2 * F));
+    L.dy_t = take((size_t)H * L.rp_max * 2);
+    L.h_t = take((size_t)F * L.rp_max * 2);
+    L.dgu_t = take((size_t)2 * F * L.rp_max * 2);
+    L.x_t = take((size_t)H * L.rp_max * 2);
+    L.poff = take((size_t)(E + 1) * 4);
+    L.total = o;
+    return L;
+}
+
+size_t moe_expert_backward_fp8_block_workspace_bytes(int R_max, int H, int F, int E) {
+    if (R_max < 0 || H <= 0 || F <= 0 || E <= 0) return 0;
+    return block_backward_layout(R_max, H, F, E).total;
+}
+
+moe_status_t moe_grouped_gemm_swiglu_fp8_block_backward(
+    const void* x_codes, const uint8_t* x_scales, const void* h_codes, const uint8_t* h_scales,
+    const void* gu, const void* dy_perm, const int32_t* expert_offsets, int R_max, int H, int F,
+    int E, const void* wgu_t_codes, const uint8_t* wgu_t_scales, const void* wd_t_codes,
+    const uint8_t* wd_t_scales, void* dx_perm, void* dw_gate, void* dw_up, void* dw_down,
+    void* workspace, size_t workspace_bytes, moe_stream_t stream) {
+    static const char* fn = "moe_grouped_gemm_swiglu_fp8_block_backward";
+    if (moe_status_t st = check_block_ffn(fn, R_max, H, F, E)) return st;
+    REQUIRE_PTR(fn, expert_offsets);
+    REQUIRE_PTR(fn, dw_gate);
+    REQUIRE_PTR(fn, dw_up);
+    REQUIRE_PTR(fn, dw_down);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (R_max == 0) {
+        launch_wgrad_zero_empty(expert_offsets, E, (size_t)H * F, dw_down, dw_gate, dw_up, s);
+        return check_launch(fn);
+    }
+    const BlockBackwardLayout L = block_backward_layout(R_max, H, F, E);
+    REQUIRE_PTR(fn, x_codes);
+    REQUIRE_SCALES(fn, x_scales);
+    REQUIRE_PTR(fn, h_codes);
+    REQUIRE_SCALES(fn, h_scales);
+    REQUIRE_PTR(fn, gu);
+    REQUIRE_PTR(fn, dy_perm);
+    REQUIRE_PTR(fn, wgu_t_codes);
+    REQUIRE_SCALES(fn, wgu_t_scales);
+    REQUIRE_PTR(fn, wd_t_codes);
+    REQUIRE_SCALES(fn, wd_t_scales);
+    REQUIRE_PTR(fn, dx_perm);
+    if (workspace == nullptr || workspace_bytes < L.total)
+        return fail(MOE_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, L.total,
+                    workspace ? workspace_bytes : (size_t)0);
+    REQUIRE_PTR(fn, workspace);
+    uint8_t* const ws = static_cast<uint8_t*>(workspace);
+    auto bytes = [](const void* p) { return static_cast<const uint8_t*>(p); };
+    launch_wgrad_zero_empty(expert_offsets, E, (size_t)H * F, dw_down, dw_gate, dw_up, s);
+    // dh, in its epilogue dg | du, and from them the rows' gradient
+    launch_block_quantize(dy_perm, MOE_BF16, R_max, expert_offsets + E, H, ws + L.dy, ws + L.dy_scales, s);
+    launch_block_gemm(kBlockGrad, {ws + L.dy, ws + L.dy_scales, expert_offsets, bytes(wd_t_codes), nullptr, wd_t_scales, nullptr,
+                                   ws + L.dgu_codes, ws + L.dgu_scales, static_cast<bf16_t*>(const_cast<void*>(gu)),
+                                   reinterpret_cast<bf16_t*>(ws + L.dgu), E, F, H, R_max}, s);
+    launch_block_gemm(kBlockPlain, {ws + L.dgu_codes, ws + L.dgu_scales, expert_offsets, bytes(wgu_t_codes), nullptr, wgu_t_scales,
+                                    nullptr, dx_perm, nullptr, nullptr, nullptr, E, H, 2 * F, R_max}, s);
+    // the weights' gradients: operands transposed with every expert's rows as a zero-padded column segment
+    int32_t* const poff = reinterpret_cast<int32_t*>(ws + L.poff);
+    launch_ragged_offsets(expert_offsets, E, poff, s);
+    launch_ragged_transpose(dy_perm, expert_offsets, poff, E, H, L.rp_max, ws + L.dy_t, s);
+    launch_ragged_transpose_block(h_codes, h_scales, expert_offsets, poff, E, F, L.rp_max, ws + L.h_t, s);
+    launch_ragged_transpose(ws + L.dgu, expert_offsets, poff, E, 2 * F, L.rp_max, ws + L.dgu_t, s);
+    launch_ragged_transpose_block(x_codes, x_scales, expert_offsets, poff, E, H, L.rp_max, ws + L.x_t, s);
+    launch_persist_wgrad(ws + L.dy_t, ws + L.h_t, expert_offsets, E, H, F, L.rp_max, dw_down, s);
+    launch_persist_wgrad(ws + L.dgu_t, ws + L.x_t, expert_offsets, E, F, H, L.rp_max, dw_gate, s);
+    launch_persist_wgrad(ws + L.dgu_t + (size_t)F * L.rp_max * 2, ws + L.x_t, expert_offsets, E, F, H, L.rp_max, dw_up, s);
+    return check_launch(fn);
 }
 
 moe_status_t moe_probe_mfma_bf16(const void* image, int iters, int workgroups, float* sink,

@@ -1,0 +1,166 @@
+// Quantisation to E4M3 with a scale for every block of 128 (fp8_block.h): rows (1 x 128), rows gathered by expert, weights
+// (128 x 128) in the layouts of the forward and of the backward.  Bound by memory: every value is read once.
+#include "fp8_block.h"
+
+namespace moe {
+
+namespace {
+
+// the largest magnitude over the 16 lanes of a row of the wave, in all of them
+__device__ __forceinline__ uint32_t max16(uint32_t v) {
+#pragma unroll
+    for (int d = 1; d < 16; d <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d, 64));
+    return v;
+}
+
+// eight values of a block that 16 neighbouring lanes hold: their codes, and the block's scale
+__device__ __forceinline__ u32x2 quantize8(const float (&f)[8], uint32_t& scale) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, magnitude(f[j]));
+    scale = block_scale(max16(top));
+    const float inv = block_inverse(scale);
+    return u32x2{block_codes(f[0], f[1], f[2], f[3], inv, scale), block_codes(f[4], f[5], f[6], f[7], inv, scale)};
+}
+
+template <bool BF16>
+__device__ __forceinline__ void load8(const void* src, size_t at, float (&f)[8]) {
+    if constexpr (BF16) {
+        bf16x8_to_f32(*reinterpret_cast<const u32x4*>(static_cast<const bf16_t*>(src) + at), f);
+    } else {
+        const f32x4 lo = *reinterpret_cast<const f32x4*>(static_cast<const float*>(src) + at);
+        const f32x4 hi = *reinterpret_cast<const f32x4*>(static_cast<const float*>(src) + at + 4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            f[j] = lo[j];
+            f[4 + j] = hi[j];
+        }
+    }
+}
+
+// One row to a wave, 512 values at a time.  Rows below *n_rows (null: `rows`).
+template <bool BF16>
+__global__ __launch_bounds__(256) void block_rows_quantize_kernel(const void* __restrict__ src, int rows,
+                                                                  const int32_t* __restrict__ n_rows, int C,
+                                                                  uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int n = n_rows ? min(rows, *n_rows) : rows, stride = block_scale_stride(C);
+    for (int r = blockIdx.x * 4 + wave; r < n; r += gridDim.x * 4)
+        for (int c0 = 0; c0 < C; c0 += 512) {   // uniform trip count: shuffles inside
+            const int c = c0 + 8 * lane;
+            float f[8] = {};
+            if (c < C) load8<BF16>(src, (size_t)r * C + c, f);
+            uint32_t scale;
+            const u32x2 q = quantize8(f, scale);
+            if (c >= C) continue;
+            *reinterpret_cast<u32x2*>(codes + (size_t)r * C + c) = q;
+            if ((lane & 15) == 0) scales[(size_t)r * stride + c / kBlock] = (uint8_t)scale;
+        }
+}
+
+// One token to a wave: its row read and quantised once, stored to each of its rows of the expert order.
+__global__ __launch_bounds__(256) void permute_copy_block_kernel(const bf16_t* __restrict__ x,
+                                                                 const int32_t* __restrict__ row_of_assign, int T, int K, int H,
+                                                                 int r_max, uint8_t* __restrict__ codes,
+                                                                 uint8_t* __restrict__ scales) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int stride = block_scale_stride(H);
+    for (int t = blockIdx.x * 4 + wave; t < T; t += gridDim.x * 4) {
+        int my_row = lane < K ? row_of_assign[(size_t)t * K + lane] : -1;
+        if ((unsigned)my_row >= (unsigned)r_max) my_row = -1;
+        const uint64_t kept = __ballot(my_row >= 0);
+        if (!kept) continue;
+        for (int c0 = 0; c0 < H; c0 += 512) {   // uniform trip count: shuffles inside
+            const int c = c0 + 8 * lane;
+            float f[8] = {};
+            if (c < H) load8<true>(x, (size_t)t * H + c, f);
+            uint32_t scale;
+            const u32x2 q = quantize8(f, scale);
+            for (uint64_t m = kept; m; m &= m - 1) {
+                const int row = __shfl(my_row, __ffsll((unsigned long long)m) - 1, 64);
+                if (c >= H) continue;
+                *reinterpret_cast<u32x2*>(codes + (size_t)row * H + c) = q;
+                if ((lane & 15) == 0) scales[(size_t)row * stride + c / kBlock] = (uint8_t)scale;
+            }
+        }
+    }
+}
+
+// A block of 128 x 128 to a workgroup: w [E, N, K] -> codes [E, N, K] and, transposed, at column t0 of [E, K, ldt]; either may
+// be null.  A thread holds eight columns of eight rows.
+template <bool BF16>
+__global__ __launch_bounds__(256) void block_weights_kernel(const void* __restrict__ w, int N, int K, uint8_t* __restrict__ codes,
+                                                            uint8_t* __restrict__ scales, uint8_t* __restrict__ codes_t,
+                                                            uint8_t* __restrict__ scales_t, int ldt, int t0) {
+    __shared__ uint32_t tops[4];
+    __shared__ __attribute__((aligned(16))) uint8_t tile[128][128 + 16];   // transposed
+    const int e = blockIdx.z, n0 = blockIdx.y * kBlock, k0 = blockIdx.x * kBlock;
+    const int cv = threadIdx.x % 16, rv = threadIdx.x / 16;
+    float f[8][8];
+    uint32_t top = 0;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) load8<BF16>(w, ((size_t)e * N + n0 + 8 * rv + r) * K + k0 + 8 * cv, f[r]);
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = max(top, magnitude(f[r][j]));
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    __syncthreads();
+    const uint32_t scale = block_scale(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
+    const float inv = block_inverse(scale);
+    u32x2 q[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+        q[r] = u32x2{block_codes(f[r][0], f[r][1], f[r][2], f[r][3], inv, scale),
+                     block_codes(f[r][4], f[r][5], f[r][6], f[r][7], inv, scale)};
+    if (codes) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+            *reinterpret_cast<u32x2*>(codes + ((size_t)e * N + n0 + 8 * rv + r) * K + k0 + 8 * cv) = q[r];
+        if (threadIdx.x == 0) scales[((size_t)e * (N / kBlock) + blockIdx.y) * block_scale_stride(K) + blockIdx.x] = (uint8_t)scale;
+    }
+    if (!codes_t) return;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        u32x2 v = {0u, 0u};
+#pragma unroll
+        for (int r = 0; r < 8; ++r) v[r / 4] |= (q[r][j / 4] >> (8 * (j % 4)) & 0xffu) << (8 * (r % 4));
+        *reinterpret_cast<u32x2*>(&tile[8 * cv + j][8 * rv]) = v;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int c = 32 * i + threadIdx.x / 8, at = threadIdx.x % 8 * 16;
+        *reinterpret_cast<u32x4*>(codes_t + ((size_t)e * K + k0 + c) * ldt + t0 + n0 + at) = *reinterpret_cast<const u32x4*>(&tile[c][at]);
+    }
+    if (threadIdx.x == 0)
+        scales_t[((size_t)e * (K / kBlock) + blockIdx.x) * block_scale_stride(ldt) + t0 / kBlock + blockIdx.y] = (uint8_t)scale;
+}
+
+}  // namespace
+
+void launch_block_quantize(const void* src, moe_dtype_t dt, int rows, const int32_t* n_rows, int C, void* codes, uint8_t* scales,
+                           hipStream_t s) {
+    const int grid = (int)min((rows + 3ll) / 4, 256ll * 16);
+    auto kern = dt == MOE_BF16 ? block_rows_quantize_kernel<true> : block_rows_quantize_kernel<false>;
+    hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, s, src, rows, n_rows, C, static_cast<uint8_t*>(codes), scales);
+}
+
+void launch_block_weights(const void* w, moe_dtype_t dt, int E, int N, int K, void* codes, uint8_t* scales, void* codes_t,
+                          uint8_t* scales_t, int ldt, int t0, hipStream_t s) {
+    auto kern = dt == MOE_BF16 ? block_weights_kernel<true> : block_weights_kernel<false>;
+    hipLaunchKernelGGL(kern, dim3(K / kBlock, N / kBlock, E), dim3(256), 0, s, w, N, K, static_cast<uint8_t*>(codes), scales,
+                       static_cast<uint8_t*>(codes_t), scales_t, ldt, t0);
+}
+
+void launch_permute_block(const void* x, const int32_t* idx, int T, int H, int E, int K, int capacity, int r_max, void* codes,
+                          uint8_t* scales, int32_t* counts, int32_t* offsets, int32_t* row_of_assign, int32_t* assign_of_row,
+                          void* ws, hipStream_t s) {
+    launch_permute(nullptr, idx, T, H, E, K, capacity, r_max, MOE_BF16, nullptr, counts, offsets, row_of_assign, assign_of_row, ws, s);
+    hipLaunchKernelGGL(permute_copy_block_kernel, dim3(min((T + 3) / 4, 256 * 16)), dim3(256), 0, s, static_cast<const bf16_t*>(x),
+                       row_of_assign, T, K, H, r_max, static_cast<uint8_t*>(codes), scales);
+}
+
+}  // namespace moe

@@ -195,6 +195,9 @@ void launch_weights_transpose(const void* w_gate, const void* w_up, const void* 
 void launch_ragged_offsets(const int32_t* offsets, int E, int32_t* poff, hipStream_t s);   // poff [E + 1]
 void launch_ragged_transpose(const void* src, const int32_t* offsets, const int32_t* poff, int E, int C, int rp_max,
                              void* dst, hipStream_t s);
+// the same of E4M3 codes with a scale for every block of 128 of a row: the bf16 values they stand for
+void launch_ragged_transpose_block(const void* codes, const uint8_t* scales, const int32_t* offsets, const int32_t* poff, int E, int C,
+                                   int rp_max, void* dst, hipStream_t s);
 // out [rows, 2F] = dg | du from dh [rows, F] and g, u (rows ld_gu elements apart); rows = *n_rows (device)
 void launch_swiglu_backward(const void* dh, const void* g, const void* u, size_t ld_gu, const int32_t* n_rows,
                             int r_max, int F, void* out, hipStream_t s);
@@ -222,6 +225,16 @@ void launch_probe_mfma_bf16(const void* image, int iters, int workgroups, float*
                             hipStream_t s);
 void launch_probe_mfma_fp8(const void* image, int iters, int workgroups, float* sink, unsigned long long* ticks,
                            hipStream_t s);
+
+// E4M3 with a scale for every block of 128 (fp8_block.h).  Rows below *n_rows (null: all `rows`)
+void launch_block_quantize(const void* src, moe_dtype_t dt, int rows, const int32_t* n_rows, int C, void* codes, uint8_t* scales,
+                           hipStream_t s);
+// w [E, N, K] to codes [E, N, K] and/or, transposed, to column t0 of [E, K, ldt] (null: not)
+void launch_block_weights(const void* w, moe_dtype_t dt, int E, int N, int K, void* codes, uint8_t* scales, void* codes_t,
+                          uint8_t* scales_t, int ldt, int t0, hipStream_t s);
+void launch_permute_block(const void* x, const int32_t* idx, int T, int H, int E, int K, int capacity, int r_max, void* codes,
+                          uint8_t* scales, int32_t* counts, int32_t* offsets, int32_t* row_of_assign, int32_t* assign_of_row,
+                          void* ws, hipStream_t s);
 
 // FP8 (E4M3) path of the expert FFN: per-tensor quantisation with amax, and the
 // two grouped GEMMs on quantised operands (phase bits as above)

@@ -12,10 +12,12 @@
 //                              every expert's segment padded with zeros to a
 //                              multiple of 64 (at least 128) columns, so the
 //                              weight-gradient GEMMs contract over whole k-tiles
+//                              (of E4M3 codes with a scale for every block of 128
+//                              the values they stand for, which are bf16 values)
 //   swiglu_backward_kernel     (dh, g, u) -> dg | du side by side
 //
 // All bf16, tiles through LDS for the transposes.
-#include "common.h"
+#include "fp8_block.h"
 
 namespace moe {
 
@@ -47,6 +49,33 @@ struct TransposeRows {   // where 64 of the tile's rows come from
     int first, valid;    // first source row; how many of the 64 exist, the rest count as zeros
 };
 
+// eight neighbouring values of a row, as bf16
+template <bool STREAM>
+struct Bf16Rows {
+    const uint16_t* src;
+    size_t ld;
+    __device__ __forceinline__ u32x4 operator()(int r, int c) const {
+        const u32x4* from = reinterpret_cast<const u32x4*>(src + (size_t)r * ld + c);
+        return STREAM ? __builtin_nontemporal_load(from) : *from;
+    }
+};
+struct BlockRows {
+    const uint8_t *codes, *scales;
+    int C, stride;
+    __device__ __forceinline__ u32x4 operator()(int r, int c) const {
+        const u32x2 q = *reinterpret_cast<const u32x2*>(codes + (size_t)r * C + c);
+        const float scale = block_value(scales[(size_t)r * stride + c / kBlock]);
+        u32x4 v;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)q[j], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)q[j], true);
+            v[2 * j] = pack2_bf16(lo[0] * scale, lo[1] * scale);
+            v[2 * j + 1] = pack2_bf16(hi[0] * scale, hi[1] * scale);
+        }
+        return v;
+    }
+};
+
 template <int TR, int TC, bool STREAM>   // tile: rows, columns
 struct TransposeTile {
     static constexpr int PARTS = TR / 64, TP = TR / 2;                  // row pairs
@@ -57,9 +86,9 @@ struct TransposeTile {
 
     static __device__ __forceinline__ int at(int group, int c) { return 4 * (group ^ ((c >> 3) * (128 / TC))); }
 
-    // columns c0 .. c0 + TC - 1 (below `cols`) of PARTS times 64 rows of `src`
-    __device__ __forceinline__ void load(const uint16_t* __restrict__ src, size_t ld, int c0, int cols,
-                                         const TransposeRows (&part)[PARTS]) {
+    // columns c0 .. c0 + TC - 1 (below `cols`) of PARTS times 64 rows
+    template <typename Rows>
+    __device__ __forceinline__ void load(const Rows& rows, int c0, int cols, const TransposeRows (&part)[PARTS]) {
         const int c = (threadIdx.x % VC) * 8, rp = threadIdx.x / VC;
         u32x4 v[NP][2];
 #pragma unroll
@@ -69,10 +98,7 @@ struct TransposeTile {
             for (int k = 0; k < 2; ++k) {
                 const int rr = 2 * (p * RPT % 32 + rp) + k;
                 v[p][k] = u32x4{0u, 0u, 0u, 0u};
-                if (rr < h.valid && c0 + c < cols) {   // cols is a multiple of 8
-                    const u32x4* from = reinterpret_cast<const u32x4*>(src + (size_t)(h.first + rr) * ld + c0 + c);
-                    v[p][k] = STREAM ? __builtin_nontemporal_load(from) : *from;
-                }
+                if (rr < h.valid && c0 + c < cols) v[p][k] = rows(h.first + rr, c0 + c);   // cols is a multiple of 8
             }
         }
 #pragma unroll
@@ -116,7 +142,7 @@ __global__ __launch_bounds__(256) void transpose_batched_kernel(const uint16_t* 
     TransposeRows part[Tile::PARTS];
 #pragma unroll
     for (int q = 0; q < Tile::PARTS; ++q) part[q] = {r0 + 64 * q, R - r0 - 64 * q};
-    tile.load(src + (size_t)b * R * C, (size_t)C, c0, C, part);
+    tile.load(Bf16Rows<STREAM>{src + (size_t)b * R * C, (size_t)C}, c0, C, part);
     __syncthreads();
     tile.store(dst + (size_t)b * C * ldo, ldo, c0, C, (size_t)col0 + r0, min(TR, R - r0));
 }
@@ -153,8 +179,8 @@ __global__ __launch_bounds__(256) void ragged_offsets_kernel(const int32_t* __re
 // padded_rows(n_e) is zero.  One workgroup per (128-column block, 128-row block of the
 // padded axis); the expert of a padded position is the one whose segment [poff_e,
 // poff_e+1) holds it (segments are multiples of 64, so a half block never straddles two).
-__global__ __launch_bounds__(256) void ragged_transpose_kernel(const uint16_t* __restrict__ src,
-                                                               const int32_t* __restrict__ offsets,
+template <typename Rows>
+__global__ __launch_bounds__(256) void ragged_transpose_kernel(Rows src, const int32_t* __restrict__ offsets,
                                                                const int32_t* __restrict__ poff, int E, int C,
                                                                uint16_t* __restrict__ dst, size_t ldo) {
     __shared__ __attribute__((aligned(16))) ActTile tile;
@@ -178,7 +204,7 @@ __global__ __launch_bounds__(256) void ragged_transpose_kernel(const uint16_t* _
     if (seg[0][1] < 0) return;   // past the last expert's padding: nothing to write
     const TransposeRows half[2] = {{seg[0][0], min(64, seg[0][1])}, {seg[1][0], min(64, seg[1][1])}};
     const int n_out = seg[1][1] < 0 ? 64 : kActTile;
-    tile.load(src, (size_t)C, c0, C, half);
+    tile.load(src, c0, C, half);
     __syncthreads();
     tile.store(dst, ldo, c0, C, (size_t)p0, n_out);
 }
@@ -238,12 +264,22 @@ void launch_ragged_offsets(const int32_t* offsets, int E, int32_t* poff, hipStre
 
 // rp_max: the static bound on the padded axis (a multiple of 64); blocks past the real padded length exit.
 // poff: the E + 1 segment starts written by launch_ragged_offsets
+template <typename Rows>
+static void ragged_transpose(const Rows& src, const int32_t* offsets, const int32_t* poff, int E, int C, int rp_max, void* dst,
+                             hipStream_t s) {
+    if (rp_max <= 0 || C <= 0) return;
+    hipLaunchKernelGGL(ragged_transpose_kernel<Rows>, dim3((C + kActTile - 1) / kActTile, (rp_max + kActTile - 1) / kActTile), dim3(256),
+                       0, s, src, offsets, poff, E, C, static_cast<uint16_t*>(dst), (size_t)rp_max);
+}
+
 void launch_ragged_transpose(const void* src, const int32_t* offsets, const int32_t* poff, int E, int C, int rp_max,
                              void* dst, hipStream_t s) {
-    if (rp_max <= 0 || C <= 0) return;
-    hipLaunchKernelGGL(ragged_transpose_kernel, dim3((C + kActTile - 1) / kActTile, (rp_max + kActTile - 1) / kActTile), dim3(256),
-                       0, s, static_cast<const uint16_t*>(src), offsets, poff, E, C, static_cast<uint16_t*>(dst),
-                       (size_t)rp_max);
+    ragged_transpose(Bf16Rows<false>{static_cast<const uint16_t*>(src), (size_t)C}, offsets, poff, E, C, rp_max, dst, s);
+}
+
+void launch_ragged_transpose_block(const void* codes, const uint8_t* scales, const int32_t* offsets, const int32_t* poff, int E, int C,
+                                   int rp_max, void* dst, hipStream_t s) {
+    ragged_transpose(BlockRows{static_cast<const uint8_t*>(codes), scales, C, block_scale_stride(C)}, offsets, poff, E, C, rp_max, dst, s);
 }
 
 void launch_swiglu_backward(const void* dh, const void* g, const void* u, size_t ld_gu, const int32_t* n_rows,

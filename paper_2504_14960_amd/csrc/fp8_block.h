@@ -1,0 +1,70 @@
+// E4M3 with a scale for every block of 128: a power of two, as E8M0 (a byte b stands for 2^(b-127), 255 for NaN).
+//
+// Powers of two, because the scaled matrix instruction multiplies both operands' E8M0 scales in on the way: a block of 128 along
+// the contraction is the instruction's whole depth, so scaling costs no vector instruction, where any other scale would cost
+// a fused multiply-add for every accumulator and block.  And what a code and its scale stand for has four significant bits, so
+// it is a bf16 value too: the weight gradients multiply exactly what the forward did.
+#pragma once
+
+#include "common.h"
+
+namespace moe {
+
+constexpr int kBlock = 128;
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+
+// Bytes of a row of scales for C values: whole words, so that four of them are one load.
+__host__ __device__ inline int block_scale_stride(int C) { return (C / kBlock + 3) & ~3; }
+
+constexpr uint32_t kNotFinite = 0x7f800000u;   // magnitudes as bits from here on are infinity or NaN
+
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// The scale of a block whose largest magnitude has these bits: the smallest power of two, from 2^-126, that leaves at most 448
+// (1.75 * 2^8: the exponent goes up where the fraction is above 0.75); 255 where a value is not finite.
+__device__ __forceinline__ uint32_t block_scale(uint32_t top) {
+    const int b = (int)((top + 0x1fffffu) >> 23) - 8;
+    return top >= kNotFinite ? 255u : (uint32_t)max(b, 1);
+}
+// what the block's values are multiplied with; any number for 255
+__device__ __forceinline__ float block_inverse(uint32_t scale) { return __uint_as_float((254u - min(scale, 254u)) << 23); }
+// what a scale stands for; infinity for 255, whose codes are NaN
+__device__ __forceinline__ float block_value(uint32_t scale) { return __uint_as_float(scale ? scale << 23 : 0x400000u); }
+
+// four values of a block to their nearest codes, ties to even (the scale leaves at most 448: nothing to clamp)
+__device__ __forceinline__ uint32_t block_codes(float a, float b, float c, float d, float inverse, uint32_t scale) {
+    int r = __builtin_amdgcn_cvt_pk_fp8_f32(a * inverse, b * inverse, 0, false);
+    r = __builtin_amdgcn_cvt_pk_fp8_f32(c * inverse, d * inverse, r, true);
+    return scale == 255u ? 0x7f7f7f7fu : (uint32_t)r;
+}
+
+// 16 bytes of bf16 as eight floats
+__device__ __forceinline__ void bf16x8_to_f32(const u32x4& v, float (&f)[8]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        f[2 * j] = __uint_as_float(v[j] << 16);
+        f[2 * j + 1] = __uint_as_float(v[j] & 0xffff0000u);
+    }
+}
+
+// What the grouped products of the block-scaled expert FFN work on: C = A [rows, K] . B[e]^T over the rows of every expert
+struct BlockGemm {
+    const uint8_t* A;             // codes [rows, K]
+    const uint8_t* a_scales;      // [rows, stride(K)]
+    const int32_t* offsets;
+    const uint8_t *B0, *B1;       // codes [E, N, K]; B1: the up projection
+    const uint8_t *b0_scales, *b1_scales;   // [E, N / 128, stride(K)]
+    void* C;                      // kBlockPlain: bf16 [rows, N]; kBlockSwiglu: codes [rows, N]; kBlockGrad: codes [rows, 2 N]
+    uint8_t* c_scales;            // of the codes
+    bf16_t* gu;                   // kBlockSwiglu: g | u [rows, 2 N] out, or null; kBlockGrad: in
+    bf16_t* dgu;                  // kBlockGrad: dg | du [rows, 2 N] out
+    int E, N, K, r_max;
+};
+// y = A B0^T; h = silu(A B0^T) * (A B1^T) quantised; dg | du from dh = A B0^T and g | u, in bf16 and quantised
+enum { kBlockPlain = 0, kBlockSwiglu = 1, kBlockGrad = 2 };
+
+constexpr int kMaxBlockRow = 1 << 22;   // values of an operand's row: 32-bit offsets inside a tile
+
+void launch_block_gemm(int mode, const BlockGemm& p, hipStream_t s);
+
+}  // namespace moe
