@@ -65,6 +65,7 @@ enum { kBlockPlain = 0, kBlockSwiglu = 1, kBlockGrad = 2 };
 
 constexpr int kMaxBlockRow = 1 << 22;   // values of an operand's row: 32-bit offsets inside a tile
 
-void launch_block_gemm(int mode, const BlockGemm& p, hipStream_t s);
+void launch_block_gemm(int mode, const BlockGemm& p, hipStream_t s);      // the choice of the kernel
+void launch_block_persist(int mode, const BlockGemm& p, hipStream_t s);   // gemm_persist_block.hip: many rows per expert, K >= 256
 
 }  // namespace moe

@@ -181,6 +181,10 @@ void launch_rows(const BlockGemm& p, hipStream_t s) {
 }  // namespace
 
 void launch_block_gemm(int mode, const BlockGemm& p, hipStream_t s) {
+    if (p.K >= 256 && p.r_max > 64 * p.E) {
+        launch_block_persist(mode, p, s);
+        return;
+    }
     if (mode == kBlockPlain) launch_rows<kBlockPlain, 4>(p, s);
     else if (mode == kBlockSwiglu) launch_rows<kBlockSwiglu, 4>(p, s);
     else launch_rows<kBlockGrad, 4>(p, s);

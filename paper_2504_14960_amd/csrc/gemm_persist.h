@@ -100,6 +100,7 @@ struct PTile {
     uint32_t a_lim;     // byte offset (from a) of the last valid activation row
     uint32_t b_lim;     // byte offset (from b0 / b1) of the last valid weight row
     int row0, rows, n0;
+    int expert;
     int kt;             // k-tiles of this output tile (weight-gradient form; 0 = the launch's common count)
     int split;          // contraction in parts: which one
     int krows;          // row-major weight-gradient form: rows of the expert, i.e. valid length of the contraction
@@ -153,7 +154,7 @@ struct TileSched {
                                          size_t row_bytes, int outn, int splits = 1) const {
         constexpr int MG = 8;
         PTile t;
-        t.a = A; t.b0 = B0; t.b1 = B1; t.a_lim = 0; t.b_lim = 0; t.row0 = 0; t.rows = 0; t.n0 = 0; t.kt = 0; t.split = 0; t.krows = 0;
+        t.a = A; t.b0 = B0; t.b1 = B1; t.a_lim = 0; t.b_lim = 0; t.row0 = 0; t.rows = 0; t.n0 = 0; t.expert = 0; t.kt = 0; t.split = 0; t.krows = 0;
         // BY_ROUND: whole rounds (one tile per workgroup of the launch) are dealt to the XCDs round by round: in
         // round i XCD x runs the nwx consecutive tiles from (8 i + x) nwx on, so at any time the eight XCDs work on
         // neighbouring stretches of the list and what they have in common (activation panels of one M-group) is
@@ -218,6 +219,7 @@ struct TileSched {
         }
         const int nt = rem / gsz;
         const int m = m_first + rem - nt * gsz;
+        t.expert = e;
         t.row0 = uni(lo_e + m * BM);
         t.rows = uni(min(BM, lo_e + n_e - t.row0));
         t.n0 = uni(nt * outn);
@@ -359,7 +361,7 @@ struct WgradSched {
     // the i-th tile of this workgroup (asked for in ascending order); ld = elements per row of A_t and B_t
     __device__ __forceinline__ PTile get(int i, const uint8_t* A, const uint8_t* B, int M, int N, int ld) {
         PTile t;
-        t.a = A; t.b0 = B; t.b1 = B; t.a_lim = 0; t.b_lim = 0; t.row0 = 0; t.rows = 0; t.n0 = 0; t.kt = 0; t.split = 0; t.krows = 0;
+        t.a = A; t.b0 = B; t.b1 = B; t.a_lim = 0; t.b_lim = 0; t.row0 = 0; t.rows = 0; t.n0 = 0; t.expert = 0; t.kt = 0; t.split = 0; t.krows = 0;
         if (uni(i >> 6) != batch) fill(uni(i >> 6));
         const int l = uni(i & 63);
         t.kt = __builtin_amdgcn_readlane(t_kt, l);
@@ -429,7 +431,7 @@ struct WgradSchedKM {
                                          int ldb) const {
         constexpr int MG = 8;
         PTile t;
-        t.a = A; t.b0 = B; t.b1 = B; t.a_lim = 0; t.b_lim = 0; t.row0 = 0; t.rows = 0; t.n0 = 0; t.kt = 0; t.split = 0; t.krows = 0;
+        t.a = A; t.b0 = B; t.b1 = B; t.a_lim = 0; t.b_lim = 0; t.row0 = 0; t.rows = 0; t.n0 = 0; t.expert = 0; t.kt = 0; t.split = 0; t.krows = 0;
         const int j = wgx + i * nwx;
         t.valid = j < total;
         if (!t.valid) return t;

@@ -1,0 +1,353 @@
+// Grouped expert GEMMs on E4M3 operands with a scale for every block of 128 (fp8_block.h): many rows per expert, on the engine of
+// gemm_persist_fp8.h.
+//
+// A k-tile is a block along the contraction, so the scaled matrix instruction takes the operands' scales as it takes their
+// codes: no instruction is added for any accumulator.  A lane needs one byte for every row of its activation fragments and, the
+// weights' blocks being 128 wide, one (gate and up: two) for all its weight rows.  The bytes of four k-tiles are one load; it is
+// issued two k-tiles ahead of its first use, behind the loads whose end the k loop's own wait covers, so that no wait is
+// added either.
+#include "fp8_block.h"
+#include "gemm_persist_fp8.h"
+
+namespace moe {
+
+namespace {
+
+// FM row fragments and, along the weight rows, NB blocks of a wave (gate and up, or one)
+template <int FM, int NB>
+struct BlockScales {
+    static constexpr bool BRANCHES = true;
+    const uint8_t *A, *B0, *B1;   // scales of all rows, and of the weights' blocks
+    int stride, n_blocks;         // bytes of a row of scales; blocks along N
+
+    struct Rows {
+        const uint8_t *a, *b[NB];
+        int last;                 // last valid row of the tile
+    };
+    Rows cur, next;
+    int row;                      // of the lane in the tile's first fragment
+    uint32_t sa[FM], na[FM], sb[NB], nb[NB];
+    bool turn;
+
+    __device__ __forceinline__ Rows rows_of(const PTile& t, int wn) const {
+        Rows r;
+        r.a = uni(A + (size_t)t.row0 * stride);
+        // behind the last block the last one again: those columns are not stored
+        const int block = min(t.n0 / kBlock + (NB == 1 ? wn : 0), n_blocks - 1);
+        const size_t at = ((size_t)t.expert * n_blocks + block) * stride;
+        r.b[0] = uni(B0 + at);
+        if constexpr (NB == 2) r.b[1] = uni(B1 + at);
+        r.last = t.rows - 1;
+        return r;
+    }
+    static __device__ __forceinline__ uint32_t word(const uint8_t* p) { return *(const __attribute__((address_space(1))) uint32_t*)p; }
+    // the bytes of k-tiles 4 g .. 4 g + 3
+    __device__ __forceinline__ void load(const Rows& r, int g) {
+        int first = row;
+        asm volatile("" : "+v"(first));   // or the rows' offsets are kept across the k loop
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+            na[i] = word(r.a + (uint32_t)(__mul24(min(first + 16 * i, r.last), stride) + 4 * g));
+        int same = 0;
+        asm volatile("" : "+v"(same));    // vector loads: scalar ones would be waited for together with LDS reads
+#pragma unroll
+        for (int i = 0; i < NB; ++i) nb[i] = word(r.b[i] + (uint32_t)(same + 4 * g));
+    }
+    __device__ __forceinline__ void start(const PTile& t, int row_, int wn) {
+        row = row_;
+        cur = rows_of(t, wn);
+        load(cur, 0);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) sa[i] = na[i];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) sb[i] = nb[i];
+        next = cur;
+    }
+    // t is the tile after the one that begins
+    __device__ __forceinline__ void next_tile(const PTile& t, int wn) {
+        cur = next;
+        if (t.valid) next = rows_of(t, wn);
+    }
+    __device__ __forceinline__ f32x4 mfma(const i32x8& w, const i32x8& a, const f32x4& c, int i, int half) const {
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, c, 0, 0, 0, (int)sb[NB == 2 ? half : 0], 0, (int)sa[i]);
+    }
+    // from k-tile kt to the one behind it (of the next tile, behind the last)
+    __device__ __forceinline__ void begin_step(int kt, int KT) { turn = kt + 1 == KT || ((kt + 1) & 3) == 0; }
+    __device__ __forceinline__ void step_row(int i) { sa[i] = turn ? na[i] : sa[i] >> 8; }
+    __device__ __forceinline__ void end_step(int kt, int KT) {
+#pragma unroll
+        for (int i = 0; i < NB; ++i) sb[i] = turn ? nb[i] : sb[i] >> 8;
+        if (kt + 2 == KT) load(next, 0);
+        else if (kt + 2 < KT && ((kt + 2) & 3) == 0) load(cur, (kt + 2) >> 2);
+    }
+};
+
+// rows of a wave's patch, 16-byte granules at places that neither side's accesses share a bank at: granule g of row r at
+// g ^ (r / rows per 256 bytes)
+template <int W>
+__device__ __forceinline__ int granule(int row, int g) {
+    constexpr int GPR = W / 16, RP256 = W >= 256 ? 1 : 256 / W;
+    return row * W + ((g ^ ((row / RP256) & (GPR - 1))) << 4);
+}
+
+// y = acc in bf16, 32 rows at a time through the patch
+struct PlainStore {
+    BlockGemm p;
+
+    template <int FM, int FN>
+    __device__ __forceinline__ void tile(f32x4 (&acc)[FM][FN], int row0, int rows, int n0, int wm, int wn, int lane, uint8_t* stage,
+                                         uint8_t*, bool) {
+        constexpr int WM = FM * 16, W = FN * 32, GPR = W / 16, RPI = 1024 / W;
+        asm volatile("" : "+v"(lane));    // keeps the addresses below from being hoisted out of the tile loop
+        const int fr = lane & 15, fk = lane >> 4, rl = lane / GPR, gl = lane % GPR;
+        const int col = n0 + wn * (FN * 16) + gl * 8;
+#pragma unroll
+        for (int i = 0; i < FM / 2; ++i) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int j = 0; j < FN; ++j) asm volatile("" : "+a"(acc[2 * i + q][j]));   // see gemm_persist.hip
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
+                    const f32x4& a = acc[2 * i + q][j];
+                    *reinterpret_cast<u32x2*>(stage + granule<W>(16 * q + fr, 2 * j + (fk >> 1)) + 8 * (fk & 1)) =
+                        u32x2{pack2_bf16(a[0], a[1]), pack2_bf16(a[2], a[3])};
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int it = 0; it < 32 / RPI; ++it) {
+                const int row = it * RPI + rl, grow = wm * WM + i * 32 + row;
+                const u32x4 v = *reinterpret_cast<const u32x4*>(stage + granule<W>(row, gl));
+                if (grow < rows && col < p.N)
+                    *reinterpret_cast<u32x4*>(static_cast<bf16_t*>(p.C) + (size_t)(row0 + grow) * p.N + col) = v;
+            }
+        }
+    }
+    __device__ __forceinline__ void finish(int) {}
+};
+
+// h = silu(g) * u as codes.  A wave has 64 of a block's 128 columns, the wave beside it the others: the rows' largest magnitudes
+// go through LDS, and the codes are formed behind a barrier.
+struct SwigluStore {
+    BlockGemm p;
+
+    template <int FM, int FN>
+    __device__ __forceinline__ void tile(f32x4 (&acc)[FM][FN], int row0, int rows, int n0, int wm, int wn, int lane, uint8_t* stage,
+                                         uint8_t* slot, bool) {
+        constexpr int FO = FN / 2, WM = FM * 16;
+        asm volatile("" : "+v"(lane));
+        const int fr = lane & 15, fk = lane >> 4;
+        const int col0 = n0 + wn * (FO * 16);
+        // the last 512 bytes of every wave's 8 KiB: its rows' largest magnitudes
+        uint32_t* const mine = reinterpret_cast<uint32_t*>(slot + (2 * wm + wn + 1) * 8192 - 512);
+        const uint32_t* const other = reinterpret_cast<const uint32_t*>(slot + (2 * wm + 1 - wn + 1) * 8192 - 512);
+        static_assert(WM * 4 <= 512 && FN * 32 * 32 == 8192, "patch");
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < FN; ++j) asm volatile("" : "+a"(acc[i][j]));
+            if (p.gu) {
+                // g | u of 16 rows, 128 bytes each
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
+                    const f32x4& a = acc[i][j];
+                    *reinterpret_cast<u32x2*>(stage + granule<256>(fr, 2 * j + (fk >> 1)) + 8 * (fk & 1)) =
+                        u32x2{pack2_bf16(a[0], a[1]), pack2_bf16(a[2], a[3])};
+                }
+                const int rl = lane >> 4, gl = lane & 15;
+                const int col = col0 + (gl & 7) * 8 + (gl >> 3) * p.N;
+#pragma unroll
+                for (int it = 0; it < 4; ++it) {
+                    const int row = 4 * it + rl, grow = wm * WM + i * 16 + row;
+                    const u32x4 v = *reinterpret_cast<const u32x4*>(stage + granule<256>(row, gl));
+                    if (grow < rows) *reinterpret_cast<u32x4*>(p.gu + (size_t)(row0 + grow) * (2 * p.N) + col) = v;
+                }
+            }
+            uint32_t top = 0;
+#pragma unroll
+            for (int j = 0; j < FO; ++j)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const float g = acc[i][j][u], up = acc[i][j + FO][u];
+                    const float h = g * __builtin_amdgcn_rcpf(1.f + __expf(-g)) * up;
+                    acc[i][j][u] = h;
+                    top = max(top, magnitude(h));
+                }
+            top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
+            top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+            if (fk == 0) mine[16 * i + fr] = top;
+#pragma unroll
+            for (int j = 0; j < FO; ++j) asm volatile("" : "+a"(acc[i][j]));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        const int stride = block_scale_stride(p.N);
+        constexpr int W = FO * 16;            // 64 bytes a row, 32 rows at a time
+#pragma unroll
+        for (int i = 0; i < FM / 2; ++i) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                __builtin_amdgcn_sched_barrier(0);
+                const int r = 32 * i + 16 * q + fr, grow = wm * WM + r;
+                const uint32_t scale = block_scale(max(mine[r], other[r]));
+                const float inv = block_inverse(scale);
+                if (wn == 0 && fk == 0 && grow < rows) p.c_scales[(size_t)(row0 + grow) * stride + n0 / kBlock] = (uint8_t)scale;
+#pragma unroll
+                for (int j = 0; j < FO; ++j) {
+                    const f32x4& h = acc[2 * i + q][j];
+                    *reinterpret_cast<uint32_t*>(stage + granule<W>(16 * q + fr, j) + 4 * fk) = block_codes(h[0], h[1], h[2], h[3], inv, scale);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            const int rl = lane >> 2, gl = lane & 3;
+#pragma unroll
+            for (int it = 0; it < 2; ++it) {
+                const int row = 16 * it + rl, grow = wm * WM + 32 * i + row;
+                const u32x4 v = *reinterpret_cast<const u32x4*>(stage + granule<W>(row, gl));
+                if (grow < rows) *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(p.C) + (size_t)(row0 + grow) * p.N + col0 + gl * 16) = v;
+            }
+        }
+    }
+    __device__ __forceinline__ void finish(int) {}
+};
+
+// dg | du from dh and the saved g | u, in bf16 and as codes.  16 rows of dh at a time go through the patch in fp32, so that a
+// lane then has eight neighbouring columns of a row, sixteen lanes a block.
+struct GradStore {
+    BlockGemm p;
+
+    template <int FM, int FN>
+    __device__ __forceinline__ void tile(f32x4 (&acc)[FM][FN], int row0, int rows, int n0, int wm, int wn, int lane, uint8_t* stage,
+                                         uint8_t*, bool) {
+        constexpr int WM = FM * 16, W = 512;
+        static_assert(FN == 8 && 16 * W == FN * 32 * 32, "patch");
+        asm volatile("" : "+v"(lane));
+        const int fr = lane & 15, fk = lane >> 4, rl = lane >> 4, gl = lane & 15;
+        const int col = n0 + wn * 128 + 8 * gl;
+        const int stride = block_scale_stride(2 * p.N);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            u32x4 gv[4], uv[4];
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+                const int grow = wm * WM + 16 * i + 4 * it + rl;
+                gv[it] = uv[it] = u32x4{0u, 0u, 0u, 0u};
+                if (grow < rows && col < p.N) {
+                    const bf16_t* const src = p.gu + (size_t)(row0 + grow) * (2 * p.N) + col;
+                    gv[it] = *reinterpret_cast<const u32x4*>(src);
+                    uv[it] = *reinterpret_cast<const u32x4*>(src + p.N);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < FN; ++j) asm volatile("" : "+a"(acc[i][j]));
+#pragma unroll
+            for (int j = 0; j < FN; ++j) *reinterpret_cast<f32x4*>(stage + fr * W + (((4 * j + fk) ^ (2 * fr & 31)) << 4)) = acc[i][j];
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+                const int row = 4 * it + rl, grow = wm * WM + 16 * i + row;
+                float g[8], u[8], dg[8], du[8];
+                bf16x8_to_f32(gv[it], g);
+                bf16x8_to_f32(uv[it], u);
+                uint32_t tg = 0, tu = 0;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const f32x4 dh = *reinterpret_cast<const f32x4*>(stage + row * W + (((2 * gl + h) ^ (2 * row & 31)) << 4));
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int e = 4 * h + q;
+                        const float sg = __builtin_amdgcn_rcpf(1.f + __expf(-g[e]));
+                        dg[e] = dh[q] * u[e] * sg * (1.f + g[e] * (1.f - sg));
+                        du[e] = dh[q] * g[e] * sg;
+                        tg = max(tg, magnitude(dg[e]));
+                        tu = max(tu, magnitude(du[e]));
+                    }
+                }
+#pragma unroll
+                for (int d = 1; d < 16; d <<= 1) {
+                    tg = max(tg, (uint32_t)__shfl_xor((int)tg, d, 64));
+                    tu = max(tu, (uint32_t)__shfl_xor((int)tu, d, 64));
+                }
+                if (grow >= rows || col >= p.N) continue;
+                const size_t at = (size_t)(row0 + grow) * (2 * p.N) + col;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float(&v)[8] = h ? du : dg;
+                    const uint32_t scale = block_scale(h ? tu : tg);
+                    const float inv = block_inverse(scale);
+                    *reinterpret_cast<u32x4*>(p.dgu + at + h * p.N) =
+                        u32x4{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])};
+                    *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(p.C) + at + h * p.N) =
+                        u32x2{block_codes(v[0], v[1], v[2], v[3], inv, scale), block_codes(v[4], v[5], v[6], v[7], inv, scale)};
+                    if (gl == 0) p.c_scales[(size_t)(row0 + grow) * stride + (col + h * p.N) / kBlock] = (uint8_t)scale;
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void finish(int) {}
+};
+
+template <int MODE>
+struct StoreOf;
+template <>
+struct StoreOf<kBlockPlain> {
+    using type = PlainStore;
+};
+template <>
+struct StoreOf<kBlockSwiglu> {
+    using type = SwigluStore;
+};
+template <>
+struct StoreOf<kBlockGrad> {
+    using type = GradStore;
+};
+
+template <int MODE, int BM, bool IDLE_SKIP>
+__device__ __forceinline__ void block_body(const BlockGemm& p, int ntn, uint8_t* smem) {
+    BlockScales<BM / 32, MODE == kBlockSwiglu ? 2 : 1> scales;
+    scales.A = p.a_scales;
+    scales.B0 = p.b0_scales;
+    scales.B1 = p.b1_scales;
+    scales.stride = block_scale_stride(p.K);
+    scales.n_blocks = p.N / kBlock;
+    fp8_body<BM, MODE == kBlockSwiglu, IDLE_SKIP, true>(p.A, p.offsets, p.E, p.N, p.K, p.B0, p.B1, ntn, scales,
+                                                        typename StoreOf<MODE>::type{p}, smem);
+}
+
+// Tiles of 256, 192 or 128 rows, chosen on the device from the rows that every expert really has; `rows` != 0: those.
+template <int MODE, bool IDLE_SKIP>
+__global__ __launch_bounds__(256) void block_persist_kernel(BlockGemm p, int ntn, int rows) {
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+    const int height = rows != 0 ? rows : pick_height(kCostFp8, p.offsets, p.E, ntn, p.K / 128, threadIdx.x & 63);
+    if (height == 256) block_body<MODE, 256, IDLE_SKIP>(p, ntn, smem);
+    else if (height == 192) block_body<MODE, 192, IDLE_SKIP>(p, ntn, smem);
+    else block_body<MODE, 128, IDLE_SKIP>(p, ntn, smem);
+}
+
+template <int MODE>
+void launch_persist(const BlockGemm& p, hipStream_t s) {
+    constexpr int OUTN = MODE == kBlockSwiglu ? 128 : 256;
+    constexpr size_t smem = (size_t)(3 * 256 + 2 * 256) * 128;
+    const int ntn = (p.N + OUTN - 1) / OUTN;
+    const bool idle_skip = persist_idle_skip(p.E);
+    auto kern = idle_skip ? block_persist_kernel<MODE, true> : block_persist_kernel<MODE, false>;
+    static OncePerDevice lds[2];
+    allow_lds(lds[idle_skip], reinterpret_cast<const void*>(kern), (int)smem);
+    const int grid = min(persist_grid(), grid_for(p.r_max, p.E, 128, ntn));
+    hipLaunchKernelGGL(kern, dim3(grid), dim3(256), smem, s, p, ntn, persist_tile_rows());
+}
+
+}  // namespace
+
+void launch_block_persist(int mode, const BlockGemm& p, hipStream_t s) {
+    if (mode == kBlockPlain) launch_persist<kBlockPlain>(p, s);
+    else if (mode == kBlockSwiglu) launch_persist<kBlockSwiglu>(p, s);
+    else launch_persist<kBlockGrad>(p, s);
+}
+
+}  // namespace moe
