@@ -3,9 +3,10 @@
 //
 // A k-tile is a block along the contraction, so the scaled matrix instruction takes the operands' scales as it takes their
 // codes: no instruction is added for any accumulator.  A lane needs one byte for every row of its activation fragments and, the
-// weights' blocks being 128 wide, one (gate and up: two) for all its weight rows.  The bytes of four k-tiles are one load; it is
-// issued two k-tiles ahead of its first use, behind the loads whose end the k loop's own wait covers, so that no wait is
-// added either.
+// weights' blocks being 128 wide, one (gate and up: two) for all its weight rows.  A wave loads the bytes
+// of four k-tiles of each of its rows once, a row to a lane, and the quarters of the wave exchange them in registers; the
+// loads are issued two k-tiles ahead of their use, in front of those whose end the k loop's own wait leaves open, so that no
+// wait is added either.
 #include "fp8_block.h"
 #include "gemm_persist_fp8.h"
 
@@ -16,69 +17,138 @@ namespace {
 // FM row fragments and, along the weight rows, NB blocks of a wave (gate and up, or one)
 template <int FM, int NB>
 struct BlockScales {
-    static constexpr bool BRANCHES = true;
-    const uint8_t *A, *B0, *B1;   // scales of all rows, and of the weights' blocks
-    int stride, n_blocks;         // bytes of a row of scales; blocks along N
+    static constexpr int NR = (FM + 3) / 4;   // loads of 64 rows
+    const uint8_t *A, *B0, *B1;               // scales of all rows, and of the weights' blocks: less than 4 GiB each, a 128th of
+    int stride, n_blocks;                     // the codes.  Bytes of a row of scales; blocks along N
 
     struct Rows {
-        const uint8_t *a, *b[NB];
-        int last;                 // last valid row of the tile
+        uint32_t a, b;                        // where the tile's scales start
+        int bytes;                            // of its rows of scales
     };
-    Rows cur, next;
-    int row;                      // of the lane in the tile's first fragment
-    uint32_t sa[FM], na[FM], sb[NB], nb[NB];
-    bool turn;
+    Rows cur, next, from;
+    int at[NR];                               // lane l loads for the wave's rows l and l + 64
+    uint32_t ra[NR], rb[NB];                  // as loaded: four k-tiles
+    uint32_t wa[NR], wb[NB];                  // the byte of the k-tile behind the one that is multiplied comes first
+    uint32_t half[NR][2];
+    uint32_t sa[FM], na[FM], sb[NB], loaded[NB];
+    int k;
+    bool fresh, wanted;
 
     __device__ __forceinline__ Rows rows_of(const PTile& t, int wn) const {
-        Rows r;
-        r.a = uni(A + (size_t)t.row0 * stride);
         // behind the last block the last one again: those columns are not stored
         const int block = min(t.n0 / kBlock + (NB == 1 ? wn : 0), n_blocks - 1);
-        const size_t at = ((size_t)t.expert * n_blocks + block) * stride;
-        r.b[0] = uni(B0 + at);
-        if constexpr (NB == 2) r.b[1] = uni(B1 + at);
-        r.last = t.rows - 1;
-        return r;
+        return {uni((uint32_t)t.row0 * (uint32_t)stride), uni((uint32_t)(t.expert * n_blocks + block) * (uint32_t)stride),
+                uni(t.rows * stride)};
     }
-    static __device__ __forceinline__ uint32_t word(const uint8_t* p) { return *(const __attribute__((address_space(1))) uint32_t*)p; }
-    // the bytes of k-tiles 4 g .. 4 g + 3
-    __device__ __forceinline__ void load(const Rows& r, int g) {
-        int first = row;
-        asm volatile("" : "+v"(first));   // or the rows' offsets are kept across the k loop
-#pragma unroll
-        for (int i = 0; i < FM; ++i)
-            na[i] = word(r.a + (uint32_t)(__mul24(min(first + 16 * i, r.last), stride) + 4 * g));
-        int same = 0;
-        asm volatile("" : "+v"(same));    // vector loads: scalar ones would be waited for together with LDS reads
-#pragma unroll
-        for (int i = 0; i < NB; ++i) nb[i] = word(r.b[i] + (uint32_t)(same + 4 * g));
+    // a word of a buffer; of one without bytes 0, which no memory is asked for
+    static __device__ __forceinline__ uint32_t word(const uint8_t* base, int bytes, int lane_at, int from) {
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, bytes, 0x00027000);
+        return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rsrc, lane_at, from, 0);
     }
-    __device__ __forceinline__ void start(const PTile& t, int row_, int wn) {
-        row = row_;
-        cur = rows_of(t, wn);
-        load(cur, 0);
+    __device__ __forceinline__ void load_a(int i) { ra[i] = word(A + from.a, wanted ? from.bytes : 0, at[i], wanted ? k : 0); }
+    __device__ __forceinline__ void load_b(int i) { rb[i] = word((i ? B1 : B0) + from.b, wanted ? stride : 0, 0, wanted ? k : 0); }
+    // na[i] of a lane: what the lane of row 16 i + lane % 16 holds.  The quarters of 16 lanes, each in all four
+    __device__ __forceinline__ void spread_half(int i) {
+        const auto h = __builtin_amdgcn_permlane32_swap(wa[i], wa[i], false, false);
+        half[i][0] = h[0];
+        half[i][1] = h[1];
+    }
+    __device__ __forceinline__ void spread_quarter(int i, int h) {
+        if (4 * i + 2 * h >= FM) return;
+        const auto q = __builtin_amdgcn_permlane16_swap(half[i][h], half[i][h], false, false);
+        na[4 * i + 2 * h] = q[0];
+        na[4 * i + 2 * h + 1] = q[1];
+    }
+    __device__ __forceinline__ void start(const PTile& t, int first_row, int lane, int wn) {
+        cur = next = from = rows_of(t, wn);
+        wanted = true;
+        k = 0;
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            at[i] = (first_row + lane + 64 * i) * stride;
+            load_a(i);
+        }
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            load_b(i);
+            wb[i] = sb[i] = uni(rb[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            wa[i] = ra[i];
+            spread_half(i);
+            spread_quarter(i, 0);
+            spread_quarter(i, 1);
+        }
 #pragma unroll
         for (int i = 0; i < FM; ++i) sa[i] = na[i];
-#pragma unroll
-        for (int i = 0; i < NB; ++i) sb[i] = nb[i];
-        next = cur;
     }
     // t is the tile after the one that begins
     __device__ __forceinline__ void next_tile(const PTile& t, int wn) {
         cur = next;
         if (t.valid) next = rows_of(t, wn);
     }
-    __device__ __forceinline__ f32x4 mfma(const i32x8& w, const i32x8& a, const f32x4& c, int i, int half) const {
-        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, c, 0, 0, 0, (int)sb[NB == 2 ? half : 0], 0, (int)sa[i]);
+    __device__ __forceinline__ f32x4 mfma(const i32x8& w, const i32x8& a, const f32x4& c, int i, int h) const {
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, c, 0, 0, 0, (int)sb[NB == 2 ? h : 0], 0, (int)sa[i]);
     }
-    // from k-tile kt to the one behind it (of the next tile, behind the last)
-    __device__ __forceinline__ void begin_step(int kt, int KT) { turn = kt + 1 == KT || ((kt + 1) & 3) == 0; }
-    __device__ __forceinline__ void step_row(int i) { sa[i] = turn ? na[i] : sa[i] >> 8; }
-    __device__ __forceinline__ void end_step(int kt, int KT) {
+    // What there is to do in the second half of k-tile kt, in pieces of a few instructions, so that each is covered by a matrix
+    // instruction: the next k-tile's scales to their lanes, and the load for the one behind it if it is the first of four (or of
+    // the next tile).  No branches: they split the k loop, and what is loaded is then copied, and waited for, at the split.
+    static constexpr int PIECES = 16;
+    __device__ __forceinline__ void piece(int p, int kt, int KT) {
+        if (p == 0) fresh = kt + 1 == KT || ((kt + 1) & 3) == 0;
+        if (p == 1 || (p == 2 && NR == 2)) wa[p - 1] = fresh ? ra[p - 1] : wa[p - 1] >> 8;
+        if (p == 3) {
 #pragma unroll
-        for (int i = 0; i < NB; ++i) sb[i] = turn ? nb[i] : sb[i] >> 8;
-        if (kt + 2 == KT) load(next, 0);
-        else if (kt + 2 < KT && ((kt + 2) & 3) == 0) load(cur, (kt + 2) >> 2);
+            for (int i = 0; i < NB; ++i) loaded[i] = uni(rb[i]);
+        }
+        if (p == 4) {
+#pragma unroll
+            for (int i = 0; i < NB; ++i) wb[i] = fresh ? loaded[i] : wb[i] >> 8;
+        }
+        if (p == 5 || (p == 8 && NR == 2)) spread_half((p - 5) / 3);
+        if (p == 6 || (p == 9 && NR == 2)) spread_quarter((p - 6) / 3, 0);
+        if (p == 7 || (p == 10 && NR == 2)) spread_quarter((p - 7) / 3, 1);
+        if (p == 11) {
+            const bool over = kt + 2 >= KT;
+            from.a = over ? next.a : cur.a;
+            from.b = over ? next.b : cur.b;
+            from.bytes = over ? next.bytes : cur.bytes;
+            k = over ? kt + 2 - KT : kt + 2;
+            wanted = (k & 3) == 0;
+        }
+        if (p == 12 || (p == 13 && NR == 2)) load_a(p - 12);
+        if (p == 14 || (p == 15 && NB == 2)) load_b(p - 14);
+    }
+    __device__ __forceinline__ void step_row(int i) {
+        sa[i] = na[i];
+        asm volatile("" : "+v"(sa[i]));       // here, between matrix instructions, and not at the loop's end
+    }
+    // behind matrix instruction `slot` of `slots`, four to a row
+    __device__ __forceinline__ void behind(int slot, int slots, int kt, int KT) {
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p)
+            if (p * slots / PIECES == slot) piece(p, kt, KT);
+        const int all = 10 * slots / PIECES + 1;   // na is complete
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+            if (min(max(4 * i + 4, all + i), slots - 1) == slot && 4 * i + 4 <= slots - 1) step_row(i);
+    }
+    __device__ __forceinline__ void end_step() {
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+            if (4 * i + 4 > 4 * FM - 1) step_row(i);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) sb[i] = wb[i];
+    }
+    // a k-tile whose products are left out
+    __device__ __forceinline__ void skip(int kt, int KT) {
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) piece(p, kt, KT);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) sa[i] = na[i];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) sb[i] = wb[i];
     }
 };
 

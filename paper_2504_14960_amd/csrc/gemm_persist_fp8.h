@@ -30,15 +30,14 @@ namespace {
 
 // no scales inside the product
 struct NoScales {
-    static constexpr bool BRANCHES = false;
-    __device__ __forceinline__ void start(const PTile&, int, int) {}
+    __device__ __forceinline__ void start(const PTile&, int, int, int) {}
     __device__ __forceinline__ void next_tile(const PTile&, int) {}
     __device__ __forceinline__ f32x4 mfma(const i32x8& w, const i32x8& a, const f32x4& c, int, int) const {
         return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, c, 0, 0, 0, 0, 0, 0);
     }
-    __device__ __forceinline__ void begin_step(int, int) {}
-    __device__ __forceinline__ void step_row(int) {}
-    __device__ __forceinline__ void end_step(int, int) {}
+    __device__ __forceinline__ void behind(int, int, int, int) {}
+    __device__ __forceinline__ void end_step() {}
+    __device__ __forceinline__ void skip(int, int) {}
 };
 
 // A [rows, K] E4M3, B0/B1 [E, N, K] E4M3 (SWIGLU: gate and up), K a multiple of 128 and at least 256.
@@ -88,7 +87,7 @@ __device__ __forceinline__ void fp8_body(
         if (!t.valid) return;
         c_a = t.a; c_b0 = t.b0; c_b1 = t.b1; c_alim = t.a_lim; c_blim = t.b_lim;
         c_row0 = t.row0; c_rows = t.rows; c_n0 = t.n0;
-        scales.start(t, wm * WM + fr, wn);
+        scales.start(t, wm * WM, lane, wn);
     }
     auto fetch_next_tile = [&](int i) {
         const PTile t = sched.get(i, A, B0, B1b, N, (size_t)K, OUTN);
@@ -199,7 +198,7 @@ __device__ __forceinline__ void fp8_body(
     // Half a period: all rows by the weight fragments of half HALF.  Slots of {one MFMA; the next fragment's reads; at most one
     // direct load}.  Half 0 reads the weight fragments of half 1 (sb: this k-tile); half 1 the activation fragments, each
     // behind its last use, and the weight fragments of half 0 (sa, sb: the next k-tile).
-    auto half_period = [&](auto half, const uint8_t* sa, const uint8_t* sb, int ld_begin, int ld_end, uint8_t* ld_b, uint8_t* ld_a) {
+    auto half_period = [&](auto half, int kt, const uint8_t* sa, const uint8_t* sb, int ld_begin, int ld_end, uint8_t* ld_b, uint8_t* ld_a) {
         constexpr int HALF = decltype(half)::value;
         int ld = ld_begin;
 #pragma unroll
@@ -211,10 +210,8 @@ __device__ __forceinline__ void fp8_body(
             // the first MFMA waits for the reads before this half: keep the new ones behind it
             if (slot == 0) __builtin_amdgcn_sched_barrier(0);
             if (slot % 4 == 1 && slot / 4 < FH) read_b(sb, (1 - HALF) * FH + slot / 4);
-            if (HALF == 1 && slot % FH == FH - 1) {
-                read_a(sa, i);
-                scales.step_row(i);
-            }
+            if (HALF == 1) scales.behind(slot, NSLOT, kt, KT);
+            if (HALF == 1 && slot % FH == FH - 1) read_a(sa, i);
             if (ld < ld_end && slot == 1 + (ld - ld_begin) * NSLOT / (ld_end - ld_begin)) {
                 fetch_one(ld, ld_b, ld_a);
                 ++ld;
@@ -277,33 +274,22 @@ __device__ __forceinline__ void fp8_body(
 #pragma unroll
                 for (int i = 0; i < PE; ++i) fetch_one(i, b_region + b0, a_region + a0);
                 rotate();
-                scales.begin_step(kt, KT);
-#pragma unroll
-                for (int i = 0; i < FM; ++i) scales.step_row(i);
-                scales.end_step(kt, KT);
+                scales.skip(kt, KT);
             }
         }
         for (; kt < KT; ++kt) {
             advance(kt);
             __builtin_amdgcn_sched_barrier(0);
             // half 0: late(kt+2)
-            half_period(First{}, a_region + a0, b_region + b0, PE, NLOAD, b_region + (DEEP_B ? b2 : b1), a_region + (DEEP_B ? a1 : a2));
+            half_period(First{}, kt, a_region + a0, b_region + b0, PE, NLOAD, b_region + (DEEP_B ? b2 : b1), a_region + (DEEP_B ? a1 : a2));
             // all but the PL youngest loads (those of late(kt+2)) have landed; this
             // wave's fragment reads of k-tile kt are in registers
             __builtin_amdgcn_s_waitcnt((PL & 0xF) | ((PL >> 4) << 14));
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
             // half 1: first fragments of k-tile kt+1, early(kt+2) into the freed slot
-            scales.begin_step(kt, KT);
-            half_period(Second{}, a_region + a1, b_region + b1, 0, PE, b_region + b0, a_region + a0);
-            if constexpr (Scales::BRANCHES) {
-                // named here, or the matrix instructions of the whole period are moved behind the branches of end_step
-#pragma unroll
-                for (int i = 0; i < FM; ++i)
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) asm volatile("" : "+a"(acc[i][j]));
-            }
-            scales.end_step(kt, KT);
+            half_period(Second{}, kt, a_region + a1, b_region + b1, 0, PE, b_region + b0, a_region + a0);
+            scales.end_step();
             rotate();
         }
         uint8_t* stage = (DEEP_B ? b_region + b2 : a_region + a2) + wave * (32 * FN * 32);
