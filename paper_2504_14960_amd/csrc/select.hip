@@ -4,6 +4,8 @@
 //
 // Scores decide what is selected, so they are rounded to fp32 once, from 64 bits: two programs that follow the definition then
 // select the same experts.
+#include <type_traits>
+
 #include "common.h"
 #include "wave_sum.h"
 
@@ -29,6 +31,13 @@ __device__ __forceinline__ double select_key(float choice, int e) {
     choice = fminf(choice, __FLT_MAX__) + 0.f;               // -0 to +0
     uint64_t b = __builtin_bit_cast(uint64_t, (double)choice);
     b |= (uint64_t)(choice < 0.f ? e : 255 - e);
+    return __builtin_bit_cast(double, b);
+}
+// the same with kLow for kNever; the bias has no NaN
+__device__ __forceinline__ double list_key(float logit, float choice, int e) {
+    choice = logit > -INFINITY ? __builtin_amdgcn_fmed3f(choice, -__FLT_MAX__, __FLT_MAX__) : -__FLT_MAX__;
+    uint64_t b = __builtin_bit_cast(uint64_t, (double)choice);
+    b |= (uint64_t)(uint32_t)(choice < 0.f ? e : 255 - e);
     return __builtin_bit_cast(double, b);
 }
 __device__ __forceinline__ int key_expert(double key) {
@@ -66,16 +75,12 @@ __device__ __forceinline__ double sigmoid64(float x) { return 1. / (1. + exp(-(d
 // exp(x - m) for x <= m; of equal infinities 1
 __device__ __forceinline__ double shifted_exp64(float x, float m) { return x == m ? 1. : exp((double)x - (double)m); }
 
+// ---- any number of experts a token ----
 constexpr int kSelectWaves = 4;
 
-// One token to a wave, any K, any groups.  Lane l holds experts l + 64 j.
+// Token t by a wave, any groups, scores in 64 bits.  Lane l holds experts l + 64 j; keys, best: LDS of this wave, 64 VPL each.
 template <int VPL>
-__global__ __launch_bounds__(64 * kSelectWaves) void select_wave_kernel(SelectArgs p) {
-    __shared__ double keys[kSelectWaves][64 * VPL];
-    __shared__ double best[kSelectWaves][64 * VPL];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int t = blockIdx.x * kSelectWaves + wave;
-    if (t >= p.T) return;
+__device__ __forceinline__ void select_token(const SelectArgs& p, int t, int lane, double* keys, double* best) {
     const float* const row = p.logits + (size_t)t * p.E;
     float x[VPL], m = -INFINITY;
 #pragma unroll
@@ -104,7 +109,7 @@ __global__ __launch_bounds__(64 * kSelectWaves) void select_wave_kernel(SelectAr
         // a lane takes a group: the sum of its best keys, then its rank among the groups
         const int size = p.E / p.groups;
 #pragma unroll
-        for (int j = 0; j < VPL; ++j) keys[wave][lane + 64 * j] = key[j];
+        for (int j = 0; j < VPL; ++j) keys[lane + 64 * j] = key[j];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
         double mine[VPL];
@@ -115,7 +120,7 @@ __global__ __launch_bounds__(64 * kSelectWaves) void select_wave_kernel(SelectAr
             if (g < p.groups) {
                 double first = kNever, second = kNever;
                 for (int i = 0; i < size; ++i) {
-                    const double k = keys[wave][g * size + i];
+                    const double k = keys[g * size + i];
                     second = k > first ? first : max_key(second, k);
                     first = max_key(first, k);
                 }
@@ -124,14 +129,14 @@ __global__ __launch_bounds__(64 * kSelectWaves) void select_wave_kernel(SelectAr
                     if (p.group_best > 1 && second > kNever) sum += key_choice(second);
                     mine[j] = select_key(sum, g);
                 }
-                best[wave][g] = mine[j];
+                best[g] = mine[j];
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
         int rank[VPL] = {};
         for (int g = 0; g < p.groups; ++g) {
-            const double other = best[wave][g];
+            const double other = best[g];
 #pragma unroll
             for (int j = 0; j < VPL; ++j) rank[j] += other > mine[j];
         }
@@ -139,13 +144,13 @@ __global__ __launch_bounds__(64 * kSelectWaves) void select_wave_kernel(SelectAr
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int j = 0; j < VPL; ++j)
-            if (lane + 64 * j < p.groups && rank[j] >= p.topk_groups) best[wave][lane + 64 * j] = kNever;
+            if (lane + 64 * j < p.groups && rank[j] >= p.topk_groups) best[lane + 64 * j] = kNever;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int j = 0; j < VPL; ++j) {
             const int e = lane + 64 * j;
-            if (e < p.E && !(best[wave][e / size] > kNever)) key[j] = kNever;
+            if (e < p.E && !(best[e / size] > kNever)) key[j] = kNever;
         }
     }
     int my_e = -1;
@@ -171,6 +176,282 @@ __global__ __launch_bounds__(64 * kSelectWaves) void select_wave_kernel(SelectAr
         p.idx[(size_t)t * p.K + lane] = my_e;
         p.gate[(size_t)t * p.K + lane] = (float)(g * (double)p.scale);
     }
+}
+
+template <int VPL>
+__global__ __launch_bounds__(64 * kSelectWaves) void select_wave_kernel(SelectArgs p) {
+    __shared__ double keys[kSelectWaves][64 * VPL], best[kSelectWaves][64 * VPL];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = blockIdx.x * kSelectWaves + wave;
+    if (t < p.T) select_token<VPL>(p, t, threadIdx.x & 63, keys[wave], best[wave]);
+}
+
+// ---- up to eight experts a token ----
+// L lanes to a token, a run of `run` <= VPL experts to a lane (where there are groups: a group).  A lane sorts its keys in
+// eights and merges them to its eight largest, and the lanes of a token merge theirs: bitonic networks of v_max_f64 and
+// v_min_f64, which run at the full rate and carry the expert's index along in the key.
+//
+// Bound by the vector unit.  Scores in 64 bits would be half of its work, so they are first formed in fp32, and what was
+// selected by them stands if no difference that decided it is within what they may be off; else the wave does it all again
+// in 64 bits (a token in some hundreds).
+constexpr double kLow = -(double)__FLT_MAX__;   // keys up to here belong to experts that are not selected
+
+__device__ __forceinline__ double min_key(double a, double b) {
+    double r;
+    asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ void order(double& a, double& b) {   // the larger one first
+    const double hi = max_key(a, b), lo = min_key(a, b);
+    a = hi;
+    b = lo;
+}
+// eight keys in descending order (odd-even merging: 19 comparisons)
+__device__ __forceinline__ void sort8(double* v) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) order(v[i], v[i + 1]);
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+        order(v[i], v[i + 2]);
+        order(v[i + 1], v[i + 3]);
+        order(v[i + 1], v[i + 2]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) order(v[i], v[i + 4]);
+    order(v[2], v[4]);
+    order(v[3], v[5]);
+    order(v[1], v[2]);
+    order(v[3], v[4]);
+    order(v[5], v[6]);
+}
+// the eight largest of two descending eights, descending: a is the one, b the other; next: the largest key left out so far
+__device__ __forceinline__ void merge8(double (&a)[8], const double (&b)[8], double& next) {
+    double out[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        out[i] = min_key(a[i], b[7 - i]);
+        a[i] = max_key(a[i], b[7 - i]);
+    }
+#pragma unroll
+    for (int d = 4; d > 0; d >>= 1)
+#pragma unroll
+        for (int i = 0; i < d; ++i) out[i] = max_key(out[i], out[i + d]);
+    next = max_key(next, out[0]);
+#pragma unroll
+    for (int d = 4; d > 0; d >>= 1)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if ((i & d) == 0) order(a[i], a[i + d]);
+}
+// the same of a lane's list and that of its partner: neighbouring lanes, pairs, fours and eights
+template <int CTRL>
+__device__ __forceinline__ void merge_lanes(double (&a)[8], double& next) {
+    double b[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) b[i] = dpp<CTRL>(a[i]);
+    next = max_key(next, dpp<CTRL>(next));
+    merge8(a, b, next);
+}
+
+// How far apart two keys are that fp32 scores tell apart for certain.  A score is off by less than 2^-17 of itself (the rounding of
+// the exponential's argument, at most 88, and a few units; a softmax's sum), and by less than 2^-20 altogether unless a softmax's
+// probability is near 1, where it is 2^-19.
+__device__ __forceinline__ float doubt(float key, bool biased) {
+    return biased ? fmaxf(1.f, fabsf(key)) * 0x1p-18f : fabsf(key) * 0x1p-16f;
+}
+
+// exp(d) for d <= 0 to about a unit in the last place: the product's rounding is made up for
+__device__ __forceinline__ float exp_near(float d) {
+    d = fmaxf(d, -150.f);   // 0 from there on, and the lines below would take infinities apart
+    const float hi = d * 1.44269502f, lo = fmaf(d, 1.44269502f, -hi) + d * 1.92596303e-8f;
+    const float e = __builtin_amdgcn_exp2f(hi);
+    return fmaf(e, lo * 0.693147181f, e);
+}
+
+template <int VPL, int L, bool VEC, bool SIGMOID>
+__global__ __launch_bounds__(256, 4) void select_lists_kernel(SelectArgs p, int run) {
+    constexpr int TOKENS = 256 / L, SLOTS = (8 + L - 1) / L, LDB = VPL + 4;
+    __shared__ __attribute__((aligned(16))) float biases[L * LDB];   // 4 more floats a lane: other banks
+    __shared__ double keys[4][kMaxExperts], best[4][kMaxExperts];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int sub = lane & (L - 1), e0 = sub * run;
+    const int mine = min(run, p.E - e0);   // experts of this lane; none, or fewer, in the last lanes
+    const bool biased = p.bias != nullptr;
+    for (int i = threadIdx.x; i < L * VPL; i += 256) {
+        const int l = i / VPL, j = i % VPL, e = l * run + j;
+        const float b = biased && j < run && e < p.E ? p.bias[e] : 0.f;
+        biases[l * LDB + j] = b == b ? b : -INFINITY;
+    }
+    __syncthreads();
+    auto lanes = [](auto v, auto&& f) {
+        if constexpr (L > 1) v = f(v, dpp<0xB1>(v));
+        if constexpr (L > 2) v = f(v, dpp<0x4E>(v));
+        if constexpr (L > 4) v = f(v, dpp<0x141>(v));
+        if constexpr (L > 8) v = f(v, dpp<0x140>(v));
+        return v;
+    };
+    auto add = [](auto a, auto b) { return a + b; };
+    for (int t0 = blockIdx.x * TOKENS; t0 < p.T; t0 += gridDim.x * TOKENS) {   // uniform trip count: lanes work together
+        const int t = t0 + (int)threadIdx.x / L;
+        const bool valid = t < p.T;
+        const float* const row = p.logits + (size_t)(valid ? t : p.T - 1) * p.E;
+        float x[VPL];
+        if constexpr (VEC) {
+#pragma unroll
+            for (int j = 0; j < VPL; j += 4) {
+                f32x4 v = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                if (j < mine) v = *reinterpret_cast<const f32x4*>(row + e0 + j);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) x[j + q] = v[q];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < VPL; ++j) x[j] = j < mine ? row[e0 + j] : -INFINITY;
+        }
+        // keys from scores in fp32
+        float m = -INFINITY;
+        double z = 1.;
+        float rz = 1.f;
+        if constexpr (!SIGMOID) {
+#pragma unroll
+            for (int j = 0; j < VPL; ++j) {
+                x[j] = x[j] > -INFINITY ? fminf(x[j], __FLT_MAX__) : -INFINITY;   // of infinite ones the differences are 0
+                m = fmaxf(m, x[j]);
+            }
+            m = lanes(m, [](float a, float b) { return fmaxf(a, b); });
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < VPL; ++j) {
+                const float e = exp_near(x[j] - m);          // 0 for -inf
+                sum += e;
+                x[j] = x[j] > -INFINITY ? e : -INFINITY;     // from here on
+            }
+            z = lanes((double)sum, add);
+            rz = 1.f / (float)z;
+        }
+        // the lane's eight largest, and the largest behind them
+        double list[8], next = kLow;
+#pragma unroll
+        for (int j = 0; j < VPL; j += 8) {
+            double key[8];
+#pragma unroll
+            for (int q = 0; q < 8; q += 4) {
+                const f32x4 b = *reinterpret_cast<const f32x4*>(&biases[sub * LDB + j + q]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float v = x[j + q + i];
+                    const float s = SIGMOID ? __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -1.44269504f)) : v * rz;
+                    key[q + i] = list_key(v, s + b[i], e0 + j + q + i);
+                }
+            }
+            sort8(key);
+            if (j == 0) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) list[i] = key[i];
+            } else {
+                merge8(list, key, next);
+            }
+        }
+        bool sure = true, keep = true;
+        if (p.groups > 1) {
+            // this lane's group: its value, its rank, and the largest value that ranks behind it
+            float total = key_choice(list[0]);
+            if (p.group_best > 1 && list[1] > kLow) total += key_choice(list[1]);
+            if (!(list[0] > kLow)) total = -INFINITY;
+            int rank = 0;
+            float below = -INFINITY;
+#pragma unroll
+            for (int d = 1; d < L; ++d) {
+                const float other = __shfl_xor(total, d, 64);
+                const bool ahead = other > total || (other == total && (sub ^ d) < sub);
+                rank += ahead;
+                below = ahead ? below : fmaxf(below, other);
+            }
+            keep = rank < p.topk_groups && total > -INFINITY;
+            if (rank == p.topk_groups - 1 && below > -INFINITY) sure = total - below > 2.f * doubt(total, biased);
+            if (!keep) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) list[i] = kLow;
+                next = kLow;
+            }
+        }
+        if constexpr (L > 1) merge_lanes<0xB1>(list, next);
+        if constexpr (L > 2) merge_lanes<0x4E>(list, next);
+        if constexpr (L > 4) merge_lanes<0x141>(list, next);
+        if constexpr (L > 8) merge_lanes<0x140>(list, next);
+        // neighbours among the first K and the one behind them
+        float last = key_choice(list[0]);
+#pragma unroll
+        for (int k = 1; k <= 8; ++k) {
+            const double key = k < 8 ? list[k] : next;
+            if (k <= p.K && key > kLow) {
+                const float c = key_choice(key);
+                sure &= last - c > doubt(last, biased);
+                last = c;
+            }
+        }
+        const uint64_t unsure = __ballot(!sure && valid);
+        // slot k in lane k mod L
+        double g[SLOTS], sum = 0.;
+        int e[SLOTS];
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i) {
+            const int k = sub + L * i;
+            double found = kLow;
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (q == k) found = list[q];
+            e[i] = k < p.K && found > kLow ? key_expert(found) : -1;
+            g[i] = 0.;
+            if (e[i] >= 0) g[i] = SIGMOID ? sigmoid64(row[e[i]]) : shifted_exp64(fminf(row[e[i]], __FLT_MAX__), m);
+            sum += g[i];
+        }
+        if (p.renorm) z = lanes(sum, add);
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i) {
+            const int k = sub + L * i;
+            if (!valid || k >= p.K) continue;
+            p.idx[(size_t)t * p.K + k] = e[i];
+            p.gate[(size_t)t * p.K + k] = z > 0. ? (float)(g[i] / z * (double)p.scale) : 0.f;
+        }
+        // tokens in doubt once more, by the whole wave and in 64 bits
+        for (int first = 0; unsure && first < 64; first += L)
+            if (unsure >> first & ((1ull << L) - 1)) select_token<kMaxExperts / 64>(p, t0 + (wave * 64 + first) / L, lane, keys[wave], best[wave]);
+    }
+}
+
+template <int VPL, int L>
+bool launch_lists_of(const SelectArgs& p, int run, hipStream_t s) {
+    const int grid = min((p.T + 256 / L - 1) / (256 / L), 256 * 8);
+    auto go = [&](auto vec, auto sigmoid) {
+        hipLaunchKernelGGL((select_lists_kernel<VPL, L, decltype(vec)::value, decltype(sigmoid)::value>), dim3(grid), dim3(256), 0, s, p, run);
+    };
+    const std::true_type yes;
+    const std::false_type no;
+    if (run % 4 == 0 && p.E % 4 == 0) p.sigmoid ? go(yes, yes) : go(yes, no);
+    else p.sigmoid ? go(no, yes) : go(no, no);
+    return true;
+}
+
+// false where the groups do not fit the lanes
+bool launch_lists(const SelectArgs& p, hipStream_t s) {
+    int L = 1, run;
+    if (p.groups > 1) {
+        while (L < p.groups) L <<= 1;
+        run = p.E / p.groups;
+    } else {
+        while (L < 8 && p.E > 8 * L) L <<= 1;
+        run = ((p.E + L - 1) / L + 3) & ~3;
+    }
+    if (L > 16 || run > 32) return false;
+    auto of = [&](auto vpl) {
+        constexpr int VPL = decltype(vpl)::value;
+        return L <= 2 ? launch_lists_of<VPL, 2>(p, run, s) : L == 4 ? launch_lists_of<VPL, 4>(p, run, s)
+             : L == 8 ? launch_lists_of<VPL, 8>(p, run, s) : launch_lists_of<VPL, 16>(p, run, s);
+    };
+    if (L == 1) return launch_lists_of<8, 1>(p, run, s);   // up to eight experts
+    if (run <= 8) return of(std::integral_constant<int, 8>{});
+    if (run <= 16) return of(std::integral_constant<int, 16>{});
+    return of(std::integral_constant<int, 32>{});
 }
 
 // ---- the gradient ----
@@ -339,6 +620,7 @@ __global__ __launch_bounds__(256) void bias_step_kernel(const N* __restrict__ ro
 void launch_select(const float* logits, const float* bias, int T, int E, int K, moe_score_t score, int groups, int topk_groups,
                    int group_best, int renorm, float scale, int32_t* idx, float* gate, hipStream_t s) {
     const SelectArgs p = {logits, bias, idx, gate, scale, T, E, K, score == MOE_SCORE_SIGMOID, groups, topk_groups, group_best, renorm};
+    if (K <= 8 && launch_lists(p, s)) return;
     const dim3 grid((T + kSelectWaves - 1) / kSelectWaves), block(64 * kSelectWaves);
     if (E <= 64) hipLaunchKernelGGL(select_wave_kernel<1>, grid, block, 0, s, p);
     else if (E <= 128) hipLaunchKernelGGL(select_wave_kernel<2>, grid, block, 0, s, p);
