@@ -58,30 +58,27 @@ __global__ __launch_bounds__(256) void block_rows_quantize_kernel(const void* __
         }
 }
 
-// One token to a wave: its row read and quantised once, stored to each of its rows of the expert order.
+// 512 values of a token to a wave, read and quantised once and stored to each of its rows of the expert order.
 __global__ __launch_bounds__(256) void permute_copy_block_kernel(const bf16_t* __restrict__ x,
                                                                  const int32_t* __restrict__ row_of_assign, int T, int K, int H,
                                                                  int r_max, uint8_t* __restrict__ codes,
                                                                  uint8_t* __restrict__ scales) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int stride = block_scale_stride(H);
-    for (int t = blockIdx.x * 4 + wave; t < T; t += gridDim.x * 4) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int stride = block_scale_stride(H), pieces = (H + 511) / 512;
+    const int64_t items = (int64_t)T * pieces;
+    for (int64_t item = (int64_t)blockIdx.x * 4 + wave; item < items; item += (int64_t)gridDim.x * 4) {
+        const int t = (int)(item / pieces), c = (int)(item - (int64_t)t * pieces) * 512 + 8 * lane;
+        float f[8] = {};
+        if (c < H) load8<true>(x, (size_t)t * H + c, f);
         int my_row = lane < K ? row_of_assign[(size_t)t * K + lane] : -1;
         if ((unsigned)my_row >= (unsigned)r_max) my_row = -1;
-        const uint64_t kept = __ballot(my_row >= 0);
-        if (!kept) continue;
-        for (int c0 = 0; c0 < H; c0 += 512) {   // uniform trip count: shuffles inside
-            const int c = c0 + 8 * lane;
-            float f[8] = {};
-            if (c < H) load8<true>(x, (size_t)t * H + c, f);
-            uint32_t scale;
-            const u32x2 q = quantize8(f, scale);
-            for (uint64_t m = kept; m; m &= m - 1) {
-                const int row = __shfl(my_row, __ffsll((unsigned long long)m) - 1, 64);
-                if (c >= H) continue;
-                *reinterpret_cast<u32x2*>(codes + (size_t)row * H + c) = q;
-                if ((lane & 15) == 0) scales[(size_t)row * stride + c / kBlock] = (uint8_t)scale;
-            }
+        uint32_t scale;
+        const u32x2 q = quantize8(f, scale);
+        for (uint64_t m = __ballot(my_row >= 0); m; m &= m - 1) {
+            const int row = __shfl(my_row, __ffsll((unsigned long long)m) - 1, 64);
+            if (c >= H) continue;
+            *reinterpret_cast<u32x2*>(codes + (size_t)row * H + c) = q;
+            if ((lane & 15) == 0) scales[(size_t)row * stride + c / kBlock] = (uint8_t)scale;
         }
     }
 }
@@ -159,8 +156,8 @@ void launch_permute_block(const void* x, const int32_t* idx, int T, int H, int E
                           uint8_t* scales, int32_t* counts, int32_t* offsets, int32_t* row_of_assign, int32_t* assign_of_row,
                           void* ws, hipStream_t s) {
     launch_permute(nullptr, idx, T, H, E, K, capacity, r_max, MOE_BF16, nullptr, counts, offsets, row_of_assign, assign_of_row, ws, s);
-    hipLaunchKernelGGL(permute_copy_block_kernel, dim3(min((T + 3) / 4, 256 * 16)), dim3(256), 0, s, static_cast<const bf16_t*>(x),
-                       row_of_assign, T, K, H, r_max, static_cast<uint8_t*>(codes), scales);
+    hipLaunchKernelGGL(permute_copy_block_kernel, dim3((unsigned)min(((long long)T * ((H + 511) / 512) + 3) / 4, 256ll * 32)), dim3(256), 0, s,
+                       static_cast<const bf16_t*>(x), row_of_assign, T, K, H, r_max, static_cast<uint8_t*>(codes), scales);
 }
 
 }  // namespace moe

@@ -11,8 +11,6 @@ namespace moe {
 
 namespace {
 
-constexpr int kCols = 128;   // columns of a workgroup's tile: a block of the quantised results
-
 // c += 2^(sa + sb) a . b: the weight fragment comes first, so that a lane holds row lane % 16 of the activations and four
 // neighbouring columns of the result
 __device__ __forceinline__ f32x4 mfma_block(const Piece& w, const Piece& a, f32x4 c, uint32_t sw, uint32_t sa) {
@@ -33,17 +31,21 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v) {
     return max(v, (uint32_t)__shfl_xor((int)v, 32, 64));
 }
 
-// Tile of 16 MB rows x 128 columns; CW waves of 128 / CW columns each, the contraction's blocks dealt to KS waves in turn.
-template <int MODE, int MB>
-__global__ __launch_bounds__(256) void block_rows_kernel(BlockGemm p) {
+// Tile of 16 MB rows x 32 CW columns.  A wave has 32 of the columns (of gate and of up); KS waves share them and take the blocks
+// along the contraction in turn.
+template <int MODE, int MB, int CW, int KS>
+__global__ __launch_bounds__(64 * CW * KS) void block_rows_kernel(BlockGemm p) {
+    static_assert(MODE == kBlockPlain || CW == 4, "a block of the quantised result");
     constexpr int BM = 16 * MB, FO = 2, FN = MODE == kBlockSwiglu ? 2 * FO : FO;
     __shared__ uint32_t tops[2][4][BM];   // largest magnitude of a wave's columns of every row (kBlockGrad: dg and du)
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Tile t = locate_tile<BM>(p.offsets, p.E, p.N / kCols, blockIdx.x);
+    __shared__ __attribute__((aligned(16))) f32x4 parts[KS > 1 ? KS - 1 : 1][KS > 1 ? CW * MB * FN : 1][64];
+    const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = id % CW, kpart = id / CW;
+    const Tile t = locate_tile<BM>(p.offsets, p.E, p.N / (32 * CW), blockIdx.x);
     if (!t.valid) return;
     const int fr = lane & 15, fk = lane >> 4;
     const int KT = p.K / kBlock, ks = block_scale_stride(p.K);
-    const int col0 = t.ntile * kCols + wave * (16 * FO);
+    const int col0 = (t.ntile * CW + wave) * 32;
 
     const uint8_t *a[MB], *as[MB], *b[FN];
 #pragma unroll
@@ -55,7 +57,7 @@ __global__ __launch_bounds__(256) void block_rows_kernel(BlockGemm p) {
     const size_t wrow = (size_t)t.expert * p.N + col0 + fr;
 #pragma unroll
     for (int j = 0; j < FN; ++j) b[j] = (j < FO ? p.B0 : p.B1) + (wrow + 16 * (j % FO)) * p.K + 32 * fk;
-    const size_t srow = ((size_t)t.expert * (p.N / kBlock) + t.ntile) * ks;
+    const size_t srow = ((size_t)t.expert * (p.N / kBlock) + col0 / kBlock) * ks;
     const uint8_t *const bs0 = p.b0_scales + srow, *const bs1 = MODE == kBlockSwiglu ? p.b1_scales + srow : nullptr;
 
     f32x4 acc[MB][FN];
@@ -67,7 +69,10 @@ __global__ __launch_bounds__(256) void block_rows_kernel(BlockGemm p) {
         Piece a[MB], b[FN];
         uint32_t sa[MB], sb[2];
     };
-    auto load = [&](Step& s, int k) {
+    const int first = rotation(t, KT);   // see there: the order of a row's sum is that of its weight tile and expert
+    auto load = [&](Step& s, int n) {
+        int k = n + first;
+        k = k >= KT ? k - KT : k;
 #pragma unroll
         for (int j = 0; j < FN; ++j) s.b[j] = {ld16(b[j] + (size_t)k * kBlock), ld16(b[j] + (size_t)k * kBlock + 16)};
 #pragma unroll
@@ -79,15 +84,32 @@ __global__ __launch_bounds__(256) void block_rows_kernel(BlockGemm p) {
         s.sb[1] = MODE == kBlockSwiglu ? bs1[k] : 0u;
     };
     Step cur, next;
-    load(cur, 0);
-    for (int k = 0; k < KT; ++k) {
-        if (k + 1 < KT) load(next, k + 1);
+    if (kpart < KT) load(cur, kpart);
+    for (int n = kpart; n < KT; n += KS) {
+        if (n + KS < KT) load(next, n + KS);
 #pragma unroll
         for (int j = 0; j < FN; ++j)
 #pragma unroll
             for (int i = 0; i < MB; ++i) acc[i][j] = mfma_block(cur.b[j], cur.a[i], acc[i][j], cur.sb[j / FO], cur.sa[i]);
         cur = next;
     }
+    if constexpr (KS > 1) {
+        if (kpart > 0) {
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) parts[kpart - 1][(wave * MB + i) * FN + j][lane] = acc[i][j];
+        }
+        __syncthreads();
+        if (kpart > 0 && MODE == kBlockPlain) return;
+#pragma unroll
+        for (int q = 0; q < KS - 1; ++q)
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) acc[i][j] += parts[q][(wave * MB + i) * FN + j][lane];
+    }
+    const bool writes = kpart == 0;   // the other waves go along to the barrier
 
     // a lane's values: row fr of block i, columns col0 + 16 j + 4 fk .. + 3
     if constexpr (MODE == kBlockPlain) {
@@ -108,7 +130,7 @@ __global__ __launch_bounds__(256) void block_rows_kernel(BlockGemm p) {
 #pragma unroll
         for (int i = 0; i < MB; ++i) {
             const int r = 16 * i + fr;
-            const bool in = r < t.rows;
+            const bool in = r < t.rows && writes;
             uint32_t top[PARTS] = {};
 #pragma unroll
             for (int j = 0; j < FO; ++j) {
@@ -147,7 +169,7 @@ __global__ __launch_bounds__(256) void block_rows_kernel(BlockGemm p) {
 #pragma unroll
             for (int h = 0; h < PARTS; ++h) {
                 const uint32_t m = row_max(top[h]);
-                if (fk == 0) tops[h][wave][r] = m;
+                if (fk == 0 && writes) tops[h][wave][r] = m;
             }
         }
         __syncthreads();
@@ -155,7 +177,7 @@ __global__ __launch_bounds__(256) void block_rows_kernel(BlockGemm p) {
 #pragma unroll
         for (int i = 0; i < MB; ++i) {
             const int r = 16 * i + fr;
-            if (r >= t.rows) continue;
+            if (r >= t.rows || !writes) continue;
 #pragma unroll
             for (int h = 0; h < PARTS; ++h) {
                 const uint32_t m = max(max(tops[h][0][r], tops[h][1][r]), max(tops[h][2][r], tops[h][3][r]));
@@ -173,21 +195,39 @@ __global__ __launch_bounds__(256) void block_rows_kernel(BlockGemm p) {
     }
 }
 
-template <int MODE, int MB>
+template <int MODE, int MB, int CW, int KS>
 void launch_rows(const BlockGemm& p, hipStream_t s) {
-    hipLaunchKernelGGL((block_rows_kernel<MODE, MB>), dim3(grid_for(p.r_max, p.E, 16 * MB, p.N / kCols)), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((block_rows_kernel<MODE, MB, CW, KS>), dim3(grid_for(p.r_max, p.E, 16 * MB, p.N / (32 * CW))),
+                       dim3(64 * CW * KS), 0, s, p);
+}
+
+// The persistent tiles from more than kFewRows rows for every expert that can have any: they stream the weights as well, but a
+// tile's 128 rows are multiplied whatever they hold, and with few tiles they leave compute units without one.  us, gate/up and down,
+// rows / tiles: 64 experts, 3584 x 2560, 32 tokens (4 rows each) 189 and 94 / 195 and 93, 64 tokens 218 and 122 / 202 and 115, 512 tokens 508
+// and 334 / 231 and 132; 8 experts, 4096 x 14336, 1 token 38 and 20 / 40 and 74, 16 tokens (4 rows each) 172 and 83 / 204 and 110, 64 tokens 203
+// and 114 / 206 and 112; 64 experts, 4096 x 1408, 64 tokens (6 rows each) 130 and 67 / 135 and 70.  The weights alone take 165 and
+// 83, 187 and 93; 39 and 20, 157 and 78; 115 and 58 at 6 TB/s.
+constexpr int kFewRows = 6;
+// One product with up to so many tiles of 128 columns is cut into columns of 32, its contraction dealt to eight waves (us, 128
+// columns and two waves / so: 8 experts, 4096 x 14336, down, 1 token 59 / 20, 4 tokens 69 / 53; 64 experts, 3584 x 2560, 32 tokens, with
+// 1792 tiles, 94 / 96).
+constexpr int kFewTiles = 256;
+
+template <int MODE>
+void launch_block(const BlockGemm& p, hipStream_t s) {
+    const int taken = min(p.E, p.r_max);   // experts that can have rows
+    if (p.K < 256) launch_rows<MODE, 4, 4, 1>(p, s);   // one block along the contraction: nothing to pipeline
+    else if (p.r_max > kFewRows * taken) launch_block_persist(MODE, p, s);
+    else if (MODE == kBlockPlain && (long long)taken * (p.N / kBlock) <= kFewTiles) launch_rows<kBlockPlain, 1, 1, 8>(p, s);
+    else launch_rows<MODE, 1, 4, 2>(p, s);
 }
 
 }  // namespace
 
 void launch_block_gemm(int mode, const BlockGemm& p, hipStream_t s) {
-    if (p.K >= 256 && p.r_max > 64 * p.E) {
-        launch_block_persist(mode, p, s);
-        return;
-    }
-    if (mode == kBlockPlain) launch_rows<kBlockPlain, 4>(p, s);
-    else if (mode == kBlockSwiglu) launch_rows<kBlockSwiglu, 4>(p, s);
-    else launch_rows<kBlockGrad, 4>(p, s);
+    if (mode == kBlockPlain) launch_block<kBlockPlain>(p, s);
+    else if (mode == kBlockSwiglu) launch_block<kBlockSwiglu>(p, s);
+    else launch_block<kBlockGrad>(p, s);
 }
 
 }  // namespace moe

@@ -465,154 +465,218 @@ struct SelectBackwardArgs {
     int T, E, K, sigmoid, renorm;
 };
 
-// f over L consecutive lanes (a power of two), in all of them
+// f over N consecutive lanes (a power of two), in all of them
 template <typename F>
-__device__ __forceinline__ float lanes_fold(float v, int L, F&& f) {
-    for (int d = 1; d < L; d <<= 1) v = f(v, __shfl_xor(v, d, 64));
+__device__ __forceinline__ float lanes_fold(float v, int N, F&& f) {
+    for (int d = 1; d < N; d <<= 1) v = f(v, __shfl_xor(v, d, 64));
     return v;
 }
 
-// L = 1 .. 64 lanes to a token, four experts to a lane: 4 sub .. 4 sub + 3 (VEC: E is a multiple of 4), else sub + L j.  Lane sub
-// works out the slots sub, sub + L, ..: as E <= 4 L there are at most four.
-template <bool VEC>
-__global__ __launch_bounds__(256) void select_dlogits_kernel(SelectBackwardArgs p, int L) {
-    const int sub = threadIdx.x & (L - 1);
-    const int t = (int)(((size_t)blockIdx.x * 256 + threadIdx.x) / L);
-    const bool valid = t < p.T;                              // the same for the lanes of a token
-    const size_t at = (size_t)(valid ? t : 0);
-    const float* const row = p.logits + at * p.E;
+// TW tokens to a wave: 8 of up to 8 slots, 4 of up to 64.  The slots' work, of which there is little, is dealt over the wave, 64 / TW
+// lanes to a token; the rows of dlogits are put together in LDS and written in one piece, which starts at a multiple of 16
+// bytes whatever E is.  Bound by that write (softmax: and by the read of the logits).
+template <bool SIGMOID, int TW, bool STREAM>
+__global__ __launch_bounds__(256) void select_dlogits_kernel(SelectBackwardArgs p) {
+    constexpr int PER = 64 / TW, SLOTS = TW == 8 ? 1 : 4;
+    extern __shared__ __attribute__((aligned(16))) float rows_of_waves[];
+    __shared__ float totals[4][TW];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int t0 = (blockIdx.x * 4 + wave) * TW, E = p.E;
+    if (t0 >= p.T) return;
+    const int nt = min(TW, p.T - t0);
+    float* const rows = rows_of_waves + wave * (TW * E);
+    const size_t base = (size_t)t0 * E;
     auto add = [](float a, float b) { return a + b; };
-    auto expert = [&](int j) { return VEC ? 4 * sub + j : sub + L * j; };
-    // probabilities (softmax), 0 of experts that are not open
-    float pe[4] = {}, m = -INFINITY, rz = 0.f;
-    if (!p.sigmoid) {
-        float x[4];
-        if (VEC) {
-            f32x4 v = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-            if (4 * sub < p.E) v = *reinterpret_cast<const f32x4*>(row + 4 * sub);
+    auto sync = [] {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
+    // softmax: probabilities, L lanes to a token, experts q + L i of lane q, 64 / L tokens at a time; 0 of experts that are not open
+    constexpr int PASSES = SIGMOID ? 1 : TW;
+    int L = 1;
+    float prob[PASSES][4];
+    if constexpr (!SIGMOID) {
+        while (4 * L < E) L <<= 1;
+        const int q = lane & (L - 1), at = lane / L, step = 64 / L;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = v[j];
-        } else {
+        for (int s = 0; s < PASSES; ++s) {
+            if (s * step >= TW) continue;
+            const int t = s * step + at;
+            const bool in = t < nt;                          // the same for the lanes of a token
+            float m = -INFINITY, z = 0.f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = expert(j) < p.E ? row[expert(j)] : -INFINITY;
+            for (int i = 0; i < 4; ++i) {
+                prob[s][i] = in && q + L * i < E ? p.logits[base + (size_t)t * E + q + L * i] : -INFINITY;
+                m = fmaxf(m, prob[s][i]);                    // of NaN and a number the number
+            }
+            m = lanes_fold(m, L, [](float a, float b) { return fmaxf(a, b); });
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float x = prob[s][i];
+                prob[s][i] = x > -INFINITY ? (x == m ? 1.f : exp_near(x - m)) : 0.f;
+                z += prob[s][i];
+            }
+            z = lanes_fold(z, L, add);
+            const float rz = z > 0.f ? 1.f / z : 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                prob[s][i] *= rz;
+                if (t < TW && q + L * i < E) rows[t * E + q + L * i] = prob[s][i];
+            }
         }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) m = fmaxf(m, x[j]);      // of NaN and a number the number
-        m = lanes_fold(m, L, [](float a, float b) { return fmaxf(a, b); });
-        float z = 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (x[j] > -INFINITY) pe[j] = x[j] == m ? 1.f : expf(x[j] - m);
-            z += pe[j];
-        }
-        z = lanes_fold(z, L, add);
-        rz = z > 0.f ? 1.f / z : 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) pe[j] *= rz;
+        sync();
     }
-    // this lane's slots: expert, score, 1 - score (sigmoid), gradient of the gate
-    int e[4];
-    float s[4], rest[4], d[4], sum = 0.f;
+    // slots sub, sub + PER, ..: expert, score, 1 - score (sigmoid), gradient of the gate
+    const int tok = lane / PER, sub = lane % PER;
+    int e[SLOTS];
+    float s[SLOTS], rest[SLOTS], d[SLOTS], sum = 0.f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int k = sub + L * j;
+    for (int j = 0; j < SLOTS; ++j) {
+        const int k = sub + PER * j;
         e[j] = -1;
-        s[j] = rest[j] = d[j] = 0.f;
-        if (k < p.K) {
-            const int i = p.idx[at * p.K + k];
-            if ((unsigned)i < (unsigned)p.E) {
-                const float l = row[i];
+        s[j] = d[j] = 0.f;
+        rest[j] = 1.f;
+        if (k < p.K && tok < nt) {
+            const size_t slot = (size_t)(t0 + tok) * p.K + k;
+            const int i = p.idx[slot];
+            if ((unsigned)i < (unsigned)E) {
+                const float l = p.logits[base + (size_t)tok * E + i];
                 if (l > -INFINITY) {
-                    e[j] = i;
-                    d[j] = p.dgate[at * p.K + k] * p.scale;
-                    if (p.sigmoid) {
-                        const float q = expf(-fabsf(l)), r = 1.f / (1.f + q);
-                        s[j] = l >= 0.f ? r : q * r;
-                        rest[j] = l >= 0.f ? q * r : r;
+                    e[j] = tok * E + i;
+                    d[j] = p.dgate[slot] * p.scale;
+                    if constexpr (SIGMOID) {
+                        const float x = exp_near(-fabsf(l)), r = 1.f / (1.f + x);
+                        s[j] = l >= 0.f ? r : x * r;
+                        rest[j] = l >= 0.f ? x * r : r;
                     } else {
-                        s[j] = (l == m ? 1.f : expf(l - m)) * rz;
+                        s[j] = rows[e[j]];
                     }
                 }
             }
         }
         sum += s[j];
     }
-    float c[4], total = 0.f;                                 // gradient of the logarithm of the score (sigmoid: divided by `rest`)
+    // c: gradient of the logarithm of the score, times 1 - score (sigmoid)
+    float c[SLOTS], total = 0.f, mean = 0.f;
     if (p.renorm) {
-        sum = lanes_fold(sum, L, add);
-        float mean = 0.f;
+        sum = lanes_fold(sum, PER, add);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < SLOTS; ++j) {
             s[j] = sum > 0.f ? s[j] / sum : 0.f;
-            mean += e[j] >= 0 ? d[j] * s[j] : 0.f;
+            mean += d[j] * s[j];
         }
-        mean = lanes_fold(mean, L, add);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) c[j] = e[j] >= 0 ? (d[j] - mean) * s[j] : 0.f;
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) c[j] = e[j] >= 0 ? d[j] * s[j] : 0.f;
+        mean = lanes_fold(mean, PER, add);
     }
-    if (p.sigmoid) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) c[j] *= rest[j];
-    } else {
-        total = lanes_fold(c[0] + c[1] + c[2] + c[3], L, add);
+    for (int j = 0; j < SLOTS; ++j) {
+        c[j] = e[j] >= 0 ? (d[j] - mean) * s[j] : 0.f;
+        total += c[j];
+        c[j] *= rest[j];
     }
-    float out[4];
+    // an expert named twice by a token: of the slots that leave their number at its place, one finds another's there
+    sync();
 #pragma unroll
-    for (int j = 0; j < 4; ++j) out[j] = -pe[j] * total;
-    // slots in ascending order; an expert named twice adds up
-    const int lane = threadIdx.x & 63, first = lane & ~(L - 1);
+    for (int j = 0; j < SLOTS; ++j)
+        if (e[j] >= 0) rows[e[j]] = __int_as_float(lane * SLOTS + j);
+    sync();
+    bool twice = false;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        for (int k = 0; k < L && k + L * j < p.K; ++k) {
-            const int ek = __shfl(e[j], first + k, 64);
-            const float ck = __shfl(c[j], first + k, 64);
+    for (int j = 0; j < SLOTS; ++j)
+        if (e[j] >= 0) twice |= __float_as_int(rows[e[j]]) != lane * SLOTS + j;
+    sync();
+    if constexpr (SIGMOID) {
+        for (int i = lane; i < TW * E / 4; i += 64) reinterpret_cast<f32x4*>(rows)[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    } else {
+        total = lanes_fold(total, PER, add);
+        if (sub == 0) totals[wave][tok] = total;
+        sync();
+        const int q = lane & (L - 1), at = lane / L, step = 64 / L;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (ek == expert(i)) out[i] += ck;
+        for (int i = 0; i < PASSES; ++i) {
+            const int t = i * step + at;
+            if (i * step >= TW || t >= TW) continue;
+            const float of = totals[wave][t];
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+                if (q + L * n < E) rows[t * E + q + L * n] = -prob[i][n] * of;
         }
-    if (!valid) return;
-    if (VEC) {
-        if (4 * sub >= p.E) return;
-        f32x4 v = {out[0], out[1], out[2], out[3]};
-        if (p.addend) v += *reinterpret_cast<const f32x4*>(p.addend + at * p.E + 4 * sub);
-        *reinterpret_cast<f32x4*>(p.dlogits + at * p.E + 4 * sub) = v;
-    } else {
+    }
+    sync();
+    if (__ballot(twice) == 0) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (expert(j) < p.E) p.dlogits[at * p.E + expert(j)] = out[j] + (p.addend ? p.addend[at * p.E + expert(j)] : 0.f);
+        for (int j = 0; j < SLOTS; ++j)
+            if (e[j] >= 0) rows[e[j]] += c[j];
+    } else {   // one after the other
+#pragma unroll
+        for (int j = 0; j < SLOTS; ++j)
+            for (int k = 0; k < PER; ++k) {
+                if (sub == k && e[j] >= 0) rows[e[j]] += c[j];
+                sync();
+            }
+    }
+    sync();
+    const int n = nt * E;
+    float* const out = p.dlogits + base;
+    for (int i = 4 * lane; i < n; i += 256) {
+        f32x4 v = *reinterpret_cast<const f32x4*>(rows + i);
+        if (i + 4 <= n) {
+            if (p.addend) v += *reinterpret_cast<const f32x4*>(p.addend + base + i);
+            if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<f32x4*>(out + i));
+            else *reinterpret_cast<f32x4*>(out + i) = v;
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (i + q < n) out[i + q] = v[q] + (p.addend ? p.addend[base + i + q] : 0.f);
+        }
     }
 }
 
 // ---- the step of the bias ----
+// A chain of loads: rows of counts are dealt to four groups of threads, and each has all its loads in flight.
 constexpr int kBiasRows = 64;   // rows of counts that a workgroup adds up
 
-// part[b][e] = sum of a workgroup's rows
-__global__ __launch_bounds__(256) void bias_sum_kernel(const int32_t* __restrict__ counts, int n_rows, int E,
-                                                       int64_t* __restrict__ part) {
-    const int r0 = blockIdx.x * kBiasRows, r1 = min(n_rows, r0 + kBiasRows);
+// sum of rows [r0, r0 + kBiasRows) below n_rows of column e, for threads e < 256 (the first group)
+template <typename N>
+__device__ __forceinline__ int64_t column_sum(const N* __restrict__ rows, int r0, int n_rows, int E, int64_t (&part)[4][256]) {
+    const int e = threadIdx.x & 255, g = threadIdx.x >> 8;
+    N v[kBiasRows / 4];
+#pragma unroll
+    for (int i = 0; i < kBiasRows / 4; ++i) {
+        const int r = r0 + 4 * i + g;
+        v[i] = e < E && r < n_rows ? rows[(size_t)r * E + e] : 0;
+    }
     int64_t n = 0;
-    if ((int)threadIdx.x < E)
-        for (int r = r0; r < r1; ++r) n += counts[(size_t)r * E + threadIdx.x];
-    if ((int)threadIdx.x < E) part[(size_t)blockIdx.x * E + threadIdx.x] = n;
+#pragma unroll
+    for (int i = 0; i < kBiasRows / 4; ++i) n += v[i];
+    part[g][e] = n;
+    __syncthreads();
+    n = part[0][e] + part[1][e] + part[2][e] + part[3][e];
+    __syncthreads();
+    return n;
 }
 
-// bias[e] += rate * sign(sum_j n_j - E n_e), n the sums of `rows` rows
+// sums[b][e] = sum of a workgroup's rows
+__global__ __launch_bounds__(1024) void bias_sum_kernel(const int32_t* __restrict__ counts, int n_rows, int E,
+                                                        int64_t* __restrict__ sums) {
+    __shared__ int64_t part[4][256];
+    const int64_t n = column_sum(counts, blockIdx.x * kBiasRows, n_rows, E, part);
+    if ((int)threadIdx.x < E) sums[(size_t)blockIdx.x * E + threadIdx.x] = n;
+}
+
+// bias[e] += rate * sign(sum_j n_j - E n_e), n the sums of n_rows rows
 template <typename N>
-__global__ __launch_bounds__(256) void bias_step_kernel(const N* __restrict__ rows, int n_rows, int E, float rate,
-                                                        float* __restrict__ bias) {
-    __shared__ int64_t part[4];
+__global__ __launch_bounds__(1024) void bias_step_kernel(const N* __restrict__ rows, int n_rows, int E, float rate,
+                                                         float* __restrict__ bias) {
+    __shared__ int64_t part[4][256];
     const int e = threadIdx.x;
+    const float before = e < E ? bias[e] : 0.f;
     int64_t n = 0;
-    if (e < E)
-        for (int r = 0; r < n_rows; ++r) n += rows[(size_t)r * E + e];
-    const int64_t sum = wave_sum(n);
-    if ((e & 63) == 0) part[e >> 6] = sum;
+    for (int r = 0; r < n_rows; r += kBiasRows) n += column_sum(rows, r, n_rows, E, part);
+    const int64_t sum = wave_sum(e < E ? n : 0);
+    if ((e & 63) == 0 && e < 256) part[0][e >> 6] = sum;
     __syncthreads();
-    const int64_t off = part[0] + part[1] + part[2] + part[3] - (int64_t)E * n;
-    if (e < E && off != 0) bias[e] += off > 0 ? rate : -rate;
+    const int64_t off = part[0][0] + part[0][1] + part[0][2] + part[0][3] - (int64_t)E * n;
+    if (e < E && off != 0) bias[e] = before + (off > 0 ? rate : -rate);
 }
 
 }  // namespace
@@ -629,12 +693,17 @@ void launch_select(const float* logits, const float* bias, int T, int E, int K, 
 
 void launch_select_dlogits(const float* logits, const int32_t* idx, const float* dgate, const float* addend, int T, int E, int K,
                            moe_score_t score, int renorm, float scale, float* dlogits, hipStream_t s) {
+    // streamed where what follows would not find them in the 256 MB cache (262144 tokens x 256 experts: 84 us, streamed 74)
+    const bool stream = (size_t)T * E * sizeof(float) > 140u << 20;
     const SelectBackwardArgs p = {logits, idx, dgate, addend, dlogits, scale, T, E, K, score == MOE_SCORE_SIGMOID, renorm};
-    int L = 1;
-    while (4 * L < E) L <<= 1;
-    const dim3 grid((unsigned)(((size_t)T * L + 255) / 256));
-    if (E % 4 == 0) hipLaunchKernelGGL(select_dlogits_kernel<true>, grid, dim3(256), 0, s, p, L);
-    else hipLaunchKernelGGL(select_dlogits_kernel<false>, grid, dim3(256), 0, s, p, L);
+    const int tw = K <= 8 ? 8 : 4;
+    auto pick = [&](auto st) {
+        constexpr bool S = decltype(st)::value;
+        return K <= 8 ? (p.sigmoid ? select_dlogits_kernel<true, 8, S> : select_dlogits_kernel<false, 8, S>)
+                      : (p.sigmoid ? select_dlogits_kernel<true, 4, S> : select_dlogits_kernel<false, 4, S>);
+    };
+    const auto kern = stream ? pick(std::true_type{}) : pick(std::false_type{});
+    hipLaunchKernelGGL(kern, dim3((unsigned)((T + 4ll * tw - 1) / (4 * tw))), dim3(256), (size_t)4 * tw * E * sizeof(float), s, p);
 }
 
 size_t bias_update_workspace_bytes(int n_rows, int E) {
@@ -643,13 +712,13 @@ size_t bias_update_workspace_bytes(int n_rows, int E) {
 
 void launch_bias_update(const int32_t* counts, int n_rows, int E, float rate, float* bias, void* ws, hipStream_t s) {
     if (n_rows <= kBiasRows) {
-        hipLaunchKernelGGL(bias_step_kernel<int32_t>, dim3(1), dim3(256), 0, s, counts, n_rows, E, rate, bias);
+        hipLaunchKernelGGL(bias_step_kernel<int32_t>, dim3(1), dim3(1024), 0, s, counts, n_rows, E, rate, bias);
         return;
     }
     const int parts = (n_rows + kBiasRows - 1) / kBiasRows;
     int64_t* part = static_cast<int64_t*>(ws);
-    hipLaunchKernelGGL(bias_sum_kernel, dim3(parts), dim3(256), 0, s, counts, n_rows, E, part);
-    hipLaunchKernelGGL(bias_step_kernel<int64_t>, dim3(1), dim3(256), 0, s, part, parts, E, rate, bias);
+    hipLaunchKernelGGL(bias_sum_kernel, dim3(parts), dim3(1024), 0, s, counts, n_rows, E, part);
+    hipLaunchKernelGGL(bias_step_kernel<int64_t>, dim3(1), dim3(1024), 0, s, part, parts, E, rate, bias);
 }
 
 }  // namespace moe
