@@ -400,8 +400,8 @@ moe_status_t moe_balance_loss_backward(const float* logits, const uint8_t* token
  *              sum is 0)
  *
  * Of equal keys and of equal groups the lower index comes first.  The bias chooses and has
- * no part in the gates.  An expert whose logit is -inf or NaN, or whose key is, is not
- * selected (nor counted in the softmax, where its logit is); slots for which no expert is
+ * no part in the gates.  An expert whose logit is -inf or NaN, or whose key is NaN or not
+ * above the lowest finite number, is not selected (nor counted in the softmax, where its logit is); slots for which no expert is
  * left get topk_idx = -1 (a dropped assignment everywhere in this library) and gate 0.
  *
  * x, w_router, logit_bias, logits, T, H, E, K, dt, limits and errors as moe_router_topk

@@ -27,17 +27,10 @@ constexpr double kNever = -__builtin_huge_val();   // the key of an expert that 
 // What an expert is ranked by, as one number: its score and bias, and in the bits behind fp32's its index, so that of equal ones
 // the lower index is the larger number.
 __device__ __forceinline__ double select_key(float choice, int e) {
-    if (!(choice > -INFINITY)) return kNever;                // NaN and -inf
+    if (!(choice > -__FLT_MAX__)) return kNever;             // NaN, -inf and the lowest number
     choice = fminf(choice, __FLT_MAX__) + 0.f;               // -0 to +0
     uint64_t b = __builtin_bit_cast(uint64_t, (double)choice);
     b |= (uint64_t)(choice < 0.f ? e : 255 - e);
-    return __builtin_bit_cast(double, b);
-}
-// the same with kLow for kNever; the bias has no NaN
-__device__ __forceinline__ double list_key(float logit, float choice, int e) {
-    choice = logit > -INFINITY ? __builtin_amdgcn_fmed3f(choice, -__FLT_MAX__, __FLT_MAX__) : -__FLT_MAX__;
-    uint64_t b = __builtin_bit_cast(uint64_t, (double)choice);
-    b |= (uint64_t)(uint32_t)(choice < 0.f ? e : 255 - e);
     return __builtin_bit_cast(double, b);
 }
 __device__ __forceinline__ int key_expert(double key) {
@@ -193,7 +186,8 @@ __global__ __launch_bounds__(64 * kSelectWaves) void select_wave_kernel(SelectAr
 // Bound by the vector unit.  Scores in 64 bits would be half of its work, so they are first formed in fp32, and what was
 // selected by them stands if no difference that decided it is within what they may be off; else the wave does it all again
 // in 64 bits (a token in some hundreds).
-constexpr double kLow = -(double)__FLT_MAX__;   // keys up to here belong to experts that are not selected
+// Keys up to here belong to experts that are not selected.  (Their low bits make them smaller.)
+constexpr double kLow = -(double)__FLT_MAX__;
 
 __device__ __forceinline__ double min_key(double a, double b) {
     double r;
@@ -254,10 +248,12 @@ __device__ __forceinline__ void merge_lanes(double (&a)[8], double& next) {
 
 // How far apart two keys are that fp32 scores tell apart for certain.  A score is off by less than 2^-17 of itself (the rounding of
 // the exponential's argument, at most 88, and a few units; a softmax's sum), and by less than 2^-20 altogether unless a softmax's
-// probability is near 1, where it is 2^-19.
-__device__ __forceinline__ float doubt(float key, bool biased) {
-    return biased ? fmaxf(1.f, fabsf(key)) * 0x1p-18f : fabsf(key) * 0x1p-16f;
-}
+// probability is near 1, where it is 2^-19.  Equal keys are always in doubt, so a key carries its expert's number in any order.
+struct Doubt {
+    double part, least;
+    __device__ __forceinline__ Doubt(bool biased) : part(biased ? 0x1p-18 : 0x1p-16), least(biased ? 0x1p-18 : 0x1p-126) {}
+    __device__ __forceinline__ bool apart(double large, double small) const { return large - small > fma(fabs(small), part, least); }
+};
 
 // exp(d) for d <= 0 to about a unit in the last place: the product's rounding is made up for
 __device__ __forceinline__ float exp_near(float d) {
@@ -279,8 +275,9 @@ __global__ __launch_bounds__(256, 4) void select_lists_kernel(SelectArgs p, int 
     for (int i = threadIdx.x; i < L * VPL; i += 256) {
         const int l = i / VPL, j = i % VPL, e = l * run + j;
         const float b = biased && j < run && e < p.E ? p.bias[e] : 0.f;
-        biases[l * LDB + j] = b == b ? b : -INFINITY;
+        biases[l * LDB + j] = b == b ? fminf(fmaxf(b, -__FLT_MAX__), __FLT_MAX__) : -__FLT_MAX__;   // a score adds nothing to these
     }
+    const Doubt doubt(biased);
     __syncthreads();
     auto lanes = [](auto v, auto&& f) {
         if constexpr (L > 1) v = f(v, dpp<0xB1>(v));
@@ -328,19 +325,25 @@ __global__ __launch_bounds__(256, 4) void select_lists_kernel(SelectArgs p, int 
             z = lanes((double)sum, add);
             rz = 1.f / (float)z;
         }
+        int at = sub * LDB;
+        asm volatile("" : "+v"(at));   // or the biases are kept in registers over all tokens
         // the lane's eight largest, and the largest behind them
         double list[8], next = kLow;
 #pragma unroll
         for (int j = 0; j < VPL; j += 8) {
+            __builtin_amdgcn_sched_barrier(0);   // eight keys at a time, not all of them: registers
             double key[8];
 #pragma unroll
             for (int q = 0; q < 8; q += 4) {
-                const f32x4 b = *reinterpret_cast<const f32x4*>(&biases[sub * LDB + j + q]);
+                const f32x4 b = *reinterpret_cast<const f32x4*>(&biases[at + j + q]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float v = x[j + q + i];
                     const float s = SIGMOID ? __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -1.44269504f)) : v * rz;
-                    key[q + i] = list_key(v, s + b[i], e0 + j + q + i);
+                    float choice = s + b[i];
+                    asm("" : "+v"(choice));              // a select below, and no branch around the exponential
+                    choice = v > -INFINITY ? choice : -__FLT_MAX__;
+                    key[q + i] = __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, (double)choice) | (uint64_t)(j + q + i));
                 }
             }
             sort8(key);
@@ -351,11 +354,19 @@ __global__ __launch_bounds__(256, 4) void select_lists_kernel(SelectArgs p, int 
                 merge8(list, key, next);
             }
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)   // the lane beside the place in its run
+            list[i] = __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, list[i]) | (uint64_t)(sub * 32));
         bool sure = true, keep = true;
         if (p.groups > 1) {
             // this lane's group: its value, its rank, and the largest value that ranks behind it
-            float total = key_choice(list[0]);
-            if (p.group_best > 1 && list[1] > kLow) total += key_choice(list[1]);
+            float total = key_choice(list[0]), size = list[0] > kLow ? fabsf(total) : 0.f;
+            if (p.group_best > 1 && list[1] > kLow) {
+                const float second = key_choice(list[1]);
+                total += second;
+                size += fabsf(second);
+            }
+            size = lanes(size, [](float a, float b) { return fmaxf(a, b); });
             if (!(list[0] > kLow)) total = -INFINITY;
             int rank = 0;
             float below = -INFINITY;
@@ -367,7 +378,9 @@ __global__ __launch_bounds__(256, 4) void select_lists_kernel(SelectArgs p, int 
                 below = ahead ? below : fmaxf(below, other);
             }
             keep = rank < p.topk_groups && total > -INFINITY;
-            if (rank == p.topk_groups - 1 && below > -INFINITY) sure = total - below > 2.f * doubt(total, biased);
+            // a sum may be far smaller than what was added up
+            if (rank == p.topk_groups - 1 && below > -INFINITY)
+                sure = (double)total - (double)below > 2. * fma((double)size, doubt.part, doubt.least);
             if (!keep) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) list[i] = kLow;
@@ -379,15 +392,10 @@ __global__ __launch_bounds__(256, 4) void select_lists_kernel(SelectArgs p, int 
         if constexpr (L > 4) merge_lanes<0x141>(list, next);
         if constexpr (L > 8) merge_lanes<0x140>(list, next);
         // neighbours among the first K and the one behind them
-        float last = key_choice(list[0]);
 #pragma unroll
         for (int k = 1; k <= 8; ++k) {
             const double key = k < 8 ? list[k] : next;
-            if (k <= p.K && key > kLow) {
-                const float c = key_choice(key);
-                sure &= last - c > doubt(last, biased);
-                last = c;
-            }
+            if (k <= p.K && key > kLow) sure &= doubt.apart(list[k - 1], key);
         }
         const uint64_t unsure = __ballot(!sure && valid);
         // slot k in lane k mod L
@@ -400,7 +408,8 @@ __global__ __launch_bounds__(256, 4) void select_lists_kernel(SelectArgs p, int 
 #pragma unroll
             for (int q = 0; q < 8; ++q)
                 if (q == k) found = list[q];
-            e[i] = k < p.K && found > kLow ? key_expert(found) : -1;
+            const int place = (int)(__builtin_bit_cast(uint64_t, found) & 0x1ffu);   // 32 times the lane, and in its run
+            e[i] = k < p.K && found > kLow ? (place >> 5) * run + (place & 31) : -1;
             g[i] = 0.;
             if (e[i] >= 0) g[i] = SIGMOID ? sigmoid64(row[e[i]]) : shifted_exp64(fminf(row[e[i]], __FLT_MAX__), m);
             sum += g[i];

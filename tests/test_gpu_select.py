@@ -93,6 +93,15 @@ def test_extreme_logits_and_biases(score, E, groups, topk_groups):
     _check(x, min(4, E), score, None, groups, topk_groups, 2, renormalize=False)
 
 
+def test_large_biases_that_cancel_in_a_group():
+    """Pairs of experts with biases of +b and -b: a group's value is what is left of two far larger keys."""
+    rng = np.random.default_rng(2)
+    for b in (3.0, 1e3, 1e6, 1e7):
+        x = (rng.normal(size=(3000, 16)) * 2).astype(np.float32)
+        bias = np.tile([b, -b], 8).astype(np.float32)
+        _check(x, 3, routing.SIGMOID, bias, groups=8, topk_groups=2, group_best=2)
+
+
 def test_infinite_biases_choose_first_in_order():
     x = _logits(50, 16, 4)
     bias = np.zeros(16, dtype=np.float32)
