@@ -842,7 +842,8 @@ moe_status_t moe_expert_down_fp8_block(const void* h_codes, const uint8_t* h_sca
  * quantisations count as identities.  The weight gradients contract over rows, along which
  * no operand has its blocks: they are bf16 products of dy_perm, of dg and du rounded to bf16
  * once, and of the values that the codes of h and x stand for.  Shapes, outputs, limits and
- * errors as moe_grouped_gemm_swiglu_backward; experts without rows get zeros.  workspace:
+ * errors as moe_grouped_gemm_swiglu_backward, and R_max <= 2^22 (otherwise
+ * MOE_ERR_UNSUPPORTED); experts without rows get zeros.  workspace:
  * moe_expert_backward_fp8_block_workspace_bytes.
  */
 size_t moe_expert_backward_fp8_block_workspace_bytes(int R_max, int H, int F, int E);

@@ -1226,7 +1226,7 @@ static moe_status_t check_block_ffn(const char* fn, int R_max, int H, int F, int
     if (E > kMaxExperts) return fail(MOE_ERR_UNSUPPORTED, "%s: E=%d exceeds the limit %d", fn, E, kMaxExperts);
     if (!blocks_fit(H, F)) return fail(MOE_ERR_UNSUPPORTED, "%s: H=%d and F=%d must be multiples of 128", fn, H, F);
     if (H > kMaxBlockRow || F > kMaxBlockRow / 2)
-        return fail(MOE_ERR_UNSUPPORTED, "%s: H=%d and 2F=%d exceed the limit %d", fn, H, 2 * F, kMaxBlockRow);
+        return fail(MOE_ERR_UNSUPPORTED, "%s: H=%d and 2F=%lld exceed the limit %d", fn, H, 2ll * F, kMaxBlockRow);
     return MOE_OK;
 }
 
@@ -1247,7 +1247,7 @@ moe_status_t moe_fp8_block_quantize(const void* src, moe_dtype_t dt, int rows, i
     REQUIRE_PTR(fn, src);
     REQUIRE_PTR(fn, codes);
     REQUIRE_SCALES(fn, scales);
-    launch_block_quantize(src, dt, rows, nullptr, C, codes, scales, static_cast<hipStream_t>(stream));
+    launch_block_quantize(src, dt, rows, C, codes, scales, static_cast<hipStream_t>(stream));
     return check_launch(fn);
 }
 
@@ -1419,6 +1419,8 @@ moe_status_t moe_grouped_gemm_swiglu_fp8_block_backward(
     void* workspace, size_t workspace_bytes, moe_stream_t stream) {
     static const char* fn = "moe_grouped_gemm_swiglu_fp8_block_backward";
     if (moe_status_t st = check_block_ffn(fn, R_max, H, F, E)) return st;
+    if (R_max > kMaxBlockBackwardRows)
+        return fail(MOE_ERR_UNSUPPORTED, "%s: R_max=%d exceeds the limit %d", fn, R_max, kMaxBlockBackwardRows);
     REQUIRE_PTR(fn, expert_offsets);
     REQUIRE_PTR(fn, dw_gate);
     REQUIRE_PTR(fn, dw_up);
@@ -1446,21 +1448,17 @@ moe_status_t moe_grouped_gemm_swiglu_fp8_block_backward(
     REQUIRE_PTR(fn, workspace);
     uint8_t* const ws = static_cast<uint8_t*>(workspace);
     auto bytes = [](const void* p) { return static_cast<const uint8_t*>(p); };
-    launch_wgrad_zero_empty(expert_offsets, E, (size_t)H * F, dw_down, dw_gate, dw_up, s);
+    int32_t* const poff = reinterpret_cast<int32_t*>(ws + L.poff);
+    launch_block_prepare(dy_perm, expert_offsets, E, H, F, R_max, ws + L.dy, ws + L.dy_scales, poff, dw_down, dw_gate, dw_up, s);
     // dh, in its epilogue dg | du, and from them the rows' gradient
-    launch_block_quantize(dy_perm, MOE_BF16, R_max, expert_offsets + E, H, ws + L.dy, ws + L.dy_scales, s);
     launch_block_gemm(kBlockGrad, {ws + L.dy, ws + L.dy_scales, expert_offsets, bytes(wd_t_codes), nullptr, wd_t_scales, nullptr,
                                    ws + L.dgu_codes, ws + L.dgu_scales, static_cast<bf16_t*>(const_cast<void*>(gu)),
                                    reinterpret_cast<bf16_t*>(ws + L.dgu), E, F, H, R_max}, s);
     launch_block_gemm(kBlockPlain, {ws + L.dgu_codes, ws + L.dgu_scales, expert_offsets, bytes(wgu_t_codes), nullptr, wgu_t_scales,
                                     nullptr, dx_perm, nullptr, nullptr, nullptr, E, H, 2 * F, R_max}, s);
     // the weights' gradients: operands transposed with every expert's rows as a zero-padded column segment
-    int32_t* const poff = reinterpret_cast<int32_t*>(ws + L.poff);
-    launch_ragged_offsets(expert_offsets, E, poff, s);
-    launch_ragged_transpose(dy_perm, expert_offsets, poff, E, H, L.rp_max, ws + L.dy_t, s);
-    launch_ragged_transpose_block(h_codes, h_scales, expert_offsets, poff, E, F, L.rp_max, ws + L.h_t, s);
-    launch_ragged_transpose(ws + L.dgu, expert_offsets, poff, E, 2 * F, L.rp_max, ws + L.dgu_t, s);
-    launch_ragged_transpose_block(x_codes, x_scales, expert_offsets, poff, E, H, L.rp_max, ws + L.x_t, s);
+    launch_block_transposes(dy_perm, ws + L.dgu, h_codes, h_scales, x_codes, x_scales, expert_offsets, poff, E, H, F, L.rp_max,
+                            ws + L.dy_t, ws + L.dgu_t, ws + L.h_t, ws + L.x_t, s);
     launch_persist_wgrad(ws + L.dy_t, ws + L.h_t, expert_offsets, E, H, F, L.rp_max, dw_down, s);
     launch_persist_wgrad(ws + L.dgu_t, ws + L.x_t, expert_offsets, E, F, H, L.rp_max, dw_gate, s);
     launch_persist_wgrad(ws + L.dgu_t + (size_t)F * L.rp_max * 2, ws + L.x_t, expert_offsets, E, F, H, L.rp_max, dw_up, s);

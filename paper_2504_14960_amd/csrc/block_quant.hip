@@ -6,56 +6,10 @@ namespace moe {
 
 namespace {
 
-// the largest magnitude over the 16 lanes of a row of the wave, in all of them
-__device__ __forceinline__ uint32_t max16(uint32_t v) {
-#pragma unroll
-    for (int d = 1; d < 16; d <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d, 64));
-    return v;
-}
-
-// eight values of a block that 16 neighbouring lanes hold: their codes, and the block's scale
-__device__ __forceinline__ u32x2 quantize8(const float (&f)[8], uint32_t& scale) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, magnitude(f[j]));
-    scale = block_scale(max16(top));
-    const float inv = block_inverse(scale);
-    return u32x2{block_codes(f[0], f[1], f[2], f[3], inv, scale), block_codes(f[4], f[5], f[6], f[7], inv, scale)};
-}
-
 template <bool BF16>
-__device__ __forceinline__ void load8(const void* src, size_t at, float (&f)[8]) {
-    if constexpr (BF16) {
-        bf16x8_to_f32(*reinterpret_cast<const u32x4*>(static_cast<const bf16_t*>(src) + at), f);
-    } else {
-        const f32x4 lo = *reinterpret_cast<const f32x4*>(static_cast<const float*>(src) + at);
-        const f32x4 hi = *reinterpret_cast<const f32x4*>(static_cast<const float*>(src) + at + 4);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            f[j] = lo[j];
-            f[4 + j] = hi[j];
-        }
-    }
-}
-
-// One row to a wave, 512 values at a time.  Rows below *n_rows (null: `rows`).
-template <bool BF16>
-__global__ __launch_bounds__(256) void block_rows_quantize_kernel(const void* __restrict__ src, int rows,
-                                                                  const int32_t* __restrict__ n_rows, int C,
+__global__ __launch_bounds__(256) void block_rows_quantize_kernel(const void* __restrict__ src, int rows, int C,
                                                                   uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int n = n_rows ? min(rows, *n_rows) : rows, stride = block_scale_stride(C);
-    for (int r = blockIdx.x * 4 + wave; r < n; r += gridDim.x * 4)
-        for (int c0 = 0; c0 < C; c0 += 512) {   // uniform trip count: shuffles inside
-            const int c = c0 + 8 * lane;
-            float f[8] = {};
-            if (c < C) load8<BF16>(src, (size_t)r * C + c, f);
-            uint32_t scale;
-            const u32x2 q = quantize8(f, scale);
-            if (c >= C) continue;
-            *reinterpret_cast<u32x2*>(codes + (size_t)r * C + c) = q;
-            if ((lane & 15) == 0) scales[(size_t)r * stride + c / kBlock] = (uint8_t)scale;
-        }
+    block_quantize_rows<BF16>(src, rows, C, codes, scales, blockIdx.x, gridDim.x);
 }
 
 // 512 values of a token to a wave, read and quantised once and stored to each of its rows of the expert order.
@@ -138,11 +92,9 @@ __global__ __launch_bounds__(256) void block_weights_kernel(const void* __restri
 
 }  // namespace
 
-void launch_block_quantize(const void* src, moe_dtype_t dt, int rows, const int32_t* n_rows, int C, void* codes, uint8_t* scales,
-                           hipStream_t s) {
-    const int grid = (int)min((rows + 3ll) / 4, 256ll * 16);
+void launch_block_quantize(const void* src, moe_dtype_t dt, int rows, int C, void* codes, uint8_t* scales, hipStream_t s) {
     auto kern = dt == MOE_BF16 ? block_rows_quantize_kernel<true> : block_rows_quantize_kernel<false>;
-    hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, s, src, rows, n_rows, C, static_cast<uint8_t*>(codes), scales);
+    hipLaunchKernelGGL(kern, dim3(block_quantize_grid(rows)), dim3(256), 0, s, src, rows, C, static_cast<uint8_t*>(codes), scales);
 }
 
 void launch_block_weights(const void* w, moe_dtype_t dt, int E, int N, int K, void* codes, uint8_t* scales, void* codes_t,

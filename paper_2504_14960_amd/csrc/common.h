@@ -31,6 +31,7 @@ constexpr int kMaxTopK = 64;
 constexpr int kMaxBalanceTokens = 1 << 30;         // of one balance-loss call
 constexpr int kMaxSequences = 65536;               // of one balance-loss call
 constexpr int kMaxCountRows = 1 << 20;             // of one bias update
+constexpr int kMaxBlockBackwardRows = 1 << 22;     // of one backward on block-scaled E4M3: 32-bit offsets in the transposed rows
 constexpr int kMaxListTensors = 1 << 26;           // of one gradient-norm or AdamW call
 constexpr int64_t kMaxListElements = 1ll << 33;    // of one tensor of a gradient-norm or AdamW call
 
@@ -50,6 +51,14 @@ __device__ __forceinline__ uint32_t pack2_bf16(float lo, float hi) {
     typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
     const f32x2_t v = {lo, hi};
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
+}
+
+// dw[e] = 0 if expert e has no rows, by workgroup `block` of `blocks` of 256 threads; per_expert is a multiple of 8
+__device__ __forceinline__ void zero_empty_expert(const int32_t* __restrict__ offsets, int e, size_t per_expert, bf16_t* __restrict__ dw,
+                                                  int block, int blocks) {
+    if (offsets[e + 1] - offsets[e] > 0) return;
+    u32x4* dst = reinterpret_cast<u32x4*>(dw + (size_t)e * per_expert);
+    for (size_t i = (size_t)block * 256 + threadIdx.x; i < per_expert / 8; i += (size_t)blocks * 256) dst[i] = u32x4{0u, 0u, 0u, 0u};
 }
 
 // XOR term of the GEMM kernels' LDS tiles.  A tile row is 128 bytes = eight 16-byte pieces; piece c of row r lives
@@ -195,9 +204,13 @@ void launch_weights_transpose(const void* w_gate, const void* w_up, const void* 
 void launch_ragged_offsets(const int32_t* offsets, int E, int32_t* poff, hipStream_t s);   // poff [E + 1]
 void launch_ragged_transpose(const void* src, const int32_t* offsets, const int32_t* poff, int E, int C, int rp_max,
                              void* dst, hipStream_t s);
-// the same of E4M3 codes with a scale for every block of 128 of a row: the bf16 values they stand for
-void launch_ragged_transpose_block(const void* codes, const uint8_t* scales, const int32_t* offsets, const int32_t* poff, int E, int C,
-                                   int rp_max, void* dst, hipStream_t s);
+// the four of a backward on E4M3 operands with a scale for every block of 128 (h and x as the bf16 values they stand for)
+void launch_block_transposes(const void* dy, const void* dgu, const void* h, const uint8_t* h_scales, const void* x,
+                             const uint8_t* x_scales, const int32_t* offsets, const int32_t* poff, int E, int H, int F, int rp_max,
+                             void* dy_t, void* dgu_t, void* h_t, void* x_t, hipStream_t s);
+// what such a backward does first: dy quantised, launch_ragged_offsets, launch_wgrad_zero_empty
+void launch_block_prepare(const void* dy, const int32_t* offsets, int E, int H, int F, int r_max, void* codes, uint8_t* scales,
+                          int32_t* poff, void* dw0, void* dw1, void* dw2, hipStream_t s);
 // out [rows, 2F] = dg | du from dh [rows, F] and g, u (rows ld_gu elements apart); rows = *n_rows (device)
 void launch_swiglu_backward(const void* dh, const void* g, const void* u, size_t ld_gu, const int32_t* n_rows,
                             int r_max, int F, void* out, hipStream_t s);
@@ -226,9 +239,8 @@ void launch_probe_mfma_bf16(const void* image, int iters, int workgroups, float*
 void launch_probe_mfma_fp8(const void* image, int iters, int workgroups, float* sink, unsigned long long* ticks,
                            hipStream_t s);
 
-// E4M3 with a scale for every block of 128 (fp8_block.h).  Rows below *n_rows (null: all `rows`)
-void launch_block_quantize(const void* src, moe_dtype_t dt, int rows, const int32_t* n_rows, int C, void* codes, uint8_t* scales,
-                           hipStream_t s);
+// E4M3 with a scale for every block of 128 (fp8_block.h)
+void launch_block_quantize(const void* src, moe_dtype_t dt, int rows, int C, void* codes, uint8_t* scales, hipStream_t s);
 // w [E, N, K] to codes [E, N, K] and/or, transposed, to column t0 of [E, K, ldt] (null: not)
 void launch_block_weights(const void* w, moe_dtype_t dt, int E, int N, int K, void* codes, uint8_t* scales, void* codes_t,
                           uint8_t* scales_t, int ldt, int t0, hipStream_t s);

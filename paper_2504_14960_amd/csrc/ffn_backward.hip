@@ -49,26 +49,35 @@ struct TransposeRows {   // where 64 of the tile's rows come from
     int first, valid;    // first source row; how many of the 64 exist, the rest count as zeros
 };
 
-// eight neighbouring values of a row, as bf16
+// eight neighbouring values of a row: read, and (once all of a thread's are under way) made bf16
 template <bool STREAM>
 struct Bf16Rows {
+    using Raw = u32x4;
     const uint16_t* src;
     size_t ld;
-    __device__ __forceinline__ u32x4 operator()(int r, int c) const {
+    __device__ __forceinline__ Raw read(int r, int c) const {
         const u32x4* from = reinterpret_cast<const u32x4*>(src + (size_t)r * ld + c);
         return STREAM ? __builtin_nontemporal_load(from) : *from;
     }
+    static __device__ __forceinline__ u32x4 value(const Raw& raw) { return raw; }
 };
 struct BlockRows {
+    struct Raw {
+        u32x2 codes;
+        uint32_t scale;
+    };
     const uint8_t *codes, *scales;
     int C, stride;
-    __device__ __forceinline__ u32x4 operator()(int r, int c) const {
-        const u32x2 q = *reinterpret_cast<const u32x2*>(codes + (size_t)r * C + c);
-        const float scale = block_value(scales[(size_t)r * stride + c / kBlock]);
+    __device__ __forceinline__ Raw read(int r, int c) const {
+        return {*reinterpret_cast<const u32x2*>(codes + (size_t)r * C + c), scales[(size_t)r * stride + c / kBlock]};
+    }
+    static __device__ __forceinline__ u32x4 value(const Raw& raw) {
+        const float scale = block_value(raw.scale);
         u32x4 v;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)q[j], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)q[j], true);
+            const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)raw.codes[j], false);
+            const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)raw.codes[j], true);
             v[2 * j] = pack2_bf16(lo[0] * scale, lo[1] * scale);
             v[2 * j + 1] = pack2_bf16(hi[0] * scale, hi[1] * scale);
         }
@@ -90,24 +99,25 @@ struct TransposeTile {
     template <typename Rows>
     __device__ __forceinline__ void load(const Rows& rows, int c0, int cols, const TransposeRows (&part)[PARTS]) {
         const int c = (threadIdx.x % VC) * 8, rp = threadIdx.x / VC;
-        u32x4 v[NP][2];
+        typename Rows::Raw raw[NP][2];
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
             const TransposeRows h = part[p * RPT / 32];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const int rr = 2 * (p * RPT % 32 + rp) + k;
-                v[p][k] = u32x4{0u, 0u, 0u, 0u};
-                if (rr < h.valid && c0 + c < cols) v[p][k] = rows(h.first + rr, c0 + c);   // cols is a multiple of 8
+                raw[p][k] = {};   // zeros
+                if (rr < h.valid && c0 + c < cols) raw[p][k] = rows.read(h.first + rr, c0 + c);   // cols is a multiple of 8
             }
         }
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
             const int q = p * RPT + rp, to = at(q >> 2, c) + (q & 3);
+            const u32x4 even = Rows::value(raw[p][0]), odd = Rows::value(raw[p][1]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                pair[c + 2 * j][to] = (v[p][0][j] & 0xffffu) | (v[p][1][j] << 16);
-                pair[c + 2 * j + 1][to] = (v[p][0][j] >> 16) | (v[p][1][j] & 0xffff0000u);
+                pair[c + 2 * j][to] = (even[j] & 0xffffu) | (odd[j] << 16);
+                pair[c + 2 * j + 1][to] = (even[j] >> 16) | (odd[j] & 0xffff0000u);
             }
         }
     }
@@ -158,8 +168,7 @@ __device__ __forceinline__ int padded_rows(int n) { return n <= 0 ? 0 : max(128,
 
 // poff[e] = first column of expert e's zero-padded segment (exclusive prefix of the padded row counts), e = 0..E.
 // One workgroup of 256 threads; E <= 256.
-__global__ __launch_bounds__(256) void ragged_offsets_kernel(const int32_t* __restrict__ offsets, int E,
-                                                             int32_t* __restrict__ poff) {
+__device__ __forceinline__ void ragged_offsets(const int32_t* __restrict__ offsets, int E, int32_t* __restrict__ poff) {
     __shared__ int scan[2][256];
     const int tid = threadIdx.x;
     const int pn = (tid < E) ? padded_rows(offsets[tid + 1] - offsets[tid]) : 0;
@@ -175,38 +184,95 @@ __global__ __launch_bounds__(256) void ragged_offsets_kernel(const int32_t* __re
     if (tid == 0) poff[0] = 0;
 }
 
+__global__ __launch_bounds__(256) void ragged_offsets_kernel(const int32_t* __restrict__ offsets, int E,
+                                                             int32_t* __restrict__ poff) {
+    ragged_offsets(offsets, E, poff);
+}
+
 // dst[c][poff_e + (r - lo_e)] = src[r][c] for the rows r of expert e; the pad up to
 // padded_rows(n_e) is zero.  One workgroup per (128-column block, 128-row block of the
 // padded axis); the expert of a padded position is the one whose segment [poff_e,
 // poff_e+1) holds it (segments are multiples of 64, so a half block never straddles two).
-template <typename Rows>
-__global__ __launch_bounds__(256) void ragged_transpose_kernel(Rows src, const int32_t* __restrict__ offsets,
-                                                               const int32_t* __restrict__ poff, int E, int C,
-                                                               uint16_t* __restrict__ dst, size_t ldo) {
-    __shared__ __attribute__((aligned(16))) ActTile tile;
-    __shared__ int seg[2][2];   // of each half: first source row, valid rows from there on (-1: past the last segment)
-    const int p0 = blockIdx.y * kActTile, c0 = blockIdx.x * kActTile;
-    if (threadIdx.x < 2) seg[threadIdx.x][1] = -1;
-    __syncthreads();
-    for (int e = threadIdx.x; e < E; e += 256) {
-        const int lo_p = poff[e], hi_p = poff[e + 1];
+struct RaggedTile {
+    ActTile tile;
+    int seg[2][2];   // of each half: first source row, valid rows from there on (-1: past the last segment)
+
+    // false: past the last expert's padding, nothing to write
+    __device__ __forceinline__ bool find(const int32_t* __restrict__ offsets, const int32_t* __restrict__ poff, int E, int p0) {
+        if (threadIdx.x < 2) seg[threadIdx.x][1] = -1;
+        __syncthreads();
+        for (int e = threadIdx.x; e < E; e += 256) {
+            const int lo_p = poff[e], hi_p = poff[e + 1];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int p = p0 + 64 * h;
-            if (lo_p <= p && p < hi_p) {   // at most one expert
-                const int lo = offsets[e], n = offsets[e + 1] - lo;
-                seg[h][0] = lo + (p - lo_p);
-                seg[h][1] = max(0, n - (p - lo_p));   // 0: 64 positions of pure padding
+            for (int h = 0; h < 2; ++h) {
+                const int p = p0 + 64 * h;
+                if (lo_p <= p && p < hi_p) {   // at most one expert
+                    const int lo = offsets[e], n = offsets[e + 1] - lo;
+                    seg[h][0] = lo + (p - lo_p);
+                    seg[h][1] = max(0, n - (p - lo_p));   // 0: 64 positions of pure padding
+                }
             }
         }
+        __syncthreads();
+        return seg[0][1] >= 0;
     }
-    __syncthreads();
-    if (seg[0][1] < 0) return;   // past the last expert's padding: nothing to write
-    const TransposeRows half[2] = {{seg[0][0], min(64, seg[0][1])}, {seg[1][0], min(64, seg[1][1])}};
-    const int n_out = seg[1][1] < 0 ? 64 : kActTile;
-    tile.load(src, c0, C, half);
-    __syncthreads();
-    tile.store(dst, ldo, c0, C, (size_t)p0, n_out);
+    template <typename Rows>
+    __device__ __forceinline__ void move(const Rows& src, int C, int c0, int p0, uint16_t* __restrict__ dst, size_t ldo) {
+        const TransposeRows half[2] = {{seg[0][0], min(64, seg[0][1])}, {seg[1][0], min(64, seg[1][1])}};
+        tile.load(src, c0, C, half);
+        __syncthreads();
+        tile.store(dst, ldo, c0, C, (size_t)p0, seg[1][1] < 0 ? 64 : kActTile);
+    }
+};
+
+__global__ __launch_bounds__(256) void ragged_transpose_kernel(Bf16Rows<false> src, const int32_t* __restrict__ offsets,
+                                                               const int32_t* __restrict__ poff, int E, int C,
+                                                               uint16_t* __restrict__ dst, size_t ldo) {
+    __shared__ __attribute__((aligned(16))) RaggedTile t;
+    const int p0 = blockIdx.y * kActTile;
+    if (t.find(offsets, poff, E, p0)) t.move(src, C, blockIdx.x * kActTile, p0, dst, ldo);
+}
+
+// The four of a backward on E4M3 operands in one launch: dy [., H] and dg | du [., 2F] in bf16, h [., F] and x [., H] as codes.
+// Column blocks of one after those of the other; a workgroup's kind is the same in all its lanes.
+struct BlockTransposes {
+    Bf16Rows<false> dy, dgu;
+    BlockRows h, x;
+    uint16_t *dy_t, *dgu_t, *h_t, *x_t;
+};
+__global__ __launch_bounds__(256) void block_transposes_kernel(BlockTransposes p, const int32_t* __restrict__ offsets,
+                                                               const int32_t* __restrict__ poff, int E, int H, int F, size_t ldo) {
+    __shared__ __attribute__((aligned(16))) RaggedTile t;
+    const int p0 = blockIdx.y * kActTile, hb = H / kActTile, fb = F / kActTile;
+    if (!t.find(offsets, poff, E, p0)) return;
+    int b = (int)blockIdx.x;
+    if (b < hb) return t.move(p.dy, H, b * kActTile, p0, p.dy_t, ldo);
+    if ((b -= hb) < 2 * fb) return t.move(p.dgu, 2 * F, b * kActTile, p0, p.dgu_t, ldo);
+    if ((b -= 2 * fb) < fb) return t.move(p.h, F, b * kActTile, p0, p.h_t, ldo);
+    t.move(p.x, H, (b - fb) * kActTile, p0, p.x_t, ldo);
+}
+
+// What a backward on E4M3 operands does before its products, in one launch (one that finds nothing to do takes 4 us): workgroup 0
+// lays out the padded segments, the next `quantizers` quantise the rows of dy, 64 for each expert and gradient clear those
+// without rows.
+struct BlockPrepare {
+    const int32_t* offsets;
+    int32_t* poff;
+    const void* dy;
+    uint8_t *codes, *scales;
+    bf16_t* dw[3];
+    size_t per_expert;
+    int E, H, r_max, quantizers;
+};
+constexpr int kZeroBlocks = 64;
+__global__ __launch_bounds__(256) void block_prepare_kernel(BlockPrepare p) {
+    int b = (int)blockIdx.x;
+    if (b == 0) return ragged_offsets(p.offsets, p.E, p.poff);
+    if (--b < p.quantizers)
+        return block_quantize_rows<true>(p.dy, min(p.r_max, p.offsets[p.E]), p.H, p.codes, p.scales, b, p.quantizers);
+    b -= p.quantizers;
+    const int i = b % kZeroBlocks, e = b / kZeroBlocks % p.E;
+    zero_empty_expert(p.offsets, e, p.per_expert, p.dw[b / (kZeroBlocks * p.E)], i, kZeroBlocks);
 }
 
 // dg | du from dh [rows, F] and g, u (bf16, rows ld_gu elements apart; out [rows, 2F]): with s = 1/(1+e^-g),
@@ -264,22 +330,35 @@ void launch_ragged_offsets(const int32_t* offsets, int E, int32_t* poff, hipStre
 
 // rp_max: the static bound on the padded axis (a multiple of 64); blocks past the real padded length exit.
 // poff: the E + 1 segment starts written by launch_ragged_offsets
-template <typename Rows>
-static void ragged_transpose(const Rows& src, const int32_t* offsets, const int32_t* poff, int E, int C, int rp_max, void* dst,
-                             hipStream_t s) {
-    if (rp_max <= 0 || C <= 0) return;
-    hipLaunchKernelGGL(ragged_transpose_kernel<Rows>, dim3((C + kActTile - 1) / kActTile, (rp_max + kActTile - 1) / kActTile), dim3(256),
-                       0, s, src, offsets, poff, E, C, static_cast<uint16_t*>(dst), (size_t)rp_max);
-}
-
 void launch_ragged_transpose(const void* src, const int32_t* offsets, const int32_t* poff, int E, int C, int rp_max,
                              void* dst, hipStream_t s) {
-    ragged_transpose(Bf16Rows<false>{static_cast<const uint16_t*>(src), (size_t)C}, offsets, poff, E, C, rp_max, dst, s);
+    if (rp_max <= 0 || C <= 0) return;
+    hipLaunchKernelGGL(ragged_transpose_kernel, dim3((C + kActTile - 1) / kActTile, (rp_max + kActTile - 1) / kActTile), dim3(256), 0, s,
+                       Bf16Rows<false>{static_cast<const uint16_t*>(src), (size_t)C}, offsets, poff, E, C, static_cast<uint16_t*>(dst),
+                       (size_t)rp_max);
 }
 
-void launch_ragged_transpose_block(const void* codes, const uint8_t* scales, const int32_t* offsets, const int32_t* poff, int E, int C,
-                                   int rp_max, void* dst, hipStream_t s) {
-    ragged_transpose(BlockRows{static_cast<const uint8_t*>(codes), scales, C, block_scale_stride(C)}, offsets, poff, E, C, rp_max, dst, s);
+void launch_block_transposes(const void* dy, const void* dgu, const void* h, const uint8_t* h_scales, const void* x,
+                             const uint8_t* x_scales, const int32_t* offsets, const int32_t* poff, int E, int H, int F, int rp_max,
+                             void* dy_t, void* dgu_t, void* h_t, void* x_t, hipStream_t s) {
+    auto bf16 = [](const void* p, int C) { return Bf16Rows<false>{static_cast<const uint16_t*>(p), (size_t)C}; };
+    auto block = [](const void* p, const uint8_t* sc, int C) {
+        return BlockRows{static_cast<const uint8_t*>(p), sc, C, block_scale_stride(C)};
+    };
+    auto out = [](void* p) { return static_cast<uint16_t*>(p); };
+    hipLaunchKernelGGL(block_transposes_kernel, dim3((2 * H + 3 * F) / kActTile, (rp_max + kActTile - 1) / kActTile), dim3(256), 0, s,
+                       BlockTransposes{bf16(dy, H), bf16(dgu, 2 * F), block(h, h_scales, F), block(x, x_scales, H), out(dy_t), out(dgu_t),
+                                       out(h_t), out(x_t)},
+                       offsets, poff, E, H, F, (size_t)rp_max);
+}
+
+void launch_block_prepare(const void* dy, const int32_t* offsets, int E, int H, int F, int r_max, void* codes, uint8_t* scales,
+                          int32_t* poff, void* dw0, void* dw1, void* dw2, hipStream_t s) {
+    const int quantizers = block_quantize_grid(r_max);
+    hipLaunchKernelGGL(block_prepare_kernel, dim3(1 + quantizers + 3 * kZeroBlocks * E), dim3(256), 0, s,
+                       BlockPrepare{offsets, poff, dy, static_cast<uint8_t*>(codes), scales,
+                                    {static_cast<bf16_t*>(dw0), static_cast<bf16_t*>(dw1), static_cast<bf16_t*>(dw2)},
+                                    (size_t)H * F, E, H, r_max, quantizers});
 }
 
 void launch_swiglu_backward(const void* dh, const void* g, const void* u, size_t ld_gu, const int32_t* n_rows,

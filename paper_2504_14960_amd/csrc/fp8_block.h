@@ -47,6 +47,57 @@ __device__ __forceinline__ void bf16x8_to_f32(const u32x4& v, float (&f)[8]) {
     }
 }
 
+// the largest magnitude over the 16 lanes of a row of the wave, in all of them
+__device__ __forceinline__ uint32_t max16(uint32_t v) {
+#pragma unroll
+    for (int d = 1; d < 16; d <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d, 64));
+    return v;
+}
+
+// eight values of a block that 16 neighbouring lanes hold: their codes, and the block's scale
+__device__ __forceinline__ u32x2 quantize8(const float (&f)[8], uint32_t& scale) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, magnitude(f[j]));
+    scale = block_scale(max16(top));
+    const float inv = block_inverse(scale);
+    return u32x2{block_codes(f[0], f[1], f[2], f[3], inv, scale), block_codes(f[4], f[5], f[6], f[7], inv, scale)};
+}
+
+template <bool BF16>
+__device__ __forceinline__ void load8(const void* src, size_t at, float (&f)[8]) {
+    if constexpr (BF16) {
+        bf16x8_to_f32(*reinterpret_cast<const u32x4*>(static_cast<const bf16_t*>(src) + at), f);
+    } else {
+        const f32x4 lo = *reinterpret_cast<const f32x4*>(static_cast<const float*>(src) + at);
+        const f32x4 hi = *reinterpret_cast<const f32x4*>(static_cast<const float*>(src) + at + 4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            f[j] = lo[j];
+            f[4 + j] = hi[j];
+        }
+    }
+}
+
+// Rows 0 .. n - 1, one to a wave, 512 values at a time, by workgroup `block` of `blocks` of four waves
+template <bool BF16>
+__device__ __forceinline__ void block_quantize_rows(const void* __restrict__ src, int n, int C, uint8_t* __restrict__ codes,
+                                                    uint8_t* __restrict__ scales, int block, int blocks) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, stride = block_scale_stride(C);
+    for (int r = block * 4 + wave; r < n; r += blocks * 4)
+        for (int c0 = 0; c0 < C; c0 += 512) {   // uniform trip count: shuffles inside
+            const int c = c0 + 8 * lane;
+            float f[8] = {};
+            if (c < C) load8<BF16>(src, (size_t)r * C + c, f);
+            uint32_t scale;
+            const u32x2 q = quantize8(f, scale);
+            if (c >= C) continue;
+            *reinterpret_cast<u32x2*>(codes + (size_t)r * C + c) = q;
+            if ((lane & 15) == 0) scales[(size_t)r * stride + c / kBlock] = (uint8_t)scale;
+        }
+}
+inline int block_quantize_grid(int rows) { return (int)min((rows + 3ll) / 4, 256ll * 16); }
+
 // What the grouped products of the block-scaled expert FFN work on: C = A [rows, K] . B[e]^T over the rows of every expert
 struct BlockGemm {
     const uint8_t* A;             // codes [rows, K]

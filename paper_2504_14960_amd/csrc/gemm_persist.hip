@@ -767,12 +767,7 @@ void launch_persist(const void* A, const int32_t* offsets, int r_max, int E, int
 __global__ __launch_bounds__(256) void wgrad_zero_empty_kernel(const int32_t* __restrict__ offsets, size_t per_expert,
                                                                bf16_t* __restrict__ dw0, bf16_t* __restrict__ dw1,
                                                                bf16_t* __restrict__ dw2) {
-    const int e = blockIdx.y;
-    if (offsets[e + 1] - offsets[e] > 0) return;
-    bf16_t* const dw = blockIdx.z == 0 ? dw0 : blockIdx.z == 1 ? dw1 : dw2;
-    u32x4* dst = reinterpret_cast<u32x4*>(dw + (size_t)e * per_expert);   // per_expert is a multiple of 8
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < per_expert / 8; i += (size_t)gridDim.x * 256)
-        dst[i] = u32x4{0u, 0u, 0u, 0u};
+    zero_empty_expert(offsets, blockIdx.y, per_expert, blockIdx.z == 0 ? dw0 : blockIdx.z == 1 ? dw1 : dw2, blockIdx.x, gridDim.x);
 }
 
 template <int BM, int BN, int WGM, int WGN, bool STREAM_OUT, bool DEEP_B = false>

@@ -102,7 +102,7 @@ def _backward(**kw):
     (dict(R=-1), 1), (dict(E=0), 1), (dict(H=64), 2), (dict(x=None), 1), (dict(xs=None), 1), (dict(h=None), 1), (dict(hs=P + 3), 1),
     (dict(gu=None), 1), (dict(dy=None), 1), (dict(off=None), 1), (dict(t=None), 1), (dict(ts=None), 1), (dict(d=None), 1),
     (dict(ds=None), 1), (dict(dx=None), 1), (dict(dg=None), 1), (dict(du=None), 1), (dict(dd=P + 8), 1), (dict(ws=None), 3),
-    (dict(bytes=100), 3),
+    (dict(bytes=100), 3), (dict(R=(1 << 22) + 1, bytes=1 << 50), 2),
 ])
 def test_backward_refusals(kw, status):
     assert _backward(**kw) == status
