@@ -1,5 +1,7 @@
 // Quantisation to E4M3 with a scale for every block of 128 (fp8_block.h): rows (1 x 128), rows gathered by expert, weights
 // (128 x 128) in the layouts of the forward and of the backward.  Bound by memory: every value is read once.
+#include <type_traits>
+
 #include "fp8_block.h"
 
 namespace moe {
@@ -37,9 +39,20 @@ __global__ __launch_bounds__(256) void permute_copy_block_kernel(const bf16_t* _
     }
 }
 
+template <bool STREAM, typename V>
+__device__ __forceinline__ void store_codes(uint8_t* to, const V& v) {
+    if (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<V*>(to));
+    else *reinterpret_cast<V*>(to) = v;
+}
+
 // A block of 128 x 128 to a workgroup: w [E, N, K] -> codes [E, N, K] and, transposed, at column t0 of [E, K, ldt]; either may
 // be null.  A thread holds eight columns of eight rows.
-template <bool BF16>
+// STREAM, past the caches, where the codes that a call writes are more than the memory-side cache keeps: the stores, and the
+// loads of bf16 weights (an fp32 thread's two loads share a line, which the first would drop).  The call, us, not streamed /
+// so, and with the FFN of 64 rows per expert behind it: 12 experts, 1024 x 1408, fp32 (104 MB of codes) 72 / 67 and 100 / 101;
+// 8, 2048 x 2048, bf16 (201 MB) with it 131 / 132; 16, 2048 x 2048, bf16 (403 MB) with it 234 / 216; 8, 4096 x 4096, fp32
+// (805 MB) with it 577 / 554, streamed loads too 564; 64, 4096 x 1408, bf16 (2.2 GB) 845 / 788 (5.6 TB/s) and 1080 / 1024.
+template <bool BF16, bool STREAM>
 __global__ __launch_bounds__(256) void block_weights_kernel(const void* __restrict__ w, int N, int K, uint8_t* __restrict__ codes,
                                                             uint8_t* __restrict__ scales, uint8_t* __restrict__ codes_t,
                                                             uint8_t* __restrict__ scales_t, int ldt, int t0) {
@@ -50,7 +63,7 @@ __global__ __launch_bounds__(256) void block_weights_kernel(const void* __restri
     float f[8][8];
     uint32_t top = 0;
 #pragma unroll
-    for (int r = 0; r < 8; ++r) load8<BF16>(w, ((size_t)e * N + n0 + 8 * rv + r) * K + k0 + 8 * cv, f[r]);
+    for (int r = 0; r < 8; ++r) load8<BF16, BF16 && STREAM>(w, ((size_t)e * N + n0 + 8 * rv + r) * K + k0 + 8 * cv, f[r]);
 #pragma unroll
     for (int r = 0; r < 8; ++r)
 #pragma unroll
@@ -69,7 +82,7 @@ __global__ __launch_bounds__(256) void block_weights_kernel(const void* __restri
     if (codes) {
 #pragma unroll
         for (int r = 0; r < 8; ++r)
-            *reinterpret_cast<u32x2*>(codes + ((size_t)e * N + n0 + 8 * rv + r) * K + k0 + 8 * cv) = q[r];
+            store_codes<STREAM>(codes + ((size_t)e * N + n0 + 8 * rv + r) * K + k0 + 8 * cv, q[r]);
         if (threadIdx.x == 0) scales[((size_t)e * (N / kBlock) + blockIdx.y) * block_scale_stride(K) + blockIdx.x] = (uint8_t)scale;
     }
     if (!codes_t) return;
@@ -84,7 +97,7 @@ __global__ __launch_bounds__(256) void block_weights_kernel(const void* __restri
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int c = 32 * i + threadIdx.x / 8, at = threadIdx.x % 8 * 16;
-        *reinterpret_cast<u32x4*>(codes_t + ((size_t)e * K + k0 + c) * ldt + t0 + n0 + at) = *reinterpret_cast<const u32x4*>(&tile[c][at]);
+        store_codes<STREAM>(codes_t + ((size_t)e * K + k0 + c) * ldt + t0 + n0 + at, *reinterpret_cast<const u32x4*>(&tile[c][at]));
     }
     if (threadIdx.x == 0)
         scales_t[((size_t)e * (K / kBlock) + blockIdx.x) * block_scale_stride(ldt) + t0 / kBlock + blockIdx.y] = (uint8_t)scale;
@@ -99,7 +112,11 @@ void launch_block_quantize(const void* src, moe_dtype_t dt, int rows, int C, voi
 
 void launch_block_weights(const void* w, moe_dtype_t dt, int E, int N, int K, void* codes, uint8_t* scales, void* codes_t,
                           uint8_t* scales_t, int ldt, int t0, hipStream_t s) {
-    auto kern = dt == MOE_BF16 ? block_weights_kernel<true> : block_weights_kernel<false>;
+    const bool stream = (size_t)3 * E * N * K * ((codes != nullptr) + (codes_t != nullptr)) > kCachedBytes;   // of the layer's three
+    auto pick = [&](auto bf16) {
+        return stream ? block_weights_kernel<decltype(bf16)::value, true> : block_weights_kernel<decltype(bf16)::value, false>;
+    };
+    auto kern = dt == MOE_BF16 ? pick(std::true_type{}) : pick(std::false_type{});
     hipLaunchKernelGGL(kern, dim3(K / kBlock, N / kBlock, E), dim3(256), 0, s, w, N, K, static_cast<uint8_t*>(codes), scales,
                        static_cast<uint8_t*>(codes_t), scales_t, ldt, t0);
 }

@@ -26,6 +26,7 @@ inline void allow_lds(OncePerDevice& lds, const void* kern, int bytes) {
 }
 
 constexpr int kWave = 64;
+constexpr size_t kCachedBytes = 140u << 20;         // results of a call up to here are left to the caches for their reader
 constexpr int kMaxExperts = 256;
 constexpr int kMaxTopK = 64;
 constexpr int kMaxBalanceTokens = 1 << 30;         // of one balance-loss call

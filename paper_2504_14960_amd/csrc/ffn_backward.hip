@@ -138,7 +138,6 @@ struct TransposeTile {
 };
 using ActTile = TransposeTile<128, 128, false>;
 constexpr int kActTile = 128;
-constexpr size_t kCachedBytes = 140u << 20;   // results up to here are left to the caches
 
 // dst[b][c][col0 + r] = src[b][r][c];  R, C multiples of 8.  DOWN: neighbouring workgroups below one another.
 template <int TR, int TC, bool STREAM, bool DOWN>

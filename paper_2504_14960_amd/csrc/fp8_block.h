@@ -64,10 +64,11 @@ __device__ __forceinline__ u32x2 quantize8(const float (&f)[8], uint32_t& scale)
     return u32x2{block_codes(f[0], f[1], f[2], f[3], inv, scale), block_codes(f[4], f[5], f[6], f[7], inv, scale)};
 }
 
-template <bool BF16>
+template <bool BF16, bool STREAM = false>
 __device__ __forceinline__ void load8(const void* src, size_t at, float (&f)[8]) {
     if constexpr (BF16) {
-        bf16x8_to_f32(*reinterpret_cast<const u32x4*>(static_cast<const bf16_t*>(src) + at), f);
+        const u32x4* from = reinterpret_cast<const u32x4*>(static_cast<const bf16_t*>(src) + at);
+        bf16x8_to_f32(STREAM ? __builtin_nontemporal_load(from) : *from, f);
     } else {
         const f32x4 lo = *reinterpret_cast<const f32x4*>(static_cast<const float*>(src) + at);
         const f32x4 hi = *reinterpret_cast<const f32x4*>(static_cast<const float*>(src) + at + 4);

@@ -703,7 +703,7 @@ void launch_select(const float* logits, const float* bias, int T, int E, int K, 
 void launch_select_dlogits(const float* logits, const int32_t* idx, const float* dgate, const float* addend, int T, int E, int K,
                            moe_score_t score, int renorm, float scale, float* dlogits, hipStream_t s) {
     // streamed where what follows would not find them in the 256 MB cache (262144 tokens x 256 experts: 84 us, streamed 74)
-    const bool stream = (size_t)T * E * sizeof(float) > 140u << 20;
+    const bool stream = (size_t)T * E * sizeof(float) > kCachedBytes;
     const SelectBackwardArgs p = {logits, idx, dgate, addend, dlogits, scale, T, E, K, score == MOE_SCORE_SIGMOID, renorm};
     const int tw = K <= 8 ? 8 : 4;
     auto pick = [&](auto st) {

@@ -101,6 +101,20 @@ def test_weights_in_one_layout_only():
         assert torch.equal(v, both[k])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_weights_of_more_than_the_caches_hold(dtype):
+    """151 MB of codes in one call against the two layouts in calls of their own."""
+    E, H, F = 4, 4096, 1536
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    w = [(torch.randn(s, generator=gen, device="cuda") * 0.02).to(dtype) for s in ((E, F, H), (E, F, H), (E, H, F))]
+    both = _quantized_weights(w)
+    halves = _quantized_weights(w, layout=False)
+    halves.update({k: _bytes(*both[k].shape) for k in ("wgu_t", "wgu_t_scales", "wd_t", "wd_t_scales")})
+    moe.expert_weights_fp8_block(*w, *[None] * 6, *list(halves.values())[6:])
+    for k, v in both.items():
+        assert torch.equal(v, halves[k]), k
+
+
 @pytest.mark.parametrize("T,H,E,K,capacity", [(1, 128, 8, 2, 0), (5, 384, 4, 4, 0), (64, 1408, 64, 8, 0), (777, 512, 12, 3, 150), (3000, 256, 8, 2, 0),
                                               (9000, 128, 64, 6, 700), (1500, 6144, 8, 2, 0), (300, 16384, 16, 1, 0), (20000, 256, 8, 2, 0)])
 def test_permute_is_permute_and_quantisation(T, H, E, K, capacity):
