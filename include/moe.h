@@ -401,12 +401,15 @@ moe_status_t moe_balance_loss_backward(const float* logits, const uint8_t* token
  *
  * Of equal keys and of equal groups the lower index comes first.  The bias chooses and has
  * no part in the gates.  An expert whose logit is -inf or NaN, or whose key is NaN or not
- * above the lowest finite number, is not selected (nor counted in the softmax, where its logit is); slots for which no expert is
- * left get topk_idx = -1 (a dropped assignment everywhere in this library) and gate 0.
+ * above the lowest finite number, is not selected (nor, for its logit, counted in the
+ * softmax, where exp(inf - inf) is 1); slots for which no expert is left get topk_idx = -1
+ * (a dropped assignment everywhere in this library) and gate 0.  A group's value is at least
+ * the lowest finite number if it has an expert, else the group comes behind all others.
  *
  * x, w_router, logit_bias, logits, T, H, E, K, dt, limits and errors as moe_router_topk
  * (x == NULL: logits is the input).  select_bias [E] fp32 or NULL; 1 <= n_groups divides E,
- * 1 <= topk_groups <= n_groups, K <= topk_groups * (E / n_groups), gate_scale finite.
+ * 1 <= topk_groups <= n_groups, K <= topk_groups * (E / n_groups), gate_scale finite,
+ * T <= 2^27.
  */
 typedef enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 } moe_score_t;
 
@@ -428,7 +431,7 @@ moe_status_t moe_router_select(const void* x, const void* w_router, const float*
  * workspace and errors.  x and w_router may be NULL where dw_router and dx are not asked
  * for.  Slots outside [0,E) and experts whose logit is -inf or NaN get no gradient, and
  * what dgate holds there is not looked at; nor do tokens whose selected scores are all 0 in
- * fp32.
+ * fp32.  T <= 2^27.
  */
 moe_status_t moe_router_select_backward(const void* x, const void* w_router, const float* logits,
                                         const int32_t* topk_idx, const float* dgate,

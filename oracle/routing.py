@@ -34,13 +34,14 @@ def select(logits, K, score, bias=None, groups=1, topk_groups=1, group_best=2, r
         key = s.astype(np.float32)
         if bias is not None:
             key = key + np.asarray(bias, dtype=np.float32)
-        key = np.where(taken & (key > -np.inf), key, -np.inf).astype(np.float32)
+        low = np.finfo(np.float32).min
+        key = np.where(taken & (key > low), key, -np.inf).astype(np.float32)
         if groups > 1:
             g = key.reshape(T, groups, E // groups)
             best = -np.sort(-g, axis=2)[:, :, :group_best]
             value = best[:, :, 0].copy()
             if best.shape[2] > 1:
-                value = np.where(best[:, :, 1] > -np.inf, value + best[:, :, 1], value)
+                value = np.where(best[:, :, 1] > -np.inf, np.maximum(value + best[:, :, 1], low), value)
             keep = np.zeros((T, groups), dtype=bool)
             np.put_along_axis(keep, _first(value, topk_groups), True, 1)
             key = np.where(keep[:, :, None], g, -np.inf).reshape(T, E)

@@ -499,6 +499,7 @@ moe_status_t moe_router_select(const void* x, const void* w_router, const float*
     static const char* fn = "moe_router_select";
     if (x == nullptr) H = (dt == MOE_BF16) ? 8 : 4;  // ignored, keep the shape check quiet
     if (moe_status_t st = check_dims(fn, T, H, E, K, dt)) return st;
+    if (T > kMaxSelectTokens) return fail(MOE_ERR_UNSUPPORTED, "%s: T=%d exceeds the limit 2^27", fn, T);
     if (moe_status_t st = check_score(fn, score, gate_scale)) return st;
     if (n_groups < 1 || n_groups > E || E % n_groups != 0)
         return fail(MOE_ERR_INVALID_ARG, "%s: n_groups=%d must divide E=%d", fn, n_groups, E);
@@ -527,6 +528,7 @@ moe_status_t moe_router_select_backward(const void* x, const void* w_router, con
                                         moe_stream_t stream) {
     static const char* fn = "moe_router_select_backward";
     if (!dx && !dw_router) H = 8;  // ignored, keep the shape check quiet
+    if (T > kMaxSelectTokens) return fail(MOE_ERR_UNSUPPORTED, "%s: T=%d exceeds the limit 2^27", fn, T);
     if (moe_status_t st = check_score(fn, score, gate_scale)) return st;
     if (moe_status_t st = check_router_backward(fn, x, w_router, logits, topk_idx, dgate, dlogits_addend, T, H, E, K, dt, dlogits, dx,
                                                 dw_router, dbias, workspace, workspace_bytes))

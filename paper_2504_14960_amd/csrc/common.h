@@ -31,6 +31,7 @@ constexpr int kMaxExperts = 256;
 constexpr int kMaxTopK = 64;
 constexpr int kMaxBalanceTokens = 1 << 30;         // of one balance-loss call
 constexpr int kMaxSequences = 65536;               // of one balance-loss call
+constexpr int kMaxSelectTokens = 1 << 27;          // of one selection by scores, or its backward
 constexpr int kMaxCountRows = 1 << 20;             // of one bias update
 constexpr int kMaxBlockBackwardRows = 1 << 22;     // of one backward on block-scaled E4M3: 32-bit offsets in the transposed rows
 constexpr int kMaxListTensors = 1 << 26;           // of one gradient-norm or AdamW call

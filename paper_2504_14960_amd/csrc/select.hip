@@ -24,15 +24,15 @@ struct SelectArgs {
 
 constexpr double kNever = -__builtin_huge_val();   // the key of an expert that is not selected whatever else there is
 
-// What an expert is ranked by, as one number: its score and bias, and in the bits behind fp32's its index, so that of equal ones
-// the lower index is the larger number.
-__device__ __forceinline__ double select_key(float choice, int e) {
-    if (!(choice > -__FLT_MAX__)) return kNever;             // NaN, -inf and the lowest number
-    choice = fminf(choice, __FLT_MAX__) + 0.f;               // -0 to +0
-    uint64_t b = __builtin_bit_cast(uint64_t, (double)choice);
-    b |= (uint64_t)(choice < 0.f ? e : 255 - e);
+// What an expert or a group is ranked by, as one number: its value, and in the bits behind fp32's its index, so that of equal ones
+// the lower index is the larger number.  Infinity as 2^128, which leaves those bits free.
+__device__ __forceinline__ double rank_key(float value, int e) {
+    uint64_t b = __builtin_bit_cast(uint64_t, fmin((double)(value + 0.f), 0x1p128));   // -0 to +0
+    b |= (uint64_t)(value < 0.f ? e : 255 - e);
     return __builtin_bit_cast(double, b);
 }
+// score and bias; not NaN, -inf or the lowest number
+__device__ __forceinline__ double select_key(float choice, int e) { return choice > -__FLT_MAX__ ? rank_key(choice, e) : kNever; }
 __device__ __forceinline__ int key_expert(double key) {
     const uint64_t b = __builtin_bit_cast(uint64_t, key);
     return (int)(b >> 63 ? b & 255u : 255u - (b & 255u));
@@ -120,7 +120,7 @@ __device__ __forceinline__ void select_token(const SelectArgs& p, int t, int lan
                 if (first > kNever) {
                     float sum = key_choice(first);
                     if (p.group_best > 1 && second > kNever) sum += key_choice(second);
-                    mine[j] = select_key(sum, g);
+                    mine[j] = rank_key(fmaxf(sum, -__FLT_MAX__), g);
                 }
                 best[g] = mine[j];
             }
@@ -174,8 +174,9 @@ __device__ __forceinline__ void select_token(const SelectArgs& p, int t, int lan
 template <int VPL>
 __global__ __launch_bounds__(64 * kSelectWaves) void select_wave_kernel(SelectArgs p) {
     __shared__ double keys[kSelectWaves][64 * VPL], best[kSelectWaves][64 * VPL];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = blockIdx.x * kSelectWaves + wave;
-    if (t < p.T) select_token<VPL>(p, t, threadIdx.x & 63, keys[wave], best[wave]);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (int t = blockIdx.x * kSelectWaves + wave; t < p.T; t += gridDim.x * kSelectWaves)
+        select_token<VPL>(p, t, threadIdx.x & 63, keys[wave], best[wave]);
 }
 
 // ---- up to eight experts a token ----
@@ -357,7 +358,8 @@ __global__ __launch_bounds__(256, 4) void select_lists_kernel(SelectArgs p, int 
 #pragma unroll
         for (int i = 0; i < 8; ++i)   // the lane beside the place in its run
             list[i] = __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, list[i]) | (uint64_t)(sub * 32));
-        bool sure = true, keep = true;
+        // among infinite logits the largest finite one would count as infinite
+        bool sure = SIGMOID || m < __FLT_MAX__, keep = true;
         if (p.groups > 1) {
             // this lane's group: its value, its rank, and the largest value that ranks behind it
             float total = key_choice(list[0]), size = list[0] > kLow ? fabsf(total) : 0.f;
@@ -367,6 +369,7 @@ __global__ __launch_bounds__(256, 4) void select_lists_kernel(SelectArgs p, int 
                 size += fabsf(second);
             }
             size = lanes(size, [](float a, float b) { return fmaxf(a, b); });
+            sure &= size < 1e30f;                            // sums that may overflow
             if (!(list[0] > kLow)) total = -INFINITY;
             int rank = 0;
             float below = -INFINITY;
@@ -380,7 +383,7 @@ __global__ __launch_bounds__(256, 4) void select_lists_kernel(SelectArgs p, int 
             keep = rank < p.topk_groups && total > -INFINITY;
             // a sum may be far smaller than what was added up
             if (rank == p.topk_groups - 1 && below > -INFINITY)
-                sure = (double)total - (double)below > 2. * fma((double)size, doubt.part, doubt.least);
+                sure &= (double)total - (double)below > 2. * fma((double)size, doubt.part, doubt.least);
             if (!keep) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) list[i] = kLow;
@@ -694,7 +697,7 @@ void launch_select(const float* logits, const float* bias, int T, int E, int K, 
                    int group_best, int renorm, float scale, int32_t* idx, float* gate, hipStream_t s) {
     const SelectArgs p = {logits, bias, idx, gate, scale, T, E, K, score == MOE_SCORE_SIGMOID, groups, topk_groups, group_best, renorm};
     if (K <= 8 && launch_lists(p, s)) return;
-    const dim3 grid((T + kSelectWaves - 1) / kSelectWaves), block(64 * kSelectWaves);
+    const dim3 grid(min((T + kSelectWaves - 1) / kSelectWaves, 1 << 20)), block(64 * kSelectWaves);
     if (E <= 64) hipLaunchKernelGGL(select_wave_kernel<1>, grid, block, 0, s, p);
     else if (E <= 128) hipLaunchKernelGGL(select_wave_kernel<2>, grid, block, 0, s, p);
     else hipLaunchKernelGGL(select_wave_kernel<4>, grid, block, 0, s, p);

@@ -102,6 +102,25 @@ def test_large_biases_that_cancel_in_a_group():
         _check(x, 3, routing.SIGMOID, bias, groups=8, topk_groups=2, group_best=2)
 
 
+@pytest.mark.parametrize("K", [4, 12])
+@pytest.mark.parametrize("score", [routing.SOFTMAX, routing.SIGMOID])
+def test_biases_whose_sums_overflow(K, score):
+    rng = np.random.default_rng(7)
+    top = np.finfo(np.float32).max
+    for seed in range(6):
+        bias = rng.choice(np.array([3e38, -3e38, 2e38, -2e38, np.inf, -np.inf, top, -top, 0.1, 0, 1e30, -2e30], dtype=np.float32), size=32)
+        _check(_logits(40, 32, seed, masked=0.1), K, score, bias, groups=8, topk_groups=4, group_best=2)
+        _check(_logits(40, 32, seed, masked=0.1), K, score, bias)
+
+
+@pytest.mark.parametrize("K", [3, 9])
+def test_infinite_logits_beside_the_largest_finite_one(K):
+    rng = np.random.default_rng(8)
+    x = rng.choice(np.array([np.inf, np.finfo(np.float32).max, 1.0, -np.inf, np.nan], dtype=np.float32), size=(300, 12))
+    for bias in (None, (rng.normal(size=12) * 3).astype(np.float32)):
+        _check(x, K, routing.SOFTMAX, bias, renormalize=False)
+
+
 def test_infinite_biases_choose_first_in_order():
     x = _logits(50, 16, 4)
     bias = np.zeros(16, dtype=np.float32)

@@ -84,8 +84,8 @@ def _select(**kw):
     (dict(E=0), 1), (dict(K=0), 1), (dict(K=9), 1), (dict(T=-1), 1), (dict(score=2), 1), (dict(dt=7), 1), (dict(scale=float("nan")), 1),
     (dict(scale=float("inf")), 1), (dict(groups=3), 1), (dict(groups=0), 1), (dict(groups=16), 1), (dict(groups=4, topk_groups=0), 1),
     (dict(groups=4, topk_groups=5), 1), (dict(best=0), 1), (dict(best=3), 1), (dict(groups=4, topk_groups=1, K=3), 1),
-    (dict(E=257, K=1), 2), (dict(E=128, K=65), 2), (dict(T=1 << 30, K=2), 2), (dict(logits=None), 1), (dict(logits=4100), 1),
-    (dict(idx=None), 1), (dict(gate=None), 1), (dict(sb=4097), 1), (dict(x=4096), 1), (dict(x=4096, w=4096, H=12), 2),
+    (dict(E=257, K=1), 2), (dict(E=128, K=65), 2), (dict(T=1 << 30, K=2), 2), (dict(T=(1 << 27) + 1, K=1), 2), (dict(logits=None), 1),
+    (dict(logits=4100), 1), (dict(idx=None), 1), (dict(gate=None), 1), (dict(sb=4097), 1), (dict(x=4096), 1), (dict(x=4096, w=4096, H=12), 2),
 ])
 def test_select_refusals(kw, status):
     assert _select(**kw) == status
@@ -104,7 +104,7 @@ def _backward(**kw):
 
 
 @pytest.mark.parametrize("kw,status", [
-    (dict(score=3), 1), (dict(scale=float("nan")), 1), (dict(K=9), 1), (dict(E=300, K=1), 2), (dict(logits=None), 1),
+    (dict(T=(1 << 27) + 1, K=1), 2), (dict(score=3), 1), (dict(scale=float("nan")), 1), (dict(K=9), 1), (dict(E=300, K=1), 2), (dict(logits=None), 1),
     (dict(idx=None), 1), (dict(dgate=None), 1), (dict(dlogits=None), 1), (dict(addend=8192), 1), (dict(addend=8200), 1),
     (dict(dx=4096), 1), (dict(dw=4096), 1), (dict(dw=4096, x=4096), 3), (dict(dw=4096, x=4096, ws=4096, n=8), 3),
     (dict(dx=4096, w=4096, H=12), 2), (dict(db=4097), 1),
