@@ -761,7 +761,8 @@ moe_status_t moe_expert_down_fp8(const void* h_fp8, const int32_t* expert_offset
  *
  * Scales of rows of C values lie in rows of moe_fp8_block_scale_stride(C) bytes: C / 128,
  * rounded up to a multiple of 4.  The bytes behind a row's last scale are neither written
- * nor made use of.
+ * nor made use of.  In all of these calls C, H and 2F are at most 2^22 (otherwise
+ * MOE_ERR_UNSUPPORTED).
  */
 int moe_fp8_block_scale_stride(int C);
 

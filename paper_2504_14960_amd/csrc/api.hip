@@ -1245,6 +1245,7 @@ moe_status_t moe_fp8_block_quantize(const void* src, moe_dtype_t dt, int rows, i
     if (dt != MOE_F32 && dt != MOE_BF16) return fail(MOE_ERR_INVALID_ARG, "%s: unknown dtype %d", fn, (int)dt);
     if (rows < 0 || C <= 0) return fail(MOE_ERR_INVALID_ARG, "%s: need rows >= 0 and C > 0 (rows=%d C=%d)", fn, rows, C);
     if (C % kBlock) return fail(MOE_ERR_UNSUPPORTED, "%s: C=%d must be a multiple of 128", fn, C);
+    if (C > kMaxBlockRow) return fail(MOE_ERR_UNSUPPORTED, "%s: C=%d exceeds the limit %d", fn, C, kMaxBlockRow);
     if (rows == 0) return MOE_OK;
     REQUIRE_PTR(fn, src);
     REQUIRE_PTR(fn, codes);
@@ -1297,6 +1298,7 @@ moe_status_t moe_permute_fp8_block(const void* x_bf16, const int32_t* topk_idx, 
     static const char* fn = "moe_permute_fp8_block";
     if (moe_status_t st = check_dims(fn, T, H, E, K, MOE_BF16)) return st;
     if (H % kBlock) return fail(MOE_ERR_UNSUPPORTED, "%s: H=%d must be a multiple of 128", fn, H);
+    if (H > kMaxBlockRow) return fail(MOE_ERR_UNSUPPORTED, "%s: H=%d exceeds the limit %d", fn, H, kMaxBlockRow);
     REQUIRE_PTR(fn, expert_counts);
     REQUIRE_PTR(fn, expert_offsets);
     if (T == 0) {

@@ -37,7 +37,8 @@ P = 4096
 
 
 @pytest.mark.parametrize("args,status", [
-    ((P, 2, 4, 128, P, P), 1), ((P, 1, -1, 128, P, P), 1), ((P, 1, 4, 0, P, P), 1), ((P, 1, 4, 96, P, P), 2), ((None, 1, 4, 128, P, P), 1),
+    ((P, 2, 4, 128, P, P), 1), ((P, 1, -1, 128, P, P), 1), ((P, 1, 4, 0, P, P), 1), ((P, 1, 4, 96, P, P), 2), ((P, 1, 4, 1 << 23, P, P), 2),
+    ((None, 1, 4, 128, P, P), 1),
     ((P + 8, 1, 4, 128, P, P), 1), ((P, 1, 4, 128, None, P), 1), ((P, 1, 4, 128, P + 4, P), 1), ((P, 1, 4, 128, P, None), 1),
     ((P, 1, 4, 128, P, P + 2), 1), ((None, 1, 0, 128, None, None), 0),
 ])
@@ -68,7 +69,7 @@ def _permute(**kw):
 
 
 @pytest.mark.parametrize("kw,status", [
-    (dict(H=64), 2), (dict(H=136), 2), (dict(T=-1), 1), (dict(K=9), 1), (dict(E=300), 2), (dict(x=None), 1), (dict(c=None), 1),
+    (dict(H=64), 2), (dict(H=136), 2), (dict(H=1 << 23), 2), (dict(T=-1), 1), (dict(K=9), 1), (dict(E=300), 2), (dict(x=None), 1), (dict(c=None), 1),
     (dict(s=None), 1), (dict(s=P + 2), 1), (dict(idx=None), 1), (dict(roa=None), 1), (dict(aor=None), 1), (dict(n=None), 1),
     (dict(off=None), 1), (dict(ws=None), 3), (dict(bytes=8), 3),
 ])
