@@ -7,6 +7,7 @@
 #pragma once
 
 #include "common.h"
+#include "wave_sum.h"
 
 namespace moe {
 
@@ -49,9 +50,16 @@ __device__ __forceinline__ void bf16x8_to_f32(const u32x4& v, float (&f)[8]) {
 
 // the largest magnitude over the 16 lanes of a row of the wave, in all of them
 __device__ __forceinline__ uint32_t max16(uint32_t v) {
-#pragma unroll
-    for (int d = 1; d < 16; d <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d, 64));
-    return v;
+    v = max(v, dpp<0x121>(v));   // row_ror 1, 2, 4, 8
+    v = max(v, dpp<0x122>(v));
+    v = max(v, dpp<0x124>(v));
+    return max(v, dpp<0x128>(v));
+}
+
+// the largest magnitude over the lanes that are congruent modulo 16, in all of them
+__device__ __forceinline__ uint32_t max_rows(uint32_t v) {
+    auto larger = [](uint32_t a, uint32_t b) { return max(a, b); };
+    return with_swapped<true>(with_swapped<false>(v, larger), larger);
 }
 
 // eight values of a block that 16 neighbouring lanes hold: their codes, and the block's scale

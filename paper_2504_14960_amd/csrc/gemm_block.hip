@@ -25,12 +25,6 @@ __device__ __forceinline__ f32x4 mfma_block(const Piece& w, const Piece& a, f32x
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, av, c, 0, 0, 0, (int)sw, 0, (int)sa);
 }
 
-// the largest magnitude over the four lane groups that hold a row
-__device__ __forceinline__ uint32_t row_max(uint32_t v) {
-    v = max(v, (uint32_t)__shfl_xor((int)v, 16, 64));
-    return max(v, (uint32_t)__shfl_xor((int)v, 32, 64));
-}
-
 // Tile of 16 MB rows x 32 CW columns.  A wave has 32 of the columns (of gate and of up); KS waves share them and take the blocks
 // along the contraction in turn.
 template <int MODE, int MB, int CW, int KS>
@@ -168,7 +162,7 @@ __global__ __launch_bounds__(64 * CW * KS) void block_rows_kernel(BlockGemm p) {
             }
 #pragma unroll
             for (int h = 0; h < PARTS; ++h) {
-                const uint32_t m = row_max(top[h]);
+                const uint32_t m = max_rows(top[h]);
                 if (fk == 0 && writes) tops[h][wave][r] = m;
             }
         }

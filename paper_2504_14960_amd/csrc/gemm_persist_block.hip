@@ -246,8 +246,7 @@ struct SwigluStore {
                     acc[i][j][u] = h;
                     top = max(top, magnitude(h));
                 }
-            top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
-            top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+            top = max_rows(top);
             if (fk == 0) mine[16 * i + fr] = top;
 #pragma unroll
             for (int j = 0; j < FO; ++j) asm volatile("" : "+a"(acc[i][j]));
@@ -286,9 +285,14 @@ struct SwigluStore {
 };
 
 // dg | du from dh and the saved g | u, in bf16 and as codes.  16 rows of dh at a time go through the patch in fp32, so that a
-// lane then has eight neighbouring columns of a row, sixteen lanes a block.
+// lane then has eight neighbouring columns of a row, sixteen lanes a block.  The next 16 rows' g | u are asked for as these are
+// used up.  Buffer accesses, which leave out what is not in the tile without a branch: nothing waits for the stores.  (Asked for when
+// needed, behind branches: 12 experts, 2331 rows, 1024 x 1408, 28 us instead of 24; 64 experts, 16384 rows, 6144 x 2048, 350 instead
+// of 325.)
 struct GradStore {
     BlockGemm p;
+
+    static constexpr int kFlags = 0x00027000;
 
     template <int FM, int FN>
     __device__ __forceinline__ void tile(f32x4 (&acc)[FM][FN], int row0, int rows, int n0, int wm, int wn, int lane, uint8_t* stage,
@@ -298,32 +302,37 @@ struct GradStore {
         asm volatile("" : "+v"(lane));
         const int fr = lane & 15, fk = lane >> 4, rl = lane >> 4, gl = lane & 15;
         const int col = n0 + wn * 128 + 8 * gl;
-        const int stride = block_scale_stride(2 * p.N);
+        const uint32_t pitch = 4u * (uint32_t)p.N, stride = (uint32_t)block_scale_stride(2 * p.N);   // bytes
+        auto rows_of = [&](const void* base, uint32_t bytes) {
+            return __builtin_amdgcn_make_buffer_rsrc(static_cast<uint8_t*>(const_cast<void*>(base)) + (size_t)row0 * bytes, 0,
+                                                     (int)((uint32_t)rows * bytes), kFlags);
+        };
+        const auto gu = rows_of(p.gu, pitch), dgu = rows_of(p.dgu, pitch), codes = rows_of(p.C, pitch / 2),
+                   scales = rows_of(p.c_scales, stride);
+        const uint32_t first = (uint32_t)(col < p.N ? wm * WM + rl : rows);   // rows from `rows` on are none
+        u32x4 gv[4], uv[4];
+        auto load = [&](int i, int it) {
+            const uint32_t at = (first + 16 * i + 4 * it) * pitch + 2u * (uint32_t)col;
+            gv[it] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(gu, (int)at, 0, 0));
+            uv[it] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(gu, (int)(at + 2u * (uint32_t)p.N), 0, 0));
+        };
+#pragma unroll
+        for (int it = 0; it < 4; ++it) load(0, it);
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
             __builtin_amdgcn_sched_barrier(0);
-            u32x4 gv[4], uv[4];
-#pragma unroll
-            for (int it = 0; it < 4; ++it) {
-                const int grow = wm * WM + 16 * i + 4 * it + rl;
-                gv[it] = uv[it] = u32x4{0u, 0u, 0u, 0u};
-                if (grow < rows && col < p.N) {
-                    const bf16_t* const src = p.gu + (size_t)(row0 + grow) * (2 * p.N) + col;
-                    gv[it] = *reinterpret_cast<const u32x4*>(src);
-                    uv[it] = *reinterpret_cast<const u32x4*>(src + p.N);
-                }
-            }
 #pragma unroll
             for (int j = 0; j < FN; ++j) asm volatile("" : "+a"(acc[i][j]));
 #pragma unroll
             for (int j = 0; j < FN; ++j) *reinterpret_cast<f32x4*>(stage + fr * W + (((4 * j + fk) ^ (2 * fr & 31)) << 4)) = acc[i][j];
-            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int it = 0; it < 4; ++it) {
-                const int row = 4 * it + rl, grow = wm * WM + 16 * i + row;
+                __builtin_amdgcn_sched_barrier(0);
+                const int row = 4 * it + rl;
                 float g[8], u[8], dg[8], du[8];
                 bf16x8_to_f32(gv[it], g);
                 bf16x8_to_f32(uv[it], u);
+                if (i + 1 < FM) load(i + 1, it);
                 uint32_t tg = 0, tu = 0;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -338,23 +347,22 @@ struct GradStore {
                         tu = max(tu, magnitude(du[e]));
                     }
                 }
-#pragma unroll
-                for (int d = 1; d < 16; d <<= 1) {
-                    tg = max(tg, (uint32_t)__shfl_xor((int)tg, d, 64));
-                    tu = max(tu, (uint32_t)__shfl_xor((int)tu, d, 64));
-                }
-                if (grow >= rows || col >= p.N) continue;
-                const size_t at = (size_t)(row0 + grow) * (2 * p.N) + col;
+                tg = max16(tg);
+                tu = max16(tu);
+                const uint32_t grow = first + 16 * i + 4 * it;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const float(&v)[8] = h ? du : dg;
-                    const uint32_t scale = block_scale(h ? tu : tg);
+                    const uint32_t scale = block_scale(h ? tu : tg), c = (uint32_t)(col + h * p.N);
                     const float inv = block_inverse(scale);
-                    *reinterpret_cast<u32x4*>(p.dgu + at + h * p.N) =
-                        u32x4{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])};
-                    *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(p.C) + at + h * p.N) =
-                        u32x2{block_codes(v[0], v[1], v[2], v[3], inv, scale), block_codes(v[4], v[5], v[6], v[7], inv, scale)};
-                    if (gl == 0) p.c_scales[(size_t)(row0 + grow) * stride + (col + h * p.N) / kBlock] = (uint8_t)scale;
+                    __builtin_amdgcn_raw_buffer_store_b128(
+                        u32x4{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])}, dgu,
+                        (int)(grow * pitch + 2 * c), 0, 0);
+                    __builtin_amdgcn_raw_buffer_store_b64(
+                        u32x2{block_codes(v[0], v[1], v[2], v[3], inv, scale), block_codes(v[4], v[5], v[6], v[7], inv, scale)}, codes,
+                        (int)(grow * (pitch / 2) + c), 0, 0);
+                    __builtin_amdgcn_raw_buffer_store_b8((uint8_t)scale, scales, (int)((gl == 0 ? grow : (uint32_t)rows) * stride + c / kBlock),
+                                                         0, 0);
                 }
             }
         }
