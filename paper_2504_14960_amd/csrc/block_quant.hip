@@ -124,6 +124,8 @@ void launch_block_weights(const void* w, moe_dtype_t dt, int E, int N, int K, vo
 void launch_permute_block(const void* x, const int32_t* idx, int T, int H, int E, int K, int capacity, int r_max, void* codes,
                           uint8_t* scales, int32_t* counts, int32_t* offsets, int32_t* row_of_assign, int32_t* assign_of_row,
                           void* ws, hipStream_t s) {
+    if (launch_permute_block_small(x, idx, T, H, E, K, capacity, r_max, codes, scales, counts, offsets, row_of_assign, assign_of_row, s))
+        return;
     launch_permute(nullptr, idx, T, H, E, K, capacity, r_max, MOE_BF16, nullptr, counts, offsets, row_of_assign, assign_of_row, ws, s);
     hipLaunchKernelGGL(permute_copy_block_kernel, dim3((unsigned)min(((long long)T * ((H + 511) / 512) + 3) / 4, 256ll * 32)), dim3(256), 0, s,
                        static_cast<const bf16_t*>(x), row_of_assign, T, K, H, r_max, static_cast<uint8_t*>(codes), scales);

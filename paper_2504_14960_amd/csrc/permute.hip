@@ -17,6 +17,7 @@
 // hidden under the latency of the row loads.
 #include <mutex>
 
+#include "fp8_block.h"
 #include "fp8_convert.h"
 
 namespace moe {
@@ -631,18 +632,22 @@ __global__ __launch_bounds__(kFusedWaves * 64) void permute_fused_kernel(
 // histograms (assignments before the workgroup's own, and the rest), so E is not limited to the packed counters; the
 // row loads are requested first and land under the counting.  A workgroup of 16 waves owns TB tokens, and 16 / TB
 // waves share a row (piece i of wave w: the KiB i * 16 / TB + w / TB), so that a handful of tokens still occupies many
-// compute units.  FP8: the row is quantised on the way, its maximum goes to *amax.  Same maps, bit for bit, as the
+// compute units.  FP8: the row is quantised on the way, by a scale for all and its maximum goes to *amax, or with a scale for every
+// block of 128 (a piece of a wave is four blocks).  Same maps, bit for bit, as the
 // three-kernel path: rank = assignments of the same expert with a lower index.
 constexpr int kSmallWaves = 16, kSmallThreads = kSmallWaves * 64;
 constexpr int kSmallMaxOwn = 1024;   // assignments of a workgroup's own tokens
 
-template <int NV, int TB, bool FP8>
+enum { kCopyAsIs, kCopyFp8, kCopyFp8Block };
+
+template <int NV, int TB, int COPY>
 __global__ __launch_bounds__(kSmallThreads) void permute_small_kernel(
     const uint8_t* __restrict__ x, const int32_t* __restrict__ idx, int T, int K, int E, int capacity, int row_bytes,
     int r_max, uint8_t* __restrict__ x_perm, int32_t* __restrict__ counts, int32_t* __restrict__ offsets,
     int32_t* __restrict__ row_of_assign, int32_t* __restrict__ assign_of_row, float scale, float* __restrict__ amax,
-    OneExpert one) {
+    uint8_t* __restrict__ scales, OneExpert one) {
     constexpr int P = kSmallWaves / TB;
+    constexpr bool FP8 = COPY != kCopyAsIs;
     __shared__ int base[kMaxExperts];       // assignments of the expert before this workgroup's own, then the next rank
     __shared__ int rest[kMaxExperts];       // the others
     __shared__ int off[kMaxExperts + 1];
@@ -742,6 +747,7 @@ __global__ __launch_bounds__(kSmallThreads) void permute_small_kernel(
     if (copy && t < T) {
         const int* const mine = rows + (wave % TB) * K;
         u32x2 q[NV];
+        uint32_t block[NV];
         if constexpr (FP8) {
             bool any = false;
             for (int k = 0; k < K; ++k) any |= mine[k] >= 0;
@@ -750,15 +756,15 @@ __global__ __launch_bounds__(kSmallThreads) void permute_small_kernel(
                 for (int i = 0; i < NV; ++i) {
                     if ((i * P + piece0) * 1024 + lane * 16 >= row_bytes) continue;
                     float f[8];
+                    bf16x8_to_f32(v[i], f);
+                    if constexpr (COPY == kCopyFp8Block) {
+                        q[i] = quantize8(f, block[i]);
+                    } else {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        f[2 * j] = __uint_as_float(v[i][j] << 16);
-                        f[2 * j + 1] = __uint_as_float(v[i][j] & 0xffff0000u);
+                        for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(f[j]));
+                        q[i][0] = f32x4_to_e4m3(f[0] * scale, f[1] * scale, f[2] * scale, f[3] * scale);
+                        q[i][1] = f32x4_to_e4m3(f[4] * scale, f[5] * scale, f[6] * scale, f[7] * scale);
                     }
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(f[j]));
-                    q[i][0] = f32x4_to_e4m3(f[0] * scale, f[1] * scale, f[2] * scale, f[3] * scale);
-                    q[i][1] = f32x4_to_e4m3(f[4] * scale, f[5] * scale, f[6] * scale, f[7] * scale);
                 }
             }
         }
@@ -772,10 +778,12 @@ __global__ __launch_bounds__(kSmallThreads) void permute_small_kernel(
                 if (o >= row_bytes) continue;
                 if constexpr (FP8) *reinterpret_cast<u32x2*>(dst + o / 2) = q[i];
                 else *reinterpret_cast<u32x4*>(dst + o) = v[i];
+                if (COPY == kCopyFp8Block && (lane & 15) == 0)
+                    scales[(size_t)row * block_scale_stride(row_bytes / 2) + o / (2 * kBlock)] = (uint8_t)block[i];
             }
         }
     }
-    if (FP8 && amax) {
+    if (COPY == kCopyFp8 && amax) {
         // one atomic per workgroup at most, and none if the value read is already as large (*amax only grows)
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
@@ -807,13 +815,18 @@ void set_permute_fused(int v) { g_permute_fused = v; }   // 2 / 3: the packed fo
 // Every workgroup counts every assignment, so with few experts per token it is the number of workgroups that ends it:
 //   16 experts x 7168, K = 1: 4096 tokens 33.9 / 28.4, 8192 tokens 56.2 / 56.1, 16384 tokens 100.6 / 111.7
 //   the same in FP8: 2048 tokens 23.9 / 22.0, 4096 tokens 29.6 / 29.8, 8192 tokens 47.2 / 57.6
+// With a scale for every block of 128 the FP8 lines hold (the maps in one launch and the copy in another / all in one, in a graph):
+//   8 experts x 4096, K = 2: 1 token 5.0 / 4.1, 512 tokens 6.4 / 5.1, 1024 tokens 7.9 / 5.9
+//   64 experts x 3584, K = 8: 32 tokens 6.1 / 6.0, 1024 tokens 13.2 / 10.9, 2048 tokens 21.6 / 21.7
+//   16 experts x 7168, K = 1: 256 tokens 6.0 / 5.3, 2048 tokens 12.7 / 13.9, 4096 tokens 20.1 / 20.3
 constexpr int kSmallMaxAssign = 16384;
 
 // The one-launch dispatch of few assignments; false if the call is none of its own.  `x` may be null (maps only).
-template <bool FP8>
+template <int COPY>
 static bool launch_permute_small(const void* x, const int32_t* idx, int T, int K, int E, int capacity, int row_bytes,
                                  int r_max, void* x_perm, int32_t* counts, int32_t* offsets, int32_t* row_of_assign,
-                                 int32_t* assign_of_row, float scale, float* amax, OneExpert one, hipStream_t s) {
+                                 int32_t* assign_of_row, float scale, float* amax, uint8_t* scales, OneExpert one, hipStream_t s) {
+    constexpr bool FP8 = COPY != kCopyAsIs;
     if (row_bytes > 16384 || row_bytes % 16) return false;
     const bool few = E <= kFusedMaxExperts ? T <= (FP8 ? 1024 : 2048) && (FP8 || (long long)T * K <= kSmallMaxAssign / 2)
                                            : T <= (FP8 ? 4096 : 8192) && (long long)T * K <= kSmallMaxAssign;
@@ -823,9 +836,9 @@ static bool launch_permute_small(const void* x, const int32_t* idx, int T, int K
     if (tb * K > kSmallMaxOwn) return false;
     const int nv = (row_bytes + 1024 * (16 / tb) - 1) / (1024 * (16 / tb));   // pieces of a wave
 #define SMALL_CASE(NVV, TBB)                                                                                            \
-    hipLaunchKernelGGL((permute_small_kernel<NVV, TBB, FP8>), dim3((T + TBB - 1) / TBB), dim3(kSmallThreads), 0, s,      \
+    hipLaunchKernelGGL((permute_small_kernel<NVV, TBB, COPY>), dim3((T + TBB - 1) / TBB), dim3(kSmallThreads), 0, s,      \
                        static_cast<const uint8_t*>(x), idx, T, K, E, capacity, row_bytes, r_max,                         \
-                       static_cast<uint8_t*>(x_perm), counts, offsets, row_of_assign, assign_of_row, scale, amax, one)
+                       static_cast<uint8_t*>(x_perm), counts, offsets, row_of_assign, assign_of_row, scale, amax, scales, one)
     if (narrow) {
         if (nv <= 2) SMALL_CASE(2, 4); else SMALL_CASE(4, 4);
     } else {
@@ -847,8 +860,8 @@ void launch_permute(const void* x, const int32_t* idx, int T, int H, int E, int 
     const int A = T * K;
     const OneExpert one = {one_expert, T};
     const int row_bytes_all = H * (dt == MOE_BF16 ? 2 : 4);
-    if (launch_permute_small<false>((x != nullptr && x_perm != nullptr) ? x : nullptr, idx, T, K, E, capacity, row_bytes_all,
-                                    r_max, x_perm, counts, offsets, row_of_assign, assign_of_row, 0.f, nullptr, one, s))
+    if (launch_permute_small<kCopyAsIs>((x != nullptr && x_perm != nullptr) ? x : nullptr, idx, T, K, E, capacity, row_bytes_all,
+                                    r_max, x_perm, counts, offsets, row_of_assign, assign_of_row, 0.f, nullptr, nullptr, one, s))
         return;
     if (g_permute_fused && g_permute_fused != 4 && E <= kFusedMaxExperts && A <= kFusedMaxAssign && row_bytes_all <= kFusedMaxRowVecs * 1024 &&
         row_bytes_all % 16 == 0) {
@@ -964,8 +977,8 @@ void launch_permute_zero_rows(const int32_t* assign_of_row, void* x_perm, int ro
 void launch_permute_fp8(const void* x, const int32_t* idx, int T, int H, int E, int K, int capacity, int r_max,
                         float scale, void* x_perm_fp8, int32_t* counts, int32_t* offsets, int32_t* row_of_assign,
                         int32_t* assign_of_row, float* amax, void* ws, hipStream_t s) {
-    if (launch_permute_small<true>(x, idx, T, K, E, capacity, H * 2, r_max, x_perm_fp8, counts, offsets, row_of_assign,
-                                   assign_of_row, scale, amax, OneExpert{nullptr, 0}, s))
+    if (launch_permute_small<kCopyFp8>(x, idx, T, K, E, capacity, H * 2, r_max, x_perm_fp8, counts, offsets, row_of_assign,
+                                       assign_of_row, scale, amax, nullptr, OneExpert{nullptr, 0}, s))
         return;
     // maps as in launch_permute, then the quantising copy
     launch_permute(nullptr, idx, T, H, E, K, capacity, r_max, MOE_BF16, nullptr, counts, offsets, row_of_assign,
@@ -974,6 +987,13 @@ void launch_permute_fp8(const void* x, const int32_t* idx, int T, int H, int E, 
     if (grid > 256 * 4) grid = 256 * 4;   // few, longer-lived workgroups: fewer amax atomics
     hipLaunchKernelGGL(permute_copy_fp8_kernel, dim3(grid), dim3(256), 0, s, static_cast<const uint8_t*>(x),
                        row_of_assign, static_cast<uint8_t*>(x_perm_fp8), T, K, H, r_max, scale, amax);
+}
+
+bool launch_permute_block_small(const void* x, const int32_t* idx, int T, int H, int E, int K, int capacity, int r_max, void* codes,
+                                uint8_t* scales, int32_t* counts, int32_t* offsets, int32_t* row_of_assign, int32_t* assign_of_row,
+                                hipStream_t s) {
+    return H <= 8192 && launch_permute_small<kCopyFp8Block>(x, idx, T, K, E, capacity, H * 2, r_max, codes, counts, offsets, row_of_assign,
+                                                            assign_of_row, 0.f, nullptr, scales, OneExpert{nullptr, 0}, s);
 }
 
 void launch_fill_i32(int32_t* p, int n, int32_t v0, int32_t step, hipStream_t s) {

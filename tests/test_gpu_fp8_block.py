@@ -116,7 +116,8 @@ def test_weights_of_more_than_the_caches_hold(dtype):
 
 
 @pytest.mark.parametrize("T,H,E,K,capacity", [(1, 128, 8, 2, 0), (5, 384, 4, 4, 0), (64, 1408, 64, 8, 0), (777, 512, 12, 3, 150), (3000, 256, 8, 2, 0),
-                                              (9000, 128, 64, 6, 700), (1500, 6144, 8, 2, 0), (300, 16384, 16, 1, 0), (20000, 256, 8, 2, 0)])
+                                              (9000, 128, 64, 6, 700), (1500, 6144, 8, 2, 0), (300, 16384, 16, 1, 0), (20000, 256, 8, 2, 0),
+                                              (1100, 8192, 64, 2, 0), (1030, 4096, 16, 1, 50), (5, 8192, 8, 3, 0)])
 def test_permute_is_permute_and_quantisation(T, H, E, K, capacity):
     gen = torch.Generator().manual_seed(T)
     x = (torch.randn((T, H), generator=gen) * torch.exp(torch.randn((T, 1), generator=gen))).to(torch.bfloat16).cuda()
