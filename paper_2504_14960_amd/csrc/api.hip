@@ -1284,9 +1284,10 @@ moe_status_t moe_expert_weights_fp8_block(const void* w_gate, const void* w_up, 
         REQUIRE_SCALES(fn, wd_t_scales);
     }
     hipStream_t s = static_cast<hipStream_t>(stream);
-    launch_block_weights(w_gate, dt, E, F, H, gate_codes, gate_scales, wgu_t_codes, wgu_t_scales, 2 * F, 0, s);
-    launch_block_weights(w_up, dt, E, F, H, up_codes, up_scales, wgu_t_codes, wgu_t_scales, 2 * F, F, s);
-    launch_block_weights(w_down, dt, E, H, F, down_codes, down_scales, wd_t_codes, wd_t_scales, H, 0, s);
+    auto bytes = [](void* p) { return static_cast<uint8_t*>(p); };
+    launch_block_weights(dt, E, H, F, {{{w_gate, F, H, bytes(gate_codes), gate_scales, bytes(wgu_t_codes), wgu_t_scales, 2 * F, 0},
+                                        {w_up, F, H, bytes(up_codes), up_scales, bytes(wgu_t_codes), wgu_t_scales, 2 * F, F},
+                                        {w_down, H, F, bytes(down_codes), down_scales, bytes(wd_t_codes), wd_t_scales, H, 0}}}, s);
     return check_launch(fn);
 }
 

@@ -46,19 +46,22 @@ __device__ __forceinline__ void store_codes(uint8_t* to, const V& v) {
 }
 
 // A block of 128 x 128 to a workgroup: w [E, N, K] -> codes [E, N, K] and, transposed, at column t0 of [E, K, ldt]; either may
-// be null.  A thread holds eight columns of eight rows.
+// be null.  A thread holds eight columns of eight rows.  Bound by HBM.
+// A layer's three in one launch, streamed ones in three (us, in three / in one: 12 experts, 1024 x 1408, fp32 72 / 60 (5.2 TB/s); 64,
+// 4096 x 1408, bf16, streamed 792 / 817).
 // STREAM, past the caches, where the codes that a call writes are more than the memory-side cache keeps: the stores, and the
 // loads of bf16 weights (an fp32 thread's two loads share a line, which the first would drop).  The call, us, not streamed /
 // so, and with the FFN of 64 rows per expert behind it: 12 experts, 1024 x 1408, fp32 (104 MB of codes) 72 / 67 and 100 / 101;
 // 8, 2048 x 2048, bf16 (201 MB) with it 131 / 132; 16, 2048 x 2048, bf16 (403 MB) with it 234 / 216; 8, 4096 x 4096, fp32
 // (805 MB) with it 577 / 554, streamed loads too 564; 64, 4096 x 1408, bf16 (2.2 GB) 845 / 788 (5.6 TB/s) and 1080 / 1024.
 template <bool BF16, bool STREAM>
-__global__ __launch_bounds__(256) void block_weights_kernel(const void* __restrict__ w, int N, int K, uint8_t* __restrict__ codes,
-                                                            uint8_t* __restrict__ scales, uint8_t* __restrict__ codes_t,
-                                                            uint8_t* __restrict__ scales_t, int ldt, int t0) {
+__global__ __launch_bounds__(256) void block_weights_kernel(LayerWeights p, int E, int first) {
     __shared__ uint32_t tops[4];
     __shared__ __attribute__((aligned(16))) uint8_t tile[128][128 + 16];   // transposed
-    const int e = blockIdx.z, n0 = blockIdx.y * kBlock, k0 = blockIdx.x * kBlock;
+    const int z = first + (int)blockIdx.z, which = (z >= E) + (z >= 2 * E), e = z - which * E;
+    const auto [w, N, K, codes, scales, codes_t, scales_t, ldt, t0] = p.of[which];
+    const bool turned = (int)(gridDim.x * kBlock) != K;   // the down projection in the others' grid
+    const int nb = turned ? blockIdx.x : blockIdx.y, kb = turned ? blockIdx.y : blockIdx.x, n0 = nb * kBlock, k0 = kb * kBlock;
     const int cv = threadIdx.x % 16, rv = threadIdx.x / 16;
     float f[8][8];
     uint32_t top = 0;
@@ -83,7 +86,7 @@ __global__ __launch_bounds__(256) void block_weights_kernel(const void* __restri
 #pragma unroll
         for (int r = 0; r < 8; ++r)
             store_codes<STREAM>(codes + ((size_t)e * N + n0 + 8 * rv + r) * K + k0 + 8 * cv, q[r]);
-        if (threadIdx.x == 0) scales[((size_t)e * (N / kBlock) + blockIdx.y) * block_scale_stride(K) + blockIdx.x] = (uint8_t)scale;
+        if (threadIdx.x == 0) scales[((size_t)e * (N / kBlock) + nb) * block_scale_stride(K) + kb] = (uint8_t)scale;
     }
     if (!codes_t) return;
 #pragma unroll
@@ -100,7 +103,7 @@ __global__ __launch_bounds__(256) void block_weights_kernel(const void* __restri
         store_codes<STREAM>(codes_t + ((size_t)e * K + k0 + c) * ldt + t0 + n0 + at, *reinterpret_cast<const u32x4*>(&tile[c][at]));
     }
     if (threadIdx.x == 0)
-        scales_t[((size_t)e * (K / kBlock) + blockIdx.x) * block_scale_stride(ldt) + t0 / kBlock + blockIdx.y] = (uint8_t)scale;
+        scales_t[((size_t)e * (K / kBlock) + kb) * block_scale_stride(ldt) + t0 / kBlock + nb] = (uint8_t)scale;
 }
 
 }  // namespace
@@ -110,15 +113,19 @@ void launch_block_quantize(const void* src, moe_dtype_t dt, int rows, int C, voi
     hipLaunchKernelGGL(kern, dim3(block_quantize_grid(rows)), dim3(256), 0, s, src, rows, C, static_cast<uint8_t*>(codes), scales);
 }
 
-void launch_block_weights(const void* w, moe_dtype_t dt, int E, int N, int K, void* codes, uint8_t* scales, void* codes_t,
-                          uint8_t* scales_t, int ldt, int t0, hipStream_t s) {
-    const bool stream = (size_t)3 * E * N * K * ((codes != nullptr) + (codes_t != nullptr)) > kCachedBytes;   // of the layer's three
+void launch_block_weights(moe_dtype_t dt, int E, int H, int F, const LayerWeights& p, hipStream_t s) {
+    const size_t codes = (size_t)3 * E * H * F * ((p.of[0].codes != nullptr) + (p.of[0].codes_t != nullptr));
+    const bool stream = codes > kCachedBytes;
     auto pick = [&](auto bf16) {
         return stream ? block_weights_kernel<decltype(bf16)::value, true> : block_weights_kernel<decltype(bf16)::value, false>;
     };
     auto kern = dt == MOE_BF16 ? pick(std::true_type{}) : pick(std::false_type{});
-    hipLaunchKernelGGL(kern, dim3(K / kBlock, N / kBlock, E), dim3(256), 0, s, w, N, K, static_cast<uint8_t*>(codes), scales,
-                       static_cast<uint8_t*>(codes_t), scales_t, ldt, t0);
+    if (stream) {
+        for (int i = 0; i < 3; ++i)
+            hipLaunchKernelGGL(kern, dim3(p.of[i].K / kBlock, p.of[i].N / kBlock, E), dim3(256), 0, s, p, E, i * E);
+    } else {
+        hipLaunchKernelGGL(kern, dim3(H / kBlock, F / kBlock, 3 * E), dim3(256), 0, s, p, E, 0);
+    }
 }
 
 void launch_permute_block(const void* x, const int32_t* idx, int T, int H, int E, int K, int capacity, int r_max, void* codes,

@@ -244,8 +244,17 @@ void launch_probe_mfma_fp8(const void* image, int iters, int workgroups, float* 
 // E4M3 with a scale for every block of 128 (fp8_block.h)
 void launch_block_quantize(const void* src, moe_dtype_t dt, int rows, int C, void* codes, uint8_t* scales, hipStream_t s);
 // w [E, N, K] to codes [E, N, K] and/or, transposed, to column t0 of [E, K, ldt] (null: not)
-void launch_block_weights(const void* w, moe_dtype_t dt, int E, int N, int K, void* codes, uint8_t* scales, void* codes_t,
-                          uint8_t* scales_t, int ldt, int t0, hipStream_t s);
+struct BlockWeights {
+    const void* w;
+    int N, K;
+    uint8_t *codes, *scales, *codes_t, *scales_t;
+    int ldt, t0;
+};
+// gate and up [E, F, H], down [E, H, F], the same outputs of each
+struct LayerWeights {
+    BlockWeights of[3];
+};
+void launch_block_weights(moe_dtype_t dt, int E, int H, int F, const LayerWeights& p, hipStream_t s);
 // a2 of few assignments with its quantising copy in one launch; false if the call is none of its own
 bool launch_permute_block_small(const void* x, const int32_t* idx, int T, int H, int E, int K, int capacity, int r_max, void* codes,
                                 uint8_t* scales, int32_t* counts, int32_t* offsets, int32_t* row_of_assign, int32_t* assign_of_row,
