@@ -1464,9 +1464,9 @@ moe_status_t moe_grouped_gemm_swiglu_fp8_block_backward(
     // the weights' gradients: operands transposed with every expert's rows as a zero-padded column segment
     launch_block_transposes(dy_perm, ws + L.dgu, h_codes, h_scales, x_codes, x_scales, expert_offsets, poff, E, H, F, L.rp_max,
                             ws + L.dy_t, ws + L.dgu_t, ws + L.h_t, ws + L.x_t, s);
-    launch_persist_wgrad(ws + L.dy_t, ws + L.h_t, expert_offsets, E, H, F, L.rp_max, dw_down, s);
-    launch_persist_wgrad(ws + L.dgu_t, ws + L.x_t, expert_offsets, E, F, H, L.rp_max, dw_gate, s);
-    launch_persist_wgrad(ws + L.dgu_t + (size_t)F * L.rp_max * 2, ws + L.x_t, expert_offsets, E, F, H, L.rp_max, dw_up, s);
+    launch_persist_wgrads({{{ws + L.dy_t, ws + L.h_t, dw_down, H, F},
+                            {ws + L.dgu_t, ws + L.x_t, dw_gate, F, H},
+                            {ws + L.dgu_t + (size_t)F * L.rp_max * 2, ws + L.x_t, dw_up, F, H}}}, expert_offsets, E, L.rp_max, s);
     return check_launch(fn);
 }
 

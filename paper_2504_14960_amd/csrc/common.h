@@ -229,6 +229,16 @@ void launch_wgrad_zero_empty(const int32_t* offsets, int E, size_t per_expert, v
 // persistent: one workgroup per compute unit; pipe3: one workgroup per output tile
 void launch_persist_wgrad(const void* a_t, const void* b_t, const int32_t* offsets, int E, int M, int N, int ld,
                           void* dw, hipStream_t s);
+// three of them in one launch, for M, N up to 2^24: those of a layer (H x F or F x H)
+struct WgradProduct {
+    const void *a_t, *b_t;
+    void* dw;
+    int M, N;
+};
+struct WgradList {
+    WgradProduct of[3];
+};
+void launch_persist_wgrads(const WgradList& p, const int32_t* offsets, int E, int ld, hipStream_t s);
 // the same product straight from the row-major activations a [rows, lda], b [rows, ldb] (no transposed copies)
 void launch_persist_wgrad_rowmajor(const void* a, int lda, const void* b, int ldb, const int32_t* offsets, int E,
                                    int M, int N, const void* zero_row, void* dw, hipStream_t s);

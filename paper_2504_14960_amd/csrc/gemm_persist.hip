@@ -784,6 +784,31 @@ void launch_persist_groupk(const void* A, const void* B, const int32_t* offsets,
                        static_cast<bf16_t*>(nullptr), M, 0, 1, 0, g_persist_ticks);
 }
 
+// Several products over the same experts in one launch, a persistent grid to each: what is left of one product's tiles when most of
+// its workgroups are done runs beside the first of the next.  (The backward on block-scaled E4M3, us, three launches / one: 8 experts x
+// 16 rows, 1024 x 2048, 95 / 90; 12 x 194, 1024 x 1408, 128 / 114; 8 x 512, 2048 x 2048, 308 / 270; 32 x 256, 4096 x 1408, 829 / 780; 128 x
+// 256, 2048 x 768, 1215 / 1089; 8 x 2048, 4096 x 4096, level; 64 x 256, 6144 x 2048, 3148 / 3166.)
+template <int BM, int BN, int WGM, int WGN, bool STREAM_OUT, bool DEEP_B>
+__global__ __launch_bounds__(WGM * WGN * 64) void wgrad_list_kernel(WgradList p, const int32_t* __restrict__ offsets, int E, int ld) {
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+    const WgradProduct& w = p.of[blockIdx.y];
+    persist_body<BM, BN, WGM, WGN, 0, true, false, false, DEEP_B, true, STREAM_OUT, false>(
+        static_cast<const bf16_t*>(w.a_t), offsets, E, w.N, ld, static_cast<const bf16_t*>(w.b_t), static_cast<const bf16_t*>(w.b_t),
+        static_cast<bf16_t*>(w.dw), nullptr, w.M, 0, 1, 0, nullptr, smem);
+}
+
+template <int BM, int BN, int WGM, int WGN, bool STREAM_OUT, bool DEEP_B = false>
+void launch_wgrad_list(const WgradList& p, const int32_t* offsets, int E, int ld, hipStream_t s) {
+    constexpr size_t smem = (size_t)(DEEP_B ? 2 * BM + 3 * BN : 3 * BM + 2 * BN) * 64 * 2;
+    auto kern = wgrad_list_kernel<BM, BN, WGM, WGN, STREAM_OUT, DEEP_B>;
+    static OncePerDevice lds;
+    allow_lds(lds, reinterpret_cast<const void*>(kern), (int)smem);
+    long long tiles = 0;
+    for (const WgradProduct& w : p.of) tiles = max(tiles, (long long)E * ((w.M + BM - 1) / BM) * ((w.N + BN - 1) / BN));
+    const int grid = (int)min((long long)persist_grid(), (tiles + 7) / 8 * 8);
+    hipLaunchKernelGGL(kern, dim3(grid, 3), dim3(WGM * WGN * 64), smem, s, p, offsets, E, ld);
+}
+
 // weight gradients straight from the row-major activations (no transposed copies): see the kernel's KMAJ form
 template <int BM, int BN, int WGM, int WGN>
 void launch_persist_groupk_rowmajor(const void* A, int lda, const void* B, int ldb, const int32_t* offsets, int E,
@@ -860,9 +885,8 @@ void launch_wgrad_zero_empty(const int32_t* offsets, int E, size_t per_expert, v
                        static_cast<bf16_t*>(dw0), static_cast<bf16_t*>(dw1), static_cast<bf16_t*>(dw2));
 }
 
-// dw [E, M, N] = per expert a_t[:, seg_e] . b_t[:, seg_e]^T (see WgradSched); M, N multiples of 8, ld of 64
-void launch_persist_wgrad(const void* a_t, const void* b_t, const int32_t* offsets, int E, int M, int N, int ld,
-                          void* dw, hipStream_t s) {
+enum WgradTiles { kWgradEightWaves, kWgradFewTiles, kWgradStreamed, kWgradCached };
+static WgradTiles wgrad_tiles(int E, int M, int N, int ld) {
     const long long per_expert = (long long)((M + 255) / 256) * ((N + 255) / 256), tiles = E * per_expert;
     // Up to some 97 rows per expert (the padding included, a tile is then two k-tiles and its store): four waves wait between the two,
     // eight of 64 x 64 cover it.  Tiles of 128 rows, the 256 columns in three stages, streamed.  The backward, us, four waves of 256 rows / so:
@@ -870,26 +894,37 @@ void launch_persist_wgrad(const void* a_t, const void* b_t, const int32_t* offse
     // 40 x 60, 3072 x 1792, 670 / 640; 16 x 60, 6144 x 2048, 580 / 576; 64 x 100, 2560 x 1536, level.  On the other side of the lines: 128 experts
     // x 60 rows, 2048 x 768, 698 / 722; 96 x 59, 2048 x 1024, 694 / 717; 64 x 60, 2816 x 2048, 1054 / 1080; 32 x 43, 4096 x 2048, 759 / 797; 4 x 60, 4096 x 4096, 257 / 261; 48 x 122, 4096 x
     // 1024, 710 / 742 (8 to 16 experts gain up to 160 rows, 2 to 9 %).  The tiles' operands, one and a half times as many, are what costs.
-    if (ld <= 224ll * E && E <= 64 && per_expert < 256 && (long long)E * M * N < 1ll << 28 && N <= kMaxColumns) {
-        launch_persist_groupk<128, 256, 2, 4, true, true>(a_t, b_t, offsets, E, M, N, ld, dw, s);
-        return;
-    }
+    if (ld <= 224ll * E && E <= 64 && per_expert < 256 && (long long)E * M * N < 1ll << 28 && N <= kMaxColumns) return kWgradEightWaves;
     // Tiles of 128 rows where those of 256 are at most one to every second workgroup: a compute unit has one tile then, as long
     // as its k-tiles are one after the other, and with four waves nothing covers what they wait for.  One gradient, us, 256 rows /
     // 128 (streamed too, at any number of rows): 4 experts x 53 rows, 1024 x 1024, 9.8 / 8.4 not streamed; 4 x 60, 4 x 250 and
     // 4 x 600, 1024 x 1792, 15.1, 21.4 and 36.6 / 8.0, 10.3 and 16.1; 8 x 60, 500 and 2000, 1024 x 1024 (128 tiles of 256)
     // 10.4, 18.3 and 53.0 / 8.3, 15.6 and 41.6, not streamed 10.1, 18.9 and 42.1.
-    if (2 * tiles <= persist_grid() && N <= kMaxColumns) {
-        launch_persist_groupk<128, 256, 2, 2, true, true>(a_t, b_t, offsets, E, M, N, ld, dw, s);
-        return;
-    }
+    if (2 * tiles <= persist_grid() && N <= kMaxColumns) return kWgradFewTiles;
     // Streamed past the L2 whatever the rows (the expert FFN's backward streamed, of what it takes stored as usual; 19 layers of 1 to 128
     // experts: 200 rows per expert 0.83 to 0.94, 450 rows 0.86 to 1.02, 800 rows 0.93 to 1.02, 1280 rows 0.95 to 1.01, 2048 rows 0.98 to
     // 0.99; the two above 1 are 8 experts, 6144 x 16384, 1.6 and 2.1 % at 450 and 800 rows, which at 2048 take 0.7 % less).
-    if (N <= kMaxColumns)
-        launch_persist_groupk<256, 256, 2, 2, true>(a_t, b_t, offsets, E, M, N, ld, dw, s);
-    else
-        launch_persist_groupk<256, 256, 2, 2, false>(a_t, b_t, offsets, E, M, N, ld, dw, s);
+    return N <= kMaxColumns ? kWgradStreamed : kWgradCached;
+}
+
+// dw [E, M, N] = per expert a_t[:, seg_e] . b_t[:, seg_e]^T (see WgradSched); M, N multiples of 8, ld of 64
+void launch_persist_wgrad(const void* a_t, const void* b_t, const int32_t* offsets, int E, int M, int N, int ld,
+                          void* dw, hipStream_t s) {
+    switch (wgrad_tiles(E, M, N, ld)) {
+        case kWgradEightWaves: return launch_persist_groupk<128, 256, 2, 4, true, true>(a_t, b_t, offsets, E, M, N, ld, dw, s);
+        case kWgradFewTiles: return launch_persist_groupk<128, 256, 2, 2, true, true>(a_t, b_t, offsets, E, M, N, ld, dw, s);
+        case kWgradStreamed: return launch_persist_groupk<256, 256, 2, 2, true>(a_t, b_t, offsets, E, M, N, ld, dw, s);
+        default: return launch_persist_groupk<256, 256, 2, 2, false>(a_t, b_t, offsets, E, M, N, ld, dw, s);
+    }
+}
+
+// The products of a layer: M x N of all of them are H x F or F x H, which the choice of the tiles does not tell apart (N <= kMaxColumns).
+void launch_persist_wgrads(const WgradList& p, const int32_t* offsets, int E, int ld, hipStream_t s) {
+    switch (wgrad_tiles(E, p.of[0].M, p.of[0].N, ld)) {
+        case kWgradEightWaves: return launch_wgrad_list<128, 256, 2, 4, true, true>(p, offsets, E, ld, s);
+        case kWgradFewTiles: return launch_wgrad_list<128, 256, 2, 2, true, true>(p, offsets, E, ld, s);
+        default: return launch_wgrad_list<256, 256, 2, 2, true>(p, offsets, E, ld, s);
+    }
 }
 
 // dw [E, M, N] = per expert A[rows_e, 0:M]^T . B[rows_e, 0:N], A [rows, lda] and B [rows, ldb] row-major; M, N
