@@ -1,8 +1,9 @@
 /*
  * moe.h -- C ABI of the MI355X (gfx950) MoE-layer hot path: the forward of the
- * layer's four stages, their backward, the FP8 expert FFN, one GPU's step of
- * expert-parallel dispatch, and what follows the gradients in a training step:
- * the router's balance loss, the gradients' norm and the AdamW step.
+ * layer's four stages, their backward, the FP8 expert FFN (one scale a tensor, or
+ * one for every block of 128 with a backward), routing by scores with a balancing
+ * bias, one GPU's step of expert-parallel dispatch, and what follows the gradients
+ * in a training step: the router's balance loss, the gradients' norm and the AdamW step.
  *
  * The library computes, on one GPU with all experts local, the
  * Mixture-of-Experts layer of arXiv 2504.14960:

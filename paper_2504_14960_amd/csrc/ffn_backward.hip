@@ -233,7 +233,8 @@ __global__ __launch_bounds__(256) void ragged_transpose_kernel(Bf16Rows<false> s
 }
 
 // The four of a backward on E4M3 operands in one launch: dy [., H] and dg | du [., 2F] in bf16, h [., F] and x [., H] as codes.
-// Column blocks of one after those of the other; a workgroup's kind is the same in all its lanes.
+// Column blocks of one after those of the other; a workgroup's kind is the same in all its lanes.  16384 rows, 6144 x 2048: 210 us, 5.1
+// TB/s; 2331 rows, 1024 x 1408: 12 us.  (In four launches, each code waited for and converted before the next was asked for, 252 and 26.)
 struct BlockTransposes {
     Bf16Rows<false> dy, dgu;
     BlockRows h, x;

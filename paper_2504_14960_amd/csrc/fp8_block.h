@@ -88,7 +88,8 @@ __device__ __forceinline__ void load8(const void* src, size_t at, float (&f)[8])
     }
 }
 
-// Rows 0 .. n - 1, one to a wave, 512 values at a time, by workgroup `block` of `blocks` of four waves
+// Rows 0 .. n - 1, one to a wave, 512 values at a time, by workgroup `block` of `blocks` of four waves (16384 rows of 6144 bf16, in
+// block_prepare_kernel: 54 us, 5.6 TB/s)
 template <bool BF16>
 __device__ __forceinline__ void block_quantize_rows(const void* __restrict__ src, int n, int C, uint8_t* __restrict__ codes,
                                                     uint8_t* __restrict__ scales, int block, int blocks) {

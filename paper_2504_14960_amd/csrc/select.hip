@@ -186,7 +186,8 @@ __global__ __launch_bounds__(64 * kSelectWaves) void select_wave_kernel(SelectAr
 //
 // Bound by the vector unit.  Scores in 64 bits would be half of its work, so they are first formed in fp32, and what was
 // selected by them stands if no difference that decided it is within what they may be off; else the wave does it all again
-// in 64 bits (a token in some hundreds).
+// in 64 bits (a token in some hundreds).  262144 tokens x 256 experts in 8 groups, 8 of 4 groups: 111 us, 163 vector
+// instructions a token (75 us of issue; the bytes take 47 at 6 TB/s).  A token to a wave with all scores in 64 bits took 449.
 // Keys up to here belong to experts that are not selected.  (Their low bits make them smaller.)
 constexpr double kLow = -(double)__FLT_MAX__;
 
@@ -486,7 +487,8 @@ __device__ __forceinline__ float lanes_fold(float v, int N, F&& f) {
 
 // TW tokens to a wave: 8 of up to 8 slots, 4 of up to 64.  The slots' work, of which there is little, is dealt over the wave, 64 / TW
 // lanes to a token; the rows of dlogits are put together in LDS and written in one piece, which starts at a multiple of 16
-// bytes whatever E is.  Bound by that write (softmax: and by the read of the logits).
+// bytes whatever E is.  Bound by that write (softmax: and by the read of the logits).  262144 tokens x 256 experts, 8 slots, sigmoid: 74
+// us for 294 MB, 420 with the 64-byte sectors around the logits it picks (5.7 TB/s); every lane storing for itself took 164.
 template <bool SIGMOID, int TW, bool STREAM>
 __global__ __launch_bounds__(256) void select_dlogits_kernel(SelectBackwardArgs p) {
     constexpr int PER = 64 / TW, SLOTS = TW == 8 ? 1 : 4;
@@ -644,7 +646,8 @@ __global__ __launch_bounds__(256) void select_dlogits_kernel(SelectBackwardArgs 
 }
 
 // ---- the step of the bias ----
-// A chain of loads: rows of counts are dealt to four groups of threads, and each has all its loads in flight.
+// A chain of loads: rows of counts are dealt to four groups of threads, and each has all its loads in flight (a row of 64 experts 2.7
+// us in the kernel; 4096 rows of 256 4.8 and 3.6, one load after another 24 together).
 constexpr int kBiasRows = 64;   // rows of counts that a workgroup adds up
 
 // sum of rows [r0, r0 + kBiasRows) below n_rows of column e, for threads e < 256 (the first group)
