@@ -179,6 +179,19 @@ __global__ __launch_bounds__(64 * kSelectWaves) void select_wave_kernel(SelectAr
         select_token<VPL>(p, t, threadIdx.x & 63, keys[wave], best[wave]);
 }
 
+// In idx[t][0] of a token whose selection is left to this kernel
+constexpr int kDoubtful = -2;
+
+// 64 tokens to a wave, the doubtful ones one after the other.
+template <int VPL>
+__global__ __launch_bounds__(64 * kSelectWaves) void select_doubtful_kernel(SelectArgs p) {
+    __shared__ double keys[kSelectWaves][64 * VPL], best[kSelectWaves][64 * VPL];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int t0 = (blockIdx.x * kSelectWaves + wave) * 64;
+    for (uint64_t m = __ballot(t0 + lane < p.T && p.idx[(size_t)(t0 + lane) * p.K] == kDoubtful); m; m &= m - 1)
+        select_token<VPL>(p, t0 + __ffsll((unsigned long long)m) - 1, lane, keys[wave], best[wave]);
+}
+
 // ---- up to eight experts a token ----
 // L lanes to a token, a run of `run` <= VPL experts to a lane (where there are groups: a group).  A lane sorts its keys in
 // eights and merges them to its eight largest, and the lanes of a token merge theirs: bitonic networks of v_max_f64 and
@@ -186,7 +199,8 @@ __global__ __launch_bounds__(64 * kSelectWaves) void select_wave_kernel(SelectAr
 //
 // Bound by the vector unit.  Scores in 64 bits would be half of its work, so they are first formed in fp32, and what was
 // selected by them stands if no difference that decided it is within what they may be off; else the wave does it all again
-// in 64 bits (a token in some hundreds).  262144 tokens x 256 experts in 8 groups, 8 of 4 groups: 111 us, 163 vector
+// in 64 bits (a token in some hundreds).  LATER: in a launch behind this one, which finds them marked; the code that does it takes a
+// fifth of this kernel's time by its registers alone.  262144 tokens x 256 experts in 8 groups, 8 of 4 groups: 104 us, some 160 vector
 // instructions a token (75 us of issue; the bytes take 47 at 6 TB/s).  A token to a wave with all scores in 64 bits took 449.
 // Keys up to here belong to experts that are not selected.  (Their low bits make them smaller.)
 constexpr double kLow = -(double)__FLT_MAX__;
@@ -248,13 +262,26 @@ __device__ __forceinline__ void merge_lanes(double (&a)[8], double& next) {
     merge8(a, b, next);
 }
 
-// How far apart two keys are that fp32 scores tell apart for certain.  A score is off by less than 2^-17 of itself (the rounding of
-// the exponential's argument, at most 88, and a few units; a softmax's sum), and by less than 2^-20 altogether unless a softmax's
-// probability is near 1, where it is 2^-19.  Equal keys are always in doubt, so a key carries its expert's number in any order.
+// How far apart two keys are that fp32 scores tell apart for certain: either bound is enough.
+// A sigmoid 1 / (1 + x), x = 2^(c v): the product is off by 1.22 * 2^-24 of itself (its rounding and c's), which moves the score by
+// s (1 - s) |v| of that, at most 0.28 * 2^-24; x by 2^-23 of itself, s (1 - s) of that, 0.5 * 2^-24; the sum by 2^-24; the reciprocal by
+// 2^-23: together less than 2^-22, with the definition's rounding 1.13 * 2^-22.  Key = score + bias adds 2^-23 of itself, in
+// both.  Two keys: 1.13 * 2^-21 + 2^-22 of the smaller one, for which stand 2^-20 and 2^-21.  (With 2^-18
+// for both, which a softmax needs, one token in 180 was done again and not one in 900: 262144 x 256 119 us instead of 114.)  Far from 0 the score itself
+// is small, and off by less than 2^-17 of itself (|v| up to 88).
+// A softmax's probability is off by less than 2^-17 of itself (the rounding of the exponential's argument, and the sum's 32 terms), and by
+// less than 2^-19 altogether.
+// Equal keys are always in doubt, so a key carries its expert's number in any order.
+template <bool SIGMOID>
 struct Doubt {
-    double part, least;
-    __device__ __forceinline__ Doubt(bool biased) : part(biased ? 0x1p-18 : 0x1p-16), least(biased ? 0x1p-18 : 0x1p-126) {}
-    __device__ __forceinline__ bool apart(double large, double small) const { return large - small > fma(fabs(small), part, least); }
+    double part, least, own_part, own_least;
+    __device__ __forceinline__ Doubt(bool biased)
+        : part(SIGMOID ? 0x1p-21 : 0x1p-18), least(SIGMOID ? 0x1p-20 : 0x1p-18), own_part(biased ? part : 0x1p-16),
+          own_least(biased ? least : 0x1p-126) {}
+    __device__ __forceinline__ double of(double magnitude) const {
+        return fmin(fma(magnitude, part, least), fma(magnitude, own_part, own_least));
+    }
+    __device__ __forceinline__ bool apart(double large, double small) const { return large - small > of(fabs(small)); }
 };
 
 // exp(d) for d <= 0 to about a unit in the last place: the product's rounding is made up for
@@ -265,11 +292,11 @@ __device__ __forceinline__ float exp_near(float d) {
     return fmaf(e, lo * 0.693147181f, e);
 }
 
-template <int VPL, int L, bool VEC, bool SIGMOID>
+template <int VPL, int L, bool VEC, bool SIGMOID, bool LATER>
 __global__ __launch_bounds__(256, 4) void select_lists_kernel(SelectArgs p, int run) {
     constexpr int TOKENS = 256 / L, SLOTS = (8 + L - 1) / L, LDB = VPL + 4;
     __shared__ __attribute__((aligned(16))) float biases[L * LDB];   // 4 more floats a lane: other banks
-    __shared__ double keys[4][kMaxExperts], best[4][kMaxExperts];
+    __shared__ double keys[4][LATER ? 1 : kMaxExperts], best[4][LATER ? 1 : kMaxExperts];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int sub = lane & (L - 1), e0 = sub * run;
     const int mine = min(run, p.E - e0);   // experts of this lane; none, or fewer, in the last lanes
@@ -279,7 +306,7 @@ __global__ __launch_bounds__(256, 4) void select_lists_kernel(SelectArgs p, int 
         const float b = biased && j < run && e < p.E ? p.bias[e] : 0.f;
         biases[l * LDB + j] = b == b ? fminf(fmaxf(b, -__FLT_MAX__), __FLT_MAX__) : -__FLT_MAX__;   // a score adds nothing to these
     }
-    const Doubt doubt(biased);
+    const Doubt<SIGMOID> doubt(biased);
     __syncthreads();
     auto lanes = [](auto v, auto&& f) {
         if constexpr (L > 1) v = f(v, dpp<0xB1>(v));
@@ -384,7 +411,7 @@ __global__ __launch_bounds__(256, 4) void select_lists_kernel(SelectArgs p, int 
             keep = rank < p.topk_groups && total > -INFINITY;
             // a sum may be far smaller than what was added up
             if (rank == p.topk_groups - 1 && below > -INFINITY)
-                sure &= (double)total - (double)below > 2. * fma((double)size, doubt.part, doubt.least);
+                sure &= (double)total - (double)below > 2. * doubt.of((double)size);
             if (!keep) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) list[i] = kLow;
@@ -423,25 +450,44 @@ __global__ __launch_bounds__(256, 4) void select_lists_kernel(SelectArgs p, int 
         for (int i = 0; i < SLOTS; ++i) {
             const int k = sub + L * i;
             if (!valid || k >= p.K) continue;
+            if (LATER && k == 0 && (unsure >> (lane & ~(L - 1)) & ((1ull << L) - 1))) e[i] = kDoubtful;
             p.idx[(size_t)t * p.K + k] = e[i];
             p.gate[(size_t)t * p.K + k] = z > 0. ? (float)(g[i] / z * (double)p.scale) : 0.f;
         }
         // tokens in doubt once more, by the whole wave and in 64 bits
+        if constexpr (LATER) continue;
         for (int first = 0; unsure && first < 64; first += L)
             if (unsure >> first & ((1ull << L) - 1)) select_token<kMaxExperts / 64>(p, t0 + (wave * 64 + first) / L, lane, keys[wave], best[wave]);
     }
 }
 
+// From so many tokens and logits on the doubtful tokens get a launch of their own, which takes 5 to 8 us.  us, in the same launch / so,
+// sigmoid: 256 experts in 8 groups, 65536 tokens 35.6 / 38.6, 131072 tokens 55.5 / 56.5, 262144 tokens 104 / 99; 64 experts, 65536 tokens 15.0
+// / 15.2, 131072 tokens 23.6 / 22.3, 1048576 tokens 152 / 133; 8 experts, 131072 tokens 7.6 / 9.7, 1048576 tokens 22.0 / 20.3.
+constexpr int kLaterTokens = 1 << 17;
+constexpr int64_t kLaterLogits = 1 << 23;
+
 template <int VPL, int L>
 bool launch_lists_of(const SelectArgs& p, int run, hipStream_t s) {
     const int grid = min((p.T + 256 / L - 1) / (256 / L), 256 * 8);
-    auto go = [&](auto vec, auto sigmoid) {
-        hipLaunchKernelGGL((select_lists_kernel<VPL, L, decltype(vec)::value, decltype(sigmoid)::value>), dim3(grid), dim3(256), 0, s, p, run);
+    auto go = [&](auto vec, auto sigmoid, auto later) {
+        hipLaunchKernelGGL((select_lists_kernel<VPL, L, decltype(vec)::value, decltype(sigmoid)::value, decltype(later)::value>), dim3(grid),
+                           dim3(256), 0, s, p, run);
     };
     const std::true_type yes;
     const std::false_type no;
-    if (run % 4 == 0 && p.E % 4 == 0) p.sigmoid ? go(yes, yes) : go(yes, no);
-    else p.sigmoid ? go(no, yes) : go(no, no);
+    if (run % 4 == 0 && p.E % 4 == 0) {
+        if (p.T >= kLaterTokens && (int64_t)p.T * p.E >= kLaterLogits) {
+            p.sigmoid ? go(yes, yes, yes) : go(yes, no, yes);
+            const dim3 rest((p.T + 64 * kSelectWaves - 1) / (64 * kSelectWaves)), block(64 * kSelectWaves);
+            if (p.E <= 64) hipLaunchKernelGGL(select_doubtful_kernel<1>, rest, block, 0, s, p);
+            else hipLaunchKernelGGL(select_doubtful_kernel<4>, rest, block, 0, s, p);
+        } else {
+            p.sigmoid ? go(yes, yes, no) : go(yes, no, no);
+        }
+    } else {
+        p.sigmoid ? go(no, yes, no) : go(no, no, no);
+    }
     return true;
 }
 

@@ -137,6 +137,28 @@ def test_many_tokens(E, groups, topk_groups, K, score):
     _check(x, K, score, bias, groups, topk_groups, 2, scale=2.5)
 
 
+@pytest.mark.parametrize("T,E,groups,topk_groups,K,score", [(131072, 64, 1, 1, 6, routing.SIGMOID), (131073, 64, 8, 3, 8, routing.SOFTMAX),
+                                                            (140001, 128, 4, 2, 8, routing.SIGMOID), (1 << 20, 8, 1, 1, 2, routing.SIGMOID)])
+def test_so_many_tokens_that_doubtful_ones_come_later(T, E, groups, topk_groups, K, score):
+    """Rows of many equal and nearly equal keys among others; the same tokens in calls of few tokens."""
+    rng = np.random.default_rng(T)
+    x = _logits(T, E, 5)
+    x[::50] = rng.integers(-3, 4, size=x[::50].shape).astype(np.float32) * np.float32(0.25)
+    x[7::1000] = -np.inf
+    bias = (rng.integers(-1, 2, size=E) * 0.125).astype(np.float32)
+    kw = dict(n_groups=groups, topk_groups=topk_groups)
+    idx, gate = _select(x, K, score, bias, **kw)
+    assert (idx[7::1000] == -1).all() and (gate[7::1000] == 0).all()
+    for lo in range(0, T, 65536):
+        i, g = _select(x[lo:lo + 65536], K, score, bias, **kw)
+        np.testing.assert_array_equal(idx[lo:lo + 65536], i)
+        np.testing.assert_array_equal(gate[lo:lo + 65536], g)
+    some = np.concatenate([np.arange(0, T, 50), np.arange(T - 3, T), rng.integers(0, T, 2000)])
+    want, g = routing.select(x[some], K, score, bias, groups, topk_groups, 2, True, 1.0)
+    np.testing.assert_array_equal(idx[some], want)
+    assert (abs(gate[some] - g) <= 8 * ULP * g + 2.0 ** -148).all()
+
+
 @pytest.mark.parametrize("dtype,T,H,E", [(torch.bfloat16, 1, 64, 8), (torch.bfloat16, 100, 1000, 12), (torch.bfloat16, 2100, 512, 64),
                                          (torch.bfloat16, 300, 256, 200), (torch.float32, 50, 132, 8), (torch.float32, 1500, 256, 32)])
 def test_from_tokens(dtype, T, H, E):
