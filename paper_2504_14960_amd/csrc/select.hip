@@ -112,6 +112,7 @@ __device__ __forceinline__ void select_token(const SelectArgs& p, int t, int lan
             mine[j] = kNever;
             if (g < p.groups) {
                 double first = kNever, second = kNever;
+#pragma unroll 4
                 for (int i = 0; i < size; ++i) {
                     const double k = keys[g * size + i];
                     second = k > first ? first : max_key(second, k);
@@ -182,14 +183,26 @@ __global__ __launch_bounds__(64 * kSelectWaves) void select_wave_kernel(SelectAr
 // In idx[t][0] of a token whose selection is left to this kernel
 constexpr int kDoubtful = -2;
 
-// 64 tokens to a wave, the doubtful ones one after the other.
+// 64 tokens for every wave; the workgroup's doubtful ones are dealt to its waves.  A chain of some 5 us for each.
 template <int VPL>
 __global__ __launch_bounds__(64 * kSelectWaves) void select_doubtful_kernel(SelectArgs p) {
     __shared__ double keys[kSelectWaves][64 * VPL], best[kSelectWaves][64 * VPL];
+    __shared__ int tokens[64 * kSelectWaves], counts[kSelectWaves];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int t0 = (blockIdx.x * kSelectWaves + wave) * 64;
-    for (uint64_t m = __ballot(t0 + lane < p.T && p.idx[(size_t)(t0 + lane) * p.K] == kDoubtful); m; m &= m - 1)
-        select_token<VPL>(p, t0 + __ffsll((unsigned long long)m) - 1, lane, keys[wave], best[wave]);
+    const int t = blockIdx.x * (64 * kSelectWaves) + (int)threadIdx.x;
+    const bool doubtful = t < p.T && p.idx[(size_t)t * p.K] == kDoubtful;
+    const uint64_t m = __ballot(doubtful);
+    if (lane == 0) counts[wave] = __popcll(m);
+    __syncthreads();
+    int first = 0, n = 0;
+    for (int w = 0; w < kSelectWaves; ++w) {
+        first += w < wave ? counts[w] : 0;
+        n += counts[w];
+    }
+    if (doubtful) tokens[first + __popcll(m & ((1ull << lane) - 1))] = t;
+    __syncthreads();
+    for (int i = wave; i < n; i += kSelectWaves)
+        select_token<VPL>(p, __builtin_amdgcn_readfirstlane(tokens[i]), lane, keys[wave], best[wave]);
 }
 
 // ---- up to eight experts a token ----
@@ -200,7 +213,7 @@ __global__ __launch_bounds__(64 * kSelectWaves) void select_doubtful_kernel(Sele
 // Bound by the vector unit.  Scores in 64 bits would be half of its work, so they are first formed in fp32, and what was
 // selected by them stands if no difference that decided it is within what they may be off; else the wave does it all again
 // in 64 bits (a token in some hundreds).  LATER: in a launch behind this one, which finds them marked; the code that does it takes a
-// fifth of this kernel's time by its registers alone.  262144 tokens x 256 experts in 8 groups, 8 of 4 groups: 104 us, some 160 vector
+// fifth of this kernel's time by its registers alone.  262144 tokens x 256 experts in 8 groups, 8 of 4 groups: 101 us, some 160 vector
 // instructions a token (75 us of issue; the bytes take 47 at 6 TB/s).  A token to a wave with all scores in 64 bits took 449.
 // Keys up to here belong to experts that are not selected.  (Their low bits make them smaller.)
 constexpr double kLow = -(double)__FLT_MAX__;
@@ -463,7 +476,8 @@ __global__ __launch_bounds__(256, 4) void select_lists_kernel(SelectArgs p, int 
 
 // From so many tokens and logits on the doubtful tokens get a launch of their own, which takes 5 to 8 us.  us, in the same launch / so,
 // sigmoid: 256 experts in 8 groups, 65536 tokens 35.6 / 38.6, 131072 tokens 55.5 / 56.5, 262144 tokens 104 / 99; 64 experts, 65536 tokens 15.0
-// / 15.2, 131072 tokens 23.6 / 22.3, 1048576 tokens 152 / 133; 8 experts, 131072 tokens 7.6 / 9.7, 1048576 tokens 22.0 / 20.3.
+// / 15.2, 131072 tokens 23.6 / 22.3, 1048576 tokens 152 / 133; 8 experts, 131072 tokens 7.6 / 9.7, 1048576 tokens 22.0 / 20.3.  (Measured
+// with a wave's doubtful tokens one after the other; dealt to the workgroup's waves, 262144 tokens of 256 take 7 us less.)
 constexpr int kLaterTokens = 1 << 17;
 constexpr int64_t kLaterLogits = 1 << 23;
 
