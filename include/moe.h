@@ -431,8 +431,8 @@ moe_status_t moe_router_select(const void* x, const void* w_router, const float*
  * then dx, dw_router and dbias as in moe_router_backward_addend, with its arguments, limits,
  * workspace and errors.  x and w_router may be NULL where dw_router and dx are not asked
  * for.  Slots outside [0,E) and experts whose logit is -inf or NaN get no gradient, and
- * what dgate holds there is not looked at; nor do tokens whose selected scores are all 0 in
- * fp32.  T <= 2^27.
+ * what dgate holds there is not looked at; nor, with renormalize, do tokens whose selected
+ * scores are all 0 in 64 bits.  T <= 2^27.
  */
 moe_status_t moe_router_select_backward(const void* x, const void* w_router, const float* logits,
                                         const int32_t* topk_idx, const float* dgate,

@@ -538,6 +538,19 @@ struct SelectBackwardArgs {
     int T, E, K, sigmoid, renorm;
 };
 
+// 2^64 exp(d) for d <= 0, as near: what the hardware's exponential would take for 0, fp32's denormal numbers, is there with all its bits
+__device__ __forceinline__ float exp_lifted(float d) {
+    d = fmaxf(d, -150.f);
+    const float hi = d * 1.44269502f, up = hi + 64.f, lo = fmaf(d, 1.44269502f, -hi) + fmaf(d, 1.92596303e-8f, hi - (up - 64.f));
+    const float e = __builtin_amdgcn_exp2f(up);
+    return fmaf(e, lo * 0.693147181f, e);
+}
+__device__ __forceinline__ float exp_gradual(float d) { return exp_lifted(d) * 0x1p-64f; }
+
+// Selected scores that are 0 in 64 bits, where sigmoid and softmax are formed forward: logits, and logits against the row's largest,
+// from here down
+constexpr float kNoSigmoid = -709.7827f, kNoSoftmax = -745.133f;
+
 // f over N consecutive lanes (a power of two), in all of them
 template <typename F>
 __device__ __forceinline__ float lanes_fold(float v, int N, F&& f) {
@@ -553,7 +566,7 @@ template <bool SIGMOID, int TW, bool STREAM>
 __global__ __launch_bounds__(256) void select_dlogits_kernel(SelectBackwardArgs p) {
     constexpr int PER = 64 / TW, SLOTS = TW == 8 ? 1 : 4;
     extern __shared__ __attribute__((aligned(16))) float rows_of_waves[];
-    __shared__ float totals[4][TW];
+    __shared__ float totals[4][TW], largest[4][TW];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int t0 = (blockIdx.x * 4 + wave) * TW, E = p.E;
     if (t0 >= p.T) return;
@@ -561,6 +574,7 @@ __global__ __launch_bounds__(256) void select_dlogits_kernel(SelectBackwardArgs 
     float* const rows = rows_of_waves + wave * (TW * E);
     const size_t base = (size_t)t0 * E;
     auto add = [](float a, float b) { return a + b; };
+    auto max_of = [](float a, float b) { return fmaxf(a, b); };
     auto sync = [] {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -583,11 +597,12 @@ __global__ __launch_bounds__(256) void select_dlogits_kernel(SelectBackwardArgs 
                 prob[s][i] = in && q + L * i < E ? p.logits[base + (size_t)t * E + q + L * i] : -INFINITY;
                 m = fmaxf(m, prob[s][i]);                    // of NaN and a number the number
             }
-            m = lanes_fold(m, L, [](float a, float b) { return fmaxf(a, b); });
+            m = lanes_fold(m, L, max_of);
+            if (q == 0 && t < TW) largest[wave][t] = m;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float x = prob[s][i];
-                prob[s][i] = x > -INFINITY ? (x == m ? 1.f : exp_near(x - m)) : 0.f;
+                prob[s][i] = x > -INFINITY ? (x == m ? 0x1p64f : exp_lifted(x - m)) : 0.f;   // the sum cancels the factor
                 z += prob[s][i];
             }
             z = lanes_fold(z, L, add);
@@ -603,29 +618,43 @@ __global__ __launch_bounds__(256) void select_dlogits_kernel(SelectBackwardArgs 
     // slots sub, sub + PER, ..: expert, score, 1 - score (sigmoid), gradient of the gate
     const int tok = lane / PER, sub = lane % PER;
     int e[SLOTS];
-    float s[SLOTS], rest[SLOTS], d[SLOTS], sum = 0.f;
+    float l[SLOTS], s[SLOTS], rest[SLOTS], d[SLOTS], sum = 0.f, top = -INFINITY;
 #pragma unroll
     for (int j = 0; j < SLOTS; ++j) {
         const int k = sub + PER * j;
         e[j] = -1;
+        l[j] = -INFINITY;
         s[j] = d[j] = 0.f;
         rest[j] = 1.f;
         if (k < p.K && tok < nt) {
             const size_t slot = (size_t)(t0 + tok) * p.K + k;
             const int i = p.idx[slot];
             if ((unsigned)i < (unsigned)E) {
-                const float l = p.logits[base + (size_t)tok * E + i];
-                if (l > -INFINITY) {
+                l[j] = p.logits[base + (size_t)tok * E + i];
+                if (l[j] > -INFINITY) {
                     e[j] = tok * E + i;
                     d[j] = p.dgate[slot] * p.scale;
-                    if constexpr (SIGMOID) {
-                        const float x = exp_near(-fabsf(l)), r = 1.f / (1.f + x);
-                        s[j] = l >= 0.f ? r : x * r;
-                        rest[j] = l >= 0.f ? x * r : r;
-                    } else {
-                        s[j] = rows[e[j]];
-                    }
+                    top = fmaxf(top, l[j]);
                 }
+            }
+        }
+    }
+    // Of renormalised gates only the scores' ratios count: they are formed against the largest of the token's, so that small ones,
+    // which the forward has in 64 bits, keep theirs
+    if (p.renorm) top = lanes_fold(top, PER, max_of);
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j) {
+        if (e[j] >= 0) {
+            if constexpr (SIGMOID) {
+                const float x = exp_gradual(-fabsf(l[j])), r = 1.f / (1.f + x);
+                s[j] = l[j] >= 0.f ? r : p.renorm ? exp_gradual(l[j] - fminf(top, 0.f)) * r : x * r;
+                rest[j] = l[j] >= 0.f ? x * r : r;
+                if (p.renorm && !(top > kNoSigmoid)) s[j] = 0.f;
+            } else if (p.renorm) {
+                const float m = largest[wave][tok];
+                if (top == m || top - m > kNoSoftmax) s[j] = l[j] == top ? 1.f : exp_gradual(l[j] - top);
+            } else {
+                s[j] = rows[e[j]];
             }
         }
         sum += s[j];
