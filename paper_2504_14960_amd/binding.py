@@ -414,7 +414,9 @@ def expert_weights_fp8_block(w_gate: torch.Tensor, w_up: torch.Tensor, w_down: t
     for name, codes, scales, shape in (("gate", gate, gate_scales, (E, F, H)), ("up", up, up_scales, (E, F, H)),
                                        ("down", down, down_scales, (E, H, F)), ("wgu_t", wgu_t, wgu_t_scales, (E, H, 2 * F)),
                                        ("wd_t", wd_t, wd_t_scales, (E, F, H))):
-        out += (None, None) if codes is None or scales is None else _blocks(name, codes, scales, shape, E * (shape[1] // 128))
+        if (codes is None) != (scales is None):
+            raise ValueError(f"{name} and {name}_scales are given together or left out together")
+        out += (None, None) if codes is None else _blocks(name, codes, scales, shape, E * (shape[1] // 128))
     _check(lib().moe_expert_weights_fp8_block(_ptr(w_gate), _ptr(w_up), _ptr(w_down), _dt(w_gate), H, F, E, *out, _stream()))
 
 
