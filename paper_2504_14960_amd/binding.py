@@ -408,7 +408,9 @@ def expert_weights_fp8_block(w_gate: torch.Tensor, w_up: torch.Tensor, w_down: t
     """A layer's weights (fp32 or bf16) as codes and scales of the forward (gate, up [E, F, H], down [E, H, F]) and of the
     backward (wgu_t [E, H, 2F], wd_t [E, F, H]); either set may be left out."""
     E, F, H = w_gate.shape
-    for name, t in (("w_up", w_up), ("w_down", w_down)):
+    for name, t, shape in (("w_up", w_up, (E, F, H)), ("w_down", w_down, (E, H, F))):
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name} must have shape {shape}, not {tuple(t.shape)}")
         _is(name, t, (w_gate.dtype,), E * F * H)
     out = []
     for name, codes, scales, shape in (("gate", gate, gate_scales, (E, F, H)), ("up", up, up_scales, (E, F, H)),

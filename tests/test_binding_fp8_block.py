@@ -56,3 +56,12 @@ def test_a_whole_set_may_be_left_out(anywhere):
         out[name] = None
     _call(_weights(), out)
     assert len(anywhere) == 1 and anywhere[0][13:17] == (None,) * 4 and None not in anywhere[0][7:13]
+
+
+@pytest.mark.parametrize("which", [0, 1, 2])
+def test_weights_of_another_shape_are_refused(anywhere, which):
+    w = _weights()
+    w[which] = w[which].transpose(1, 2).contiguous()
+    with pytest.raises(ValueError):
+        _call(w, _outputs())
+    assert not anywhere
