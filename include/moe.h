@@ -849,7 +849,7 @@ moe_status_t moe_expert_down_fp8_block(const void* h_codes, const uint8_t* h_sca
  * once, and of the values that the codes of h and x stand for.  Shapes, outputs, limits and
  * errors as moe_grouped_gemm_swiglu_backward, and R_max <= 2^22 (otherwise
  * MOE_ERR_UNSUPPORTED); experts without rows get zeros.  workspace:
- * moe_expert_backward_fp8_block_workspace_bytes.
+ * moe_expert_backward_fp8_block_workspace_bytes (0 for what the call refuses).
  */
 size_t moe_expert_backward_fp8_block_workspace_bytes(int R_max, int H, int F, int E);
 moe_status_t moe_grouped_gemm_swiglu_fp8_block_backward(

@@ -1412,7 +1412,9 @@ static BlockBackwardLayout block_backward_layout(int R_max, int H, int F, int E)
 }
 
 size_t moe_expert_backward_fp8_block_workspace_bytes(int R_max, int H, int F, int E) {
-    if (R_max < 0 || H <= 0 || F <= 0 || E <= 0) return 0;
+    if (R_max < 0 || R_max > kMaxBlockBackwardRows || H <= 0 || F <= 0 || E <= 0 || E > kMaxExperts || !blocks_fit(H, F) ||
+        H > kMaxBlockRow || F > kMaxBlockRow / 2)
+        return 0;
     return block_backward_layout(R_max, H, F, E).total;
 }
 
