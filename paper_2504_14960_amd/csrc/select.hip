@@ -366,6 +366,12 @@ __global__ __launch_bounds__(256, 4) void select_lists_kernel(SelectArgs p, int 
             }
             z = lanes((double)sum, add);
             rz = 1.f / (float)z;
+            if (!p.renorm) {   // the gates' divisor: 32 terms of very different sizes lose too much in fp32
+                z = 0.;
+#pragma unroll
+                for (int j = 0; j < VPL; ++j) z += (double)fmaxf(x[j], 0.f);
+                z = lanes(z, add);
+            }
         }
         int at = sub * LDB;
         asm volatile("" : "+v"(at));   // or the biases are kept in registers over all tokens

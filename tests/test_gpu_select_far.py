@@ -1,10 +1,10 @@
 """Routing by scores where scores are far from 1: gradients of selected experts whose scores are small against fp32's range, or
-against the largest of their row; against the oracle in 64 bits."""
+against the largest of their row, and gates whose softmax adds up many small terms; against the oracle in 64 bits."""
 import numpy as np
 import pytest
 
 from oracle import routing
-from test_gpu_select import ULP, _backward
+from test_gpu_select import ULP, _backward, _check
 
 pytestmark = pytest.mark.gpu
 
@@ -58,3 +58,12 @@ def test_tokens_whose_gates_are_zero_get_no_gradient(score, low):
     idx = np.tile(np.array([1, 2], dtype=np.int32), (3, 1))
     got = _backward(x, idx, np.ones((3, 2), dtype=np.float32), score, True, 1.0)
     assert (got == 0).all()
+
+
+@pytest.mark.parametrize("E,K", [(256, 1), (256, 8), (160, 4), (64, 2), (256, 12), (255, 3)])
+def test_softmax_gates_beside_many_small_terms(E, K):
+    """One logit of 0 and all others where their exponentials, one by one, are half a step of 1: together up to 2^-17 of the sum."""
+    x = (np.log(2.0 ** -25) - np.tile(np.linspace(0, 0.05, E), (5, 1))).astype(np.float32)
+    for t in range(5):
+        x[t, (t * 37) % E] = 0.0
+    _check(x, K, routing.SOFTMAX, renormalize=False)
