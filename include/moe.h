@@ -757,8 +757,10 @@ moe_status_t moe_expert_down_fp8(const void* h_fp8, const int32_t* expert_offset
  * nearest E4M3 values of x / scale, ties to even.  A block with a value that is not finite
  * gets scale 255 and codes 0x7f.  Activations have a scale for every 128 values of a row,
  * weights one for every 128 x 128.  The powers of two are what the matrix instruction of
- * this GPU multiplies in by itself, and they make the value of a code and its scale a
- * bf16 value (four significant bits): weight gradients are formed from just those.
+ * this GPU multiplies in by itself, and from 2^-124 on they make the value of a code and
+ * its scale a bf16 value (four significant bits, down to 2^-133, the smallest there is):
+ * weight gradients are formed from just those.  With the two scales below that they are
+ * formed from the nearest bf16 values.
  *
  * Scales of rows of C values lie in rows of moe_fp8_block_scale_stride(C) bytes: C / 128,
  * rounded up to a multiple of 4.  The bytes behind a row's last scale are neither written
@@ -813,7 +815,9 @@ moe_status_t moe_permute_fp8_block(const void* x_bf16, const int32_t* topk_idx, 
  *
  * with fp32 accumulation.  (The matrix instruction adds the products of eight codes that
  * are neighbours along the contraction with what lies 2^13 below the largest of them cut
- * off, here as in the products above: sums of 128 random codes are some 2e-5 off.)
+ * off, here as in the products above: sums of 128 random codes are some 2e-5 off.  So a code
+ * of h near the middle of two is now and then its neighbour, in some 0.3 %, and a scale is
+ * twice or half what exact sums give, in some 0.01 % of the blocks.)
  * h_codes [R_max,F], h_scales [R_max, stride(F)]: workspace and
  * output.  gu [R_max,2F] = (g | u) in bf16 for the backward, or NULL.  H and F multiples of
  * 128, E <= 256; otherwise MOE_ERR_UNSUPPORTED.  Rows in [R, R_max) are not touched.
@@ -846,7 +850,8 @@ moe_status_t moe_expert_down_fp8_block(const void* h_codes, const uint8_t* h_sca
  * The products for dh and dx_perm are 8-bit products with fp32 accumulation.  The
  * quantisations count as identities.  The weight gradients contract over rows, along which
  * no operand has its blocks: they are bf16 products of dy_perm, of dg and du rounded to bf16
- * once, and of the values that the codes of h and x stand for.  Shapes, outputs, limits and
+ * once, and of the values that the codes of h and x stand for (to bf16 where a scale is below
+ * 2^-124).  Shapes, outputs, limits and
  * errors as moe_grouped_gemm_swiglu_backward, and R_max <= 2^22 (otherwise
  * MOE_ERR_UNSUPPORTED); experts without rows get zeros.  workspace:
  * moe_expert_backward_fp8_block_workspace_bytes (0 for what the call refuses).

@@ -13,7 +13,8 @@
 //                              multiple of 64 (at least 128) columns, so the
 //                              weight-gradient GEMMs contract over whole k-tiles
 //                              (of E4M3 codes with a scale for every block of 128
-//                              the values they stand for, which are bf16 values)
+//                              the values they stand for, which are bf16 values
+//                              from a scale of 2^-124 on, and rounded below)
 //   swiglu_backward_kernel     (dh, g, u) -> dg | du side by side
 //
 // All bf16, tiles through LDS for the transposes.

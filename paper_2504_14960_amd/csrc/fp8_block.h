@@ -3,7 +3,8 @@
 // Powers of two, because the scaled matrix instruction multiplies both operands' E8M0 scales in on the way: a block of 128 along
 // the contraction is the instruction's whole depth, so scaling costs no vector instruction, where any other scale would cost
 // a fused multiply-add for every accumulator and block.  And what a code and its scale stand for has four significant bits, so
-// it is a bf16 value too: the weight gradients multiply exactly what the forward did.
+// it is a bf16 value too, and the weight gradients multiply exactly what the forward did: from a scale of 2^-124 on, with which the
+// smallest code is bf16's smallest value, 2^-133.  With 2^-125 and 2^-126 what lies below that is rounded.
 #pragma once
 
 #include "common.h"
