@@ -72,6 +72,8 @@ __device__ __forceinline__ double shifted_exp64(float x, float m) { return x == 
 constexpr int kSelectWaves = 4;
 
 // Token t by a wave, any groups, scores in 64 bits.  Lane l holds experts l + 64 j; keys, best: LDS of this wave, 64 VPL each.
+// Bound by the vector unit.  262144 tokens x 256 experts, us: 12 experts a token 447 (1057 vector instructions a token), 8 in 4 groups of
+// 64 experts 672 (1346, and conflicts in LDS, where a lane reads a group), in 32 groups of 8 555; the bytes take 47 at 6 TB/s.
 template <int VPL>
 __device__ __forceinline__ void select_token(const SelectArgs& p, int t, int lane, double* keys, double* best) {
     const float* const row = p.logits + (size_t)t * p.E;
@@ -212,9 +214,12 @@ __global__ __launch_bounds__(64 * kSelectWaves) void select_doubtful_kernel(Sele
 //
 // Bound by the vector unit.  Scores in 64 bits would be half of its work, so they are first formed in fp32, and what was
 // selected by them stands if no difference that decided it is within what they may be off; else the wave does it all again
-// in 64 bits (a token in some hundreds).  LATER: in a launch behind this one, which finds them marked; the code that does it takes a
+// in 64 bits (a token in some hundreds, of logits that are hardly ever equal: equal keys are always in doubt.  Logits that were rounded
+// to bf16 leave a third of the tokens in doubt where no bias tells their experts apart: 262144 x 256 then takes 319 us in 8 groups
+// and 243 without, instead of 103 and 98).  LATER: in a launch behind this one, which finds them marked; the code that does it takes a
 // fifth of this kernel's time by its registers alone.  262144 tokens x 256 experts in 8 groups, 8 of 4 groups: 101 us, some 160 vector
-// instructions a token (75 us of issue; the bytes take 47 at 6 TB/s).  A token to a wave with all scores in 64 bits took 449.
+// instructions a token (75 us of issue; the bytes take 47 at 6 TB/s); with softmax scores 120, 203 instructions.  250 experts, whose
+// rows are not read in fours, 172 with as many instructions, the rest of it waiting.  A token to a wave with all scores in 64 bits took 449.
 // Keys up to here belong to experts that are not selected.  (Their low bits make them smaller.)
 constexpr double kLow = -(double)__FLT_MAX__;
 
@@ -567,7 +572,8 @@ __device__ __forceinline__ float lanes_fold(float v, int N, F&& f) {
 // TW tokens to a wave: 8 of up to 8 slots, 4 of up to 64.  The slots' work, of which there is little, is dealt over the wave, 64 / TW
 // lanes to a token; the rows of dlogits are put together in LDS and written in one piece, which starts at a multiple of 16
 // bytes whatever E is.  Bound by that write (softmax: and by the read of the logits).  262144 tokens x 256 experts, 8 slots, sigmoid: 74
-// us for 294 MB, 420 with the 64-byte sectors around the logits it picks (5.7 TB/s); every lane storing for itself took 164.
+// us for 294 MB, 420 with the 64-byte sectors around the logits it picks (5.7 TB/s); every lane storing for itself took 164.  Softmax: 180
+// us for 554 MB, 244 vector instructions a token (112 us of issue) in four waves a SIMD, as many as LDS has room for.
 template <bool SIGMOID, int TW, bool STREAM>
 __global__ __launch_bounds__(256) void select_dlogits_kernel(SelectBackwardArgs p) {
     constexpr int PER = 64 / TW, SLOTS = TW == 8 ? 1 : 4;
